@@ -46,7 +46,7 @@ extern "C" {
 
 typedef struct c2t_ctx c2t_ctx; /* opaque, host memory */
 
-enum { C2T_F32 = 0, C2T_BF16 = 1 };
+enum { C2T_F32 = 0, C2T_BF16 = 1, C2T_F16 = 2 /* the paged cache and its attention only */ };
 
 enum {
   C2T_OK = 0,
@@ -65,6 +65,9 @@ enum {
 #define C2T_MAX_BUDGET 1024
 #define C2T_MAX_CANDIDATES 2048 /* max_frontier * top_k */
 #define C2T_MAX_HISTORY 32768   /* max_depth * max_frontier * top_k with rerank = 1 */
+#define C2T_MAX_BIAS 1024       /* biases of a sequence (c2t_adjustments) */
+#define C2T_MAX_CACHE_BATCH 4096 /* sequences of a c2t_cache */
+#define C2T_MAX_PATH 1025       /* tokens of an accepted path: the root and C2T_MAX_BUDGET nodes */
 
 typedef struct {
   int32_t batch;        /* B: independent sequences                                   */
@@ -222,6 +225,127 @@ int c2t_stream_read(const void* dev_ptr, size_t bytes, uint32_t* dev_out, void* 
  * per row): the ceiling for that access pattern. */
 int c2t_stream_read_rows(const void* dev_ptr, int32_t rows, size_t row_bytes, size_t row_stride_bytes,
                          uint32_t* dev_out, void* stream);
+
+/* ---- Around the draft phase: adjusted logits, a paged K/V cache, attention over it ----------------
+ *
+ * A step of a serving loop: c2t_adjust_logits ahead of each c2t_expand_layer, c2t_finalize_tree,
+ * c2t_cache_reserve for the root and the nodes, the target model's forward pass (per layer: c2t_cache_write, then
+ * c2t_cache_attention with the tree's mask), c2t_adjust_tree_logits on its logits, the caller's acceptance, and
+ * c2t_cache_commit of the accepted path.  Lengths, tables and counts stay on the device, and the calls check them there:
+ * whatever these arrays hold, no call reads or writes outside the buffers that it is given.  The calls
+ * below keep nothing on the host, so they may be made from several threads; calls that change one cache belong on one stream. */
+
+/* What is done to a token's logit x.  a: how often the token occurs in the sequence's context and on the path from the root to
+ * the row's node, the node included; o: the same without the prompt.  In fp32, rounded once to the logits' type at the end:
+ *   a > 0:  x > 0 ? x / repetition : x * repetition;   o > 0: minus frequency * o + presence;
+ *   plus the token's biases (those of one token added up in the order listed);   not allowed: -inf, whatever it was.
+ * A logit to which nothing is done keeps its bits.  NULL leaves a term out.  All pointers [device]. */
+typedef struct {
+  const int32_t* tokens;       /* [batch][token_stride] context: prompt, then what was generated; ids outside the vocabulary count nowhere */
+  int64_t token_stride;
+  const int32_t* n_tokens;     /* [batch] tokens of each context (at most token_stride are read); needed with `tokens` */
+  const int32_t* n_prompt;     /* [batch] the first n_prompt are prompt, for which only the repetition penalty counts; NULL: none are */
+  const float* repetition;     /* [batch] above 0; 1 = no penalty */
+  const float* frequency;      /* [batch] */
+  const float* presence;       /* [batch] */
+  const int32_t* bias_tokens;  /* [batch][bias_stride] token ids (outside the vocabulary: ignored) */
+  const float* bias;           /* [batch][bias_stride] */
+  const int32_t* n_bias;       /* [batch] entries used; NULL: all bias_stride */
+  int32_t bias_stride;         /* at most C2T_MAX_BIAS */
+  const uint32_t* allowed;     /* grammar mask: bit v % 32 of word v / 32 of the row's ceil(vocab / 32) words: token v may follow */
+  int64_t allowed_row_stride;  /* words from row to row (0: one mask for a sequence's rows) and from sequence to sequence */
+  int64_t allowed_batch_stride;
+} c2t_adjustments;
+
+/* The draft model's rows of the current frontier, ahead of c2t_expand_layer: logits and out [device] [B][F][row stride] as there, of
+ * the configured dtype; out may be logits (same stride), else the two do not overlap.  Rows f < n_frontier[b] are written, their first
+ * `vocab` logits; everything else is left as it is.  Same place in the call order as c2t_expand_layer, any number of times. */
+int c2t_adjust_logits(c2t_ctx* ctx, const c2t_adjustments* adjustments, const void* logits, int64_t row_stride_elems, void* out,
+                      int64_t out_row_stride_elems, void* stream);
+
+/* The target model's rows of a tree: [batch][1 + nodes][row stride], row 0 the root's and row 1 + i node i's, in C2T_F32 or C2T_BF16.
+ * tree_tokens, tree_parent [batch][nodes] and n_nodes [batch] as c2t_finalize_tree writes them (nodes = its N, at most C2T_MAX_BUDGET;
+ * nodes = 0: one row a sequence, no tree; n_nodes then holds zeros).  Rows 0 .. n_nodes[b] are written. */
+int c2t_adjust_tree_logits(const c2t_adjustments* adjustments, int32_t batch, int32_t vocab, int32_t nodes, int32_t dtype,
+                           const int32_t* tree_tokens, const int32_t* tree_parent, const int32_t* n_nodes, const void* logits,
+                           int64_t row_stride_elems, void* out, int64_t out_row_stride_elems, void* stream);
+
+/* A paged K/V cache.  All arrays are the caller's, on the device.  A page holds page_size tokens of all layers and heads; a
+ * sequence's token i lies on page page_table[b][i / page_size].  Start with page_table -1, length 0, refcount 0, status 0.
+ * (A caller that hands pages out itself may: the calls need refcount <= 1 for pages that are written and otherwise only the table.) */
+typedef struct {
+  int32_t batch, layers, pages;
+  int32_t page_size;           /* 16, 32, 64, 128 or 256 tokens; pages * page_size < 2^31 */
+  int32_t kv_heads;            /* at most 1024 */
+  int32_t head_dim;            /* 64, 128 or 256 */
+  int32_t max_pages;           /* entries of a sequence's row of page_table; max_pages * page_size <= 2^30 */
+  int32_t dtype;               /* C2T_BF16 or C2T_F16 */
+  void* k;                     /* [layers][pages][kv_heads][page_size][head_dim], 16-byte aligned */
+  void* v;
+  int32_t* page_table;         /* [batch][max_pages], -1: no page */
+  int32_t* length;             /* [batch] tokens in the cache */
+  int32_t* refcount;           /* [pages] sequences that hold the page; 0: free */
+  uint32_t* status;            /* [batch] C2T_CACHE_* bits; calls set them, the caller clears them */
+} c2t_cache;
+
+enum {
+  C2T_CACHE_POOL_EMPTY = 1, /* reserve: not enough free pages; this sequence got none                             */
+  C2T_CACHE_ROW_FULL = 2,   /* its row of page_table has no room for the tokens                                    */
+  C2T_CACHE_INVALID = 4,    /* a page number, path or pair of a fork that cannot be; what needed it was left out      */
+  C2T_CACHE_SHARED = 8      /* a page to be written is held by others too (nothing was reserved); not written      */
+};
+
+/* Bytes of [device] workspace (256-byte aligned) that c2t_cache_reserve needs; nothing in it is kept between calls.  [host] out. */
+int c2t_cache_workspace_bytes(const c2t_cache* cache, size_t* out);
+
+/* Room for n_new[b] ([device]) tokens behind each sequence's length (0 or less: nothing is done).  Entries of its row in that range that are -1,
+ * or whose page others hold too, get free pages, the lowest-numbered first, in order of sequence and entry; of a shared page the tokens
+ * below the length are copied, in all layers.  All decisions are made on the counts as the call finds them: where all holders of a page reserve
+ * at once, all of them leave it.  A sequence gets all of its pages or none; if the pool does not suffice for sequences 0 .. b
+ * together, b gets none. */
+int c2t_cache_reserve(const c2t_cache* cache, const int32_t* n_new, void* dev_workspace, size_t workspace_bytes, void* stream);
+
+/* K and V of new tokens of one layer into their pages: k, v [device] [batch][tokens][kv_heads][head_dim] of the cache's dtype, strides in
+ * elements (multiples of 8; heads next to each other), e.g. slices of one projection's output.  Token t < n_new[b] (NULL: all `tokens`)
+ * goes to position length[b] + t; the length stays. */
+int c2t_cache_write(const c2t_cache* cache, int32_t layer, const void* k, const void* v, int64_t batch_stride, int64_t token_stride, int32_t tokens,
+                    const int32_t* n_new, void* stream);
+
+/* The accepted path: path [device] [batch][path_stride], n_path [batch]: the tokens at length[b] + path[b][i] move to length[b] + i in all
+ * layers, i < n_path[b], and length[b] grows by n_path[b].  A path rises strictly from 0 or more (slots of a root and its nodes in
+ * breadth-first order do); of one that does not, or that leaves the reserved pages, nothing is moved. */
+int c2t_cache_commit(const c2t_cache* cache, const int32_t* path, int32_t path_stride, const int32_t* n_path, void* stream);
+
+/* length[b] = min(length[b], new_length[b]) (NULL: as it is), then pages that hold none of the tokens below length[b] + keep are let go. */
+int c2t_cache_truncate(const c2t_cache* cache, const int32_t* new_length, int32_t keep, void* stream);
+
+/* Sequence dst[i] becomes a copy of src[i], i < n ([device]): its own pages are let go, and it holds those of src's tokens too.  Pairs with an index
+ * outside the batch, or of a sequence with itself, do nothing; pairs that name a dst which another pair names are refused. */
+int c2t_cache_fork(const c2t_cache* cache, const int32_t* src, const int32_t* dst, int32_t n, void* stream);
+
+/* Attention of the new tokens over the cache.  The last n_new[b] tokens, at positions length[b] + t, have been written (the length still
+ * counts those before them).  All strides in elements, multiples of 8; heads next to each other. */
+typedef struct {
+  const void* q;               /* [device] [batch][tokens][q_heads][head_dim] of the cache's dtype, 16-byte aligned */
+  int64_t q_batch_stride, q_token_stride;
+  void* out;                   /* [device] the same shape; rows t >= n_new[b] are left as they are; not q */
+  int64_t out_batch_stride, out_token_stride;
+  float* lse;                  /* [device] [batch][tokens][q_heads]: log of the sum of e^score, -inf for a row that sees nothing; or NULL */
+  const int32_t* n_new;        /* [device] [batch], NULL: all `tokens` */
+  int32_t tokens;              /* slots of new tokens a sequence */
+  int32_t q_heads;             /* a multiple of kv_heads; head i reads cached head i / (q_heads / kv_heads) */
+  int32_t layer;
+  int32_t nodes;               /* the last `nodes` slots (at most C2T_MAX_BUDGET) are a tree's, those before them a causal chain (e.g. the root) */
+  const uint8_t* mask;         /* [device] [batch][nodes][nodes] as c2t_finalize_tree writes it, NULL with nodes = 0 */
+  float scale;                 /* of the scores, usually head_dim^-0.5; 0 or more */
+} c2t_attention;
+
+/* Every slot sees the length[b] tokens before; a chain slot the chain up to itself; node i the whole chain and the nodes j with mask[b][i][j] != 0
+ * (j < n_new[b] - chain).  A key that a row does not see has no influence on it, whatever its bits.  A row that sees no key gets zeros.
+ * Products in the cache's dtype, sums and the softmax in fp32.  The workspace ([device], 256-byte aligned, its size from the call's sizes
+ * alone) holds nothing between calls. */
+int c2t_attention_workspace_bytes(const c2t_cache* cache, const c2t_attention* attention, size_t* out);
+int c2t_cache_attention(const c2t_cache* cache, const c2t_attention* attention, void* dev_workspace, size_t workspace_bytes, void* stream);
 
 /* Profiling build only (the library compiled with -DC2T_PHASE_TIMES; paper_2502_13652_amd/phase_times.py
  * builds and drives it): copies to [host] out, for the first n_workgroups (<= 8192) workgroups of the

@@ -13,7 +13,7 @@ _LIB_DIR = os.path.join(_HERE, "lib")
 _LIB = os.path.join(_LIB_DIR, "libc2t_hip.so")
 _lib = None
 
-F32, BF16 = 0, 1
+F32, BF16, F16 = 0, 1, 2
 _ERR = {-1: "invalid argument", -2: "unsupported", -3: "workspace", -4: "state", -5: "hip", -6: "out of host memory"}
 
 _PRELOADED = 11                            # the layer kernels' first arguments, which arrive in registers (compared with their list in k_tree.h as it is compiled)
@@ -93,6 +93,16 @@ def load_library(path=None):
     L.c2t_stream_read.argtypes = [vp, sz, vp, vp]
     L.c2t_stream_read_rows.argtypes = [vp, i32, sz, sz, vp, vp]
     L.c2t_phase_times_read.argtypes = [vp, i32]
+    L.c2t_adjust_logits.argtypes = [vp, vp, vp, i64, vp, i64, vp]
+    L.c2t_adjust_tree_logits.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, vp, i64, vp, i64, vp]
+    L.c2t_cache_workspace_bytes.argtypes = [vp, P(sz)]
+    L.c2t_cache_reserve.argtypes = [vp, vp, vp, sz, vp]
+    L.c2t_cache_write.argtypes = [vp, i32, vp, vp, i64, i64, i32, vp, vp]
+    L.c2t_cache_commit.argtypes = [vp, vp, i32, vp, vp]
+    L.c2t_cache_truncate.argtypes = [vp, vp, i32, vp]
+    L.c2t_cache_fork.argtypes = [vp, vp, vp, i32, vp]
+    L.c2t_attention_workspace_bytes.argtypes = [vp, vp, P(sz)]
+    L.c2t_cache_attention.argtypes = [vp, vp, vp, sz, vp]
     L.c2t_strerror.argtypes = [ctypes.c_int]
     L.c2t_strerror.restype = ctypes.c_char_p
     _lib = L
@@ -180,6 +190,12 @@ class C2TContext:
         rc = self._expand(self.ctx, logits.data_ptr(), strides[1], _stream_ptr(stream))
         if rc != 0:
             raise C2TError(rc, "c2t_expand_layer")
+
+    def adjust_logits(self, logits, adjustments, out=None, stream=None):
+        """Penalties, biases and masks (a LogitAdjustments) on the frontier's rows ahead of expand_layer, each row with the tokens of its own path;
+        in place unless `out` is given.  logits as for expand_layer."""
+        from .serving import adjust_frontier_logits
+        return adjust_frontier_logits(self, logits, adjustments, out, stream)
 
     def frontier(self):
         t, s, n = ctypes.c_void_p(), ctypes.c_void_p(), ctypes.c_void_p()

@@ -18,6 +18,7 @@
 #include "k_direct.h"
 #include "k_logits.h"
 #include "k_tree.h"
+#include "verify.h"
 
 using namespace c2t;
 
@@ -462,6 +463,23 @@ int c2t_expand_layer(c2t_ctx* x, const void* logits, int64_t row_stride_elems, v
   if (timed) x->ev_used += 2;
   x->layer += 1;
   return C2T_OK;
+}
+
+int c2t_adjust_logits(c2t_ctx* x, const c2t_adjustments* t, const void* logits, int64_t row_stride_elems, void* out, int64_t out_row_stride_elems, void* stream) {
+  if (!x) return C2T_ERR_INVALID_ARG;
+  const c2t_config& c = x->cfg;
+  AdjustArgs a{};
+  int rc = fill_adjust(a, t);
+  if (rc) return rc;
+  const int esz = c.logits_dtype == C2T_BF16 ? 2 : 4;
+  a.in = (const char*)logits; a.out = (char*)out;
+  a.batch = c.batch; a.rows = c.max_frontier; a.vocab = c.vocab;
+  a.n_rows = x->st.nf[(x->layer < 0 ? 0 : x->layer) & 1];
+  a.row_node = x->st.fr_node; a.node_token = x->st.t_tok; a.node_parent = x->st.t_parent; a.nodes = c.budget; a.n_nodes = x->st.n_nodes;
+  rc = check_adjust(a, c.logits_dtype, row_stride_elems, out_row_stride_elems);
+  if (rc) return rc;
+  if (x->layer < 0 || x->layer >= c.max_depth || x->finalized) return C2T_ERR_STATE;
+  return launch_adjust(a, c.logits_dtype, (hipStream_t)stream);
 }
 
 int c2t_get_frontier(c2t_ctx* x, const int32_t** tokens, const int32_t** parent_slot, const int32_t** n_frontier) {

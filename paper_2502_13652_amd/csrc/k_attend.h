@@ -1,0 +1,439 @@
+// Attention of new tokens (one token, a tree behind its root, a chunk of a prompt) over a paged K/V cache.
+//
+//   s_j = scale q.k_j over the keys j that the row sees,  p_j = e^(s_j - m),  m = max s,  out = sum p_j v_j / sum p_j
+//
+// One pass over the keys: a wavefront keeps, for every row it has, the running maximum m (of s log2 e), the sum l of p and
+// sum p v, and multiplies the last two by 2^(m_old - m_new) where a tile raises m.  A row that sees no key has m = -inf, l = 0
+// and is put out as zeros.
+//
+// Rows: the query heads of one cached head share its keys, so rows are (slot, head of the group) with the head
+// fastest.  Products are taken transposed: S^T = K Q^T leaves in a lane one row (lane & 15) and 4 neighbouring keys of each
+// block of 16, which are just the operand that out^T = V^T P^T takes of two blocks: P never leaves its registers, and row
+// statistics are one number a lane, reduced over 4 lanes.
+#pragma once
+#include "k_common.h"
+#include "k_paged.h"
+
+namespace c2t {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+struct Bf16 {
+  typedef __bf16 T; typedef __bf16 T4 __attribute__((ext_vector_type(4))); typedef __bf16 T8 __attribute__((ext_vector_type(8)));
+  static __device__ __forceinline__ f32x4 mfma(T8 a, T8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+  static constexpr uint32_t EXPONENT = 0x7f80u;
+};
+struct F16 {
+  typedef _Float16 T; typedef _Float16 T4 __attribute__((ext_vector_type(4))); typedef _Float16 T8 __attribute__((ext_vector_type(8)));
+  static __device__ __forceinline__ f32x4 mfma(T8 a, T8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+  static constexpr uint32_t EXPONENT = 0x7c00u;
+};
+
+struct AttendArgs {
+  const char* q; char* out; float* lse;    // [batch][slots][heads][head_dim], strides in bytes; lse [batch][slots][heads] or null
+  int64_t q_batch, q_token, out_batch, out_token;
+  const int32_t* n_new;                    // [batch] or null: all slots
+  const uint8_t* mask;                     // [batch][nodes][nodes] or null
+  int32_t nodes, chain;                    // slots = chain + nodes
+  int32_t layer;
+  float scale_log2e;
+  float* part_o; float2* part_ml;          // records of parts: [2 target][rows][head_dim], [2 target][rows] (m, l)
+  AttendShape shape;
+};
+
+// What a workgroup, and the join of its unit, know of where they are.
+struct Unit { int b, len, n_new, row_tile, head, part, parts, slot0; };   // slot0: record of the unit's first part
+
+// Deals item `w` of the launch.  Every wavefront computes it for itself, each lane summing a stretch of sequences: no barrier.
+// units: w counts units, not their parts.  False: there is no such item.
+template <bool UNITS>
+__device__ __forceinline__ bool find_unit(const CacheView& c, const AttendArgs& a, int w, Unit* u) {
+  const int lane = lane_id(), each = div_up(c.batch, WAVE), b0 = min(lane * each, c.batch), b1 = min(b0 + each, c.batch);
+  double mine = 0.0;
+  auto of = [&](int b, int* n) { const int len = tokens_in_cache(c, c.length[b]); *n = new_tokens(c, len, a.n_new ? a.n_new[b] : a.shape.slots, a.shape.slots); return len; };
+  for (int b = b0; b < b1; ++b) { int n; const int len = of(b, &n); mine += (double)sequence_tiles(c, a.shape, len, n); }
+  const int per = tiles_per_part(a.shape, (int64_t)wave_sum(mine));
+  int items = 0, slots = 0;
+  for (int b = b0; b < b1; ++b) {
+    int n; const int len = of(b, &n);
+    const int parts = sequence_parts(c, a.shape, per, len, n), p = parts_of(a.shape, per, len, n);
+    items += UNITS ? parts / p : parts;
+    if (p > 1) slots += parts;
+  }
+  int item0 = wave_scan_incl(items) - items, slot0 = wave_scan_incl(slots) - slots;
+  const uint64_t has = __ballot(w >= item0 && w < item0 + items);
+  if (has == 0ull) return false;
+  int found = -1, rel = 0, at_slot = 0;
+  if (w >= item0 && w < item0 + items) {
+    for (int b = b0; b < b1; ++b) {
+      int n; const int len = of(b, &n);
+      const int parts = sequence_parts(c, a.shape, per, len, n), p = parts_of(a.shape, per, len, n), here = UNITS ? parts / p : parts;
+      if (w < item0 + here) { found = b; rel = w - item0; at_slot = slot0; break; }
+      item0 += here;
+      if (p > 1) slot0 += parts;
+    }
+  }
+  const int from = __builtin_ctzll(has);
+  u->b = __builtin_amdgcn_readlane(found, from);
+  rel = __builtin_amdgcn_readlane(rel, from);
+  at_slot = __builtin_amdgcn_readlane(at_slot, from);
+  int n; u->len = uniform(of(u->b, &n)); u->n_new = uniform(n);
+  u->parts = parts_of(a.shape, per, u->len, u->n_new);
+  const int tiles = row_tiles(a.shape, u->n_new);
+  // row tiles of the same keys next to each other: they run at the same time
+  u->row_tile = rel % tiles; rel /= tiles;
+  if (UNITS) { u->part = 0; u->head = rel; } else { u->part = rel % u->parts; u->head = rel / u->parts; }
+  u->slot0 = at_slot + (u->head * tiles + u->row_tile) * u->parts;
+  return true;
+}
+
+template <typename E, int D> struct TileLayout {
+  // rows of a tile in LDS, bytes: the reads of 16 rows' fragments (K) and of four rows' 32 bytes (V, transposed) then fall on different banks
+  static constexpr int K_ROW = D * 2 + 16, V_ROW = D * 2 + 32;
+};
+
+__device__ __forceinline__ uint4 zero16() { return make_uint4(0u, 0u, 0u, 0u); }
+template <typename E> __device__ __forceinline__ uint32_t odd_halves(uint32_t w) {     // halves whose exponent is all ones, as a mask of them
+  return ((w & E::EXPONENT) == E::EXPONENT ? 0xffffu : 0u) | (((w >> 16) & E::EXPONENT) == E::EXPONENT ? 0xffff0000u : 0u);
+}
+
+// A product's result, used in a later block than the product: the compiler has been seen to read it there before the matrix unit has
+// written it (it counts the wait from the wrong instruction), so it is moved to ordinary registers in the product's own block, where the wait is right.
+template <typename X> __device__ __forceinline__ void settle(X& x) { asm volatile("" : "+v"(x)); }
+
+// MT tiles of 16 rows a wavefront; RW wavefronts share the key tiles and have rows of their own, or (RW = 1) KW wavefronts have the same rows
+// and key tiles of their own, joined at the end.  KB blocks of 16 keys a tile.
+template <typename E, int D, int MT, int RW, int KW, int KB>
+__global__ __launch_bounds__(64 * RW * KW) void k_attend(CacheView c, AttendArgs a) {
+  static_assert(RW == 1 || KW == 1, "rows or keys");
+  typedef typename E::T T; typedef typename E::T4 T4; typedef typename E::T8 T8;
+  typedef TileLayout<E, D> L;
+  constexpr int NT = 64 * RW * KW, KT = 16 * KB, CH = D / 8 /* 16-byte chunks of a row */, DB = D / 16, DK = D / 32;
+  constexpr int SHARERS = 64 * RW;                          // threads that load a tile together
+  constexpr int LOADS = KT * CH / SHARERS;                  // chunks each of K and V a thread
+  constexpr bool K_LDS = RW > 1;
+  constexpr int TILE_BYTES = KT * L::V_ROW + (K_LDS ? KT * L::K_ROW : 0);
+  constexpr int JOIN_BYTES = KW > 1 ? KW * 16 * (D + 2) * 4 : 0;
+  constexpr int LDS_BYTES = KW * TILE_BYTES > JOIN_BYTES ? KW * TILE_BYTES : JOIN_BYTES;
+  __shared__ __align__(16) char lds[LDS_BYTES];
+  __shared__ int odd_tile;
+
+  Unit u;
+  if (!find_unit<false>(c, a, blockIdx.x, &u)) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 15, quad = lane >> 4;
+  const int rw = RW > 1 ? wave : 0, kw = KW > 1 ? wave : 0;
+  const int rows = u.n_new * a.shape.group, G = a.shape.group;
+  const int wave_row0 = u.row_tile * a.shape.rows_per_tile + rw * 16 * MT;
+  char* const v_lds = lds + kw * TILE_BYTES;
+  char* const k_lds = v_lds + KT * L::V_ROW;
+
+  // this lane's rows and their queries
+  int slot[MT];
+  T8 q[MT][DK];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    const int r = wave_row0 + m * 16 + col;
+    slot[m] = r < rows ? r / G : -1;
+#pragma unroll
+    for (int kk = 0; kk < DK; ++kk) {
+      if (slot[m] >= 0) q[m][kk] = *(const T8*)(a.q + u.b * a.q_batch + slot[m] * a.q_token + (((int64_t)u.head * G + r % G) * D + kk * 32 + quad * 8) * 2);
+      else q[m][kk] = T8{};
+    }
+  }
+
+  const int seen = keys_seen(a.shape, u.len, u.n_new, a.chain, u.row_tile);
+  int tile, tile_end;
+  part_range(key_tiles(a.shape, seen), u.parts, u.part, &tile, &tile_end);
+  // keys below this are seen by every row of the wavefront
+  const int first_slot = wave_row0 < rows ? wave_row0 / G : 0;
+  const int all_see = u.len + min(first_slot + 1, a.chain);
+  const int32_t* const table = c.table + (int64_t)u.b * c.max_pages;
+  const uint8_t* const mask = a.mask ? a.mask + (int64_t)u.b * a.nodes * a.nodes : nullptr;
+  auto sees = [&](int t, int key) {                          // slot t, key below `seen`
+    const int s = key - u.len;
+    if (s < 0) return true;
+    if (t < a.chain) return s <= t;
+    if (s < a.chain) return true;
+    return mask[(int64_t)(t - a.chain) * a.nodes + (s - a.chain)] != 0;
+  };
+  // the page that a block of 16 keys lies in, -1 behind the last key or if the table has none
+  auto page_of = [&](int key) { return key < seen ? valid_page(c, table[key >> c.page_shift]) : -1; };
+  const int in_page = (1 << c.page_shift) - 1;
+
+  f32x4 o[MT][DB];
+  float m_run[MT], l_run[MT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    m_run[m] = -INFINITY; l_run[m] = 0.f;
+#pragma unroll
+    for (int d = 0; d < DB; ++d) o[m][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  uint4 vr[LOADS];
+  uint4 kr[K_LDS ? LOADS : KB * DK];
+  const int lt = RW > 1 ? tid : lane;                        // this thread among those that load the tile
+  auto request = [&](int t) {
+    const int key0 = t * KT;
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+      const int chunk = j * SHARERS + lt, row = chunk / CH, key = key0 + row;
+      const int page = page_of(key0 + row / 16 * 16);
+      const bool ok = page >= 0 && key < seen;               // rows behind the last key hold anything
+      const int64_t off = (row_offset(c, a.layer, ok ? page : 0, u.head, key & in_page) + chunk % CH * 8) * 2;
+      vr[j] = ok ? *(const uint4*)(c.v + off) : zero16();
+      if (K_LDS) kr[j] = ok ? *(const uint4*)(c.k + off) : zero16();
+    }
+    if (!K_LDS) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        const int page = page_of(key0 + kb * 16), key = key0 + kb * 16 + col;
+        const bool ok = page >= 0 && key < seen;
+        const int64_t off = row_offset(c, a.layer, ok ? page : 0, u.head, key & in_page) * 2 + quad * 16;
+#pragma unroll
+        for (int kk = 0; kk < DK; ++kk) kr[kb * DK + kk] = ok ? *(const uint4*)(c.k + off + kk * 64) : zero16();
+      }
+    }
+  };
+
+  const int step = KW;
+  tile += kw;
+  // (RW > 1: the loop is the same for all wavefronts, which meet in it)
+  if (tile < tile_end) request(tile);
+  for (; tile < tile_end; tile += step) {
+    const int key0 = tile * KT;
+    // keys of the tile that some row may not see, or that lie on no page
+    bool whole = key0 + KT <= all_see;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) whole = whole && page_of(key0 + kb * 16) >= 0;
+    const bool mixed = key0 + KT > u.len;                    // holds new tokens: some rows may see a value that others do not
+    bool odd = false;
+    if (RW > 1) { if (tid == 0) odd_tile = 0; __syncthreads(); }
+    if (mixed) {
+      // 0 x infinity is not 0: a value that is not finite is left out of the product and added for the rows that see it
+#pragma unroll
+      for (int j = 0; j < LOADS; ++j) {
+        const uint32_t x = odd_halves<E>(vr[j].x), y = odd_halves<E>(vr[j].y), z = odd_halves<E>(vr[j].z), w = odd_halves<E>(vr[j].w);
+        odd = odd || (x | y | z | w) != 0u;
+        vr[j].x &= ~x; vr[j].y &= ~y; vr[j].z &= ~z; vr[j].w &= ~w;
+      }
+      odd = __any(odd);
+      if (RW > 1 && odd && lane == 0) odd_tile = 1;
+    }
+    T8 kf[KB][DK];
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+      const int chunk = j * SHARERS + lt, row = chunk / CH;
+      *(uint4*)(v_lds + row * L::V_ROW + chunk % CH * 16) = vr[j];
+      if (K_LDS) *(uint4*)(k_lds + row * L::K_ROW + chunk % CH * 16) = kr[j];
+    }
+    if (!K_LDS) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int kk = 0; kk < DK; ++kk) kf[kb][kk] = __builtin_bit_cast(T8, kr[kb * DK + kk]);
+    }
+    if (RW > 1) __syncthreads(); else { __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront"); __builtin_amdgcn_wave_barrier(); __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront"); }
+    if (RW > 1) odd = odd_tile != 0;
+    if (tile + step < tile_end) request(tile + step);
+
+    f32x4 s[MT][KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+#pragma unroll
+      for (int m = 0; m < MT; ++m) s[m][kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kk = 0; kk < DK; ++kk) {
+        const T8 k = K_LDS ? *(const T8*)(k_lds + (kb * 16 + col) * L::K_ROW + kk * 64 + quad * 16) : kf[kb][kk];
+#pragma unroll
+        for (int m = 0; m < MT; ++m) s[m][kb] = E::mfma(k, q[m][kk], s[m][kb]);
+      }
+    }
+
+    // Scores leave the matrix unit's registers here, in the block of the products: see settle().
+    float pf[MT][KB][4];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) { pf[m][kb][r] = s[m][kb][r] * a.scale_log2e; settle(pf[m][kb][r]); }
+    if (!whole) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        const bool there = page_of(key0 + kb * 16) >= 0;
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int key = key0 + kb * 16 + quad * 4 + r;
+            if (!(there && key < seen && slot[m] >= 0 && sees(slot[m], key))) pf[m][kb][r] = -INFINITY;
+          }
+      }
+    }
+
+    T8 p[MT][KB / 2];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) top = fmaxf(top, pf[m][kb][r]);
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float m_new = fmaxf(m_run[m], top), ref = m_new == -INFINITY ? 0.f : m_new;
+      const float back = __builtin_amdgcn_exp2f(m_run[m] - ref);
+      m_run[m] = m_new;
+      float sum = 0.f;
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) { pf[m][kb][r] = __builtin_amdgcn_exp2f(pf[m][kb][r] - ref); sum += pf[m][kb][r]; }
+      l_run[m] = l_run[m] * back + sum;
+#pragma unroll
+      for (int d = 0; d < DB; ++d) o[m][d] *= back;
+      // P in the operands' 16 bits: relative 2^-9 (2^-12 for halves) a weight, of either sign
+#pragma unroll
+      for (int h = 0; h < KB / 2; ++h)
+#pragma unroll
+        for (int r = 0; r < 8; ++r) p[m][h][r] = (T)pf[m][h * 2 + r / 4][r % 4];
+    }
+#pragma unroll
+    for (int h = 0; h < KB / 2; ++h)
+#pragma unroll
+      for (int d = 0; d < DB; ++d) {
+        // keys 4 quad + r of two blocks, as P holds them
+        const char* at = v_lds + (h * 32 + quad * 4 + col / 4) * L::V_ROW + d * 32 + col % 4 * 8;
+        typedef __attribute__((address_space(3))) s16x4* lds4;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at + 16 * L::V_ROW));
+        struct { s16x4 a, b; } pair{lo, hi};
+        const T8 v = __builtin_bit_cast(T8, pair);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) o[m][d] = E::mfma(v, p[m][h], o[m][d]);
+      }
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int d = 0; d < DB; ++d) settle(o[m][d]);
+    if (mixed && odd) {
+      for (int kk = 0; kk < KT; ++kk) {
+        const int key = key0 + kk, page = page_of(key0 + kk / 16 * 16);
+        if (page < 0 || key >= seen) continue;
+        const char* row = c.v + row_offset(c, a.layer, page, u.head, key & in_page) * 2;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          float w = 0.f;
+#pragma unroll
+          for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) { const float x = __shfl(pf[m][kb][r], col + (kk % 16 / 4) * 16); if (kb == kk / 16 && r == kk % 4) w = x; }
+          if (slot[m] < 0 || !sees(slot[m], key)) continue;
+#pragma unroll
+          for (int d = 0; d < DB; ++d) {
+            const T4 v = *(const T4*)(row + (d * 16 + quad * 4) * 2);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) { const float x = (float)v[r]; if (!(__builtin_fabsf(x) < INFINITY)) o[m][d][r] += w * x; }
+          }
+        }
+      }
+    }
+    if (RW > 1) __syncthreads();
+  }
+
+#pragma unroll
+  for (int m = 0; m < MT; ++m) { l_run[m] += __shfl_xor(l_run[m], 16); l_run[m] += __shfl_xor(l_run[m], 32); }
+
+  // what this workgroup has of a row: to the record of its part, or out
+  auto put = [&](int row_in_tile, int t, int g, int dim, f32x4 x, float m, float l, bool first) {
+    if (u.parts > 1) {
+      const int64_t rec = (int64_t)(u.slot0 + u.part) * a.shape.rows_per_tile + row_in_tile;
+      *(f32x4*)(a.part_o + rec * D + dim) = x;
+      if (first) a.part_ml[rec] = make_float2(m, l);
+    } else {
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      T4 y;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) y[r] = (T)(x[r] * inv);
+      const int64_t head = (int64_t)u.head * G + g;
+      *(T4*)(a.out + u.b * a.out_batch + t * a.out_token + (head * D + dim) * 2) = y;
+      if (first && a.lse) a.lse[((int64_t)u.b * a.shape.slots + t) * c.kv_heads * G + head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+    }
+  };
+  if (KW == 1) {
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      const int r = wave_row0 + m * 16 + col;
+      if (slot[m] < 0) continue;
+#pragma unroll
+      for (int d = 0; d < DB; ++d) put(rw * 16 * MT + m * 16 + col, slot[m], r - slot[m] * G, d * 16 + quad * 4, o[m][d], m_run[m], l_run[m], d == 0 && quad == 0);
+    }
+  } else {
+    // the wavefronts' results of 16 rows at a time through LDS
+    float* const jo = (float*)lds;                           // [KW][16][D]
+    float* const jm = jo + KW * 16 * D; float* const jl = jm + KW * 16;
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      __syncthreads();
+#pragma unroll
+      for (int d = 0; d < DB; ++d) *(f32x4*)(jo + (kw * 16 + col) * D + d * 16 + quad * 4) = o[m][d];
+      if (quad == 0) { jm[kw * 16 + col] = m_run[m]; jl[kw * 16 + col] = l_run[m]; }
+      __syncthreads();
+      for (int i = tid; i < 16 * D / 4; i += NT) {
+        const int row = i / (D / 4), dim = i % (D / 4) * 4, r = wave_row0 + m * 16 + row;
+        if (r >= rows) continue;
+        float mm = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < KW; ++w) mm = fmaxf(mm, jm[w * 16 + row]);
+        const float ref = mm == -INFINITY ? 0.f : mm;
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+        float l = 0.f;
+#pragma unroll
+        for (int w = 0; w < KW; ++w) {
+          const float f = __builtin_amdgcn_exp2f(jm[w * 16 + row] - ref);
+          l += f * jl[w * 16 + row];
+          x += f * *(const f32x4*)(jo + (w * 16 + row) * D + dim);
+        }
+        const int t = r / G;
+        put(m * 16 + row, t, r - t * G, dim, x, mm, l, dim == 0);
+      }
+    }
+  }
+}
+
+// The parts of a unit joined.  One workgroup a unit; units of one part are done already.
+constexpr int JOIN_NT = 256;
+template <typename E, int D>
+__global__ __launch_bounds__(JOIN_NT) void k_attend_join(CacheView c, AttendArgs a) {
+  typedef typename E::T T; typedef typename E::T4 T4;
+  Unit u;
+  if (!find_unit<true>(c, a, blockIdx.x, &u) || u.parts == 1) return;
+  const int G = a.shape.group, row0 = u.row_tile * a.shape.rows_per_tile, rows = min(u.n_new * G - row0, a.shape.rows_per_tile);
+  for (int i = threadIdx.x; i < rows * (D / 4); i += JOIN_NT) {
+    const int row = i / (D / 4), dim = i % (D / 4) * 4;
+    const float2* ml = a.part_ml + (int64_t)u.slot0 * a.shape.rows_per_tile + row;
+    const float* po = a.part_o + ((int64_t)u.slot0 * a.shape.rows_per_tile + row) * D + dim;
+    float mm = -INFINITY;
+    for (int p = 0; p < u.parts; ++p) mm = fmaxf(mm, ml[(int64_t)p * a.shape.rows_per_tile].x);
+    const float ref = mm == -INFINITY ? 0.f : mm;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    float l = 0.f;
+    for (int p = 0; p < u.parts; ++p) {
+      const float2 r = ml[(int64_t)p * a.shape.rows_per_tile];
+      const float f = __builtin_amdgcn_exp2f(r.x - ref);
+      l += f * r.y;
+      x += f * *(const f32x4*)(po + (int64_t)p * a.shape.rows_per_tile * D);
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    T4 y;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) y[r] = (T)(x[r] * inv);
+    const int at = row0 + row, t = at / G;
+    const int64_t head = (int64_t)u.head * G + (at - t * G);
+    *(T4*)(a.out + u.b * a.out_batch + t * a.out_token + (head * D + dim) * 2) = y;
+    if (dim == 0 && a.lse) a.lse[((int64_t)u.b * a.shape.slots + t) * c.kv_heads * G + head] = l == 0.f ? -INFINITY : (mm + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+  }
+}
+
+}  // namespace c2t

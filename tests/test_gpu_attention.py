@@ -1,0 +1,272 @@
+"""Attention over the paged cache against the definition in 64 bits: types, head layouts, lengths, masks that leave rows empty, values that
+must not matter, pages that are none, strides, streams, graphs."""
+import pytest
+import torch
+
+from _serving import attention_reference, gen, make_cache, random_tree
+
+pytestmark = pytest.mark.gpu
+BF, HF = torch.bfloat16, torch.float16
+
+
+def check(cache, layer, q, n_new, mask=None, scale=None, lse=True, tag="", **kw):
+    B, T, H, D = q.shape
+    scale = D ** -0.5 if scale is None else scale
+    n_list = [T] * B if n_new is None else n_new
+    n_dev = None if n_new is None else torch.tensor(n_new, dtype=torch.int32, device="cuda")
+    out = torch.full((B, T, H, D), 7.0, dtype=q.dtype, device="cuda")
+    ls = torch.full((B, T, H), 7.0, device="cuda") if lse else None
+    print("attention", tag, tuple(q.shape), "nodes", 0 if mask is None else mask.shape[-1], "lens", cache.length.tolist()[:8], "n_new", n_list[:8], flush=True)
+    got = cache.attention(layer, q, n_new=n_dev, mask=mask, scale=scale, out=out, lse=ls, **kw)
+    torch.cuda.synchronize()
+    assert got is out
+    caps = cache.max_pages * cache.page_size
+    lens = [min(max(l, 0), caps) for l in cache.length.tolist()]
+    real = [max(0, min(n, T, caps - l)) for n, l in zip(n_list, lens)]
+    want, want_lse, tol, tol_lse = attention_reference(cache, layer, q, real, mask, scale, lens)
+    for b in range(B):
+        n = real[b]
+        assert bool((out[b, n:] == 7.0).all()), "rows behind n_new were written"
+        if ls is not None:
+            assert bool((ls[b, n:] == 7.0).all())
+        if n == 0:
+            continue
+        w, g, t = want[b, :n], out[b, :n].double(), tol[b, :n]
+        bad = torch.isnan(w)
+        assert bool((torch.isnan(g) == bad).all()), "NaN where it should not be, or none"
+        inf = torch.isinf(w)
+        assert bool((g[inf] == w[inf]).all())
+        err = torch.where(bad | inf, 0.0, (g - w).abs() - torch.where(torch.isfinite(t), t, 0.0))
+        assert float(err.max()) <= 0, "%s seq %d: off by %g more than %g" % (tag, b, float(err.max()), float(t.flatten()[err.flatten().argmax()]))
+        if ls is not None:
+            w, g, t = want_lse[b, :n], ls[b, :n].double(), tol_lse[b, :n]
+            same = (w == g) | (torch.isnan(w) & torch.isnan(g))
+            assert bool((same | ((g - w).abs() <= t)).all()), "%s seq %d lse" % (tag, b)
+    return out
+
+
+def queries(B, T, H, D, dtype, seed, fused=0):
+    """Contiguous, or a slice of a wider projection's output."""
+    x = torch.randn((B, T, H + fused, D), generator=gen(seed, "cuda"), device="cuda").to(dtype)
+    return x[:, :, :H]
+
+
+# rows a cached head: 1 .. 16, 17 .. 32, 33 .. 64 and more take different kernels
+SHAPES = [(1, 1, 1, 1), (3, 1, 8, 2), (2, 1, 32, 1), (2, 3, 24, 4), (2, 17, 4, 4), (3, 8, 16, 4), (2, 9, 28, 4), (1, 33, 4, 1), (2, 40, 12, 2), (1, 130, 6, 2)]
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("B,T,H,Hkv", SHAPES)
+def test_causal_chunks(B, T, H, Hkv, D, dtype):
+    lens = [0, 77, 300][:B] if B > 1 else [45]
+    cache = make_cache(lens, T, 16, Hkv, D, dtype, seed=B * 1000 + T * 10 + H)
+    check(cache, 0, queries(B, T, H, D, dtype, T, fused=3), None, tag="causal")
+
+
+@pytest.mark.parametrize("ps", [16, 32, 64, 128, 256])
+def test_page_sizes_and_lengths_round_tiles_and_pages(ps):
+    lens = [0, 1, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257, 511, 513]
+    for T in (1, 2, 21):
+        cache = make_cache(lens, T, ps, 2, 64, BF, seed=ps + T, layers=3)
+        check(cache, 2, queries(len(lens), T, 6, 64, BF, ps), None, tag="page %d" % ps)
+
+
+@pytest.mark.parametrize("D,dtype,H,Hkv", [(128, BF, 8, 2), (64, HF, 4, 4), (256, BF, 4, 1), (128, HF, 32, 4)])
+@pytest.mark.parametrize("chain,nodes,width", [(1, 1, 1), (1, 10, 4), (1, 60, 10), (0, 12, 4), (5, 33, 16), (2, 131, 32)])
+def test_trees(chain, nodes, width, D, dtype, H, Hkv):
+    lens = [0, 3, 90, 257]
+    T = chain + nodes
+    cache = make_cache(lens, T, 16, Hkv, D, dtype, seed=nodes)
+    mask = torch.stack([random_tree(nodes, width, gen(b + nodes))[1] for b in range(4)])
+    n_new = [T, chain + nodes // 2, 0, max(1, chain)]
+    for b, n in enumerate(n_new):                            # nodes a tree does not have: finalize_tree leaves zeros
+        mask[b, max(0, n - chain):] = 0
+        mask[b, :, max(0, n - chain):] = 0
+    check(cache, 0, queries(4, T, H, D, dtype, chain), n_new, mask.cuda(), tag="tree")
+
+
+def test_rows_that_see_nothing():
+    # no prefix, no chain: a node whose mask row is empty sees nothing; neither does one whose page there is none of
+    for H, Hkv in ((4, 4), (16, 2), (32, 1)):
+        cache = make_cache([0, 0, 40], 20, 16, Hkv, 128, BF, seed=3)
+        mask = torch.stack([random_tree(20, 5, gen(b))[1] for b in range(3)])
+        mask[0, 7] = 0
+        mask[1] = 0
+        mask[2, 19] = 0
+        out = check(cache, 0, queries(3, 20, H, 128, BF, 1), [20, 20, 20], mask.cuda(), tag="empty rows")
+        assert bool((out[0, 7] == 0).all()) and bool((out[1] == 0).all()) and bool((out[2, 19] != 0).any())
+        cache.page_table[0] = -1
+        out = check(cache, 0, queries(3, 20, H, 128, BF, 1), [20, 20, 20], mask.cuda(), tag="no pages")
+        assert bool((out[0] == 0).all())
+
+
+@pytest.mark.parametrize("H,T", [(2, 1), (8, 3), (8, 8), (16, 40)])
+def test_pages_that_are_none_are_left_out(H, T):
+    cache = make_cache([100, 200, 30], T, 16, 2, 64, BF, seed=9)
+    cache.page_table[0, 2] = -1
+    cache.page_table[1, 0] = cache.pages
+    cache.page_table[1, 5] = 2 ** 31 - 1
+    cache.page_table[2, 1] = -2 ** 31
+    check(cache, 0, queries(3, T, H, 64, BF, 1), None, tag="bad pages")
+
+
+def test_lengths_and_counts_out_of_range():
+    cache = make_cache([40, 40, 40, 40], 8, 16, 2, 64, BF, seed=1)
+    cache.length.copy_(torch.tensor([-5, 10 ** 9, 44, 40], dtype=torch.int32))
+    check(cache, 0, queries(4, 8, 4, 64, BF, 2), [8, 8, 100, -3], tag="clamped")
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("H,Hkv,T0", [(2, 2, 1), (8, 2, 1), (16, 2, 1), (8, 1, 5)])
+def test_what_a_row_does_not_see_cannot_matter(H, Hkv, T0, D):
+    """Infinities and NaN behind the last token, in slots behind n_new, and in nodes that a row does not see."""
+    nodes, chain = 12, T0
+    T = chain + nodes
+    lens = [5, 70, 31]
+    cache = make_cache(lens, T, 16, Hkv, D, BF, seed=21)
+    mask = torch.stack([random_tree(nodes, 4, gen(b))[1] for b in range(3)])
+    n_new = [T, T - 4, T]
+    mask[1, nodes - 4:] = 0
+    mask[1, :, nodes - 4:] = 0
+    q = queries(3, T, H, D, BF, 5)
+    clean = check(cache, 0, q, n_new, mask.cuda(), tag="clean").clone()
+    bad = torch.tensor([float("nan"), float("inf"), float("-inf"), torch.finfo(BF).max], device="cuda").to(BF)
+
+    def poison(b, at, what, x):
+        page, row = int(cache.page_table[b, at // 16]), at % 16
+        what[0, page, :, row] = x
+    held = [-(-(l + T) // 16) * 16 for l in lens]
+    for b in range(3):                                       # behind the last token
+        for at in range(lens[b] + n_new[b], held[b]):
+            poison(b, at, cache.k, bad[at % 4])
+            poison(b, at, cache.v, bad[(at + 1) % 4])
+    dirty = check(cache, 0, q, n_new, mask.cuda(), tag="behind the last")
+    for b in range(3):
+        assert torch.equal(dirty[b, :n_new[b]], clean[b, :n_new[b]])
+    leaf = nodes - 1                                         # nobody else sees the last node
+    assert int(mask[0, :, leaf].sum()) == 1
+    for kind in range(3):
+        poison(0, lens[0] + chain + leaf, cache.v, bad[kind])
+        poison(0, lens[0] + chain + leaf, cache.k, bad[3 - kind if kind else 0])
+        got = check(cache, 0, q, n_new, mask.cuda(), tag="a node that others do not see")
+        assert torch.equal(got[0, :T - 1], clean[0, :T - 1])
+    # one element of a value that two rows see
+    page, row = int(cache.page_table[2, (lens[2] + chain) // 16]), (lens[2] + chain) % 16
+    cache.v[0, page, :, row, 3] = float("inf")
+    got = check(cache, 0, q, n_new, mask.cuda(), tag="an infinite value")
+    sees = mask[2, :, 0].bool()
+    assert bool(torch.isinf(got[2, chain:, :, 3][sees.cuda()]).all()) and torch.equal(got[2, chain:][~sees.cuda()], clean[2, chain:][~sees.cuda()])
+
+
+@pytest.mark.parametrize("B,T,H,Hkv,D,lens", [(1, 1, 8, 1, 128, [20011]), (2, 1, 4, 4, 64, [9000, 3]), (1, 4, 32, 4, 128, [7777]), (3, 20, 16, 2, 128, [5000, 1, 12000]),
+                                              (1, 2, 16, 1, 256, [6001]), (1, 40, 8, 2, 256, [3003]), (70, 1, 8, 2, 64, None), (130, 2, 4, 1, 64, None)])
+def test_long_sequences_are_split_and_joined(B, T, H, Hkv, D, lens):
+    lens = lens or [(b * 37) % 900 + (6000 if b == 5 else 0) for b in range(B)]
+    cache = make_cache(lens, T, 32, Hkv, D, BF, seed=B)
+    check(cache, 0, queries(B, T, H, D, BF, 3), [T - (b % 2) * (T > 1) for b in range(B)], tag="split")
+
+
+def test_a_long_prompt_in_chunks():
+    cache = make_cache([0, 700], 600, 64, 2, 64, HF, seed=4)
+    check(cache, 0, queries(2, 600, 6, 64, HF, 3), [600, 333], tag="chunk")
+
+
+def test_large_scores_and_scales():
+    cache = make_cache([64, 5], 3, 16, 2, 128, BF, seed=8)
+    q = queries(2, 3, 4, 128, BF, 3)
+    check(cache, 0, q, None, scale=0.0, tag="flat")
+    cache.k.mul_(30)
+    check(cache, 0, q, None, scale=1.0, tag="sharp")
+    q[0, 0] = float("nan")
+    q[1, 2, 1, 5] = float("inf")
+    check(cache, 0, q, None, tag="queries that are no numbers")
+
+
+def test_offsets_past_32_bits():
+    # the last layer's pages begin beyond 2^32 bytes, and beyond 2^31 elements, of each pool
+    from paper_2502_13652_amd import PagedCache
+    layers, pages, Hkv, ps, D = 9, 1024, 8, 256, 128
+    cache = PagedCache(2, layers, pages, ps, Hkv, D, 8, dtype=BF)
+    assert cache.k.numel() > 2 ** 31
+    small = make_cache([300, 777], 2, ps, Hkv, D, BF, seed=2)
+    n = small.pages
+    cache.k[layers - 1, pages - n:] = small.k[0]
+    cache.v[layers - 1, pages - n:] = small.v[0]
+    t = small.page_table
+    cache.page_table[:, :t.shape[1]] = torch.where(t >= 0, t + (pages - n), t)
+    cache.length.copy_(small.length)
+    q = queries(2, 2, 16, D, BF, 1)
+    a, b = cache.attention(layers - 1, q), small.attention(0, q)
+    assert torch.equal(a, b)
+
+
+def test_strided_outputs_and_single_heads():
+    cache = make_cache([33, 64], 5, 16, 1, 64, BF, seed=6)
+    q = queries(2, 5, 3, 64, BF, 2, fused=2)
+    want = cache.attention(0, q)
+    wide = torch.full((2, 5, 7, 64), 3.0, dtype=BF, device="cuda")
+    out = wide[:, :, 2:5]
+    cache.attention(0, q, out=out)
+    assert torch.equal(out, want) and bool((wide[:, :, :2] == 3).all()) and bool((wide[:, :, 5:] == 3).all())
+    one = q[:, :, :1]
+    assert torch.equal(cache.attention(0, one), want[:, :, :1])
+
+
+def test_the_same_call_gives_the_same_bits_on_streams_and_in_graphs():
+    lens = [5000, 10, 900]
+    cache = make_cache(lens, 33, 16, 2, 128, BF, seed=12)
+    mask = torch.stack([random_tree(32, 8, gen(b))[1] for b in range(3)]).cuda()
+    q = queries(3, 33, 8, 128, BF, 4)
+    n_new = torch.tensor([33, 20, 1], dtype=torch.int32, device="cuda")
+    want = cache.attention(0, q, n_new=n_new, mask=mask, out=torch.zeros_like(q))
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    got = torch.zeros_like(q)
+    cache.attention(0, q, n_new=n_new, mask=mask, out=got, stream=s)
+    s.synchronize()
+    assert torch.equal(got, want)
+    out = torch.zeros_like(q)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        cache.attention(0, q, n_new=n_new, mask=mask, out=out)
+    for length in ([5000, 10, 900], [1, 3000, 0], [4999, 11, 901]):
+        cache.length.copy_(torch.tensor(length, dtype=torch.int32))
+        out.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        again = cache.attention(0, q, n_new=n_new, mask=mask, out=torch.zeros_like(q))
+        torch.cuda.synchronize()
+        assert torch.equal(out, again)
+
+
+def test_refusals():
+    from paper_2502_13652_amd import PagedCache
+    from paper_2502_13652_amd.binding import C2TError
+    cache = make_cache([10, 20], 4, 16, 2, 64, BF, seed=1)
+    q = queries(2, 4, 4, 64, BF, 1)
+    for bad in (q.float(), q[:1], q[:, :, :, :32], q.transpose(1, 2), q.cpu()):
+        with pytest.raises(ValueError):
+            cache.attention(0, bad)
+    for kw in (dict(n_new=torch.zeros(2, device="cuda")), dict(n_new=torch.zeros(3, dtype=torch.int32, device="cuda")),
+               dict(mask=torch.zeros((2, 3, 4), dtype=torch.uint8, device="cuda")), dict(mask=torch.zeros((2, 3, 3), device="cuda")),
+               dict(lse=torch.zeros((2, 4, 3), device="cuda")), dict(out=torch.zeros((2, 4, 4, 32), dtype=BF, device="cuda"))):
+        with pytest.raises(ValueError):
+            cache.attention(0, q, **kw)
+    for kw, code in ((dict(layer=1), -1), (dict(layer=-1), -1), (dict(layer=0, mask=torch.zeros((2, 5, 5), dtype=torch.uint8, device="cuda")), -1),
+                     (dict(layer=0, scale=float("nan")), -1), (dict(layer=0, scale=-1.0), -1)):
+        with pytest.raises(C2TError) as e:
+            cache.attention(q=q, **kw)
+        assert e.value.code == code
+    with pytest.raises(C2TError) as e:
+        cache.attention(0, q[:, :, :3])                      # three query heads over two cached ones
+    assert e.value.code == -1
+    with pytest.raises(C2TError) as e:
+        cache.attention(0, q, workspace=torch.zeros(256, dtype=torch.uint8, device="cuda"))
+    assert e.value.code == -3
+    for kw in (dict(page_size=24), dict(page_size=512), dict(head_dim=96), dict(batch=5000)):
+        a = dict(batch=2, layers=1, pages=4, page_size=16, kv_heads=1, head_dim=64, max_pages=2)
+        a.update(kw)
+        with pytest.raises(C2TError) as e:
+            PagedCache(**a)
+        assert e.value.code == -2
