@@ -45,13 +45,28 @@ struct AttendArgs {
 // What a workgroup, and the join of its unit, know of where they are.
 struct Unit { int b, len, n_new, row_tile, head, part, parts, slot0; };   // slot0: record of the unit's first part
 
-// Deals item `w` of the launch.  Every wavefront computes it for itself, each lane summing a stretch of sequences: no barrier.
-// units: w counts units, not their parts.  False: there is no such item.
+// Workgroups go to the chip's eight dies in turn; neighbouring items, whose rows share keys, belong on one die and its L2.
+constexpr int DIES = 8;
+__device__ __forceinline__ int item_of_workgroup(int workgroup, int items) {
+  const int run = div_up(items, DIES), i = workgroup / DIES;
+  const int w = workgroup % DIES * run + i;
+  return i < run && w < items ? w : -1;
+}
+
+// Deals a workgroup its item.  Every wavefront computes it for itself, each lane summing a stretch of sequences: no barrier.
+// UNITS: items are units, not their parts.  False: there is none for it.
 template <bool UNITS>
-__device__ __forceinline__ bool find_unit(const CacheView& c, const AttendArgs& a, int w, Unit* u) {
+__device__ __forceinline__ bool find_unit(const CacheView& c, const AttendArgs& a, int workgroup, Unit* u) {
   const int lane = lane_id(), each = div_up(c.batch, WAVE), b0 = min(lane * each, c.batch), b1 = min(b0 + each, c.batch);
+  auto load = [&](int b, int* n) {
+    const int len = tokens_in_cache(c, c.length[b]);
+    *n = new_tokens(c, len, a.n_new ? a.n_new[b] : a.shape.slots, a.shape.slots);
+    return len;
+  };
+  int n_first = 0, len_first = 0;
+  if (b0 < b1) len_first = load(b0, &n_first);
+  auto of = [&](int b, int* n) { if (b == b0) { *n = n_first; return len_first; } return load(b, n); };
   double mine = 0.0;
-  auto of = [&](int b, int* n) { const int len = tokens_in_cache(c, c.length[b]); *n = new_tokens(c, len, a.n_new ? a.n_new[b] : a.shape.slots, a.shape.slots); return len; };
   for (int b = b0; b < b1; ++b) { int n; const int len = of(b, &n); mine += (double)sequence_tiles(c, a.shape, len, n); }
   const int per = tiles_per_part(a.shape, (int64_t)wave_sum(mine));
   int items = 0, slots = 0;
@@ -61,16 +76,19 @@ __device__ __forceinline__ bool find_unit(const CacheView& c, const AttendArgs& 
     items += UNITS ? parts / p : parts;
     if (p > 1) slots += parts;
   }
-  int item0 = wave_scan_incl(items) - items, slot0 = wave_scan_incl(slots) - slots;
-  const uint64_t has = __ballot(w >= item0 && w < item0 + items);
+  const int items_to = wave_scan_incl(items);
+  const int w = item_of_workgroup(workgroup, __builtin_amdgcn_readlane(items_to, WAVE - 1));
+  int item0 = items_to - items, slot0 = wave_scan_incl(slots) - slots;
+  const bool here = w >= item0 && w < item0 + items;
+  const uint64_t has = __ballot(here);
   if (has == 0ull) return false;
-  int found = -1, rel = 0, at_slot = 0;
-  if (w >= item0 && w < item0 + items) {
+  int found = b0, rel = w - item0, at_slot = slot0;
+  if (here && each > 1) {
     for (int b = b0; b < b1; ++b) {
       int n; const int len = of(b, &n);
-      const int parts = sequence_parts(c, a.shape, per, len, n), p = parts_of(a.shape, per, len, n), here = UNITS ? parts / p : parts;
-      if (w < item0 + here) { found = b; rel = w - item0; at_slot = slot0; break; }
-      item0 += here;
+      const int parts = sequence_parts(c, a.shape, per, len, n), p = parts_of(a.shape, per, len, n), mine_here = UNITS ? parts / p : parts;
+      if (w < item0 + mine_here) { found = b; rel = w - item0; at_slot = slot0; len_first = len; n_first = n; break; }
+      item0 += mine_here;
       if (p > 1) slot0 += parts;
     }
   }
@@ -78,11 +96,12 @@ __device__ __forceinline__ bool find_unit(const CacheView& c, const AttendArgs& 
   u->b = __builtin_amdgcn_readlane(found, from);
   rel = __builtin_amdgcn_readlane(rel, from);
   at_slot = __builtin_amdgcn_readlane(at_slot, from);
-  int n; u->len = uniform(of(u->b, &n)); u->n_new = uniform(n);
+  u->len = __builtin_amdgcn_readlane(len_first, from);
+  u->n_new = __builtin_amdgcn_readlane(n_first, from);
   u->parts = parts_of(a.shape, per, u->len, u->n_new);
   const int tiles = row_tiles(a.shape, u->n_new);
-  // row tiles of the same keys next to each other: they run at the same time
-  u->row_tile = rel % tiles; rel /= tiles;
+  // row tiles of the same keys next to each other: they run at the same time.  The last first: of a causal chunk they see the most keys
+  u->row_tile = tiles - 1 - rel % tiles; rel /= tiles;
   if (UNITS) { u->part = 0; u->head = rel; } else { u->part = rel % u->parts; u->head = rel / u->parts; }
   u->slot0 = at_slot + (u->head * tiles + u->row_tile) * u->parts;
   return true;
@@ -103,19 +122,23 @@ template <typename E> __device__ __forceinline__ uint32_t odd_halves(uint32_t w)
 template <typename X> __device__ __forceinline__ void settle(X& x) { asm volatile("" : "+v"(x)); }
 
 // MT tiles of 16 rows a wavefront; RW wavefronts share the key tiles and have rows of their own, or (RW = 1) KW wavefronts have the same rows
-// and key tiles of their own, joined at the end.  KB blocks of 16 keys a tile.
-template <typename E, int D, int MT, int RW, int KW, int KB>
-__global__ __launch_bounds__(64 * RW * KW) void k_attend(CacheView c, AttendArgs a) {
+// and key tiles of their own, joined at the end.  KB blocks of 16 keys a tile.  OCC workgroups a CU.
+template <typename E, int D, int MT, int RW, int KW, int KB, int OCC>
+__global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, AttendArgs a) {
   static_assert(RW == 1 || KW == 1, "rows or keys");
   typedef typename E::T T; typedef typename E::T4 T4; typedef typename E::T8 T8;
   typedef TileLayout<E, D> L;
   constexpr int NT = 64 * RW * KW, KT = 16 * KB, CH = D / 8 /* 16-byte chunks of a row */, DB = D / 16, DK = D / 32;
   constexpr int SHARERS = 64 * RW;                          // threads that load a tile together
   constexpr int LOADS = KT * CH / SHARERS;                  // chunks each of K and V a thread
+  constexpr int ROWS_A_LOAD = SHARERS / CH;
+  static_assert(ROWS_A_LOAD <= 16 ? 16 % ROWS_A_LOAD == 0 : ROWS_A_LOAD % 16 == 0, "");
   constexpr bool K_LDS = RW > 1;
   constexpr int TILE_BYTES = KT * L::V_ROW + (K_LDS ? KT * L::K_ROW : 0);
   constexpr int JOIN_BYTES = KW > 1 ? KW * 16 * (D + 2) * 4 : 0;
   constexpr int LDS_BYTES = KW * TILE_BYTES > JOIN_BYTES ? KW * TILE_BYTES : JOIN_BYTES;
+  // a row's reference is only raised where a score passes it by this much: weights stay below 2^8
+  constexpr float SLACK = 8.f;
   __shared__ __align__(16) char lds[LDS_BYTES];
   __shared__ int odd_tile;
 
@@ -148,21 +171,24 @@ __global__ __launch_bounds__(64 * RW * KW) void k_attend(CacheView c, AttendArgs
   // keys below this are seen by every row of the wavefront
   const int first_slot = wave_row0 < rows ? wave_row0 / G : 0;
   const int all_see = u.len + min(first_slot + 1, a.chain);
+  const bool idle = wave_row0 >= rows;                       // no row of the wavefront's: it only helps to load
   const int32_t* const table = c.table + (int64_t)u.b * c.max_pages;
   const uint8_t* const mask = a.mask ? a.mask + (int64_t)u.b * a.nodes * a.nodes : nullptr;
   auto sees = [&](int t, int key) {                          // slot t, key below `seen`
     const int s = key - u.len;
-    if (s < 0) return true;
-    if (t < a.chain) return s <= t;
-    if (s < a.chain) return true;
-    return mask[(int64_t)(t - a.chain) * a.nodes + (s - a.chain)] != 0;
+    bool yes = s < a.chain && (t >= a.chain || s <= t);
+    if (t >= a.chain && s >= a.chain) yes = mask[(int64_t)(t - a.chain) * a.nodes + (s - a.chain)] != 0;
+    return yes;
   };
   // the page that a block of 16 keys lies in, -1 behind the last key or if the table has none
   auto page_of = [&](int key) { return key < seen ? valid_page(c, table[key >> c.page_shift]) : -1; };
   const int in_page = (1 << c.page_shift) - 1;
+  const int64_t head_offset = row_offset(c, a.layer, 0, u.head, 0) * 2, page_bytes = ((int64_t)c.kv_heads << c.page_shift) * (D * 2);
+  const char* const k_head = c.k + head_offset;
+  const char* const v_head = c.v + head_offset;
 
   f32x4 o[MT][DB];
-  float m_run[MT], l_run[MT];
+  float m_run[MT], l_run[MT];                                // l_run: of this lane's keys
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
     m_run[m] = -INFINITY; l_run[m] = 0.f;
@@ -173,25 +199,38 @@ __global__ __launch_bounds__(64 * RW * KW) void k_attend(CacheView c, AttendArgs
   uint4 vr[LOADS];
   uint4 kr[K_LDS ? LOADS : KB * DK];
   const int lt = RW > 1 ? tid : lane;                        // this thread among those that load the tile
+  bool there[KB];                                            // blocks of the requested tile that lie on a page
   auto request = [&](int t) {
     const int key0 = t * KT;
+    const char* kp[KB]; const char* vp[KB];
+    bool plain = key0 + KT <= seen;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      const int key = key0 + kb * 16, page = uniform(page_of(key));
+      there[kb] = page >= 0;
+      plain = plain && there[kb];
+      const int64_t off = (there[kb] ? page : 0) * page_bytes + (key & in_page) * (D * 2);
+      kp[kb] = k_head + off; vp[kb] = v_head + off;
+    }
+    // rows behind the last key hold anything; with `plain` there are none (uniform)
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
-      const int chunk = j * SHARERS + lt, row = chunk / CH, key = key0 + row;
-      const int page = page_of(key0 + row / 16 * 16);
-      const bool ok = page >= 0 && key < seen;               // rows behind the last key hold anything
-      const int64_t off = (row_offset(c, a.layer, ok ? page : 0, u.head, key & in_page) + chunk % CH * 8) * 2;
-      vr[j] = ok ? *(const uint4*)(c.v + off) : zero16();
-      if (K_LDS) kr[j] = ok ? *(const uint4*)(c.k + off) : zero16();
+      const int row = j * ROWS_A_LOAD + lt / CH, in = row % 16 * (D * 2) + lt % CH * 16;
+      const int kb_low = j * ROWS_A_LOAD / 16;              // ROWS_A_LOAD <= 16: the block of all of them
+      const char* kq = kp[kb_low]; const char* vq = vp[kb_low];
+      bool ok = there[kb_low];
+#pragma unroll
+      for (int x = 1; x * 16 < ROWS_A_LOAD; ++x) if (lt / CH >= x * 16) { kq = kp[kb_low + x]; vq = vp[kb_low + x]; ok = there[kb_low + x]; }
+      ok = plain || (ok && key0 + row < seen);
+      vr[j] = ok ? *(const uint4*)(vq + in) : zero16();
+      if (K_LDS) kr[j] = ok ? *(const uint4*)(kq + in) : zero16();
     }
     if (!K_LDS) {
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
-        const int page = page_of(key0 + kb * 16), key = key0 + kb * 16 + col;
-        const bool ok = page >= 0 && key < seen;
-        const int64_t off = row_offset(c, a.layer, ok ? page : 0, u.head, key & in_page) * 2 + quad * 16;
+        const bool ok = plain || (there[kb] && key0 + kb * 16 + col < seen);
 #pragma unroll
-        for (int kk = 0; kk < DK; ++kk) kr[kb * DK + kk] = ok ? *(const uint4*)(c.k + off + kk * 64) : zero16();
+        for (int kk = 0; kk < DK; ++kk) kr[kb * DK + kk] = ok ? *(const uint4*)(kp[kb] + col * (D * 2) + quad * 16 + kk * 64) : zero16();
       }
     }
   };
@@ -202,13 +241,13 @@ __global__ __launch_bounds__(64 * RW * KW) void k_attend(CacheView c, AttendArgs
   if (tile < tile_end) request(tile);
   for (; tile < tile_end; tile += step) {
     const int key0 = tile * KT;
-    // keys of the tile that some row may not see, or that lie on no page
-    bool whole = key0 + KT <= all_see;
+    bool whole = key0 + KT <= all_see;                       // every row sees every key of the tile
+    bool on_page[KB];
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) whole = whole && page_of(key0 + kb * 16) >= 0;
+    for (int kb = 0; kb < KB; ++kb) { on_page[kb] = there[kb]; whole = whole && on_page[kb]; }
     const bool mixed = key0 + KT > u.len;                    // holds new tokens: some rows may see a value that others do not
     bool odd = false;
-    if (RW > 1) { if (tid == 0) odd_tile = 0; __syncthreads(); }
+    if (RW > 1 && mixed) { if (tid == 0) odd_tile = 0; __syncthreads(); }
     if (mixed) {
       // 0 x infinity is not 0: a value that is not finite is left out of the product and added for the rows that see it
 #pragma unroll
@@ -220,130 +259,134 @@ __global__ __launch_bounds__(64 * RW * KW) void k_attend(CacheView c, AttendArgs
       odd = __any(odd);
       if (RW > 1 && odd && lane == 0) odd_tile = 1;
     }
-    T8 kf[KB][DK];
+    T8 kf[K_LDS ? 1 : KB][K_LDS ? 1 : DK];
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
-      const int chunk = j * SHARERS + lt, row = chunk / CH;
-      *(uint4*)(v_lds + row * L::V_ROW + chunk % CH * 16) = vr[j];
-      if (K_LDS) *(uint4*)(k_lds + row * L::K_ROW + chunk % CH * 16) = kr[j];
+      const int row = j * ROWS_A_LOAD + lt / CH;
+      *(uint4*)(v_lds + row * L::V_ROW + lt % CH * 16) = vr[j];
+      if (K_LDS) *(uint4*)(k_lds + row * L::K_ROW + lt % CH * 16) = kr[j];
     }
     if (!K_LDS) {
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-        for (int kk = 0; kk < DK; ++kk) kf[kb][kk] = __builtin_bit_cast(T8, kr[kb * DK + kk]);
+        for (int kk = 0; kk < DK; ++kk) kf[K_LDS ? 0 : kb][K_LDS ? 0 : kk] = __builtin_bit_cast(T8, kr[kb * DK + kk]);
     }
     if (RW > 1) __syncthreads(); else { __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront"); __builtin_amdgcn_wave_barrier(); __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront"); }
-    if (RW > 1) odd = odd_tile != 0;
+    if (RW > 1 && mixed) odd = odd_tile != 0;
     if (tile + step < tile_end) request(tile + step);
 
-    f32x4 s[MT][KB];
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-#pragma unroll
-      for (int m = 0; m < MT; ++m) s[m][kb] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int kk = 0; kk < DK; ++kk) {
-        const T8 k = K_LDS ? *(const T8*)(k_lds + (kb * 16 + col) * L::K_ROW + kk * 64 + quad * 16) : kf[kb][kk];
-#pragma unroll
-        for (int m = 0; m < MT; ++m) s[m][kb] = E::mfma(k, q[m][kk], s[m][kb]);
-      }
-    }
-
-    // Scores leave the matrix unit's registers here, in the block of the products: see settle().
-    float pf[MT][KB][4];
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) { pf[m][kb][r] = s[m][kb][r] * a.scale_log2e; settle(pf[m][kb][r]); }
-    if (!whole) {
+    if (!idle) {
+      f32x4 s[MT][KB];
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
-        const bool there = page_of(key0 + kb * 16) >= 0;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) s[m][kb] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kk = 0; kk < DK; ++kk) {
+          const T8 k = K_LDS ? *(const T8*)(k_lds + (kb * 16 + col) * L::K_ROW + kk * 64 + quad * 16) : kf[K_LDS ? 0 : kb][K_LDS ? 0 : kk];
+#pragma unroll
+          for (int m = 0; m < MT; ++m) s[m][kb] = E::mfma(k, q[m][kk], s[m][kb]);
+        }
+      }
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) settle(s[m][kb]);
+      if (!whole) {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int key = key0 + kb * 16 + quad * 4 + r;
+              const bool yes = on_page[kb] && key < seen && slot[m] >= 0 && sees(slot[m], key);
+              s[m][kb][r] = yes ? s[m][kb][r] : -INFINITY;
+            }
+      }
+
+      T8 p[MT][KB / 2];
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) top = fmaxf(top, s[m][kb][r]);
+        top *= a.scale_log2e;
+        if (__any(top > m_run[m] + SLACK)) {                 // (uniform) of all four lanes of a row, then
+          top = fmaxf(top, __shfl_xor(top, 16));
+          top = fmaxf(top, __shfl_xor(top, 32));
+          const float m_new = fmaxf(m_run[m], top), back = __builtin_amdgcn_exp2f(m_run[m] - (m_new == -INFINITY ? 0.f : m_new));
+          m_run[m] = m_new;
+          l_run[m] *= back;
+#pragma unroll
+          for (int d = 0; d < DB; ++d) o[m][d] *= back;
+        }
+        const float ref = m_run[m] == -INFINITY ? 0.f : m_run[m];
+        // P in the operands' 16 bits: relative 2^-9 (2^-12 for halves) a weight, of either sign; l is the sum of the weights as they were, for lse
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int h = 0; h < KB / 2; ++h)
+#pragma unroll
+          for (int r = 0; r < 8; ++r) {
+            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[m][h * 2 + r / 4][r % 4], a.scale_log2e, -ref));
+            sum[r % 4] += w;
+            p[m][h][r] = (T)w;
+          }
+        l_run[m] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      }
+#pragma unroll
+      for (int h = 0; h < KB / 2; ++h) {
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+          // keys 4 quad + r of two blocks, as P holds them
+          const char* at = v_lds + (h * 32 + quad * 4 + col / 4) * L::V_ROW + d * 32 + col % 4 * 8;
+          typedef __attribute__((address_space(3))) s16x4* lds4;
+          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at));
+          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at + 16 * L::V_ROW));
+          struct { s16x4 a, b; } pair{lo, hi};
+          const T8 v = __builtin_bit_cast(T8, pair);
+#pragma unroll
+          for (int m = 0; m < MT; ++m) o[m][d] = E::mfma(v, p[m][h], o[m][d]);
+        }
+      }
+      if (mixed && odd) {
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int key = key0 + kb * 16 + quad * 4 + r;
-            if (!(there && key < seen && slot[m] >= 0 && sees(slot[m], key))) pf[m][kb][r] = -INFINITY;
-          }
-      }
-    }
-
-    T8 p[MT][KB / 2];
+          for (int d = 0; d < DB; ++d) settle(o[m][d]);
+        for (int kk = 0; kk < KT; ++kk) {
+          const int key = key0 + kk, page = page_of(key0 + kk / 16 * 16);
+          if (page < 0 || key >= seen) continue;
+          const char* row = v_head + page * page_bytes + (key & in_page) * (D * 2);
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-      float top = -INFINITY;
+          for (int m = 0; m < MT; ++m) {
+            float w = 0.f;
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
+            for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) top = fmaxf(top, pf[m][kb][r]);
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
-      const float m_new = fmaxf(m_run[m], top), ref = m_new == -INFINITY ? 0.f : m_new;
-      const float back = __builtin_amdgcn_exp2f(m_run[m] - ref);
-      m_run[m] = m_new;
-      float sum = 0.f;
+              for (int r = 0; r < 4; ++r) { const float x = __shfl((float)p[m][kb / 2][kb % 2 * 4 + r], col + (kk % 16 / 4) * 16); if (kb == kk / 16 && r == kk % 4) w = x; }
+            if (slot[m] < 0 || !sees(slot[m], key)) continue;
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
+            for (int d = 0; d < DB; ++d) {
+              const T4 v = *(const T4*)(row + (d * 16 + quad * 4) * 2);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) { pf[m][kb][r] = __builtin_amdgcn_exp2f(pf[m][kb][r] - ref); sum += pf[m][kb][r]; }
-      l_run[m] = l_run[m] * back + sum;
-#pragma unroll
-      for (int d = 0; d < DB; ++d) o[m][d] *= back;
-      // P in the operands' 16 bits: relative 2^-9 (2^-12 for halves) a weight, of either sign
-#pragma unroll
-      for (int h = 0; h < KB / 2; ++h)
-#pragma unroll
-        for (int r = 0; r < 8; ++r) p[m][h][r] = (T)pf[m][h * 2 + r / 4][r % 4];
-    }
-#pragma unroll
-    for (int h = 0; h < KB / 2; ++h)
-#pragma unroll
-      for (int d = 0; d < DB; ++d) {
-        // keys 4 quad + r of two blocks, as P holds them
-        const char* at = v_lds + (h * 32 + quad * 4 + col / 4) * L::V_ROW + d * 32 + col % 4 * 8;
-        typedef __attribute__((address_space(3))) s16x4* lds4;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at + 16 * L::V_ROW));
-        struct { s16x4 a, b; } pair{lo, hi};
-        const T8 v = __builtin_bit_cast(T8, pair);
-#pragma unroll
-        for (int m = 0; m < MT; ++m) o[m][d] = E::mfma(v, p[m][h], o[m][d]);
-      }
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-      for (int d = 0; d < DB; ++d) settle(o[m][d]);
-    if (mixed && odd) {
-      for (int kk = 0; kk < KT; ++kk) {
-        const int key = key0 + kk, page = page_of(key0 + kk / 16 * 16);
-        if (page < 0 || key >= seen) continue;
-        const char* row = c.v + row_offset(c, a.layer, page, u.head, key & in_page) * 2;
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-          float w = 0.f;
-#pragma unroll
-          for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) { const float x = __shfl(pf[m][kb][r], col + (kk % 16 / 4) * 16); if (kb == kk / 16 && r == kk % 4) w = x; }
-          if (slot[m] < 0 || !sees(slot[m], key)) continue;
-#pragma unroll
-          for (int d = 0; d < DB; ++d) {
-            const T4 v = *(const T4*)(row + (d * 16 + quad * 4) * 2);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) { const float x = (float)v[r]; if (!(__builtin_fabsf(x) < INFINITY)) o[m][d][r] += w * x; }
+              for (int r = 0; r < 4; ++r) { const float x = (float)v[r]; if (!(__builtin_fabsf(x) < INFINITY)) o[m][d][r] += w * x; }
+            }
           }
         }
       }
     }
     if (RW > 1) __syncthreads();
   }
-
 #pragma unroll
-  for (int m = 0; m < MT; ++m) { l_run[m] += __shfl_xor(l_run[m], 16); l_run[m] += __shfl_xor(l_run[m], 32); }
+  for (int m = 0; m < MT; ++m) {
+    l_run[m] += __shfl_xor(l_run[m], 16); l_run[m] += __shfl_xor(l_run[m], 32);
+#pragma unroll
+    for (int d = 0; d < DB; ++d) settle(o[m][d]);
+  }
 
   // what this workgroup has of a row: to the record of its part, or out
   auto put = [&](int row_in_tile, int t, int g, int dim, f32x4 x, float m, float l, bool first) {

@@ -43,15 +43,17 @@ inline size_t reserve_bytes(const c2t_cache& c) { return ((size_t)2 * reserve_ca
 // Which kernel a launch of that many rows a cached head takes.
 struct AttendBuild { int rows_per_tile, keys_per_tile, threads; };
 enum { AB_ROWS_16, AB_ROWS_32, AB_ROWS_64, AB_ROWS_128 };
-inline int attend_build(int64_t rows) { return rows <= 16 ? AB_ROWS_16 : rows <= 32 ? AB_ROWS_32 : rows <= 64 ? AB_ROWS_64 : AB_ROWS_128; }
+inline int attend_build(int64_t rows, int head_dim) {
+  return rows <= 16 ? AB_ROWS_16 : rows <= 32 && head_dim <= 128 ? AB_ROWS_32 : rows <= 64 ? AB_ROWS_64 : AB_ROWS_128;
+}
 typedef void (*AttendKernel)(CacheView, AttendArgs);
 template <typename E, int D> AttendKernel attend_kernel(int build) {
   constexpr int KB = D > 128 ? 2 : 4;
   switch (build) {
-    case AB_ROWS_16: return k_attend<E, D, 1, 1, 4, 2>;
-    case AB_ROWS_32: return k_attend<E, D, 2, 1, 4, 2>;
-    case AB_ROWS_64: return k_attend<E, D, 1, 4, 1, KB>;
-    default: return k_attend<E, D, 2, 4, 1, KB>;
+    case AB_ROWS_16: return k_attend<E, D, 1, 1, 4, 2, (D > 128 ? 1 : 2)>;
+    case AB_ROWS_32: if constexpr (D <= 128) return k_attend<E, D, 2, 1, 4, 2, 2>; [[fallthrough]];      // (wider heads: not chosen)
+    case AB_ROWS_64: return k_attend<E, D, 1, 4, 1, KB, 2>;
+    default: return k_attend<E, D, 2, 4, 1, KB, (D > 128 ? 1 : 2)>;
   }
 }
 template <typename E> AttendKernel attend_kernel(int build, int head_dim) {
@@ -69,7 +71,7 @@ inline int attend_plan(const c2t_cache& c, const c2t_attention& a, AttendPlan* p
   if (a.nodes > C2T_MAX_BUDGET || (int64_t)a.tokens * a.q_heads > (1 << 30)) return C2T_ERR_UNSUPPORTED;
   const int group = a.q_heads / c.kv_heads;
   const int64_t rows = (int64_t)a.tokens * group;
-  p->build = attend_build(rows);
+  p->build = attend_build(rows, c.head_dim);
   p->shape.slots = a.tokens; p->shape.group = group;
   static constexpr int ROWS[] = {16, 32, 64, 128};
   const bool by_keys = p->build <= AB_ROWS_32;
@@ -78,7 +80,7 @@ inline int attend_plan(const c2t_cache& c, const c2t_attention& a, AttendPlan* p
   p->shape.target = 1024;
   p->shape.min_per = by_keys ? 8 : 4;
   p->units = (int64_t)c.batch * c.kv_heads * div_up64(rows, p->shape.rows_per_tile);
-  p->items = p->units + p->shape.target;
+  p->items = (p->units + p->shape.target + DIES - 1) / DIES * DIES;
   if (p->items > INT32_MAX / 2) return C2T_ERR_UNSUPPORTED;
   p->part_o = 0;
   p->part_ml = (size_t)2 * p->shape.target * p->shape.rows_per_tile * c.head_dim * 4;
@@ -227,7 +229,7 @@ int c2t_cache_attention(const c2t_cache* c, const c2t_attention* a, void* ws, si
   g.q = (const char*)a->q; g.out = (char*)a->out; g.lse = a->lse;
   g.q_batch = a->q_batch_stride * 2; g.q_token = a->q_token_stride * 2; g.out_batch = a->out_batch_stride * 2; g.out_token = a->out_token_stride * 2;
   g.n_new = a->n_new; g.mask = a->mask; g.nodes = a->nodes; g.chain = a->tokens - a->nodes; g.layer = a->layer;
-  g.scale_log2e = a->scale * 1.44269504088896341f;
+  g.scale_log2e = std::max(a->scale, 1e-30f) * 1.44269504088896341f;       // (a masked score is -infinity times it: not 0)
   g.part_o = (float*)((char*)ws + p.part_o); g.part_ml = (float2*)((char*)ws + p.part_ml);
   g.shape = p.shape;
   const CacheView v = view_of(*c);
@@ -235,7 +237,7 @@ int c2t_cache_attention(const c2t_cache* c, const c2t_attention* a, void* ws, si
   const AttendKernel fn = bf16 ? attend_kernel<Bf16>(p.build, c->head_dim) : attend_kernel<F16>(p.build, c->head_dim);
   hipLaunchKernelGGL(fn, dim3((unsigned)p.items), dim3(256), 0, (hipStream_t)stream, v, g);
   const AttendKernel join = bf16 ? join_kernel<Bf16>(c->head_dim) : join_kernel<F16>(c->head_dim);
-  hipLaunchKernelGGL(join, dim3((unsigned)p.units), dim3(JOIN_NT), 0, (hipStream_t)stream, v, g);
+  hipLaunchKernelGGL(join, dim3((unsigned)((p.units + DIES - 1) / DIES * DIES)), dim3(JOIN_NT), 0, (hipStream_t)stream, v, g);
   return hip_status();
 }
 
