@@ -200,13 +200,15 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
   uint4 kr[K_LDS ? LOADS : KB * DK];
   const int lt = RW > 1 ? tid : lane;                        // this thread among those that load the tile
   bool there[KB];                                            // blocks of the requested tile that lie on a page
-  auto request = [&](int t) {
+  // the pages of a tile's blocks, one a lane: asked for a tile ahead of the keys, which cannot be asked for without them
+  auto pages_of = [&](int t) { const int key = t * KT + (lane % KB) * 16; return key < seen ? table[key >> c.page_shift] : -1; };
+  auto request = [&](int t, int pages) {
     const int key0 = t * KT;
     const char* kp[KB]; const char* vp[KB];
     bool plain = key0 + KT <= seen;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
-      const int key = key0 + kb * 16, page = uniform(page_of(key));
+      const int key = key0 + kb * 16, page = valid_page(c, __builtin_amdgcn_readlane(pages, kb));
       there[kb] = page >= 0;
       plain = plain && there[kb];
       const int64_t off = (there[kb] ? page : 0) * page_bytes + (key & in_page) * (D * 2);
@@ -238,7 +240,9 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
   const int step = KW;
   tile += kw;
   // (RW > 1: the loop is the same for all wavefronts, which meet in it)
-  if (tile < tile_end) request(tile);
+  int pages = pages_of(tile);
+  if (tile < tile_end) request(tile, pages);
+  pages = pages_of(tile + step);
   for (; tile < tile_end; tile += step) {
     const int key0 = tile * KT;
     bool whole = key0 + KT <= all_see;                       // every row sees every key of the tile
@@ -274,7 +278,8 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
     }
     if (RW > 1) __syncthreads(); else { __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront"); __builtin_amdgcn_wave_barrier(); __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront"); }
     if (RW > 1 && mixed) odd = odd_tile != 0;
-    if (tile + step < tile_end) request(tile + step);
+    if (tile + step < tile_end) request(tile + step, pages);
+    pages = pages_of(tile + 2 * step);
 
     if (!idle) {
       f32x4 s[MT][KB];

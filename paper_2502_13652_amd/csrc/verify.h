@@ -77,8 +77,14 @@ inline int attend_plan(const c2t_cache& c, const c2t_attention& a, AttendPlan* p
   const bool by_keys = p->build <= AB_ROWS_32;
   p->shape.rows_per_tile = ROWS[p->build];
   p->shape.keys_per_tile = by_keys || c.head_dim > 128 ? 32 : 64;
-  p->shape.target = 1024;
-  p->shape.min_per = by_keys ? 8 : 4;
+#ifndef TKW
+#define TKW 1024
+#define TRW 1024
+#define MKW 8
+#define MRW 4
+#endif
+  p->shape.target = by_keys ? TKW : TRW;
+  p->shape.min_per = by_keys ? MKW : MRW;
   p->units = (int64_t)c.batch * c.kv_heads * div_up64(rows, p->shape.rows_per_tile);
   p->items = (p->units + p->shape.target + DIES - 1) / DIES * DIES;
   if (p->items > INT32_MAX / 2) return C2T_ERR_UNSUPPORTED;
