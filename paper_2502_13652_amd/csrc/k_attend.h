@@ -18,6 +18,7 @@ namespace c2t {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 struct Bf16 {
   typedef __bf16 T; typedef __bf16 T4 __attribute__((ext_vector_type(4))); typedef __bf16 T8 __attribute__((ext_vector_type(8)));
@@ -112,7 +113,6 @@ template <typename E, int D> struct TileLayout {
   static constexpr int K_ROW = D * 2 + 16, V_ROW = D * 2 + 32;
 };
 
-__device__ __forceinline__ uint4 zero16() { return make_uint4(0u, 0u, 0u, 0u); }
 template <typename E> __device__ __forceinline__ uint32_t odd_halves(uint32_t w) {     // halves whose exponent is all ones, as a mask of them
   return ((w & E::EXPONENT) == E::EXPONENT ? 0xffffu : 0u) | (((w >> 16) & E::EXPONENT) == E::EXPONENT ? 0xffff0000u : 0u);
 }
@@ -196,45 +196,45 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
     for (int d = 0; d < DB; ++d) o[m][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  uint4 vr[LOADS];
-  uint4 kr[K_LDS ? LOADS : KB * DK];
+  u32x4 vr[LOADS];
+  u32x4 kr[K_LDS ? LOADS : KB * DK];
   const int lt = RW > 1 ? tid : lane;                        // this thread among those that load the tile
-  bool there[KB];                                            // blocks of the requested tile that lie on a page
+  uint32_t there = 0u; bool full = false;                    // blocks of the requested tile that lie on a page; all do, and no key is past the last
   // the pages of a tile's blocks, one a lane: asked for a tile ahead of the keys, which cannot be asked for without them
   auto pages_of = [&](int t) { const int key = t * KT + (lane % KB) * 16; return key < seen ? table[key >> c.page_shift] : -1; };
+  // Every lane loads, without a condition that would make each load wait for itself: a block that is on no page comes from the pool's first page, and
+  // rows behind the last key lie on its page; both are taken out before they are used.
   auto request = [&](int t, int pages) {
     const int key0 = t * KT;
-    const char* kp[KB]; const char* vp[KB];
-    bool plain = key0 + KT <= seen;
+    constexpr int BLOCKS_A_LOAD = ROWS_A_LOAD > 16 ? ROWS_A_LOAD / 16 : 1, LOADS_A_BLOCK = ROWS_A_LOAD > 16 ? 1 : 16 / ROWS_A_LOAD;
+    const int in = lt / CH % 16 * (D * 2) + lt % CH * 16;
+    int64_t mine = 0;
+    there = 0u;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
       const int key = key0 + kb * 16, page = valid_page(c, __builtin_amdgcn_readlane(pages, kb));
-      there[kb] = page >= 0;
-      plain = plain && there[kb];
-      const int64_t off = (there[kb] ? page : 0) * page_bytes + (key & in_page) * (D * 2);
-      kp[kb] = k_head + off; vp[kb] = v_head + off;
-    }
-    // rows behind the last key hold anything; with `plain` there are none (uniform)
+      there |= page >= 0 ? 1u << kb : 0u;
+      const int64_t off = (page >= 0 ? page : 0) * page_bytes + (key & in_page) * (D * 2);
+      if (BLOCKS_A_LOAD == 1) {
 #pragma unroll
-    for (int j = 0; j < LOADS; ++j) {
-      const int row = j * ROWS_A_LOAD + lt / CH, in = row % 16 * (D * 2) + lt % CH * 16;
-      const int kb_low = j * ROWS_A_LOAD / 16;              // ROWS_A_LOAD <= 16: the block of all of them
-      const char* kq = kp[kb_low]; const char* vq = vp[kb_low];
-      bool ok = there[kb_low];
+        for (int x = 0; x < LOADS_A_BLOCK; ++x) {
+          const int j = kb * LOADS_A_BLOCK + x;
+          vr[j] = *(const u32x4*)(v_head + off + in + x * ROWS_A_LOAD * (D * 2));
+          if (K_LDS) kr[j] = *(const u32x4*)(k_head + off + in + x * ROWS_A_LOAD * (D * 2));
+        }
+      } else {
+        if (kb % BLOCKS_A_LOAD == 0 || lt / CH / 16 == kb % BLOCKS_A_LOAD) mine = off;
+        if (kb % BLOCKS_A_LOAD == BLOCKS_A_LOAD - 1) {
+          vr[kb / BLOCKS_A_LOAD] = *(const u32x4*)(v_head + mine + in);
+          if (K_LDS) kr[kb / BLOCKS_A_LOAD] = *(const u32x4*)(k_head + mine + in);
+        }
+      }
+      if (!K_LDS) {
 #pragma unroll
-      for (int x = 1; x * 16 < ROWS_A_LOAD; ++x) if (lt / CH >= x * 16) { kq = kp[kb_low + x]; vq = vp[kb_low + x]; ok = there[kb_low + x]; }
-      ok = plain || (ok && key0 + row < seen);
-      vr[j] = ok ? *(const uint4*)(vq + in) : zero16();
-      if (K_LDS) kr[j] = ok ? *(const uint4*)(kq + in) : zero16();
-    }
-    if (!K_LDS) {
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
-        const bool ok = plain || (there[kb] && key0 + kb * 16 + col < seen);
-#pragma unroll
-        for (int kk = 0; kk < DK; ++kk) kr[kb * DK + kk] = ok ? *(const uint4*)(kp[kb] + col * (D * 2) + quad * 16 + kk * 64) : zero16();
+        for (int kk = 0; kk < DK; ++kk) kr[kb * DK + kk] = *(const u32x4*)(k_head + off + col * (D * 2) + quad * 16 + kk * 64);
       }
     }
+    full = key0 + KT <= seen && there == (1u << KB) - 1u;
   };
 
   const int step = KW;
@@ -245,10 +245,16 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
   pages = pages_of(tile + step);
   for (; tile < tile_end; tile += step) {
     const int key0 = tile * KT;
-    bool whole = key0 + KT <= all_see;                       // every row sees every key of the tile
-    bool on_page[KB];
+    const uint32_t on_page = there;
+    const bool whole = full && key0 + KT <= all_see;         // every row sees every key of the tile
+    if (!full) {
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) { on_page[kb] = there[kb]; whole = whole && on_page[kb]; }
+      for (int j = 0; j < LOADS; ++j) {
+        const int row = j * ROWS_A_LOAD + lt / CH;
+        const bool ok = key0 + row < seen && (on_page >> (row / 16) & 1u);
+        vr[j] = ok ? vr[j] : u32x4{0u, 0u, 0u, 0u};
+      }
+    }
     const bool mixed = key0 + KT > u.len;                    // holds new tokens: some rows may see a value that others do not
     bool odd = false;
     if (RW > 1 && mixed) { if (tid == 0) odd_tile = 0; __syncthreads(); }
@@ -267,8 +273,8 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
       const int row = j * ROWS_A_LOAD + lt / CH;
-      *(uint4*)(v_lds + row * L::V_ROW + lt % CH * 16) = vr[j];
-      if (K_LDS) *(uint4*)(k_lds + row * L::K_ROW + lt % CH * 16) = kr[j];
+      *(u32x4*)(v_lds + row * L::V_ROW + lt % CH * 16) = vr[j];
+      if (K_LDS) *(u32x4*)(k_lds + row * L::K_ROW + lt % CH * 16) = kr[j];
     }
     if (!K_LDS) {
 #pragma unroll
@@ -306,7 +312,7 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
               const int key = key0 + kb * 16 + quad * 4 + r;
-              const bool yes = on_page[kb] && key < seen && slot[m] >= 0 && sees(slot[m], key);
+              const bool yes = (on_page >> kb & 1u) && key < seen && slot[m] >= 0 && sees(slot[m], key);
               s[m][kb][r] = yes ? s[m][kb][r] : -INFINITY;
             }
       }
