@@ -136,11 +136,12 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
   constexpr bool K_LDS = RW > 1;
   constexpr int TILE_BYTES = KT * L::V_ROW + (K_LDS ? KT * L::K_ROW : 0);
   constexpr int JOIN_BYTES = KW > 1 ? KW * 16 * (D + 2) * 4 : 0;
-  constexpr int LDS_BYTES = KW * TILE_BYTES > JOIN_BYTES ? KW * TILE_BYTES : JOIN_BYTES;
+  constexpr int BUFFERS = RW > 1 ? 2 : KW;                  // of the tile: the next one's while this one is used, or one a wavefront
+  constexpr int LDS_BYTES = BUFFERS * TILE_BYTES > JOIN_BYTES ? BUFFERS * TILE_BYTES : JOIN_BYTES;
   // a row's reference is only raised where a score passes it by this much: weights stay below 2^8
   constexpr float SLACK = 8.f;
   __shared__ __align__(16) char lds[LDS_BYTES];
-  __shared__ int odd_tile;
+  __shared__ int odd_value[2];                               // the buffer has held a value that is not finite
 
   Unit u;
   if (!find_unit<false>(c, a, blockIdx.x, &u)) return;
@@ -148,8 +149,6 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
   const int rw = RW > 1 ? wave : 0, kw = KW > 1 ? wave : 0;
   const int rows = u.n_new * a.shape.group, G = a.shape.group;
   const int wave_row0 = u.row_tile * a.shape.rows_per_tile + rw * 16 * MT;
-  char* const v_lds = lds + kw * TILE_BYTES;
-  char* const k_lds = v_lds + KT * L::V_ROW;
 
   // this lane's rows and their queries
   int slot[MT];
@@ -237,28 +236,19 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
     full = key0 + KT <= seen && there == (1u << KB) - 1u;
   };
 
-  const int step = KW;
-  tile += kw;
-  // (RW > 1: the loop is the same for all wavefronts, which meet in it)
-  int pages = pages_of(tile);
-  if (tile < tile_end) request(tile, pages);
-  pages = pages_of(tile + step);
-  for (; tile < tile_end; tile += step) {
-    const int key0 = tile * KT;
-    const uint32_t on_page = there;
-    const bool whole = full && key0 + KT <= all_see;         // every row sees every key of the tile
+  // the requested tile into LDS
+  auto stage = [&](int t, char* v_lds) {
+    const int key0 = t * KT;
     if (!full) {
 #pragma unroll
       for (int j = 0; j < LOADS; ++j) {
         const int row = j * ROWS_A_LOAD + lt / CH;
-        const bool ok = key0 + row < seen && (on_page >> (row / 16) & 1u);
+        const bool ok = key0 + row < seen && (there >> (row / 16) & 1u);
         vr[j] = ok ? vr[j] : u32x4{0u, 0u, 0u, 0u};
       }
     }
-    const bool mixed = key0 + KT > u.len;                    // holds new tokens: some rows may see a value that others do not
     bool odd = false;
-    if (RW > 1 && mixed) { if (tid == 0) odd_tile = 0; __syncthreads(); }
-    if (mixed) {
+    if (key0 + KT > u.len) {                                 // holds new tokens: some rows may see a value that others do not
       // 0 x infinity is not 0: a value that is not finite is left out of the product and added for the rows that see it
 #pragma unroll
       for (int j = 0; j < LOADS; ++j) {
@@ -267,28 +257,58 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
         vr[j].x &= ~x; vr[j].y &= ~y; vr[j].z &= ~z; vr[j].w &= ~w;
       }
       odd = __any(odd);
-      if (RW > 1 && odd && lane == 0) odd_tile = 1;
     }
-    T8 kf[K_LDS ? 1 : KB][K_LDS ? 1 : DK];
+    char* const k_lds = v_lds + KT * L::V_ROW;
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
       const int row = j * ROWS_A_LOAD + lt / CH;
       *(u32x4*)(v_lds + row * L::V_ROW + lt % CH * 16) = vr[j];
       if (K_LDS) *(u32x4*)(k_lds + row * L::K_ROW + lt % CH * 16) = kr[j];
     }
-    if (!K_LDS) {
+    return odd;
+  };
+
+  const int step = KW;
+  tile += kw;
+  int pages = pages_of(tile), buffer = 0;
+  uint32_t on_page = 0u;                                     // of the tile in LDS
+  bool all_there = false, odd = false;
+  if (tile < tile_end) request(tile, pages);
+  pages = pages_of(tile + step);
+  if (RW > 1) {                                              // (the loop is the same for all wavefronts, which meet in it)
+    if (tid < 2) odd_value[tid] = 0;
+    __syncthreads();
+    if (tile < tile_end) {
+      if (stage(tile, lds) && lane == 0) odd_value[0] = 1;
+      on_page = there; all_there = full;
+      if (tile + 1 < tile_end) request(tile + 1, pages);
+      pages = pages_of(tile + 2);
+    }
+    __syncthreads();
+  }
+  for (; tile < tile_end; tile += step) {
+    const int key0 = tile * KT;
+    char* const v_lds = lds + (RW > 1 ? buffer : kw) * TILE_BYTES;
+    char* const k_lds = v_lds + KT * L::V_ROW;
+    T8 kf[K_LDS ? 1 : KB][K_LDS ? 1 : DK];
+    if (RW > 1) {
+      odd = key0 + KT > u.len && odd_value[buffer] != 0;
+    } else {
+      odd = stage(tile, v_lds);
+      on_page = there; all_there = full;
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-        for (int kk = 0; kk < DK; ++kk) kf[K_LDS ? 0 : kb][K_LDS ? 0 : kk] = __builtin_bit_cast(T8, kr[kb * DK + kk]);
+        for (int kk = 0; kk < DK; ++kk) kf[K_LDS ? 0 : kb][K_LDS ? 0 : kk] = __builtin_bit_cast(T8, kr[K_LDS ? 0 : kb * DK + kk]);
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront"); __builtin_amdgcn_wave_barrier(); __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      if (tile + step < tile_end) request(tile + step, pages);
+      pages = pages_of(tile + 2 * step);
     }
-    if (RW > 1) __syncthreads(); else { __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront"); __builtin_amdgcn_wave_barrier(); __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront"); }
-    if (RW > 1 && mixed) odd = odd_tile != 0;
-    if (tile + step < tile_end) request(tile + step, pages);
-    pages = pages_of(tile + 2 * step);
+    const bool whole = all_there && key0 + KT <= all_see;    // every row sees every key of the tile
+    const uint32_t blocks = on_page;
 
+    f32x4 s[MT][KB];
     if (!idle) {
-      f32x4 s[MT][KB];
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
 #pragma unroll
@@ -312,7 +332,7 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
               const int key = key0 + kb * 16 + quad * 4 + r;
-              const bool yes = (on_page >> kb & 1u) && key < seen && slot[m] >= 0 && sees(slot[m], key);
+              const bool yes = (blocks >> kb & 1u) && key < seen && slot[m] >= 0 && sees(slot[m], key);
               s[m][kb][r] = yes ? s[m][kb][r] : -INFINITY;
             }
       }
@@ -363,7 +383,7 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
           for (int m = 0; m < MT; ++m) o[m][d] = E::mfma(v, p[m][h], o[m][d]);
         }
       }
-      if (mixed && odd) {
+      if (odd) {
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -390,7 +410,16 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
         }
       }
     }
-    if (RW > 1) __syncthreads();
+    if (RW > 1) {
+      if (tile + 1 < tile_end) {
+        if (stage(tile + 1, lds + (buffer ^ 1) * TILE_BYTES) && lane == 0) odd_value[buffer ^ 1] = 1;
+        on_page = there; all_there = full;
+        if (tile + 2 < tile_end) request(tile + 2, pages);
+        pages = pages_of(tile + 3);
+      }
+      __syncthreads();
+      buffer ^= 1;
+    }
   }
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
