@@ -343,9 +343,14 @@ typedef struct {
 /* Every slot sees the length[b] tokens before; a chain slot the chain up to itself; node i the whole chain and the nodes j with mask[b][i][j] != 0
  * (j < n_new[b] - chain).  A key that a row does not see has no influence on it, whatever its bits.  A row that sees no key gets zeros.
  * Products in the cache's dtype, sums and the softmax in fp32.  The workspace ([device], 256-byte aligned, its size from the call's sizes
- * alone) holds nothing between calls. */
+ * alone) is zero-filled by the caller before its first use (its counters are zero again after each call); calls that may run at the same time need
+ * one each, others may share the largest. */
 int c2t_attention_workspace_bytes(const c2t_cache* cache, const c2t_attention* attention, size_t* out);
 int c2t_cache_attention(const c2t_cache* cache, const c2t_attention* attention, void* dev_workspace, size_t workspace_bytes, void* stream);
+
+/* [host] out: a number that tells the captures of graphs apart, of the capture that `stream` is in; 0 outside of one.  For callers that keep a workspace a
+ * stream: what a graph was captured with belongs to that graph. */
+int c2t_stream_capture_id(void* stream, uint64_t* out);
 
 /* Profiling build only (the library compiled with -DC2T_PHASE_TIMES; paper_2502_13652_amd/phase_times.py
  * builds and drives it): copies to [host] out, for the first n_workgroups (<= 8192) workgroups of the

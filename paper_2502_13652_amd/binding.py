@@ -103,6 +103,7 @@ def load_library(path=None):
     L.c2t_cache_fork.argtypes = [vp, vp, vp, i32, vp]
     L.c2t_attention_workspace_bytes.argtypes = [vp, vp, P(sz)]
     L.c2t_cache_attention.argtypes = [vp, vp, vp, sz, vp]
+    L.c2t_stream_capture_id.argtypes = [vp, P(ctypes.c_uint64)]
     L.c2t_strerror.argtypes = [ctypes.c_int]
     L.c2t_strerror.restype = ctypes.c_char_p
     _lib = L

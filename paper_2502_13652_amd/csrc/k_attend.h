@@ -39,71 +39,75 @@ struct AttendArgs {
   int32_t nodes, chain;                    // slots = chain + nodes
   int32_t layer;
   float scale_log2e;
-  float* part_o; float2* part_ml;          // records of parts: [2 target][rows][head_dim], [2 target][rows] (m, l)
+  // records of parts: [records][rows of a tile][head_dim], and (m, l) of each row; tickets [records]: parts of the unit with that first record that
+  // have left theirs, zero between launches
+  float* part_o; float2* part_ml; int32_t* tickets;
   AttendShape shape;
 };
 
 // What a workgroup, and the join of its unit, know of where they are.
 struct Unit { int b, len, n_new, row_tile, head, part, parts, slot0; };   // slot0: record of the unit's first part
 
-// Workgroups go to the chip's eight dies in turn; neighbouring items, whose rows share keys, belong on one die and its L2.
-constexpr int DIES = 8;
-__device__ __forceinline__ int item_of_workgroup(int workgroup, int items) {
-  const int run = div_up(items, DIES), i = workgroup / DIES;
-  const int w = workgroup % DIES * run + i;
-  return i < run && w < items ? w : -1;
-}
-
-// Deals a workgroup its item.  Every wavefront computes it for itself, each lane summing a stretch of sequences: no barrier.
-// UNITS: items are units, not their parts.  False: there is none for it.
-template <bool UNITS>
-__device__ __forceinline__ bool find_unit(const CacheView& c, const AttendArgs& a, int workgroup, Unit* u) {
+// Deals a workgroup its item.  Every wavefront computes it for itself, each lane summing a stretch of sequences: no barrier.  Where
+// each lane has one sequence at most, the longest go first: workgroups start in about this order, and none that starts last is long.
+// False: there is no item for it.
+__device__ __forceinline__ bool find_item(const CacheView& c, const AttendArgs& a, int workgroup, Unit* u) {
   const int lane = lane_id(), each = div_up(c.batch, WAVE), b0 = min(lane * each, c.batch), b1 = min(b0 + each, c.batch);
   auto load = [&](int b, int* n) {
     const int len = tokens_in_cache(c, c.length[b]);
     *n = new_tokens(c, len, a.n_new ? a.n_new[b] : a.shape.slots, a.shape.slots);
     return len;
   };
-  int n_first = 0, len_first = 0;
-  if (b0 < b1) len_first = load(b0, &n_first);
-  auto of = [&](int b, int* n) { if (b == b0) { *n = n_first; return len_first; } return load(b, n); };
+  // of a lane with one sequence: that one; of one with more: the first, and the one that is found
+  int my_b = b0, my_n = 0, my_len = 0;
+  if (b0 < b1) my_len = load(b0, &my_n);
+  if (each == 1 && c.batch > 1) {
+    const int cost = b0 < b1 ? my_len + my_n : -1;
+    int rank = 0;
+    for (int j = 0; j < c.batch; ++j) { const int other = __builtin_amdgcn_readlane(cost, j); rank += other > cost || (other == cost && j < lane); }
+    if (b0 >= b1) rank = lane;
+    my_b = __builtin_amdgcn_ds_permute(rank * 4, my_b);
+    my_n = __builtin_amdgcn_ds_permute(rank * 4, my_n);
+    my_len = __builtin_amdgcn_ds_permute(rank * 4, my_len);
+  }
+  auto of = [&](int b, int* n) { if (b == b0) { *n = my_n; return my_len; } return load(b, n); };
   double mine = 0.0;
   for (int b = b0; b < b1; ++b) { int n; const int len = of(b, &n); mine += (double)sequence_tiles(c, a.shape, len, n); }
   const int per = tiles_per_part(a.shape, (int64_t)wave_sum(mine));
   int items = 0, slots = 0;
   for (int b = b0; b < b1; ++b) {
     int n; const int len = of(b, &n);
-    const int parts = sequence_parts(c, a.shape, per, len, n), p = parts_of(a.shape, per, len, n);
-    items += UNITS ? parts / p : parts;
-    if (p > 1) slots += parts;
+    const int parts = sequence_parts(c, a.shape, per, len, n);
+    items += parts;
+    if (parts_of(a.shape, per, len, n) > 1) slots += parts;
   }
   const int items_to = wave_scan_incl(items);
-  const int w = item_of_workgroup(workgroup, __builtin_amdgcn_readlane(items_to, WAVE - 1));
+  const int w = item_of_workgroup(a.shape, workgroup);
   int item0 = items_to - items, slot0 = wave_scan_incl(slots) - slots;
   const bool here = w >= item0 && w < item0 + items;
   const uint64_t has = __ballot(here);
   if (has == 0ull) return false;
-  int found = b0, rel = w - item0, at_slot = slot0;
+  int rel = w - item0, at_slot = slot0;
   if (here && each > 1) {
     for (int b = b0; b < b1; ++b) {
       int n; const int len = of(b, &n);
-      const int parts = sequence_parts(c, a.shape, per, len, n), p = parts_of(a.shape, per, len, n), mine_here = UNITS ? parts / p : parts;
-      if (w < item0 + mine_here) { found = b; rel = w - item0; at_slot = slot0; len_first = len; n_first = n; break; }
-      item0 += mine_here;
-      if (p > 1) slot0 += parts;
+      const int parts = sequence_parts(c, a.shape, per, len, n);
+      if (w < item0 + parts) { my_b = b; rel = w - item0; at_slot = slot0; my_len = len; my_n = n; break; }
+      item0 += parts;
+      if (parts_of(a.shape, per, len, n) > 1) slot0 += parts;
     }
   }
   const int from = __builtin_ctzll(has);
-  u->b = __builtin_amdgcn_readlane(found, from);
+  u->b = __builtin_amdgcn_readlane(my_b, from);
   rel = __builtin_amdgcn_readlane(rel, from);
   at_slot = __builtin_amdgcn_readlane(at_slot, from);
-  u->len = __builtin_amdgcn_readlane(len_first, from);
-  u->n_new = __builtin_amdgcn_readlane(n_first, from);
+  u->len = __builtin_amdgcn_readlane(my_len, from);
+  u->n_new = __builtin_amdgcn_readlane(my_n, from);
   u->parts = parts_of(a.shape, per, u->len, u->n_new);
   const int tiles = row_tiles(a.shape, u->n_new);
   // row tiles of the same keys next to each other: they run at the same time.  The last first: of a causal chunk they see the most keys
   u->row_tile = tiles - 1 - rel % tiles; rel /= tiles;
-  if (UNITS) { u->part = 0; u->head = rel; } else { u->part = rel % u->parts; u->head = rel / u->parts; }
+  u->part = rel % u->parts; u->head = rel / u->parts;
   u->slot0 = at_slot + (u->head * tiles + u->row_tile) * u->parts;
   return true;
 }
@@ -120,6 +124,15 @@ template <typename E> __device__ __forceinline__ uint32_t odd_halves(uint32_t w)
 // A product's result, used in a later block than the product: the compiler has been seen to read it there before the matrix unit has
 // written it (it counts the wait from the wrong instruction), so it is moved to ordinary registers in the product's own block, where the wait is right.
 template <typename X> __device__ __forceinline__ void settle(X& x) { asm volatile("" : "+v"(x)); }
+
+// pairs of numbers that one workgroup writes and another reads in the same launch
+__device__ __forceinline__ void st_dev64(uint64_t* p, float x, float y) {
+  __hip_atomic_store(p, (uint64_t)__float_as_uint(y) << 32 | __float_as_uint(x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 ld_dev64(const uint64_t* p) {
+  const uint64_t v = __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
+}
 
 // MT tiles of 16 rows a wavefront; RW wavefronts share the key tiles and have rows of their own, or (RW = 1) KW wavefronts have the same rows
 // and key tiles of their own, joined at the end.  KB blocks of 16 keys a tile.  OCC workgroups a CU.
@@ -141,14 +154,14 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
   // a row's reference is only raised where a score passes it by this much: weights stay below 2^8
   constexpr float SLACK = 8.f;
   __shared__ __align__(16) char lds[LDS_BYTES];
-  __shared__ int odd_value[2];                               // the buffer has held a value that is not finite
+  __shared__ int odd_value;                                  // a tile held a value that is not finite
 
   Unit u;
-  if (!find_unit<false>(c, a, blockIdx.x, &u)) return;
+  if (!find_item(c, a, blockIdx.x, &u)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 15, quad = lane >> 4;
   const int rw = RW > 1 ? wave : 0, kw = KW > 1 ? wave : 0;
   const int rows = u.n_new * a.shape.group, G = a.shape.group;
-  const int wave_row0 = u.row_tile * a.shape.rows_per_tile + rw * 16 * MT;
+  const int wave_row0 = (u.row_tile << a.shape.rows_shift) + rw * 16 * MT;
 
   // this lane's rows and their queries
   int slot[MT];
@@ -176,7 +189,7 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
   auto sees = [&](int t, int key) {                          // slot t, key below `seen`
     const int s = key - u.len;
     bool yes = s < a.chain && (t >= a.chain || s <= t);
-    if (t >= a.chain && s >= a.chain) yes = mask[(int64_t)(t - a.chain) * a.nodes + (s - a.chain)] != 0;
+    if (t >= a.chain && s >= a.chain) yes = mask[(t - a.chain) * a.nodes + (s - a.chain)] != 0;      // (nodes^2: at most 2^20)
     return yes;
   };
   // the page that a block of 16 keys lies in, -1 behind the last key or if the table has none
@@ -268,18 +281,19 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
     return odd;
   };
 
-  const int step = KW;
+  const int step = KW, first_key = tile * KT;
   tile += kw;
+  const int first_tile = tile;
   int pages = pages_of(tile), buffer = 0;
   uint32_t on_page = 0u;                                     // of the tile in LDS
   bool all_there = false, odd = false;
   if (tile < tile_end) request(tile, pages);
   pages = pages_of(tile + step);
   if (RW > 1) {                                              // (the loop is the same for all wavefronts, which meet in it)
-    if (tid < 2) odd_value[tid] = 0;
+    if (tid == 0) odd_value = 0;
     __syncthreads();
     if (tile < tile_end) {
-      if (stage(tile, lds) && lane == 0) odd_value[0] = 1;
+      if (stage(tile, lds) && lane == 0) odd_value = 1;
       on_page = there; all_there = full;
       if (tile + 1 < tile_end) request(tile + 1, pages);
       pages = pages_of(tile + 2);
@@ -291,10 +305,8 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
     char* const v_lds = lds + (RW > 1 ? buffer : kw) * TILE_BYTES;
     char* const k_lds = v_lds + KT * L::V_ROW;
     T8 kf[K_LDS ? 1 : KB][K_LDS ? 1 : DK];
-    if (RW > 1) {
-      odd = key0 + KT > u.len && odd_value[buffer] != 0;
-    } else {
-      odd = stage(tile, v_lds);
+    if (RW == 1) {
+      if (stage(tile, v_lds)) odd = true;
       on_page = there; all_there = full;
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb)
@@ -383,36 +395,10 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
           for (int m = 0; m < MT; ++m) o[m][d] = E::mfma(v, p[m][h], o[m][d]);
         }
       }
-      if (odd) {
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-          for (int d = 0; d < DB; ++d) settle(o[m][d]);
-        for (int kk = 0; kk < KT; ++kk) {
-          const int key = key0 + kk, page = page_of(key0 + kk / 16 * 16);
-          if (page < 0 || key >= seen) continue;
-          const char* row = v_head + page * page_bytes + (key & in_page) * (D * 2);
-#pragma unroll
-          for (int m = 0; m < MT; ++m) {
-            float w = 0.f;
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-              for (int r = 0; r < 4; ++r) { const float x = __shfl((float)p[m][kb / 2][kb % 2 * 4 + r], col + (kk % 16 / 4) * 16); if (kb == kk / 16 && r == kk % 4) w = x; }
-            if (slot[m] < 0 || !sees(slot[m], key)) continue;
-#pragma unroll
-            for (int d = 0; d < DB; ++d) {
-              const T4 v = *(const T4*)(row + (d * 16 + quad * 4) * 2);
-#pragma unroll
-              for (int r = 0; r < 4; ++r) { const float x = (float)v[r]; if (!(__builtin_fabsf(x) < INFINITY)) o[m][d][r] += w * x; }
-            }
-          }
-        }
-      }
     }
     if (RW > 1) {
       if (tile + 1 < tile_end) {
-        if (stage(tile + 1, lds + (buffer ^ 1) * TILE_BYTES) && lane == 0) odd_value[buffer ^ 1] = 1;
+        if (stage(tile + 1, lds + (buffer ^ 1) * TILE_BYTES) && lane == 0) odd_value = 1;
         on_page = there; all_there = full;
         if (tile + 2 < tile_end) request(tile + 2, pages);
         pages = pages_of(tile + 3);
@@ -428,20 +414,60 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
     for (int d = 0; d < DB; ++d) settle(o[m][d]);
   }
 
-  // what this workgroup has of a row: to the record of its part, or out
-  auto put = [&](int row_in_tile, int t, int g, int dim, f32x4 x, float m, float l, bool first) {
-    if (u.parts > 1) {
-      const int64_t rec = (int64_t)(u.slot0 + u.part) * a.shape.rows_per_tile + row_in_tile;
-      *(f32x4*)(a.part_o + rec * D + dim) = x;
-      if (first) a.part_ml[rec] = make_float2(m, l);
-    } else {
-      const float inv = l == 0.f ? 0.f : 1.f / l;
-      T4 y;
+  // Values that are not finite were left out of the products; rows that see their keys get them here.  A weight is made again from its key.
+  if (RW > 1 ? odd_value != 0 : odd) {
+    for (int key = first_key; key < tile_end * KT; ++key) {
+      if (key + KT - key % KT <= u.len || (KW > 1 && key / KT % KW != first_tile % KW) || key >= seen || idle) continue;
+      const int page = uniform(page_of(key));
+      if (page < 0) continue;
+      const int64_t at = page * page_bytes + (key & in_page) * (D * 2);
+      T4 v[DB];
+      bool any = false;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) y[r] = (T)(x[r] * inv);
-      const int64_t head = (int64_t)u.head * G + g;
-      *(T4*)(a.out + u.b * a.out_batch + t * a.out_token + (head * D + dim) * 2) = y;
-      if (first && a.lse) a.lse[((int64_t)u.b * a.shape.slots + t) * c.kv_heads * G + head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+      for (int d = 0; d < DB; ++d) {
+        v[d] = *(const T4*)(v_head + at + (d * 16 + quad * 4) * 2);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) any = any || !(__builtin_fabsf((float)v[d][r]) < INFINITY);
+      }
+      if (!__any(any)) continue;
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        float x = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < DK; ++kk) {
+          const T8 k = *(const T8*)(k_head + at + quad * 16 + kk * 64);
+#pragma unroll
+          for (int r = 0; r < 8; ++r) x = __builtin_fmaf((float)k[r], (float)q[m][kk][r], x);
+        }
+        x += __shfl_xor(x, 16); x += __shfl_xor(x, 32);
+        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x, a.scale_log2e, -(m_run[m] == -INFINITY ? 0.f : m_run[m])));
+        if (slot[m] < 0 || !sees(slot[m], key)) continue;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) { const float y = (float)v[d][r]; if (!(__builtin_fabsf(y) < INFINITY)) o[m][d][r] += w * y; }
+      }
+    }
+  }
+
+  const auto put_out = [&](int t, int g, int dim, f32x4 x, float m, float l) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    T4 y;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) y[r] = (T)(x[r] * inv);
+    const int64_t head = (int64_t)u.head * G + g;
+    *(T4*)(a.out + u.b * a.out_batch + t * a.out_token + (head * D + dim) * 2) = y;
+    if (dim == 0 && a.lse) a.lse[((int64_t)u.b * a.shape.slots + t) * c.kv_heads * G + head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+  };
+  // what this workgroup has of a row: to the record of its part, or out
+  const auto put = [&](int row_in_tile, int t, int g, int dim, f32x4 x, float m, float l) {
+    if (u.parts > 1) {
+      const int64_t rec = ((int64_t)(u.slot0 + u.part) << a.shape.rows_shift) + row_in_tile;
+      uint64_t* to = (uint64_t*)(a.part_o + rec * D + dim);
+      st_dev64(to, x[0], x[1]); st_dev64(to + 1, x[2], x[3]);
+      if (dim == 0) st_dev64((uint64_t*)(a.part_ml + rec), m, l);
+    } else {
+      put_out(t, g, dim, x, m, l);
     }
   };
   if (KW == 1) {
@@ -450,7 +476,7 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
       const int r = wave_row0 + m * 16 + col;
       if (slot[m] < 0) continue;
 #pragma unroll
-      for (int d = 0; d < DB; ++d) put(rw * 16 * MT + m * 16 + col, slot[m], r - slot[m] * G, d * 16 + quad * 4, o[m][d], m_run[m], l_run[m], d == 0 && quad == 0);
+      for (int d = 0; d < DB; ++d) put(rw * 16 * MT + m * 16 + col, slot[m], r - slot[m] * G, d * 16 + quad * 4, o[m][d], m_run[m], l_run[m]);
     }
   } else {
     // the wavefronts' results of 16 rows at a time through LDS
@@ -479,43 +505,38 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
           x += f * *(const f32x4*)(jo + (w * 16 + row) * D + dim);
         }
         const int t = r / G;
-        put(m * 16 + row, t, r - t * G, dim, x, mm, l, dim == 0);
+        put(m * 16 + row, t, r - t * G, dim, x, mm, l);
       }
     }
   }
-}
+  if (u.parts == 1) return;
 
-// The parts of a unit joined.  One workgroup a unit; units of one part are done already.
-constexpr int JOIN_NT = 256;
-template <typename E, int D>
-__global__ __launch_bounds__(JOIN_NT) void k_attend_join(CacheView c, AttendArgs a) {
-  typedef typename E::T T; typedef typename E::T4 T4;
-  Unit u;
-  if (!find_unit<true>(c, a, blockIdx.x, &u) || u.parts == 1) return;
-  const int G = a.shape.group, row0 = u.row_tile * a.shape.rows_per_tile, rows = min(u.n_new * G - row0, a.shape.rows_per_tile);
-  for (int i = threadIdx.x; i < rows * (D / 4); i += JOIN_NT) {
+  // The unit's last part to get here joins them, in their order whichever it is.
+  __shared__ int last;
+  wait_vector_memory();
+  __syncthreads();
+  if (tid == 0) last = __hip_atomic_fetch_add(a.tickets + u.slot0, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == u.parts - 1;
+  __syncthreads();
+  if (!last) return;
+  if (tid == 0) st_dev(a.tickets + u.slot0, 0);
+  const int row0 = u.row_tile << a.shape.rows_shift, n_rows = min(rows - row0, 1 << a.shape.rows_shift);
+  for (int i = tid; i < n_rows * (D / 4); i += NT) {
     const int row = i / (D / 4), dim = i % (D / 4) * 4;
-    const float2* ml = a.part_ml + (int64_t)u.slot0 * a.shape.rows_per_tile + row;
-    const float* po = a.part_o + ((int64_t)u.slot0 * a.shape.rows_per_tile + row) * D + dim;
-    float mm = -INFINITY;
-    for (int p = 0; p < u.parts; ++p) mm = fmaxf(mm, ml[(int64_t)p * a.shape.rows_per_tile].x);
-    const float ref = mm == -INFINITY ? 0.f : mm;
+    const int64_t rec0 = ((int64_t)u.slot0 << a.shape.rows_shift) + row;
+    float mm = -INFINITY, l = 0.f;
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
-    float l = 0.f;
     for (int p = 0; p < u.parts; ++p) {
-      const float2 r = ml[(int64_t)p * a.shape.rows_per_tile];
-      const float f = __builtin_amdgcn_exp2f(r.x - ref);
-      l += f * r.y;
-      x += f * *(const f32x4*)(po + (int64_t)p * a.shape.rows_per_tile * D);
+      const int64_t rec = rec0 + ((int64_t)p << a.shape.rows_shift);
+      const uint64_t* from = (const uint64_t*)(a.part_o + rec * D + dim);
+      const float2 ml = ld_dev64((const uint64_t*)(a.part_ml + rec)), lo = ld_dev64(from), hi = ld_dev64(from + 1);
+      const float m_new = fmaxf(mm, ml.x), ref = m_new == -INFINITY ? 0.f : m_new;
+      const float back = __builtin_amdgcn_exp2f(mm - ref), f = __builtin_amdgcn_exp2f(ml.x - ref);
+      l = l * back + ml.y * f;
+      x = x * back + f32x4{lo.x, lo.y, hi.x, hi.y} * f;
+      mm = m_new;
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    T4 y;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) y[r] = (T)(x[r] * inv);
     const int at = row0 + row, t = at / G;
-    const int64_t head = (int64_t)u.head * G + (at - t * G);
-    *(T4*)(a.out + u.b * a.out_batch + t * a.out_token + (head * D + dim) * 2) = y;
-    if (dim == 0 && a.lse) a.lse[((int64_t)u.b * a.shape.slots + t) * c.kv_heads * G + head] = l == 0.f ? -INFINITY : (mm + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+    put_out(t, at - t * G, dim, x, mm, l);
   }
 }
 

@@ -42,7 +42,7 @@ C2T_HD int64_t row_offset(const CacheView& c, int layer, int page, int head, int
 }
 
 // ---- Attention's work ----
-// A unit is a tile of query rows of one cached head of one sequence; it goes over the sequence's keys in tiles of KT.  Units
+// A unit is a tile of query rows of one cached head of one sequence; it goes over the sequence's keys tile by tile.  Units
 // are split over their keys into parts so that the launch has about `target` parts of about the same length whatever
 // the lengths of the sequences: all parts have at most `per` = max(min_per, ceil(all tiles / target)) key tiles, a
 // sequence's units have ceil(its tiles / per) parts each.  Parts of one unit leave records for the join; there are never more than
@@ -50,16 +50,25 @@ C2T_HD int64_t row_offset(const CacheView& c, int layer, int page, int head, int
 struct AttendShape {
   int32_t slots;                           // new tokens a sequence at most
   int32_t group;                           // query heads per cached head
-  int32_t rows_per_tile, keys_per_tile;
-  int32_t target, min_per;
+  int32_t rows_shift, keys_shift;          // tiles of 1 << rows_shift query rows and 1 << keys_shift keys
+  int32_t target_shift, min_per;           // about 1 << target_shift parts, of min_per key tiles or more
+  int32_t run;                             // items in a row for one die
 };
-C2T_HD int row_tiles(const AttendShape& a, int n_new) { return (int)div_up64((int64_t)n_new * a.group, a.rows_per_tile); }
-C2T_HD int key_tiles(const AttendShape& a, int keys) { return div_up(keys, a.keys_per_tile); }
+// Workgroups go to the chip's eight dies in turn.  Neighbouring items, whose rows share keys, belong on one die and its L2; runs of
+// items are dealt to the dies in turn, since items come longest first.
+constexpr int DIES = 8;
+C2T_HD int item_of_workgroup(const AttendShape& a, int workgroup) {
+  const int i = workgroup / DIES;
+  return (i / a.run * DIES + workgroup % DIES) * a.run + i % a.run;
+}
+C2T_HD int64_t workgroups_for(const AttendShape& a, int64_t items) { return div_up64(items, DIES * a.run) * DIES * a.run; }
+C2T_HD int row_tiles(const AttendShape& a, int n_new) { return (int)(((int64_t)n_new * a.group + (1 << a.rows_shift) - 1) >> a.rows_shift); }
+C2T_HD int key_tiles(const AttendShape& a, int keys) { return (keys + (1 << a.keys_shift) - 1) >> a.keys_shift; }
 C2T_HD int64_t sequence_tiles(const CacheView& c, const AttendShape& a, int len, int n_new) {
   return (int64_t)row_tiles(a, n_new) * c.kv_heads * key_tiles(a, len + n_new);
 }
 C2T_HD int tiles_per_part(const AttendShape& a, int64_t all_tiles) {
-  const int64_t per = div_up64(all_tiles, a.target);
+  const int64_t per = (all_tiles + (1 << a.target_shift) - 1) >> a.target_shift;
   return per < a.min_per ? a.min_per : per > (1 << 30) ? 1 << 30 : (int)per;
 }
 C2T_HD int parts_of(const AttendShape& a, int per, int len, int n_new) {
@@ -72,7 +81,7 @@ C2T_HD int sequence_parts(const CacheView& c, const AttendShape& a, int per, int
 }
 // keys that some row of a tile of query rows sees, from the first: rows row0 .. of the sequence's n_new * group, `chain` causal slots ahead of the nodes
 C2T_HD int keys_seen(const AttendShape& a, int len, int n_new, int chain, int row_tile) {
-  const int64_t last_row = (int64_t)(row_tile + 1) * a.rows_per_tile - 1, rows = (int64_t)n_new * a.group;
+  const int64_t last_row = ((int64_t)(row_tile + 1) << a.rows_shift) - 1, rows = (int64_t)n_new * a.group;
   const int t = (int)((last_row < rows ? last_row : rows - 1) / a.group);
   return t < chain ? len + t + 1 : len + n_new;
 }

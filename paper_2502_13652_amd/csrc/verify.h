@@ -41,8 +41,7 @@ inline size_t reserve_bytes(const c2t_cache& c) { return ((size_t)2 * reserve_ca
 
 // ---- attention ----
 // Which kernel a launch of that many rows a cached head takes.
-struct AttendBuild { int rows_per_tile, keys_per_tile, threads; };
-enum { AB_ROWS_16, AB_ROWS_32, AB_ROWS_64, AB_ROWS_128 };
+enum { AB_ROWS_16, AB_ROWS_32, AB_ROWS_64, AB_ROWS_128 };    // 16 << build rows a tile
 inline int attend_build(int64_t rows, int head_dim) {
   return rows <= 16 ? AB_ROWS_16 : rows <= 32 && head_dim <= 128 ? AB_ROWS_32 : rows <= 64 ? AB_ROWS_64 : AB_ROWS_128;
 }
@@ -59,9 +58,7 @@ template <typename E, int D> AttendKernel attend_kernel(int build) {
 template <typename E> AttendKernel attend_kernel(int build, int head_dim) {
   return head_dim == 64 ? attend_kernel<E, 64>(build) : head_dim == 128 ? attend_kernel<E, 128>(build) : attend_kernel<E, 256>(build);
 }
-template <typename E> AttendKernel join_kernel(int head_dim) {
-  return head_dim == 64 ? k_attend_join<E, 64> : head_dim == 128 ? k_attend_join<E, 128> : k_attend_join<E, 256>;
-}
+constexpr int MAX_RUN = 8;
 struct AttendPlan { AttendShape shape; int build; int64_t units, items; size_t part_o, part_ml, total; };
 
 // Sizes of a call alone: the workspace must not depend on what is on the device.
@@ -73,24 +70,19 @@ inline int attend_plan(const c2t_cache& c, const c2t_attention& a, AttendPlan* p
   const int64_t rows = (int64_t)a.tokens * group;
   p->build = attend_build(rows, c.head_dim);
   p->shape.slots = a.tokens; p->shape.group = group;
-  static constexpr int ROWS[] = {16, 32, 64, 128};
   const bool by_keys = p->build <= AB_ROWS_32;
-  p->shape.rows_per_tile = ROWS[p->build];
-  p->shape.keys_per_tile = by_keys || c.head_dim > 128 ? 32 : 64;
-#ifndef TKW
-#define TKW 1024
-#define TRW 1024
-#define MKW 8
-#define MRW 4
-#endif
-  p->shape.target = by_keys ? TKW : TRW;
-  p->shape.min_per = by_keys ? MKW : MRW;
-  p->units = (int64_t)c.batch * c.kv_heads * div_up64(rows, p->shape.rows_per_tile);
-  p->items = (p->units + p->shape.target + DIES - 1) / DIES * DIES;
+  p->shape.rows_shift = 4 + p->build;
+  p->shape.keys_shift = by_keys || c.head_dim > 128 ? 5 : 6;
+  p->shape.target_shift = 10;
+  p->shape.min_per = by_keys ? 8 : 4;
+  p->units = (int64_t)c.batch * c.kv_heads * row_tiles(p->shape, a.tokens);
+  p->shape.run = std::min(row_tiles(p->shape, a.tokens), MAX_RUN);
+  p->items = workgroups_for(p->shape, p->units + (1 << p->shape.target_shift));
   if (p->items > INT32_MAX / 2) return C2T_ERR_UNSUPPORTED;
-  p->part_o = 0;
-  p->part_ml = (size_t)2 * p->shape.target * p->shape.rows_per_tile * c.head_dim * 4;
-  p->total = p->part_ml + (size_t)2 * p->shape.target * p->shape.rows_per_tile * 8;
+  const size_t records = (size_t)2 << p->shape.target_shift, rows_of_them = records << p->shape.rows_shift;
+  p->part_o = records * 4;                                   // the counters ahead, in the same place whatever the call's sizes
+  p->part_ml = p->part_o + rows_of_them * c.head_dim * 4;
+  p->total = p->part_ml + rows_of_them * 8;
   return C2T_OK;
 }
 
@@ -236,15 +228,24 @@ int c2t_cache_attention(const c2t_cache* c, const c2t_attention* a, void* ws, si
   g.q_batch = a->q_batch_stride * 2; g.q_token = a->q_token_stride * 2; g.out_batch = a->out_batch_stride * 2; g.out_token = a->out_token_stride * 2;
   g.n_new = a->n_new; g.mask = a->mask; g.nodes = a->nodes; g.chain = a->tokens - a->nodes; g.layer = a->layer;
   g.scale_log2e = std::max(a->scale, 1e-30f) * 1.44269504088896341f;       // (a masked score is -infinity times it: not 0)
-  g.part_o = (float*)((char*)ws + p.part_o); g.part_ml = (float2*)((char*)ws + p.part_ml);
+  g.tickets = (int32_t*)ws; g.part_o = (float*)((char*)ws + p.part_o); g.part_ml = (float2*)((char*)ws + p.part_ml);
   g.shape = p.shape;
   const CacheView v = view_of(*c);
   const bool bf16 = c->dtype == C2T_BF16;
   const AttendKernel fn = bf16 ? attend_kernel<Bf16>(p.build, c->head_dim) : attend_kernel<F16>(p.build, c->head_dim);
   hipLaunchKernelGGL(fn, dim3((unsigned)p.items), dim3(256), 0, (hipStream_t)stream, v, g);
-  const AttendKernel join = bf16 ? join_kernel<Bf16>(c->head_dim) : join_kernel<F16>(c->head_dim);
-  hipLaunchKernelGGL(join, dim3((unsigned)((p.units + DIES - 1) / DIES * DIES)), dim3(JOIN_NT), 0, (hipStream_t)stream, v, g);
   return hip_status();
+}
+
+int c2t_stream_capture_id(void* stream, uint64_t* out) {
+  if (!out) return C2T_ERR_INVALID_ARG;
+  *out = 0;
+  if (!stream) return C2T_OK;                                // (the default stream cannot be captured)
+  hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+  unsigned long long id = 0;
+  if (hipStreamGetCaptureInfo((hipStream_t)stream, &status, &id) != hipSuccess) { (void)hipGetLastError(); return C2T_ERR_HIP; }
+  if (status == hipStreamCaptureStatusActive) *out = id;
+  return C2T_OK;
 }
 
 int c2t_adjust_tree_logits(const c2t_adjustments* t, int32_t batch, int32_t vocab, int32_t nodes, int32_t dtype, const int32_t* tree_tokens,

@@ -200,11 +200,13 @@ class PagedCache:
         need = ctypes.c_size_t()
         _check(self.L.c2t_cache_workspace_bytes(self._ref, ctypes.byref(need)), "c2t_cache_workspace_bytes")
         self._ws = self._workspace(need.value)
-        self._attention_ws = {}                            # (stream, sizes of the call) -> workspace; kept: a captured graph may refer to it
+        self._attention_ws = {}                            # (stream, capture, bytes) -> workspace; kept: a captured graph refers to it
+        self._capture = ctypes.c_uint64()
+        self._capture_ref = ctypes.byref(self._capture)
         self._attention_bytes = {}
 
     def _workspace(self, nbytes):
-        w = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
+        w = torch.zeros(nbytes + 256, dtype=torch.uint8, device=self.device)
         pad = (-w.data_ptr()) % 256
         return w[pad:pad + nbytes]
 
@@ -258,7 +260,7 @@ class PagedCache:
         q [B][T][q_heads][head_dim]; mask uint8 [B][N][N] as finalize_tree writes it: the last N of the T slots are the tree's nodes, those
         before them (the root) a causal chain; no mask: all of them are.  scale: of the scores, default head_dim ** -0.5.  lse: float32
         [B][T][q_heads] for the log of the softmax's sums.  out: [B][T][q_heads][head_dim] (default: a new tensor), rows behind n_new left as
-        they are.  workspace: uint8 of attention_workspace_bytes, for calls that run at once otherwise than by stream."""
+        they are.  workspace: uint8, zeros, of attention_workspace_bytes and 256-byte aligned, for calls that run at once otherwise than by stream."""
         _need(q.dim() == 4, "q: [B][T][q_heads][head_dim]")
         heads, T = q.shape[2], q.shape[1]
         sq = self._tokens(q, heads, "q")
@@ -284,14 +286,24 @@ class PagedCache:
         def call(s):
             w = workspace
             if w is None:
-                w = self._attention_ws.get((s, need))
-                if w is None:
-                    w = self._attention_ws[(s, need)] = self._workspace(need)
+                w = self._attention_workspace(s, need)
             return self.L.c2t_cache_attention(self._ref, ref, w.data_ptr(), w.numel(), s)
         rc = _launch(self.device, stream, call)
         if rc != 0:
             raise binding.C2TError(rc, "c2t_cache_attention")
         return out
+
+    def _attention_workspace(self, s, need):
+        """One a stream, and one a captured graph: graphs may be replayed at once, and an eager call beside them."""
+        capture = 0
+        if s:
+            _check(self.L.c2t_stream_capture_id(s, self._capture_ref), "c2t_stream_capture_id")
+            capture = self._capture.value
+        key = (s, capture, need)
+        w = self._attention_ws.get(key)
+        if w is None:
+            w = self._attention_ws[key] = self._workspace(need)
+        return w
 
     def attention_workspace_bytes(self, tokens, q_heads, nodes=0):
         a = _Attention(tokens=tokens, q_heads=q_heads, nodes=nodes)

@@ -48,8 +48,9 @@ int main() {
     const CacheView c = cache(batch, 1 << 20, max_pages, shift, heads, 64);
     AttendShape a;
     a.slots = pick(1, 1 << pick(0, 9)); a.group = pick(1, 9);
-    a.rows_per_tile = 16 << pick(0, 4); a.keys_per_tile = 32 << pick(0, 1);
-    a.target = pick(1, 300); a.min_per = pick(1, 16);
+    a.rows_shift = pick(4, 8); a.keys_shift = pick(5, 6);
+    a.target_shift = pick(0, 8); a.min_per = pick(1, 16);
+    const int64_t target = (int64_t)1 << a.target_shift;
     const int chain = pick(0, a.slots);
     std::vector<int> len(batch), n(batch);
     int64_t all = 0;
@@ -60,7 +61,7 @@ int main() {
     }
     const int per = tiles_per_part(a, all);
     EXPECT(per >= a.min_per);
-    const int64_t units_max = (int64_t)batch * heads * div_up64((int64_t)a.slots * a.group, a.rows_per_tile);
+    const int64_t units_max = (int64_t)batch * heads * div_up64((int64_t)a.slots * a.group, 1 << a.rows_shift);
     int64_t items = 0, records = 0, units = 0;
     for (int b = 0; b < batch; ++b) {
       const int parts = n[b] ? parts_of(a, per, len[b], n[b]) : 0, tiles = row_tiles(a, n[b]);
@@ -72,7 +73,7 @@ int main() {
         const int seen = keys_seen(a, len[b], n[b], chain, rt), kt = key_tiles(a, seen);
         EXPECT(seen >= 1 && seen <= len[b] + n[b]);
         // the last row of the tile sees no key past `seen`
-        const int64_t last = std::min<int64_t>((int64_t)(rt + 1) * a.rows_per_tile, (int64_t)n[b] * a.group) - 1;
+        const int64_t last = std::min<int64_t>((int64_t)(rt + 1) << a.rows_shift, (int64_t)n[b] * a.group) - 1;
         const int t = (int)(last / a.group);
         EXPECT(t < n[b] && seen == (t < chain ? len[b] + t + 1 : len[b] + n[b]));
         int next = 0;
@@ -85,7 +86,18 @@ int main() {
         EXPECT(next == kt);
       }
     }
-    EXPECT(units <= units_max && items <= units_max + a.target && records <= 2 * (int64_t)a.target);
+    a.run = pick(1, 9);
+    const int64_t groups = workgroups_for(a, items);
+    EXPECT(groups >= items && groups < items + DIES * a.run + 1);
+    if (groups < 20000) {
+      std::vector<char> taken(groups, 0);
+      for (int w = 0; w < groups; ++w) {
+        const int item = item_of_workgroup(a, w);
+        EXPECT(item >= 0 && item < groups && !taken[item]);
+        taken[item] = 1;
+      }
+    }
+    EXPECT(units <= units_max && items <= units_max + target && records <= 2 * target);
   }
   std::printf("paged driver ok\n");
   return 0;

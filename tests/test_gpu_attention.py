@@ -240,6 +240,34 @@ def test_the_same_call_gives_the_same_bits_on_streams_and_in_graphs():
         assert torch.equal(out, again)
 
 
+def test_graphs_replayed_at_once_have_workspaces_of_their_own():
+    """Long splits in two graphs on two streams and an eager call beside them, over and over; a graph captured before any eager call."""
+    lens = [30000, 10, 900]
+    cache = make_cache(lens, 2, 16, 1, 128, BF, seed=12)
+    qs = [queries(3, 2, 8, 128, BF, 4 + i) for i in range(3)]
+    outs = [torch.zeros_like(q) for q in qs]
+    graphs = []
+    for i in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            cache.attention(0, qs[i], out=outs[i])
+        graphs.append(g)
+    want = [make_cache(lens, 2, 16, 1, 128, BF, seed=12).attention(0, q) for q in qs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(20):
+        for o in outs:
+            o.zero_()
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        cache.attention(0, qs[2], out=outs[2])
+        torch.cuda.synchronize()
+        for o, w in zip(outs, want):
+            assert torch.equal(o, w)
+
+
 def test_refusals():
     from paper_2502_13652_amd import PagedCache
     from paper_2502_13652_amd.binding import C2TError
