@@ -3,11 +3,13 @@
 //   a = times the token occurs in the sequence's context and on the row's path, o = the same without the prompt
 //   y = x;  a > 0: y = x > 0 ? x / r : x r;   y -= alpha o + beta [o > 0];   y += sum of the token's biases;   not allowed: y = -inf
 //
-// A workgroup has a stretch of the vocabulary and some of a sequence's rows: it counts the context's tokens of its stretch
-// in LDS once, and streams its stretch of each row past them, the tokens of the row's path added to the counts before and taken off
-// after.  A chunk of 16 bytes without a counted, biased or masked token is copied as it is.
+// A workgroup has a stretch of the vocabulary and some of a sequence's rows.  It counts the context's tokens of its stretch in
+// LDS once and lists the tokens that anything is done to: a few hundred of 4096 at most usually.  Rows then pass through LDS,
+// a few at a time: in as they are, the listed tokens changed in place (each by a thread of its own, so no lane waits for
+// another's), and out with the mask.  In place and without a mask only the listed tokens are read and written.
 #pragma once
 #include "k_common.h"
+#include "k_paged.h"
 
 namespace c2t {
 
@@ -23,133 +25,185 @@ struct AdjustArgs {
   const float* repetition; const float* frequency; const float* presence;
   const int32_t* bias_token; const float* bias; const int32_t* n_bias; int32_t bias_stride;
   const uint32_t* allowed; int64_t allowed_row, allowed_batch;               // strides in words
-  int32_t stretch;                         // tokens of a workgroup's stretch, a multiple of ADJUST_ALIGN
   int32_t rows_each;                       // rows of a workgroup
+  int32_t sparse;                          // in place and without a mask
 };
+
+template <typename X> struct Bits;
+template <> struct Bits<float> { typedef uint32_t U; };
+template <> struct Bits<__bf16> { typedef uint16_t U; };
 
 constexpr int ADJUST_NT = 512;
 constexpr int ADJUST_MAX_NODES = 1024, ADJUST_MAX_BIAS = 1024;
-constexpr int ADJUST_ALIGN = 64;
-constexpr int ADJUST_STRETCH = 8192;       // tokens at most
-constexpr uint32_t IN_PROMPT = 0x80000000u, BIASED = 0x40000000u, TIMES = 0x3fffffffu;      // a token's word: flags, times in output and path
+constexpr int ADJUST_STRETCH = 4096;       // tokens of a workgroup's stretch
+constexpr int ADJUST_BATCH_CHUNKS = 4;     // 16-byte chunks a thread of the rows that are in LDS at once
+// a token's word: flags, times in the output's part of the context
+constexpr uint32_t IN_PROMPT = 0x80000000u, BIASED = 0x40000000u, IN_TREE = 0x20000000u, TIMES = 0x1fffffffu;
+constexpr int ADJUST_MAX_CONTEXT = 1 << 28;
 
-template <typename X> struct Chunk;        // 16 bytes of logits
-template <> struct Chunk<float> {
-  static constexpr int N = 4;
-  static __device__ __forceinline__ float get(const uint4& v, int i) { return __uint_as_float(i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w); }
-  static __device__ __forceinline__ void set(uint4& v, int i, float x) { (i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w) = __float_as_uint(x); }
-};
-template <> struct Chunk<__bf16> {
-  static constexpr int N = 8;
-  static __device__ __forceinline__ float get(const uint4& v, int i) {
-    const uint32_t w = i / 2 == 0 ? v.x : i / 2 == 1 ? v.y : i / 2 == 2 ? v.z : v.w;
-    return i % 2 ? bf16_hi(w) : bf16_lo(w);
-  }
-  static __device__ __forceinline__ void set(uint4& v, int i, float x) {      // rounded to the nearest, ties to even
-    uint32_t& w = i / 2 == 0 ? v.x : i / 2 == 1 ? v.y : i / 2 == 2 ? v.z : v.w;
-    const uint32_t h = __builtin_bit_cast(uint16_t, (__bf16)x);
-    w = i % 2 ? (w & 0xffffu) | (h << 16) : (w & 0xffff0000u) | h;
-  }
-};
+template <typename X> constexpr int ADJUST_ROWS = ADJUST_BATCH_CHUNKS * ADJUST_NT * (16 / (int)sizeof(X)) / ADJUST_STRETCH;     // rows in LDS at once
 
 template <typename X>
 __global__ __launch_bounds__(ADJUST_NT) void k_adjust(AdjustArgs a) {
-  constexpr int N = Chunk<X>::N;
-  __shared__ __align__(16) uint32_t word[ADJUST_STRETCH];
-  __shared__ int32_t node_token[ADJUST_MAX_NODES];
-  __shared__ int16_t node_parent[ADJUST_MAX_NODES];
+  constexpr int N = 16 / sizeof(X), CPR = ADJUST_STRETCH / N / ADJUST_NT, RB = ADJUST_ROWS<X>, BIT_WORDS = ADJUST_MAX_NODES / 32;
+  typedef uint32_t U4 __attribute__((ext_vector_type(4)));
+  static_assert(CPR * RB == ADJUST_BATCH_CHUNKS && CPR >= 1, "");
+  __shared__ __align__(16) X row_lds[RB * ADJUST_STRETCH];
+  __shared__ uint32_t word[ADJUST_STRETCH];
+  __shared__ uint16_t touched[ADJUST_STRETCH];
+  __shared__ int16_t node_parent[ADJUST_MAX_NODES], node_here[ADJUST_MAX_NODES];       // the node's place in here_token, -1: its token is not in the stretch
+  __shared__ uint16_t here_token[ADJUST_MAX_NODES];
+  __shared__ uint32_t on_path[RB][BIT_WORDS];                // of a row in LDS: places in here_token of the nodes on its path
   __shared__ int32_t bias_at[ADJUST_MAX_BIAS];               // place in the stretch, -1: not in it
   __shared__ float bias_value[ADJUST_MAX_BIAS];              // of a token's first entry: the sum of all of its entries
-  const int tid = threadIdx.x, b = blockIdx.z, v0 = blockIdx.x * a.stretch, n_words = min(a.stretch, a.vocab - v0);
+  __shared__ int n_touched, n_here, n_bias_here;
+  __shared__ uint16_t bias_here[ADJUST_MAX_BIAS];            // first entries of tokens of the stretch
+  const int tid = threadIdx.x, b = blockIdx.z, v0 = blockIdx.x * ADJUST_STRETCH, n_words = min(ADJUST_STRETCH, a.vocab - v0);
   const int rows = min(max(a.n_rows[b] + a.more_rows, 0), a.rows);
   const int row0 = blockIdx.y * a.rows_each, row1 = min(row0 + a.rows_each, rows);
   if (row0 >= row1) return;
+  const char* const in0 = a.in + b * a.in_batch + (int64_t)v0 * sizeof(X);
+  char* const out0 = a.out + b * a.out_batch + (int64_t)v0 * sizeof(X);
+  const uint8_t* const ok0 = a.allowed ? (const uint8_t*)(a.allowed + b * a.allowed_batch) + v0 / 8 : nullptr;
 
-  for (int i = tid; i < a.stretch; i += ADJUST_NT) word[i] = 0u;
+  // rows r .. r + RB - 1 of the stretch, a thread's chunks of them; what is behind the vocabulary is not ours
+  U4 x[ADJUST_BATCH_CHUNKS];
+  uint32_t ok[ADJUST_BATCH_CHUNKS];
+  auto request = [&](int r) {
+#pragma unroll
+    for (int i = 0; i < ADJUST_BATCH_CHUNKS; ++i) {
+      const int at = (i % CPR * ADJUST_NT + tid) * N, row = min(r + i / CPR, row1 - 1);
+      x[i] = U4{0u, 0u, 0u, 0u}; ok[i] = 0xffu;
+      if (at + N <= n_words) x[i] = *(const U4*)(in0 + row * a.in_row + (int64_t)at * sizeof(X));
+      if (ok0 && at < n_words) ok[i] = (uint32_t)ok0[row * a.allowed_row * 4 + at / 8] >> (at % 8);
+    }
+  };
+  if (!a.sparse) request(row0);
+
+  for (int i = tid; i < ADJUST_STRETCH; i += ADJUST_NT) word[i] = 0u;
+  if (tid == 0) { n_touched = 0; n_here = 0; n_bias_here = 0; }
+  __syncthreads();
   const int n_nodes = a.node_token ? min(max(a.n_nodes[b], 0), a.nodes) : 0;
   for (int i = tid; i < n_nodes; i += ADJUST_NT) {
-    const int p = a.node_parent[(int64_t)b * a.nodes + i];
-    node_token[i] = a.node_token[(int64_t)b * a.nodes + i] - v0;
+    const int p = a.node_parent[(int64_t)b * a.nodes + i], t = a.node_token[(int64_t)b * a.nodes + i] - v0;
     node_parent[i] = (int16_t)(p < i ? max(p, -1) : -1);     // (a path ends however the tree was made)
+    const bool here = (uint32_t)t < (uint32_t)n_words;
+    int place = -1;
+    if (here) { place = append_place(&n_here); here_token[place] = (uint16_t)t; atomicOr(&word[t], IN_TREE); }
+    node_here[i] = (int16_t)place;
   }
-  __syncthreads();
   const int n_ctx = a.tokens ? (int)min((int64_t)max(a.n_tokens[b], 0), a.token_stride) : 0, n_prompt = a.n_prompt ? a.n_prompt[b] : 0;
   for (int i = tid; i < n_ctx; i += ADJUST_NT) {
     const int t = a.tokens[(int64_t)b * a.token_stride + i] - v0;
     if ((uint32_t)t < (uint32_t)n_words) { if (i < n_prompt) atomicOr(&word[t], IN_PROMPT); else atomicAdd(&word[t], 1u); }
   }
-  // biases of one token add up in the order in which they are listed, in the place of the first
   const int n_bias = a.bias ? min(max(a.n_bias ? a.n_bias[b] : a.bias_stride, 0), a.bias_stride) : 0;
   for (int i = tid; i < n_bias; i += ADJUST_NT) {
     const int t = a.bias_token[(int64_t)b * a.bias_stride + i] - v0;
     bias_at[i] = (uint32_t)t < (uint32_t)n_words ? t : -1;
   }
   __syncthreads();
+  // biases of one token add up in the order in which they are listed, in the place of the first
   for (int i = tid; i < n_bias; i += ADJUST_NT) {
     const int t = bias_at[i];
+    if (t < 0) continue;
+    bool first = true;
+    for (int j = 0; j < i && first; ++j) first = bias_at[j] != t;
+    if (!first) continue;
     float sum = 0.f;
-    bool first = t >= 0;
-    if (t >= 0) for (int j = 0; j < n_bias; ++j) {
-      if (bias_at[j] != t) continue;
-      if (j < i) { first = false; break; }
-      sum += a.bias[(int64_t)b * a.bias_stride + j];
-    }
+    for (int j = i; j < n_bias; ++j) if (bias_at[j] == t) sum += a.bias[(int64_t)b * a.bias_stride + j];
     bias_value[i] = sum;
-    if (first) atomicOr(&word[t], BIASED);
+    bias_here[append_place(&n_bias_here)] = (uint16_t)i;
+    atomicOr(&word[t], BIASED);
   }
+  __syncthreads();
+  for (int i = tid; i < n_words; i += ADJUST_NT) if (word[i] != 0u) touched[append_place(&n_touched)] = (uint16_t)i;
   __syncthreads();
 
   const float rep = a.repetition ? a.repetition[b] : 1.f, freq = a.frequency ? a.frequency[b] : 0.f, pres = a.presence ? a.presence[b] : 0.f;
-  // the tokens of a row's path counted (+1) or taken off again (-1); one lane walks it
-  auto path = [&](int r, uint32_t by) {
-    int node = a.row_node ? a.row_node[(int64_t)b * a.rows + r] : r - 1;
-    if (node >= n_nodes) node = -1;
-    while (node >= 0) {
-      const int t = node_token[node];
-      if ((uint32_t)t < (uint32_t)n_words) atomicAdd(&word[t], by);
-      node = node_parent[node];
+  const int n_list = uniform(n_touched), n_firsts = uniform(n_bias_here), bit_words = div_up(uniform(n_here), 32);
+  auto mark_paths = [&](int r) {                             // of rows r .. r + RB - 1: one lane walks each
+    for (int i = tid; i < RB * bit_words; i += ADJUST_NT) on_path[i / bit_words][i % bit_words] = 0u;
+    __syncthreads();
+    if (tid < RB && r + tid < row1) {
+      int node = a.row_node ? a.row_node[(int64_t)b * a.rows + r + tid] : r + tid - 1;
+      if (node >= n_nodes) node = -1;
+      while (node >= 0) {
+        const int h = node_here[node];
+        if (h >= 0) on_path[tid][h / 32] |= 1u << (h % 32);
+        node = node_parent[node];
+      }
     }
   };
-  for (int r = row0; r < row1; ++r) {
-    if (tid == 0) path(r, 1u);
+  // token t of row `row` of those in LDS, made of its logit; false: nothing is done to it
+  auto adjusted = [&](int t, int row, float* y) {
+    const uint32_t w = word[t];
+    uint32_t times = w & TIMES;
+    if (w & IN_TREE) {
+      for (int k = 0; k < bit_words; ++k)
+        for (uint32_t bits = on_path[row][k]; bits; bits &= bits - 1u) times += here_token[k * 32 + __builtin_ctz(bits)] == t;
+    }
+    float z = *y;
+    if (times != 0u || (w & IN_PROMPT)) z = z > 0.f ? z / rep : z * rep;
+    if (times != 0u) z -= freq * (float)times + pres;
+    if (w & BIASED) for (int k = 0; k < n_firsts; ++k) { const int e = bias_here[k]; if (bias_at[e] == t) { z += bias_value[e]; break; } }
+    *y = z;
+    return times != 0u || (w & (IN_PROMPT | BIASED)) != 0u;
+  };
+
+  if (a.sparse) {
+    for (int r = row0; r < row1; r += RB) {
+      mark_paths(r);
+      __syncthreads();
+      const int live = min(RB, row1 - r);
+      for (int i = tid; i < n_list * live; i += ADJUST_NT) {
+        const int row = i / n_list, t = touched[i - row * n_list];
+        X* at = (X*)(out0 + (r + row) * a.out_row) + t;
+        float y = (float)*at;
+        if (adjusted(t, row, &y)) *at = (X)y;
+      }
+      __syncthreads();
+    }
+    return;
+  }
+  for (int r = row0; r < row1; r += RB) {
+    const int live = min(RB, row1 - r);
+    uint32_t ok_now[ADJUST_BATCH_CHUNKS];
+#pragma unroll
+    for (int i = 0; i < ADJUST_BATCH_CHUNKS; ++i) {
+      const int at = (i % CPR * ADJUST_NT + tid) * N, row = i / CPR;
+      if (at + N <= n_words) *(U4*)(row_lds + row * ADJUST_STRETCH + at) = x[i];
+      else if (row < live) for (int j = at; j < n_words; ++j) row_lds[row * ADJUST_STRETCH + j] = ((const X*)(in0 + (r + row) * a.in_row))[j];
+      ok_now[i] = ok[i];
+    }
+    if (r + RB < row1) request(r + RB);
+    mark_paths(r);
     __syncthreads();
-    const char* in = a.in + b * a.in_batch + r * a.in_row + (int64_t)v0 * sizeof(X);
-    char* out = a.out + b * a.out_batch + r * a.out_row + (int64_t)v0 * sizeof(X);
-    const uint8_t* ok_bits = a.allowed ? (const uint8_t*)(a.allowed + b * a.allowed_batch + r * a.allowed_row) + v0 / 8 : nullptr;
-    for (int i0 = tid * N; i0 < n_words; i0 += ADJUST_NT * N) {
-      uint32_t ok = ok_bits ? (uint32_t)ok_bits[i0 / 8] >> (i0 % 8) : 0xffu;
-      const bool end = i0 + N > n_words;                     // the row's last logits: what is behind them is not ours
-      uint4 x = make_uint4(0u, 0u, 0u, 0u);
-      if (!end) x = *(const uint4*)(in + (int64_t)i0 * sizeof(X));
-      else for (int j = 0; j < n_words - i0; ++j) Chunk<X>::set(x, j, (float)((const X*)in)[i0 + j]);
-      uint32_t w[N], any = 0u;
-#pragma unroll
-      for (int j = 0; j < N; ++j) { w[j] = word[i0 + j]; any |= w[j]; }
-      const uint4 was = x;
-      if (any != 0u) {
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-          if (w[j] == 0u) continue;
-          float y = Chunk<X>::get(x, j);
-          const uint32_t times = w[j] & TIMES;
-          if (times != 0u || (w[j] & IN_PROMPT)) y = y > 0.f ? y / rep : y * rep;
-          if (times != 0u) y -= freq * (float)times + pres;
-          if (w[j] & BIASED) for (int k = 0; k < n_bias; ++k) if (bias_at[k] == i0 + j) { y += bias_value[k]; break; }
-          Chunk<X>::set(x, j, y);
-        }
-      }
-      if ((ok & ((1u << N) - 1u)) != (1u << N) - 1u) {
-#pragma unroll
-        for (int j = 0; j < N; ++j) if (!(ok >> j & 1u)) Chunk<X>::set(x, j, -INFINITY);
-      }
-      if (!end) {
-        if (in != out || was.x != x.x || was.y != x.y || was.z != x.z || was.w != x.w) *(uint4*)(out + (int64_t)i0 * sizeof(X)) = x;
-      } else {
-        for (int j = 0; j < n_words - i0; ++j) ((X*)out)[i0 + j] = (X)Chunk<X>::get(x, j);
-      }
+    for (int i = tid; i < n_list * live; i += ADJUST_NT) {
+      const int row = i / n_list, t = touched[i - row * n_list];
+      X* at = row_lds + row * ADJUST_STRETCH + t;
+      float y = (float)*at;
+      if (adjusted(t, row, &y)) *at = (X)y;
     }
     __syncthreads();
-    if (tid == 0) path(r, ~0u);
+#pragma unroll
+    for (int i = 0; i < ADJUST_BATCH_CHUNKS; ++i) {
+      const int at = (i % CPR * ADJUST_NT + tid) * N, row = i / CPR;
+      if (row >= live || at >= n_words) continue;
+      U4 y = *(const U4*)(row_lds + row * ADJUST_STRETCH + at);
+      constexpr uint32_t ALL = (1u << N) - 1u;
+      if ((ok_now[i] & ALL) != ALL) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (sizeof(X) == 4) y[j] = ok_now[i] >> j & 1u ? y[j] : 0xff800000u;
+          else y[j] = (ok_now[i] >> (2 * j) & 1u ? y[j] & 0xffffu : 0xff80u) | (ok_now[i] >> (2 * j + 1) & 1u ? y[j] & 0xffff0000u : 0xff800000u);
+        }
+      }
+      char* to = out0 + (r + row) * a.out_row + (int64_t)at * sizeof(X);
+      if (at + N <= n_words) *(U4*)to = y;
+      else for (int j = 0; j < n_words - at; ++j) ((X*)to)[j] = sizeof(X) == 4 ? __builtin_bit_cast(X, (typename Bits<X>::U)y[j]) : __builtin_bit_cast(X, (typename Bits<X>::U)(y[j / 2] >> (j % 2 * 16)));
+    }
+    __syncthreads();
   }
 }
 

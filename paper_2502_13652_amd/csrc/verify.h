@@ -73,9 +73,11 @@ inline int attend_plan(const c2t_cache& c, const c2t_attention& a, AttendPlan* p
   const bool by_keys = p->build <= AB_ROWS_32;
   p->shape.rows_shift = 4 + p->build;
   p->shape.keys_shift = by_keys || c.head_dim > 128 ? 5 : 6;
-  p->shape.target_shift = 10;
   p->shape.min_per = by_keys ? 8 : 4;
   p->units = (int64_t)c.batch * c.kv_heads * row_tiles(p->shape, a.tokens);
+  // Parts enough to fill two workgroups a CU twice; where there are units for that already, longest first, parts only of what is longer than its share:
+  // 1536 units of 64 sequences 243 us, with twice the parts 260, four times 347; 512 units of two prompts 604 and 571.
+  p->shape.target_shift = !by_keys && p->units >= 1024 ? 9 : 10;
   p->shape.run = std::min(row_tiles(p->shape, a.tokens), MAX_RUN);
   p->items = workgroups_for(p->shape, p->units + (1 << p->shape.target_shift));
   if (p->items > INT32_MAX / 2) return C2T_ERR_UNSUPPORTED;
@@ -101,13 +103,14 @@ inline int check_adjust(AdjustArgs& a, int dtype, int64_t in_stride, int64_t out
   return C2T_OK;
 }
 
+constexpr int ADJUST_WORKGROUPS = 1024;     // four rounds of two a CU
 inline int fill_adjust(AdjustArgs& a, const c2t_adjustments* t) {
   if (!t) return C2T_ERR_INVALID_ARG;
   if (t->tokens && (!t->n_tokens || t->token_stride <= 0)) return C2T_ERR_INVALID_ARG;
   if ((t->bias != nullptr) != (t->bias_tokens != nullptr) || (t->bias && t->bias_stride <= 0)) return C2T_ERR_INVALID_ARG;
   if (t->allowed && (t->allowed_row_stride < 0 || t->allowed_batch_stride < 0)) return C2T_ERR_INVALID_ARG;
   if (t->allowed_row_stride > MAX_STRIDE || t->allowed_batch_stride > MAX_STRIDE) return C2T_ERR_UNSUPPORTED;
-  if (t->token_stride > (1 << 29) || (t->bias && t->bias_stride > C2T_MAX_BIAS)) return C2T_ERR_UNSUPPORTED;
+  if (t->token_stride > ADJUST_MAX_CONTEXT || (t->bias && t->bias_stride > C2T_MAX_BIAS)) return C2T_ERR_UNSUPPORTED;
   a.tokens = t->tokens; a.token_stride = t->token_stride; a.n_tokens = t->n_tokens; a.n_prompt = t->n_prompt;
   a.repetition = t->repetition; a.frequency = t->frequency; a.presence = t->presence;
   a.bias_token = t->bias_tokens; a.bias = t->bias; a.n_bias = t->n_bias; a.bias_stride = t->bias_stride;
@@ -116,10 +119,10 @@ inline int fill_adjust(AdjustArgs& a, const c2t_adjustments* t) {
 }
 
 inline int launch_adjust(AdjustArgs a, int dtype, hipStream_t s) {
-  a.stretch = ADJUST_STRETCH;
-  const int stretches = div_up(a.vocab, a.stretch);
-  const int64_t wanted = div_up64(1024, (int64_t)stretches * a.batch);        // groups of rows
-  a.rows_each = div_up(a.rows, (int)std::min<int64_t>(wanted, a.rows));
+  const int stretches = div_up(a.vocab, ADJUST_STRETCH), batch = dtype == C2T_BF16 ? ADJUST_ROWS<__bf16> : ADJUST_ROWS<float>;
+  const int64_t groups = div_up64(ADJUST_WORKGROUPS, (int64_t)stretches * a.batch);    // of rows
+  a.rows_each = div_up(div_up(a.rows, (int)std::min<int64_t>(groups, a.rows)), batch) * batch;
+  a.sparse = a.in == a.out && !a.allowed;
   const dim3 grid((unsigned)stretches, (unsigned)div_up(a.rows, a.rows_each), (unsigned)a.batch);
   if (dtype == C2T_BF16) hipLaunchKernelGGL(k_adjust<__bf16>, grid, dim3(ADJUST_NT), 0, s, a);
   else hipLaunchKernelGGL(k_adjust<float>, grid, dim3(ADJUST_NT), 0, s, a);
