@@ -2,6 +2,7 @@
 include/c2t.h).  Argument marshalling and checks only; like the binding it needs a GPU and has no fallback."""
 import ctypes
 import dataclasses
+import struct
 from typing import Optional
 
 import torch
@@ -31,8 +32,19 @@ class _Attention(ctypes.Structure):
                 ("layer", ctypes.c_int32), ("nodes", ctypes.c_int32), ("mask", ctypes.c_void_p), ("scale", ctypes.c_float)]
 
 
+def _packer(fields):
+    """A call's structure as bytes: a third of the time that ctypes takes to fill one.  The layout is the structure's."""
+    code = {ctypes.c_void_p: "P", ctypes.c_int64: "q", ctypes.c_int32: "i", ctypes.c_float: "f"}
+    p = struct.Struct("@" + "".join(code[t] for _, t in fields._fields_) + "0P")
+    assert p.size == ctypes.sizeof(fields)
+    return p.pack
+
+
+_pack_adjustments, _pack_attention = _packer(_Adjustments), _packer(_Attention)
+
+
 def _ptr(t):
-    return None if t is None else t.data_ptr()
+    return 0 if t is None else t.data_ptr()
 
 
 def _need(ok, what):
@@ -41,21 +53,24 @@ def _need(ok, what):
 
 
 def _whole(t, device, dtype, shape, name):
-    """A contiguous device tensor of that type; -1 in `shape`: any size."""
-    _need(torch.is_tensor(t) and t.device == device and t.dtype == dtype and t.is_contiguous() and t.dim() == len(shape) and
-          all(s in (-1, n) for s, n in zip(shape, t.shape)),
-          "%s: a contiguous %s tensor %s on %s" % (name, dtype, list(shape), device))
-    return t
+    """A contiguous device tensor of that type and shape; -1 in the shape: any size."""
+    if torch.is_tensor(t) and t.dtype is dtype and t.device == device and t.is_contiguous():
+        have = t.shape
+        if have == shape or (-1 in shape and len(have) == len(shape) and all(s in (-1, n) for s, n in zip(shape, have))):
+            return t
+    raise ValueError("%s: a contiguous %s tensor %s on %s" % (name, dtype, list(shape), device))
 
 
-def _launch(device, stream, call):
-    """call(stream handle) with the tensors' device current."""
-    if stream is not None:
-        _need(stream.device == device, "stream: of another device than the tensors")
-    if torch._C._cuda_getDevice() == device.index:
-        return call(binding._stream_ptr(stream))
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _launch(device, stream, fn, *args):
+    """fn(*args, stream handle) with the tensors' device current."""
+    if stream is None and _current_device() == device.index:
+        return fn(*args, binding._stream_ptr(None))
+    _need(stream is None or stream.device == device, "stream: of another device than the tensors")
     with torch.cuda.device(device):
-        return call(binding._stream_ptr(stream))
+        return fn(*args, binding._stream_ptr(stream))
 
 
 def _empty_like_on(stream, make):
@@ -84,38 +99,44 @@ class LogitAdjustments:
     n_bias: Optional[torch.Tensor] = None
     allowed: Optional[torch.Tensor] = None
 
-    def _struct(self, B, rows, V, device):
+    def _packed(self, B, rows, V, device):
         i32, f32 = torch.int32, torch.float32
-        _need((self.tokens is None) == (self.n_tokens is None), "tokens and n_tokens come together")
-        _need((self.bias is None) == (self.bias_tokens is None), "bias and bias_tokens come together")
-        if self.tokens is not None:
-            _whole(self.tokens, device, i32, (B, -1), "tokens")
-        for name, dtype in (("n_tokens", i32), ("n_prompt", i32), ("n_bias", i32), ("repetition", f32), ("frequency", f32), ("presence", f32)):
-            if getattr(self, name) is not None:
-                _whole(getattr(self, name), device, dtype, (B,), name)
-        if self.bias is not None:
-            _whole(self.bias, device, f32, (B, -1), "bias")
-            _whole(self.bias_tokens, device, i32, tuple(self.bias.shape), "bias_tokens")
-        row = batch = 0
-        if self.allowed is not None:
+        tokens, n_tokens, n_prompt, bias, bias_tokens, n_bias, allowed = \
+            self.tokens, self.n_tokens, self.n_prompt, self.bias, self.bias_tokens, self.n_bias, self.allowed
+        _need((tokens is None) == (n_tokens is None), "tokens and n_tokens come together")
+        _need((bias is None) == (bias_tokens is None), "bias and bias_tokens come together")
+        one = (B,)
+
+        def each(t, dtype, name):
+            return 0 if t is None else _whole(t, device, dtype, one, name).data_ptr()
+        p_tokens = p_n = p_bias = p_bias_tokens = L = M = p_allowed = row = batch = 0
+        if tokens is not None:
+            L = _whole(tokens, device, i32, (B, -1), "tokens").shape[1]
+            p_tokens, p_n = tokens.data_ptr(), each(n_tokens, i32, "n_tokens")
+        p_prompt = each(n_prompt, i32, "n_prompt")
+        if L == 0:                                         # a list without a place holds nothing; its address would be none
+            p_tokens = p_n = p_prompt = 0
+        if bias is not None:
+            M = _whole(bias, device, f32, (B, -1), "bias").shape[1]
+            p_bias, p_bias_tokens = bias.data_ptr(), _whole(bias_tokens, device, i32, (B, M), "bias_tokens").data_ptr()
+            if M == 0:
+                p_bias = p_bias_tokens = 0
+        if allowed is not None:
             words = (V + 31) // 32
-            _whole(self.allowed, device, i32, (B, -1, words), "allowed")
-            _need(self.allowed.shape[1] in (1, rows), "allowed: a mask a row, or one a sequence")
-            row, batch = (words if self.allowed.shape[1] == rows else 0), self.allowed.shape[1] * words
-        # a list without a place holds nothing; its address would be none
-        tokens = self.tokens if self.tokens is not None and self.tokens.shape[1] else None
-        bias = self.bias if self.bias is not None and self.bias.shape[1] else None
-        return _Adjustments(_ptr(tokens), tokens.shape[1] if tokens is not None else 0, _ptr(self.n_tokens) if tokens is not None else None,
-                            _ptr(self.n_prompt) if tokens is not None else None,
-                            _ptr(self.repetition), _ptr(self.frequency), _ptr(self.presence), _ptr(self.bias_tokens) if bias is not None else None, _ptr(bias),
-                            _ptr(self.n_bias), bias.shape[1] if bias is not None else 0, _ptr(self.allowed), row, batch)
+            masks = _whole(allowed, device, i32, (B, -1, words), "allowed").shape[1]
+            _need(masks in (1, rows), "allowed: a mask a row, or one a sequence")
+            p_allowed, row, batch = allowed.data_ptr(), (words if masks == rows else 0), masks * words
+        return _pack_adjustments(p_tokens, L, p_n, p_prompt, each(self.repetition, f32, "repetition"), each(self.frequency, f32, "frequency"),
+                                 each(self.presence, f32, "presence"), p_bias_tokens, p_bias, each(n_bias, i32, "n_bias"), M, p_allowed, row, batch)
 
 
 def _rows(x, B, rows, V, name):
-    _need(x.is_cuda and x.dim() == 3 and x.shape[0] == B and x.shape[1] == rows and x.shape[2] >= V and x.stride(2) == 1 and
-          (B == 1 or x.stride(0) == rows * x.stride(1) or rows == 1 and x.stride(0) >= V), "%s: [%d][%d][at least %d], rows evenly spaced" % (name, B, rows, V))
+    """The distance of a logits tensor's rows, in elements."""
+    shape, strides = x.shape, x.stride()
+    _need(x.is_cuda and len(shape) == 3 and shape[0] == B and shape[1] == rows and shape[2] >= V and strides[2] == 1 and
+          (B == 1 or strides[0] == rows * strides[1] or rows == 1 and strides[0] >= V), "%s: [%d][%d][at least %d], rows evenly spaced" % (name, B, rows, V))
     # (a sequence's one row is as far from the next one's as the sequences are; one row alone may be anywhere)
-    return x.stride(1) if rows > 1 else x.stride(0) if B > 1 else max(x.stride(1), V + (-V) % (16 // x.element_size()))
+    return strides[1] if rows > 1 else strides[0] if B > 1 else max(strides[1], V + (-V) % (16 // x.element_size()))
 
 
 def adjust_tree_logits(logits, tree, adjustments, vocab=None, out=None, stream=None):
@@ -123,39 +144,36 @@ def adjust_tree_logits(logits, tree, adjustments, vocab=None, out=None, stream=N
     LogitAdjustments) made, into `out` (a new tensor; may be `logits`).  tree: a finalize_tree output (tokens, parent, n_nodes), or None for one
     row a sequence.  Rows behind a sequence's nodes, and what is behind `vocab` (default: all), are left as they are."""
     L = load_library()
-    B, rows = logits.shape[0], logits.shape[1]
-    V = logits.shape[2] if vocab is None else int(vocab)
-    dev = logits.device
-    _need(logits.dtype in (torch.float32, torch.bfloat16), "logits: float32 or bfloat16")
+    B, rows, width = logits.shape
+    V = width if vocab is None else int(vocab)
+    dev, dtype = logits.device, logits.dtype
+    _need(dtype is torch.float32 or dtype is torch.bfloat16, "logits: float32 or bfloat16")
     stride = _rows(logits, B, rows, V, "logits")
     if tree is None:
         _need(rows == 1, "logits: one row a sequence without a tree")
         tokens = parent = None
-        n_nodes = torch.zeros(B, dtype=torch.int32, device=dev)
+        n_nodes = _empty_like_on(stream, lambda: torch.zeros(B, dtype=torch.int32, device=dev))
     else:
-        tokens, parent, n_nodes = (_whole(tree[k], dev, torch.int32, s, "tree " + k) for k, s in
-                                   (("tokens", (B, rows - 1)), ("parent", (B, rows - 1)), ("n_nodes", (B,))))
+        nodes = (B, rows - 1)
+        tokens, parent = _whole(tree["tokens"], dev, torch.int32, nodes, "tree tokens"), _whole(tree["parent"], dev, torch.int32, nodes, "tree parent")
+        n_nodes = _whole(tree["n_nodes"], dev, torch.int32, (B,), "tree n_nodes")
     if out is None:
-        out = _empty_like_on(stream, lambda: torch.empty((B, rows, stride), dtype=logits.dtype, device=dev)[:, :, :logits.shape[2]])
-    _need(out.dtype == logits.dtype and out.device == dev, "out: of the logits' type and device")
-    a = adjustments._struct(B, rows, V, dev)
-    out_stride = _rows(out, B, rows, V, "out")
-    _check(_launch(dev, stream, lambda s: L.c2t_adjust_tree_logits(ctypes.byref(a), B, V, rows - 1, _DTYPES[logits.dtype], _ptr(tokens), _ptr(parent), n_nodes.data_ptr(),
-                                                                    logits.data_ptr(), stride, out.data_ptr(), out_stride, s)), "c2t_adjust_tree_logits")
+        out = _empty_like_on(stream, lambda: torch.empty((B, rows, stride), dtype=dtype, device=dev)[:, :, :width])
+    _need(out.dtype is dtype and out.device == dev, "out: of the logits' type and device")
+    _check(_launch(dev, stream, L.c2t_adjust_tree_logits, adjustments._packed(B, rows, V, dev), B, V, rows - 1, _DTYPES[dtype], _ptr(tokens), _ptr(parent),
+                   n_nodes.data_ptr(), logits.data_ptr(), stride, out.data_ptr(), _rows(out, B, rows, V, "out")), "c2t_adjust_tree_logits")
     return out
 
 
 def adjust_frontier_logits(ctx, logits, adjustments, out=None, stream=None):
     """C2TContext.adjust_logits."""
     B, F, V = ctx.B, ctx.F, ctx.V
-    _need(logits.dtype == ctx._logits_dtype and logits.device == ctx._ws.device, "logits: of the context's type and device")
-    stride = _rows(logits, B, F, V, "logits")
+    dev = logits.device
+    _need(logits.dtype is ctx._logits_dtype and dev == ctx._ws.device, "logits: of the context's type and device")
     out = logits if out is None else out
-    _need(out.dtype == logits.dtype and out.device == logits.device, "out: of the logits' type and device")
-    a = adjustments._struct(B, F, V, logits.device)
-    out_stride = _rows(out, B, F, V, "out")
-    _check(_launch(logits.device, stream, lambda s: ctx.L.c2t_adjust_logits(ctx.ctx, ctypes.byref(a), logits.data_ptr(), stride, out.data_ptr(), out_stride, s)),
-           "c2t_adjust_logits")
+    _need(out.dtype is logits.dtype and out.device == dev, "out: of the logits' type and device")
+    _check(_launch(dev, stream, ctx.L.c2t_adjust_logits, ctx.ctx, adjustments._packed(B, F, V, dev), logits.data_ptr(), _rows(logits, B, F, V, "logits"),
+                   out.data_ptr(), _rows(out, B, F, V, "out")), "c2t_adjust_logits")
     return out
 
 
@@ -197,6 +215,7 @@ class PagedCache:
         self._c = _Cache(batch, layers, pages, page_size, kv_heads, head_dim, max_pages, _DTYPES[k.dtype], k.data_ptr(), v.data_ptr(), page_table.data_ptr(),
                          length.data_ptr(), refcount.data_ptr(), self.status.data_ptr())
         self._ref = ctypes.byref(self._c)
+        self._each, self._scale = (batch,), head_dim ** -0.5
         need = ctypes.c_size_t()
         _check(self.L.c2t_cache_workspace_bytes(self._ref, ctypes.byref(need)), "c2t_cache_workspace_bytes")
         self._ws = self._workspace(need.value)
@@ -211,31 +230,31 @@ class PagedCache:
         return w[pad:pad + nbytes]
 
     def _run(self, what, stream, *args):
-        fn = getattr(self.L, what)
-        rc = _launch(self.device, stream, lambda s: fn(self._ref, *args, s))
+        rc = _launch(self.device, stream, getattr(self.L, what), self._ref, *args)
         if rc != 0:
             raise binding.C2TError(rc, what)
 
     def _per_sequence(self, t, name):
-        return _whole(t, self.device, torch.int32, (self.batch,), name).data_ptr()
+        return _whole(t, self.device, torch.int32, self._each, name).data_ptr()
 
     def reserve(self, n_new, stream=None):
         """Pages for n_new (int32 [B]) tokens behind each sequence's length, its own to write."""
         self._run("c2t_cache_reserve", stream, self._per_sequence(n_new, "n_new"), self._ws.data_ptr(), self._ws.numel())
 
     def _tokens(self, x, heads, name):
-        _need(x.device == self.device and x.dtype == self.dtype and x.dim() == 4 and x.shape[0] == self.batch and x.shape[1] > 0 and
-              x.shape[2] == heads and x.shape[3] == self.head_dim and x.stride(3) == 1 and (heads == 1 or x.stride(2) == self.head_dim),
-              "%s: %s [%d][tokens][%d][%d] on %s, heads next to each other" % (name, self.dtype, self.batch, heads, self.head_dim, self.device))
+        """Batch and token stride of [B][tokens][heads][head_dim]."""
+        shape, strides = x.shape, x.stride()
+        D = self.head_dim
+        if not (x.dtype is self.dtype and len(shape) == 4 and shape[0] == self.batch and shape[1] > 0 and shape[2] == heads and shape[3] == D and
+                strides[3] == 1 and (heads == 1 or strides[2] == D) and x.device == self.device):
+            raise ValueError("%s: %s [%d][tokens][%d][%d] on %s, heads next to each other" % (name, self.dtype, self.batch, heads, D, self.device))
         # (a stride over one element is of no use and may be any number)
-        row = heads * self.head_dim
-        token = x.stride(1) if x.shape[1] > 1 else row
-        return (x.stride(0) if self.batch > 1 else row), token
+        return (strides[0] if self.batch > 1 else heads * D), (strides[1] if shape[1] > 1 else heads * D)
 
     def write(self, layer, k, v, n_new=None, stream=None):
         """K and V [B][tokens][kv_heads][head_dim] of new tokens, n_new (int32 [B], default all) of them, to positions length + t of `layer`."""
-        sk, sv = self._tokens(k, self.kv_heads, "k"), self._tokens(v, self.kv_heads, "v")
-        _need(k.shape == v.shape and sk == sv, "k and v: of one shape and strides")
+        sk = self._tokens(k, self.kv_heads, "k")
+        _need(self._tokens(v, self.kv_heads, "v") == sk and k.shape == v.shape, "k and v: of one shape and strides")
         self._run("c2t_cache_write", stream, int(layer), k.data_ptr(), v.data_ptr(), sk[0], sk[1], k.shape[1],
                   None if n_new is None else self._per_sequence(n_new, "n_new"))
 
@@ -262,36 +281,31 @@ class PagedCache:
         [B][T][q_heads] for the log of the softmax's sums.  out: [B][T][q_heads][head_dim] (default: a new tensor), rows behind n_new left as
         they are.  workspace: uint8, zeros, of attention_workspace_bytes and 256-byte aligned, for calls that run at once otherwise than by stream."""
         _need(q.dim() == 4, "q: [B][T][q_heads][head_dim]")
-        heads, T = q.shape[2], q.shape[1]
+        _, T, heads, _ = q.shape
         sq = self._tokens(q, heads, "q")
         if out is None:
             out = _empty_like_on(stream, lambda: torch.empty((self.batch, T, heads, self.head_dim), dtype=self.dtype, device=self.device))
-        _need(out.shape == q.shape, "out: of q's shape")
         so = self._tokens(out, heads, "out")
-        nodes = 0
+        _need(out.shape[1] == T, "out: of q's shape")
+        nodes = p_mask = p_lse = 0
         if mask is not None:
             nodes = mask.shape[-1]
-            _whole(mask, self.device, torch.uint8, (self.batch, nodes, nodes), "mask")
+            p_mask = _whole(mask, self.device, torch.uint8, (self.batch, nodes, nodes), "mask").data_ptr() if nodes else 0
         if lse is not None:
-            _whole(lse, self.device, torch.float32, (self.batch, T, heads), "lse")
-        a = _Attention(q.data_ptr(), sq[0], sq[1], out.data_ptr(), so[0], so[1], _ptr(lse), None if n_new is None else self._per_sequence(n_new, "n_new"),
-                       T, heads, int(layer), nodes, _ptr(mask) if nodes else None, self.head_dim ** -0.5 if scale is None else float(scale))
-        ref = ctypes.byref(a)
+            p_lse = _whole(lse, self.device, torch.float32, (self.batch, T, heads), "lse").data_ptr()
+        a = _pack_attention(q.data_ptr(), sq[0], sq[1], out.data_ptr(), so[0], so[1], p_lse, 0 if n_new is None else self._per_sequence(n_new, "n_new"),
+                            T, heads, layer, nodes, p_mask, self._scale if scale is None else scale)
         need = self._attention_bytes.get((T, heads, nodes))
         if need is None:
-            n = ctypes.c_size_t()
-            _check(self.L.c2t_attention_workspace_bytes(self._ref, ref, ctypes.byref(n)), "c2t_attention_workspace_bytes")
-            need = self._attention_bytes[(T, heads, nodes)] = n.value
-
-        def call(s):
-            w = workspace
-            if w is None:
-                w = self._attention_workspace(s, need)
-            return self.L.c2t_cache_attention(self._ref, ref, w.data_ptr(), w.numel(), s)
-        rc = _launch(self.device, stream, call)
+            need = self._attention_bytes[(T, heads, nodes)] = self.attention_workspace_bytes(T, heads, nodes)
+        rc = _launch(self.device, stream, self._attend, a, workspace, need)
         if rc != 0:
             raise binding.C2TError(rc, "c2t_cache_attention")
         return out
+
+    def _attend(self, a, workspace, need, s):
+        w = self._attention_workspace(s, need) if workspace is None else workspace
+        return self.L.c2t_cache_attention(self._ref, a, w.data_ptr(), w.numel(), s)
 
     def _attention_workspace(self, s, need):
         """One a stream, and one a captured graph: graphs may be replayed at once, and an eager call beside them."""
