@@ -40,12 +40,13 @@ constexpr int ADJUST_BATCH_CHUNKS = 4;     // 16-byte chunks a thread of the row
 // a token's word: flags, times in the output's part of the context
 constexpr uint32_t IN_PROMPT = 0x80000000u, BIASED = 0x40000000u, IN_TREE = 0x20000000u, TIMES = 0x1fffffffu;
 constexpr int ADJUST_MAX_CONTEXT = 1 << 28;
+constexpr int ADJUST_PATH_WORDS = 1024;    // 32 rows of a tree whose nodes' tokens all lie in the stretch, and hundreds usually
 
 template <typename X> constexpr int ADJUST_ROWS = ADJUST_BATCH_CHUNKS * ADJUST_NT * (16 / (int)sizeof(X)) / ADJUST_STRETCH;     // rows in LDS at once
 
 template <typename X>
 __global__ __launch_bounds__(ADJUST_NT) void k_adjust(AdjustArgs a) {
-  constexpr int N = 16 / sizeof(X), CPR = ADJUST_STRETCH / N / ADJUST_NT, RB = ADJUST_ROWS<X>, BIT_WORDS = ADJUST_MAX_NODES / 32;
+  constexpr int N = 16 / sizeof(X), CPR = ADJUST_STRETCH / N / ADJUST_NT, RB = ADJUST_ROWS<X>;
   typedef uint32_t U4 __attribute__((ext_vector_type(4)));
   static_assert(CPR * RB == ADJUST_BATCH_CHUNKS && CPR >= 1, "");
   __shared__ __align__(16) X row_lds[RB * ADJUST_STRETCH];
@@ -53,7 +54,7 @@ __global__ __launch_bounds__(ADJUST_NT) void k_adjust(AdjustArgs a) {
   __shared__ uint16_t touched[ADJUST_STRETCH];
   __shared__ int16_t node_parent[ADJUST_MAX_NODES], node_here[ADJUST_MAX_NODES];       // the node's place in here_token, -1: its token is not in the stretch
   __shared__ uint16_t here_token[ADJUST_MAX_NODES];
-  __shared__ uint32_t on_path[RB][BIT_WORDS];                // of a row in LDS: places in here_token of the nodes on its path
+  __shared__ uint32_t on_path[ADJUST_PATH_WORDS];            // of some rows: places in here_token of the nodes on the row's path
   __shared__ int32_t bias_at[ADJUST_MAX_BIAS];               // place in the stretch, -1: not in it
   __shared__ float bias_value[ADJUST_MAX_BIAS];              // of a token's first entry: the sum of all of its entries
   __shared__ int n_touched, n_here, n_bias_here;
@@ -104,16 +105,16 @@ __global__ __launch_bounds__(ADJUST_NT) void k_adjust(AdjustArgs a) {
   }
   __syncthreads();
   // biases of one token add up in the order in which they are listed, in the place of the first
-  for (int i = tid; i < n_bias; i += ADJUST_NT) {
-    const int t = bias_at[i];
-    if (t < 0) continue;
-    bool first = true;
-    for (int j = 0; j < i && first; ++j) first = bias_at[j] != t;
-    if (!first) continue;
-    float sum = 0.f;
-    for (int j = i; j < n_bias; ++j) if (bias_at[j] == t) sum += a.bias[(int64_t)b * a.bias_stride + j];
-    bias_value[i] = sum;
-    bias_here[append_place(&n_bias_here)] = (uint16_t)i;
+  for (int i = tid; i < n_bias; i += ADJUST_NT) if (bias_at[i] >= 0) bias_here[append_place(&n_bias_here)] = (uint16_t)i;
+  __syncthreads();
+  const int n_listed = uniform(n_bias_here);
+  for (int k = tid; k < n_listed; k += ADJUST_NT) {
+    const int i = bias_here[k], t = bias_at[i];
+    bool first = true, alone = true;
+    for (int e = 0; e < n_listed; ++e) { const int j = bias_here[e]; if (bias_at[j] == t) { alone = alone && j == i; first = first && j >= i; } }
+    float sum = a.bias[(int64_t)b * a.bias_stride + i];
+    if (!alone) { sum = 0.f; for (int j = 0; j < n_bias; ++j) if (bias_at[j] == t) sum += a.bias[(int64_t)b * a.bias_stride + j]; }
+    bias_value[i] = first ? sum : 0.f;                       // (added over all of the token's entries: the first one's counts)
     atomicOr(&word[t], BIASED);
   }
   __syncthreads();
@@ -121,51 +122,61 @@ __global__ __launch_bounds__(ADJUST_NT) void k_adjust(AdjustArgs a) {
   __syncthreads();
 
   const float rep = a.repetition ? a.repetition[b] : 1.f, freq = a.frequency ? a.frequency[b] : 0.f, pres = a.presence ? a.presence[b] : 0.f;
-  const int n_list = uniform(n_touched), n_firsts = uniform(n_bias_here), bit_words = div_up(uniform(n_here), 32);
-  auto mark_paths = [&](int r) {                             // of rows r .. r + RB - 1: one lane walks each
-    for (int i = tid; i < RB * bit_words; i += ADJUST_NT) on_path[i / bit_words][i % bit_words] = 0u;
+  const int n_list = uniform(n_touched), bit_words = div_up(uniform(n_here), 32);
+  const int rows_marked = bit_words == 0 ? a.rows_each : max(ADJUST_PATH_WORDS / bit_words / RB, 1) * RB;     // rows that on_path holds at once, a multiple of RB
+  // the paths of rows r, r + 1, ... as far as they are marked at once: one lane walks each
+  auto mark_paths = [&](int r) {
+    const int n = min(rows_marked, row1 - r);
+    for (int i = tid; i < n * bit_words; i += ADJUST_NT) on_path[i] = 0u;
     __syncthreads();
-    if (tid < RB && r + tid < row1) {
-      int node = a.row_node ? a.row_node[(int64_t)b * a.rows + r + tid] : r + tid - 1;
+    if (bit_words > 0) for (int i = tid; i < n; i += ADJUST_NT) {
+      int node = a.row_node ? a.row_node[(int64_t)b * a.rows + r + i] : r + i - 1;
       if (node >= n_nodes) node = -1;
       while (node >= 0) {
         const int h = node_here[node];
-        if (h >= 0) on_path[tid][h / 32] |= 1u << (h % 32);
         node = node_parent[node];
+        if (h >= 0) on_path[i * bit_words + h / 32] |= 1u << (h % 32);
       }
     }
+    __syncthreads();
   };
-  // token t of row `row` of those in LDS, made of its logit; false: nothing is done to it
+  // token t of the row that is `row` behind the first marked one, made of its logit; false: nothing is done to it
   auto adjusted = [&](int t, int row, float* y) {
     const uint32_t w = word[t];
     uint32_t times = w & TIMES;
     if (w & IN_TREE) {
       for (int k = 0; k < bit_words; ++k)
-        for (uint32_t bits = on_path[row][k]; bits; bits &= bits - 1u) times += here_token[k * 32 + __builtin_ctz(bits)] == t;
+        for (uint32_t bits = on_path[row * bit_words + k]; bits; bits &= bits - 1u) times += here_token[k * 32 + __builtin_ctz(bits)] == t;
     }
     float z = *y;
     if (times != 0u || (w & IN_PROMPT)) z = z > 0.f ? z / rep : z * rep;
     if (times != 0u) z -= freq * (float)times + pres;
-    if (w & BIASED) for (int k = 0; k < n_firsts; ++k) { const int e = bias_here[k]; if (bias_at[e] == t) { z += bias_value[e]; break; } }
+    if (w & BIASED) {
+      float bias = 0.f;
+      for (int k = 0; k < n_listed; ++k) { const int e = bias_here[k]; bias += bias_at[e] == t ? bias_value[e] : 0.f; }
+      z += bias;
+    }
     *y = z;
     return times != 0u || (w & (IN_PROMPT | BIASED)) != 0u;
   };
 
   if (a.sparse) {
-    for (int r = row0; r < row1; r += RB) {
+    for (int r = row0; r < row1; r += rows_marked) {
       mark_paths(r);
-      __syncthreads();
-      const int live = min(RB, row1 - r);
-      for (int i = tid; i < n_list * live; i += ADJUST_NT) {
-        const int row = i / n_list, t = touched[i - row * n_list];
-        X* at = (X*)(out0 + (r + row) * a.out_row) + t;
-        float y = (float)*at;
-        if (adjusted(t, row, &y)) *at = (X)y;
-      }
+      const int live = min(rows_marked, row1 - r);
+      for (int row = 0; row < live; ++row)
+        for (int i = tid; i < n_list; i += ADJUST_NT) {
+          const int t = touched[i];
+          X* at = (X*)(out0 + (r + row) * a.out_row) + t;
+          float y = (float)*at;
+          if (adjusted(t, row, &y)) *at = (X)y;
+        }
       __syncthreads();
     }
     return;
   }
+  int marked = row0;                                         // the first row that on_path holds
+  mark_paths(row0);
   for (int r = row0; r < row1; r += RB) {
     const int live = min(RB, row1 - r);
     uint32_t ok_now[ADJUST_BATCH_CHUNKS];
@@ -177,13 +188,13 @@ __global__ __launch_bounds__(ADJUST_NT) void k_adjust(AdjustArgs a) {
       ok_now[i] = ok[i];
     }
     if (r + RB < row1) request(r + RB);
-    mark_paths(r);
+    if (r - marked >= rows_marked) { marked = r; mark_paths(r); }
     __syncthreads();
     for (int i = tid; i < n_list * live; i += ADJUST_NT) {
       const int row = i / n_list, t = touched[i - row * n_list];
       X* at = row_lds + row * ADJUST_STRETCH + t;
       float y = (float)*at;
-      if (adjusted(t, row, &y)) *at = (X)y;
+      if (adjusted(t, r - marked + row, &y)) *at = (X)y;
     }
     __syncthreads();
 #pragma unroll

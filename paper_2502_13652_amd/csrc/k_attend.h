@@ -39,9 +39,10 @@ struct AttendArgs {
   int32_t nodes, chain;                    // slots = chain + nodes
   int32_t layer;
   float scale_log2e;
-  // records of parts: [records][rows of a tile][head_dim], and (m, l) of each row; tickets [records]: parts of the unit with that first record that
-  // have left theirs, zero between launches
+  // records of parts: [records][rows of a tile][head_dim], and (m, l) of each row.  Joined by the unit's last part: tickets [records], parts of the
+  // unit with that first record that have left theirs, zero between launches.  Joined by a launch of their own: what each record is of, and how many there are.
   float* part_o; float2* part_ml; int32_t* tickets;
+  struct Unit* units; int32_t* n_records;
   AttendShape shape;
 };
 
@@ -81,9 +82,10 @@ __device__ __forceinline__ bool find_item(const CacheView& c, const AttendArgs& 
     items += parts;
     if (parts_of(a.shape, per, len, n) > 1) slots += parts;
   }
-  const int items_to = wave_scan_incl(items);
+  const int items_to = wave_scan_incl(items), slots_to = wave_scan_incl(slots);
+  if (workgroup == 0 && threadIdx.x == WAVE - 1) *a.n_records = slots_to;
   const int w = item_of_workgroup(a.shape, workgroup);
-  int item0 = items_to - items, slot0 = wave_scan_incl(slots) - slots;
+  int item0 = items_to - items, slot0 = slots_to - slots;
   const bool here = w >= item0 && w < item0 + items;
   const uint64_t has = __ballot(here);
   if (has == 0ull) return false;
@@ -120,6 +122,31 @@ template <typename E, int D> struct TileLayout {
 template <typename E> __device__ __forceinline__ uint32_t odd_halves(uint32_t w) {     // halves whose exponent is all ones, as a mask of them
   return ((w & E::EXPONENT) == E::EXPONENT ? 0xffffu : 0u) | (((w >> 16) & E::EXPONENT) == E::EXPONENT ? 0xffff0000u : 0u);
 }
+
+// four neighbouring elements of a row's output, and with the first of them its log of the sum
+template <typename E, int D>
+__device__ __forceinline__ void put_row(const CacheView& c, const AttendArgs& a, const Unit& u, int t, int g, int dim, f32x4 x, float m, float l) {
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  typename E::T4 y;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) y[r] = (typename E::T)(x[r] * inv);
+  const int64_t head = (int64_t)u.head * a.shape.group + g;
+  *(typename E::T4*)(a.out + u.b * a.out_batch + t * a.out_token + (head * D + dim) * 2) = y;
+  if (dim == 0 && a.lse)
+    a.lse[((int64_t)u.b * a.shape.slots + t) * c.kv_heads * a.shape.group + head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+}
+// running join of parts
+struct Joined {
+  float m = -INFINITY, l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  __device__ __forceinline__ void add(float2 ml, f32x4 x) {
+    const float m_new = fmaxf(m, ml.x), ref = m_new == -INFINITY ? 0.f : m_new;
+    const float back = __builtin_amdgcn_exp2f(m - ref), f = __builtin_amdgcn_exp2f(ml.x - ref);
+    l = l * back + ml.y * f;
+    o = o * back + x * f;
+    m = m_new;
+  }
+};
 
 // A product's result, used in a later block than the product: the compiler has been seen to read it there before the matrix unit has
 // written it (it counts the wait from the wrong instruction), so it is moved to ordinary registers in the product's own block, where the wait is right.
@@ -450,25 +477,13 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
     }
   }
 
-  const auto put_out = [&](int t, int g, int dim, f32x4 x, float m, float l) {
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    T4 y;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) y[r] = (T)(x[r] * inv);
-    const int64_t head = (int64_t)u.head * G + g;
-    *(T4*)(a.out + u.b * a.out_batch + t * a.out_token + (head * D + dim) * 2) = y;
-    if (dim == 0 && a.lse) a.lse[((int64_t)u.b * a.shape.slots + t) * c.kv_heads * G + head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
-  };
   // what this workgroup has of a row: to the record of its part, or out
   const auto put = [&](int row_in_tile, int t, int g, int dim, f32x4 x, float m, float l) {
-    if (u.parts > 1) {
-      const int64_t rec = ((int64_t)(u.slot0 + u.part) << a.shape.rows_shift) + row_in_tile;
-      uint64_t* to = (uint64_t*)(a.part_o + rec * D + dim);
-      st_dev64(to, x[0], x[1]); st_dev64(to + 1, x[2], x[3]);
-      if (dim == 0) st_dev64((uint64_t*)(a.part_ml + rec), m, l);
-    } else {
-      put_out(t, g, dim, x, m, l);
-    }
+    if (u.parts == 1) { put_row<E, D>(c, a, u, t, g, dim, x, m, l); return; }
+    const int64_t rec = ((int64_t)(u.slot0 + u.part) << a.shape.rows_shift) + row_in_tile;
+    float* to = a.part_o + rec * D + dim;
+    if (KW > 1) { st_dev64((uint64_t*)to, x[0], x[1]); st_dev64((uint64_t*)to + 1, x[2], x[3]); if (dim == 0) st_dev64((uint64_t*)(a.part_ml + rec), m, l); }
+    else { *(f32x4*)to = x; if (dim == 0) a.part_ml[rec] = make_float2(m, l); }
   };
   if (KW == 1) {
 #pragma unroll
@@ -510,8 +525,10 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
     }
   }
   if (u.parts == 1) return;
+  if (KW == 1) { if (tid == 0) a.units[u.slot0 + u.part] = u; return; }      // joined by the next launch
 
-  // The unit's last part to get here joins them, in their order whichever it is.
+  // Few rows: the unit's last part to get here joins them, in their order whichever it is.  Each load is waited for some microseconds, so
+  // those of several parts are asked for at once.
   __shared__ int last;
   wait_vector_memory();
   __syncthreads();
@@ -519,24 +536,47 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
   __syncthreads();
   if (!last) return;
   if (tid == 0) st_dev(a.tickets + u.slot0, 0);
+  constexpr int AT_ONCE = 8;
   const int row0 = u.row_tile << a.shape.rows_shift, n_rows = min(rows - row0, 1 << a.shape.rows_shift);
   for (int i = tid; i < n_rows * (D / 4); i += NT) {
     const int row = i / (D / 4), dim = i % (D / 4) * 4;
     const int64_t rec0 = ((int64_t)u.slot0 << a.shape.rows_shift) + row;
-    float mm = -INFINITY, l = 0.f;
-    f32x4 x = {0.f, 0.f, 0.f, 0.f};
-    for (int p = 0; p < u.parts; ++p) {
-      const int64_t rec = rec0 + ((int64_t)p << a.shape.rows_shift);
-      const uint64_t* from = (const uint64_t*)(a.part_o + rec * D + dim);
-      const float2 ml = ld_dev64((const uint64_t*)(a.part_ml + rec)), lo = ld_dev64(from), hi = ld_dev64(from + 1);
-      const float m_new = fmaxf(mm, ml.x), ref = m_new == -INFINITY ? 0.f : m_new;
-      const float back = __builtin_amdgcn_exp2f(mm - ref), f = __builtin_amdgcn_exp2f(ml.x - ref);
-      l = l * back + ml.y * f;
-      x = x * back + f32x4{lo.x, lo.y, hi.x, hi.y} * f;
-      mm = m_new;
+    Joined x;
+    for (int p0 = 0; p0 < u.parts; p0 += AT_ONCE) {
+      float2 ml[AT_ONCE], lo[AT_ONCE], hi[AT_ONCE];
+#pragma unroll
+      for (int p = 0; p < AT_ONCE; ++p) {
+        const int64_t rec = rec0 + ((int64_t)min(p0 + p, u.parts - 1) << a.shape.rows_shift);
+        const uint64_t* from = (const uint64_t*)(a.part_o + rec * D + dim);
+        ml[p] = ld_dev64((const uint64_t*)(a.part_ml + rec)); lo[p] = ld_dev64(from); hi[p] = ld_dev64(from + 1);
+      }
+#pragma unroll
+      for (int p = 0; p < AT_ONCE; ++p) if (p0 + p < u.parts) x.add(ml[p], f32x4{lo[p].x, lo[p].y, hi[p].x, hi[p].y});
     }
     const int at = row0 + row, t = at / G;
-    put_out(t, at - t * G, dim, x, mm, l);
+    put_row<E, D>(c, a, u, t, at - t * G, dim, x.o, x.m, x.l);
+  }
+}
+
+// The parts of units of many rows, joined: a workgroup a record, which takes its share of its unit's rows.
+constexpr int JOIN_NT = 256;
+template <typename E, int D>
+__global__ __launch_bounds__(JOIN_NT) void k_attend_join(CacheView c, AttendArgs a) {
+  if ((int)blockIdx.x >= *a.n_records) return;
+  const Unit u = a.units[blockIdx.x];
+  const int G = a.shape.group, row0 = u.row_tile << a.shape.rows_shift, n_rows = min(u.n_new * G - row0, 1 << a.shape.rows_shift);
+  const int each = div_up(n_rows, u.parts), first = min(u.part * each, n_rows), end = min(first + each, n_rows);
+  for (int i = threadIdx.x; i < (end - first) * (D / 4); i += JOIN_NT) {
+    const int row = first + i / (D / 4), dim = i % (D / 4) * 4;
+    const int64_t rec0 = ((int64_t)u.slot0 << a.shape.rows_shift) + row;
+    Joined x;
+#pragma unroll 4
+    for (int p = 0; p < u.parts; ++p) {
+      const int64_t rec = rec0 + ((int64_t)p << a.shape.rows_shift);
+      x.add(a.part_ml[rec], *(const f32x4*)(a.part_o + rec * D + dim));
+    }
+    const int at = row0 + row, t = at / G;
+    put_row<E, D>(c, a, u, t, at - t * G, dim, x.o, x.m, x.l);
   }
 }
 

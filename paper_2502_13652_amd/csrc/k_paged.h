@@ -44,14 +44,15 @@ C2T_HD int64_t row_offset(const CacheView& c, int layer, int page, int head, int
 // ---- Attention's work ----
 // A unit is a tile of query rows of one cached head of one sequence; it goes over the sequence's keys tile by tile.  Units
 // are split over their keys into parts so that the launch has about `target` parts of about the same length whatever
-// the lengths of the sequences: all parts have at most `per` = max(min_per, ceil(all tiles / target)) key tiles, a
-// sequence's units have ceil(its tiles / per) parts each.  Parts of one unit leave records for the join; there are never more than
+// the lengths of the sequences: with `per` = max(min_per, ceil(all tiles / target)), a
+// sequence's units have ceil(its tiles / per) parts each, up to max_parts.  Parts of one unit leave records for the join; there are never more than
 // 2 target of those: a unit of p >= 2 parts has more than per (p - 1) >= per p / 2 tiles.
 struct AttendShape {
   int32_t slots;                           // new tokens a sequence at most
   int32_t group;                           // query heads per cached head
   int32_t rows_shift, keys_shift;          // tiles of 1 << rows_shift query rows and 1 << keys_shift keys
   int32_t target_shift, min_per;           // about 1 << target_shift parts, of min_per key tiles or more
+  int32_t max_parts;                       // of a unit, 2 or more
   int32_t run;                             // items in a row for one die
 };
 // Workgroups go to the chip's eight dies in turn.  Neighbouring items, whose rows share keys, belong on one die and its L2; runs of
@@ -73,7 +74,8 @@ C2T_HD int tiles_per_part(const AttendShape& a, int64_t all_tiles) {
 }
 C2T_HD int parts_of(const AttendShape& a, int per, int len, int n_new) {
   const int t = key_tiles(a, len + n_new);
-  return t <= per ? 1 : div_up(t, per);
+  const int parts = t <= per ? 1 : div_up(t, per);
+  return parts < a.max_parts ? parts : a.max_parts;
 }
 // parts of all units of a sequence
 C2T_HD int sequence_parts(const CacheView& c, const AttendShape& a, int per, int len, int n_new) {

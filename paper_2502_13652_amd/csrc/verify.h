@@ -58,8 +58,13 @@ template <typename E, int D> AttendKernel attend_kernel(int build) {
 template <typename E> AttendKernel attend_kernel(int build, int head_dim) {
   return head_dim == 64 ? attend_kernel<E, 64>(build) : head_dim == 128 ? attend_kernel<E, 128>(build) : attend_kernel<E, 256>(build);
 }
+template <typename E> AttendKernel join_kernel(int head_dim) {
+  return head_dim == 64 ? k_attend_join<E, 64> : head_dim == 128 ? k_attend_join<E, 128> : k_attend_join<E, 256>;
+}
 constexpr int MAX_RUN = 8;
-struct AttendPlan { AttendShape shape; int build; int64_t units, items; size_t part_o, part_ml, total; };
+constexpr int MAX_TARGET_SHIFT = 10, MAX_PARTS_ROWS = 64;
+constexpr int64_t JOIN_BYTES = 256 << 10;
+struct AttendPlan { AttendShape shape; int build, records; int64_t units, items; size_t n_records, units_at, part_o, part_ml, total; };
 
 // Sizes of a call alone: the workspace must not depend on what is on the device.
 inline int attend_plan(const c2t_cache& c, const c2t_attention& a, AttendPlan* p) {
@@ -77,12 +82,18 @@ inline int attend_plan(const c2t_cache& c, const c2t_attention& a, AttendPlan* p
   p->units = (int64_t)c.batch * c.kv_heads * row_tiles(p->shape, a.tokens);
   // Parts enough to fill two workgroups a CU twice; where there are units for that already, longest first, parts only of what is longer than its share:
   // 1536 units of 64 sequences 243 us, with twice the parts 260, four times 347; 512 units of two prompts 604 and 571.
-  p->shape.target_shift = !by_keys && p->units >= 1024 ? 9 : 10;
+  p->shape.target_shift = !by_keys && p->units >= 1024 ? 9 : MAX_TARGET_SHIFT;
   p->shape.run = std::min(row_tiles(p->shape, a.tokens), MAX_RUN);
   p->items = workgroups_for(p->shape, p->units + (1 << p->shape.target_shift));
   if (p->items > INT32_MAX / 2) return C2T_ERR_UNSUPPORTED;
+  // records of a unit: as many as its join reads in a few microseconds, by one workgroup where it has few rows, by one a record where it has more
+  const int64_t record = std::min(rows, (int64_t)1 << p->shape.rows_shift) * c.head_dim * 4;
+  p->shape.max_parts = by_keys ? (int)std::max<int64_t>(JOIN_BYTES / record, 2) : MAX_PARTS_ROWS;
   const size_t records = (size_t)2 << p->shape.target_shift, rows_of_them = records << p->shape.rows_shift;
-  p->part_o = records * 4;                                   // the counters ahead, in the same place whatever the call's sizes
+  p->n_records = (size_t)(2 << MAX_TARGET_SHIFT) * 4;        // behind the counters, whose place is the same whatever the call's sizes
+  p->units_at = p->n_records + 256;
+  p->part_o = p->units_at + (sizeof(Unit) << (MAX_TARGET_SHIFT + 1));
+  p->records = (int)records;
   p->part_ml = p->part_o + rows_of_them * c.head_dim * 4;
   p->total = p->part_ml + rows_of_them * 8;
   return C2T_OK;
@@ -231,12 +242,15 @@ int c2t_cache_attention(const c2t_cache* c, const c2t_attention* a, void* ws, si
   g.q_batch = a->q_batch_stride * 2; g.q_token = a->q_token_stride * 2; g.out_batch = a->out_batch_stride * 2; g.out_token = a->out_token_stride * 2;
   g.n_new = a->n_new; g.mask = a->mask; g.nodes = a->nodes; g.chain = a->tokens - a->nodes; g.layer = a->layer;
   g.scale_log2e = std::max(a->scale, 1e-30f) * 1.44269504088896341f;       // (a masked score is -infinity times it: not 0)
-  g.tickets = (int32_t*)ws; g.part_o = (float*)((char*)ws + p.part_o); g.part_ml = (float2*)((char*)ws + p.part_ml);
+  g.tickets = (int32_t*)ws; g.n_records = (int32_t*)((char*)ws + p.n_records); g.units = (Unit*)((char*)ws + p.units_at);
+  g.part_o = (float*)((char*)ws + p.part_o); g.part_ml = (float2*)((char*)ws + p.part_ml);
   g.shape = p.shape;
   const CacheView v = view_of(*c);
   const bool bf16 = c->dtype == C2T_BF16;
   const AttendKernel fn = bf16 ? attend_kernel<Bf16>(p.build, c->head_dim) : attend_kernel<F16>(p.build, c->head_dim);
   hipLaunchKernelGGL(fn, dim3((unsigned)p.items), dim3(256), 0, (hipStream_t)stream, v, g);
+  if (p.build >= AB_ROWS_64)
+    hipLaunchKernelGGL(bf16 ? join_kernel<Bf16>(c->head_dim) : join_kernel<F16>(c->head_dim), dim3((unsigned)p.records), dim3(JOIN_NT), 0, (hipStream_t)stream, v, g);
   return hip_status();
 }
 

@@ -49,7 +49,7 @@ int main() {
     AttendShape a;
     a.slots = pick(1, 1 << pick(0, 9)); a.group = pick(1, 9);
     a.rows_shift = pick(4, 8); a.keys_shift = pick(5, 6);
-    a.target_shift = pick(0, 8); a.min_per = pick(1, 16);
+    a.target_shift = pick(0, 8); a.min_per = pick(1, 16); a.max_parts = round % 3 ? 1 << 30 : pick(2, 40);
     const int64_t target = (int64_t)1 << a.target_shift;
     const int chain = pick(0, a.slots);
     std::vector<int> len(batch), n(batch);
@@ -80,7 +80,7 @@ int main() {
         for (int p = 0; p < parts; ++p) {
           int first, end;
           part_range(kt, parts, p, &first, &end);
-          EXPECT(first == next && first <= end && end <= kt && end - first <= per);
+          EXPECT(first == next && first <= end && end <= kt && (end - first <= per || parts == a.max_parts));
           next = end;
         }
         EXPECT(next == kt);
