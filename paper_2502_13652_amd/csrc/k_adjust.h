@@ -37,7 +37,7 @@ constexpr int ADJUST_NT = 512;
 constexpr int ADJUST_MAX_NODES = 1024, ADJUST_MAX_BIAS = 1024;
 constexpr int ADJUST_STRETCH = 4096;       // tokens of a workgroup's stretch
 constexpr int ADJUST_BATCH_CHUNKS = 4;     // 16-byte chunks a thread of the rows that are in LDS at once
-// a token's word: flags, times in the output's part of the context
+// a token's word: flags, times in the output's part of the context (of a biased token: its first entry, which has the times and the sum of its biases)
 constexpr uint32_t IN_PROMPT = 0x80000000u, BIASED = 0x40000000u, IN_TREE = 0x20000000u, TIMES = 0x1fffffffu;
 constexpr int ADJUST_MAX_CONTEXT = 1 << 28;
 constexpr int ADJUST_PATH_WORDS = 1024;    // 32 rows of a tree whose nodes' tokens all lie in the stretch, and hundreds usually
@@ -55,7 +55,7 @@ __global__ __launch_bounds__(ADJUST_NT) void k_adjust(AdjustArgs a) {
   __shared__ int16_t node_parent[ADJUST_MAX_NODES], node_here[ADJUST_MAX_NODES];       // the node's place in here_token, -1: its token is not in the stretch
   __shared__ uint16_t here_token[ADJUST_MAX_NODES];
   __shared__ uint32_t on_path[ADJUST_PATH_WORDS];            // of some rows: places in here_token of the nodes on the row's path
-  __shared__ int32_t bias_at[ADJUST_MAX_BIAS];               // place in the stretch, -1: not in it
+  __shared__ int32_t bias_at[ADJUST_MAX_BIAS];               // place in the stretch, -1: not in it; then, of a token's first entry: its times
   __shared__ float bias_value[ADJUST_MAX_BIAS];              // of a token's first entry: the sum of all of its entries
   __shared__ int n_touched, n_here, n_bias_here;
   __shared__ uint16_t bias_here[ADJUST_MAX_BIAS];            // first entries of tokens of the stretch
@@ -108,14 +108,27 @@ __global__ __launch_bounds__(ADJUST_NT) void k_adjust(AdjustArgs a) {
   for (int i = tid; i < n_bias; i += ADJUST_NT) if (bias_at[i] >= 0) bias_here[append_place(&n_bias_here)] = (uint16_t)i;
   __syncthreads();
   const int n_listed = uniform(n_bias_here);
-  for (int k = tid; k < n_listed; k += ADJUST_NT) {
+  bool is_first[ADJUST_MAX_BIAS / ADJUST_NT];
+#pragma unroll
+  for (int x = 0; x < ADJUST_MAX_BIAS / ADJUST_NT; ++x) {
+    const int k = x * ADJUST_NT + tid;
+    is_first[x] = false;
+    if (k >= n_listed) continue;
     const int i = bias_here[k], t = bias_at[i];
     bool first = true, alone = true;
     for (int e = 0; e < n_listed; ++e) { const int j = bias_here[e]; if (bias_at[j] == t) { alone = alone && j == i; first = first && j >= i; } }
     float sum = a.bias[(int64_t)b * a.bias_stride + i];
     if (!alone) { sum = 0.f; for (int j = 0; j < n_bias; ++j) if (bias_at[j] == t) sum += a.bias[(int64_t)b * a.bias_stride + j]; }
-    bias_value[i] = first ? sum : 0.f;                       // (added over all of the token's entries: the first one's counts)
-    atomicOr(&word[t], BIASED);
+    bias_value[i] = sum;
+    is_first[x] = first;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int x = 0; x < ADJUST_MAX_BIAS / ADJUST_NT; ++x) {
+    if (!is_first[x]) continue;
+    const int i = bias_here[x * ADJUST_NT + tid], t = bias_at[i];
+    bias_at[i] = (int32_t)(word[t] & TIMES);                 // (nobody else's from here on)
+    word[t] = (word[t] & ~TIMES) | BIASED | (uint32_t)i;
   }
   __syncthreads();
   for (int i = tid; i < n_words; i += ADJUST_NT) if (word[i] != 0u) touched[append_place(&n_touched)] = (uint16_t)i;
@@ -143,7 +156,8 @@ __global__ __launch_bounds__(ADJUST_NT) void k_adjust(AdjustArgs a) {
   // token t of the row that is `row` behind the first marked one, made of its logit; false: nothing is done to it
   auto adjusted = [&](int t, int row, float* y) {
     const uint32_t w = word[t];
-    uint32_t times = w & TIMES;
+    const int entry = (int)(w & TIMES);
+    uint32_t times = w & BIASED ? (uint32_t)bias_at[entry] : w & TIMES;
     if (w & IN_TREE) {
       for (int k = 0; k < bit_words; ++k)
         for (uint32_t bits = on_path[row * bit_words + k]; bits; bits &= bits - 1u) times += here_token[k * 32 + __builtin_ctz(bits)] == t;
@@ -151,11 +165,7 @@ __global__ __launch_bounds__(ADJUST_NT) void k_adjust(AdjustArgs a) {
     float z = *y;
     if (times != 0u || (w & IN_PROMPT)) z = z > 0.f ? z / rep : z * rep;
     if (times != 0u) z -= freq * (float)times + pres;
-    if (w & BIASED) {
-      float bias = 0.f;
-      for (int k = 0; k < n_listed; ++k) { const int e = bias_here[k]; bias += bias_at[e] == t ? bias_value[e] : 0.f; }
-      z += bias;
-    }
+    if (w & BIASED) z += bias_value[entry];
     *y = z;
     return times != 0u || (w & (IN_PROMPT | BIASED)) != 0u;
   };

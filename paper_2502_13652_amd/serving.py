@@ -43,21 +43,20 @@ def _packer(fields):
 _pack_adjustments, _pack_attention = _packer(_Adjustments), _packer(_Attention)
 
 
-def _ptr(t):
-    return 0 if t is None else t.data_ptr()
-
-
 def _need(ok, what):
     if not ok:
         raise ValueError(what)
 
 
 def _whole(t, device, dtype, shape, name):
-    """A contiguous device tensor of that type and shape; -1 in the shape: any size."""
-    if torch.is_tensor(t) and t.dtype is dtype and t.device == device and t.is_contiguous():
-        have = t.shape
-        if have == shape or (-1 in shape and len(have) == len(shape) and all(s in (-1, n) for s, n in zip(shape, have))):
-            return t
+    """The address of a contiguous device tensor of that type and shape; -1 in the shape: any size."""
+    try:
+        if t.dtype is dtype and t.get_device() == device.index and t.is_contiguous():
+            have = t.shape
+            if have == shape or (-1 in shape and len(have) == len(shape) and all(s in (-1, n) for s, n in zip(shape, have))):
+                return t.data_ptr()
+    except AttributeError:                                   # no tensor
+        pass
     raise ValueError("%s: a contiguous %s tensor %s on %s" % (name, dtype, list(shape), device))
 
 
@@ -108,24 +107,26 @@ class LogitAdjustments:
         one = (B,)
 
         def each(t, dtype, name):
-            return 0 if t is None else _whole(t, device, dtype, one, name).data_ptr()
+            return 0 if t is None else _whole(t, device, dtype, one, name)
         p_tokens = p_n = p_bias = p_bias_tokens = L = M = p_allowed = row = batch = 0
         if tokens is not None:
-            L = _whole(tokens, device, i32, (B, -1), "tokens").shape[1]
-            p_tokens, p_n = tokens.data_ptr(), each(n_tokens, i32, "n_tokens")
+            p_tokens, p_n = _whole(tokens, device, i32, (B, -1), "tokens"), each(n_tokens, i32, "n_tokens")
+            L = tokens.shape[1]
         p_prompt = each(n_prompt, i32, "n_prompt")
         if L == 0:                                         # a list without a place holds nothing; its address would be none
             p_tokens = p_n = p_prompt = 0
         if bias is not None:
-            M = _whole(bias, device, f32, (B, -1), "bias").shape[1]
-            p_bias, p_bias_tokens = bias.data_ptr(), _whole(bias_tokens, device, i32, (B, M), "bias_tokens").data_ptr()
+            p_bias = _whole(bias, device, f32, (B, -1), "bias")
+            M = bias.shape[1]
+            p_bias_tokens = _whole(bias_tokens, device, i32, (B, M), "bias_tokens")
             if M == 0:
                 p_bias = p_bias_tokens = 0
         if allowed is not None:
             words = (V + 31) // 32
-            masks = _whole(allowed, device, i32, (B, -1, words), "allowed").shape[1]
+            p_allowed = _whole(allowed, device, i32, (B, -1, words), "allowed")
+            masks = allowed.shape[1]
             _need(masks in (1, rows), "allowed: a mask a row, or one a sequence")
-            p_allowed, row, batch = allowed.data_ptr(), (words if masks == rows else 0), masks * words
+            row, batch = (words if masks == rows else 0), masks * words
         return _pack_adjustments(p_tokens, L, p_n, p_prompt, each(self.repetition, f32, "repetition"), each(self.frequency, f32, "frequency"),
                                  each(self.presence, f32, "presence"), p_bias_tokens, p_bias, each(n_bias, i32, "n_bias"), M, p_allowed, row, batch)
 
@@ -149,10 +150,11 @@ def adjust_tree_logits(logits, tree, adjustments, vocab=None, out=None, stream=N
     dev, dtype = logits.device, logits.dtype
     _need(dtype is torch.float32 or dtype is torch.bfloat16, "logits: float32 or bfloat16")
     stride = _rows(logits, B, rows, V, "logits")
+    tokens = parent = 0
     if tree is None:
         _need(rows == 1, "logits: one row a sequence without a tree")
-        tokens = parent = None
-        n_nodes = _empty_like_on(stream, lambda: torch.zeros(B, dtype=torch.int32, device=dev))
+        none = _empty_like_on(stream, lambda: torch.zeros(B, dtype=torch.int32, device=dev))
+        n_nodes = none.data_ptr()
     else:
         nodes = (B, rows - 1)
         tokens, parent = _whole(tree["tokens"], dev, torch.int32, nodes, "tree tokens"), _whole(tree["parent"], dev, torch.int32, nodes, "tree parent")
@@ -160,8 +162,8 @@ def adjust_tree_logits(logits, tree, adjustments, vocab=None, out=None, stream=N
     if out is None:
         out = _empty_like_on(stream, lambda: torch.empty((B, rows, stride), dtype=dtype, device=dev)[:, :, :width])
     _need(out.dtype is dtype and out.device == dev, "out: of the logits' type and device")
-    _check(_launch(dev, stream, L.c2t_adjust_tree_logits, adjustments._packed(B, rows, V, dev), B, V, rows - 1, _DTYPES[dtype], _ptr(tokens), _ptr(parent),
-                   n_nodes.data_ptr(), logits.data_ptr(), stride, out.data_ptr(), _rows(out, B, rows, V, "out")), "c2t_adjust_tree_logits")
+    _check(_launch(dev, stream, L.c2t_adjust_tree_logits, adjustments._packed(B, rows, V, dev), B, V, rows - 1, _DTYPES[dtype], tokens, parent, n_nodes,
+                   logits.data_ptr(), stride, out.data_ptr(), _rows(out, B, rows, V, "out")), "c2t_adjust_tree_logits")
     return out
 
 
@@ -204,16 +206,16 @@ class PagedCache:
         _need(k.is_cuda and k.dim() == 5 and k.dtype in _DTYPES, "k: [layers][pages][kv_heads][page_size][head_dim] on the GPU")
         self.device, self.dtype = k.device, k.dtype
         layers, pages, kv_heads, page_size, head_dim = k.shape
-        _whole(k, k.device, k.dtype, tuple(k.shape), "k")
-        self.k, self.v = k, _whole(v, k.device, k.dtype, tuple(k.shape), "v")
-        self.page_table = _whole(page_table, k.device, torch.int32, (-1, -1), "page_table")
+        dev = k.device
+        p_k, p_v = _whole(k, dev, k.dtype, k.shape, "k"), _whole(v, dev, k.dtype, k.shape, "v")
+        p_table = _whole(page_table, dev, torch.int32, (-1, -1), "page_table")
         batch, max_pages = page_table.shape
-        self.length = _whole(length, k.device, torch.int32, (batch,), "length")
-        self.refcount = _whole(refcount, k.device, torch.int32, (pages,), "refcount")
+        p_length, p_refs = _whole(length, dev, torch.int32, (batch,), "length"), _whole(refcount, dev, torch.int32, (pages,), "refcount")
+        self.k, self.v, self.page_table, self.length, self.refcount = k, v, page_table, length, refcount
         self.status = torch.zeros(batch, dtype=torch.int32, device=k.device).view(torch.uint32)
         self.batch, self.layers, self.pages, self.page_size, self.kv_heads, self.head_dim, self.max_pages = batch, layers, pages, page_size, kv_heads, head_dim, max_pages
-        self._c = _Cache(batch, layers, pages, page_size, kv_heads, head_dim, max_pages, _DTYPES[k.dtype], k.data_ptr(), v.data_ptr(), page_table.data_ptr(),
-                         length.data_ptr(), refcount.data_ptr(), self.status.data_ptr())
+        self._c = _Cache(batch, layers, pages, page_size, kv_heads, head_dim, max_pages, _DTYPES[k.dtype], p_k, p_v, p_table, p_length, p_refs,
+                         self.status.data_ptr())
         self._ref = ctypes.byref(self._c)
         self._each, self._scale = (batch,), head_dim ** -0.5
         need = ctypes.c_size_t()
@@ -235,7 +237,7 @@ class PagedCache:
             raise binding.C2TError(rc, what)
 
     def _per_sequence(self, t, name):
-        return _whole(t, self.device, torch.int32, self._each, name).data_ptr()
+        return _whole(t, self.device, torch.int32, self._each, name)
 
     def reserve(self, n_new, stream=None):
         """Pages for n_new (int32 [B]) tokens behind each sequence's length, its own to write."""
@@ -260,8 +262,8 @@ class PagedCache:
 
     def commit(self, path, n_path, stream=None):
         """The tokens in slots path[b][i] (int32 [B][P], rising) behind the length move to slots i < n_path[b]; the length grows by n_path."""
-        _whole(path, self.device, torch.int32, (self.batch, -1), "path")
-        self._run("c2t_cache_commit", stream, path.data_ptr(), path.shape[1], self._per_sequence(n_path, "n_path"))
+        p = _whole(path, self.device, torch.int32, (self.batch, -1), "path")
+        self._run("c2t_cache_commit", stream, p, path.shape[1], self._per_sequence(n_path, "n_path"))
 
     def truncate(self, new_length=None, keep=0, stream=None):
         """Lengths cut to new_length (int32 [B], default as they are); pages behind length + keep tokens let go."""
@@ -269,9 +271,9 @@ class PagedCache:
 
     def fork(self, src, dst, stream=None):
         """Sequences dst[i] become copies of src[i] (int32 [n] each); the pages are shared until they are written."""
-        n = _whole(src, self.device, torch.int32, (-1,), "src").shape[0]
-        _whole(dst, self.device, torch.int32, (n,), "dst")
-        self._run("c2t_cache_fork", stream, src.data_ptr(), dst.data_ptr(), n)
+        s = _whole(src, self.device, torch.int32, (-1,), "src")
+        n = src.shape[0]
+        self._run("c2t_cache_fork", stream, s, _whole(dst, self.device, torch.int32, (n,), "dst"), n)
 
     def attention(self, layer, q, n_new=None, mask=None, scale=None, out=None, lse=None, workspace=None, stream=None):
         """Attention of the last n_new (int32 [B], default all) tokens, which have been written behind the length, over the cache.
@@ -290,9 +292,9 @@ class PagedCache:
         nodes = p_mask = p_lse = 0
         if mask is not None:
             nodes = mask.shape[-1]
-            p_mask = _whole(mask, self.device, torch.uint8, (self.batch, nodes, nodes), "mask").data_ptr() if nodes else 0
+            p_mask = _whole(mask, self.device, torch.uint8, (self.batch, nodes, nodes), "mask") if nodes else 0
         if lse is not None:
-            p_lse = _whole(lse, self.device, torch.float32, (self.batch, T, heads), "lse").data_ptr()
+            p_lse = _whole(lse, self.device, torch.float32, (self.batch, T, heads), "lse")
         a = _pack_attention(q.data_ptr(), sq[0], sq[1], out.data_ptr(), so[0], so[1], p_lse, 0 if n_new is None else self._per_sequence(n_new, "n_new"),
                             T, heads, layer, nodes, p_mask, self._scale if scale is None else scale)
         need = self._attention_bytes.get((T, heads, nodes))
