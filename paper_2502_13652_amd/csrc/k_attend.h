@@ -63,9 +63,10 @@ __device__ __forceinline__ bool find_item(const CacheView& c, const AttendArgs& 
   int my_b = b0, my_n = 0, my_len = 0;
   if (b0 < b1) my_len = load(b0, &my_n);
   if (each == 1 && c.batch > 1) {
-    const int cost = b0 < b1 ? my_len + my_n : -1;
+    // in steps of 32 keys, equal ones by lane: numbers of their own, one comparison each
+    const uint32_t cost = b0 < b1 ? (uint32_t)((my_len + my_n) >> 5) << 6 | (uint32_t)(WAVE - lane) : 0u;
     int rank = 0;
-    for (int j = 0; j < c.batch; ++j) { const int other = __builtin_amdgcn_readlane(cost, j); rank += other > cost || (other == cost && j < lane); }
+    for (int j = 0; j < c.batch; ++j) rank += (uint32_t)__builtin_amdgcn_readlane((int)cost, j) > cost;
     if (b0 >= b1) rank = lane;
     my_b = __builtin_amdgcn_ds_permute(rank * 4, my_b);
     my_n = __builtin_amdgcn_ds_permute(rank * 4, my_n);
@@ -190,20 +191,6 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
   const int rows = u.n_new * a.shape.group, G = a.shape.group;
   const int wave_row0 = (u.row_tile << a.shape.rows_shift) + rw * 16 * MT;
 
-  // this lane's rows and their queries
-  int slot[MT];
-  T8 q[MT][DK];
-#pragma unroll
-  for (int m = 0; m < MT; ++m) {
-    const int r = wave_row0 + m * 16 + col;
-    slot[m] = r < rows ? r / G : -1;
-#pragma unroll
-    for (int kk = 0; kk < DK; ++kk) {
-      if (slot[m] >= 0) q[m][kk] = *(const T8*)(a.q + u.b * a.q_batch + slot[m] * a.q_token + (((int64_t)u.head * G + r % G) * D + kk * 32 + quad * 8) * 2);
-      else q[m][kk] = T8{};
-    }
-  }
-
   const int seen = keys_seen(a.shape, u.len, u.n_new, a.chain, u.row_tile);
   int tile, tile_end;
   part_range(key_tiles(a.shape, seen), u.parts, u.part, &tile, &tile_end);
@@ -222,9 +209,24 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
   // the page that a block of 16 keys lies in, -1 behind the last key or if the table has none
   auto page_of = [&](int key) { return key < seen ? valid_page(c, table[key >> c.page_shift]) : -1; };
   const int in_page = (1 << c.page_shift) - 1;
-  const int64_t head_offset = row_offset(c, a.layer, 0, u.head, 0) * 2, page_bytes = ((int64_t)c.kv_heads << c.page_shift) * (D * 2);
+  const int64_t head_offset = row_offset(c, a.layer, 0, u.head, 0) * 2;
+  const uint32_t page_bytes = (uint32_t)(c.kv_heads << c.page_shift) * (D * 2);      // at most 2^27: 1024 heads, 256 tokens, 256 wide
   const char* const k_head = c.k + head_offset;
   const char* const v_head = c.v + head_offset;
+
+  // this lane's rows and their queries
+  int slot[MT];
+  T8 q[MT][DK];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    const int r = wave_row0 + m * 16 + col;
+    slot[m] = r < rows ? r / G : -1;
+#pragma unroll
+    for (int kk = 0; kk < DK; ++kk) {
+      if (slot[m] >= 0) q[m][kk] = *(const T8*)(a.q + u.b * a.q_batch + slot[m] * a.q_token + (((int64_t)u.head * G + r % G) * D + kk * 32 + quad * 8) * 2);
+      else q[m][kk] = T8{};
+    }
+  }
 
   f32x4 o[MT][DB];
   float m_run[MT], l_run[MT];                                // l_run: of this lane's keys
@@ -247,13 +249,16 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
     const int key0 = t * KT;
     constexpr int BLOCKS_A_LOAD = ROWS_A_LOAD > 16 ? ROWS_A_LOAD / 16 : 1, LOADS_A_BLOCK = ROWS_A_LOAD > 16 ? 1 : 16 / ROWS_A_LOAD;
     const int in = lt / CH % 16 * (D * 2) + lt % CH * 16;
-    int64_t mine = 0;
+    uint64_t mine = 0;
     there = 0u;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
-      const int key = key0 + kb * 16, page = valid_page(c, __builtin_amdgcn_readlane(pages, kb));
-      there |= page >= 0 ? 1u << kb : 0u;
-      const int64_t off = (page >= 0 ? page : 0) * page_bytes + (key & in_page) * (D * 2);
+      // scalar, and few: a quarter of what a tile's instructions were went into this
+      const int key = key0 + kb * 16;
+      const uint32_t page = (uint32_t)__builtin_amdgcn_readlane(pages, kb);
+      const bool ok = page < (uint32_t)c.pages;
+      there |= ok ? 1u << kb : 0u;
+      const uint64_t off = (uint64_t)(ok ? page : 0u) * page_bytes + (uint32_t)((key & in_page) * (D * 2));
       if (BLOCKS_A_LOAD == 1) {
 #pragma unroll
         for (int x = 0; x < LOADS_A_BLOCK; ++x) {
@@ -447,7 +452,7 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
       if (key + KT - key % KT <= u.len || (KW > 1 && key / KT % KW != first_tile % KW) || key >= seen || idle) continue;
       const int page = uniform(page_of(key));
       if (page < 0) continue;
-      const int64_t at = page * page_bytes + (key & in_page) * (D * 2);
+      const uint64_t at = (uint64_t)(uint32_t)page * page_bytes + (uint32_t)((key & in_page) * (D * 2));
       T4 v[DB];
       bool any = false;
 #pragma unroll

@@ -34,7 +34,7 @@ C2T_HD int new_tokens(const CacheView& c, int len, int n_new, int slots) {
   return clamp_int(n_new, 0, slots < room ? slots : room);
 }
 // a page number as the table holds it; -1 if it is none of the pool's
-C2T_HD int valid_page(const CacheView& c, int page) { return page >= 0 && page < c.pages ? page : -1; }
+C2T_HD int valid_page(const CacheView& c, int page) { return (uint32_t)page < (uint32_t)c.pages ? page : -1; }
 
 // Offset, in elements, of a token's row of one head: `row` of page `page`.
 C2T_HD int64_t row_offset(const CacheView& c, int layer, int page, int head, int row) {
