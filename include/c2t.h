@@ -331,7 +331,7 @@ typedef struct {
   void* out;                   /* [device] the same shape; rows t >= n_new[b] are left as they are; not q */
   int64_t out_batch_stride, out_token_stride;
   float* lse;                  /* [device] [batch][tokens][q_heads]: log of the sum of e^score, -inf for a row that sees nothing; or NULL */
-  const int32_t* n_new;        /* [device] [batch], NULL: all `tokens` */
+  const int32_t* n_new;        /* [device] [batch], NULL: all `tokens`; cut to 0 .. tokens and to what page_table has room for */
   int32_t tokens;              /* slots of new tokens a sequence */
   int32_t q_heads;             /* a multiple of kv_heads; head i reads cached head i / (q_heads / kv_heads) */
   int32_t layer;

@@ -64,7 +64,7 @@ __device__ __forceinline__ bool find_item(const CacheView& c, const AttendArgs& 
   if (b0 < b1) my_len = load(b0, &my_n);
   if (each == 1 && c.batch > 1) {
     // in steps of 32 keys, equal ones by lane: numbers of their own, one comparison each
-    const uint32_t cost = b0 < b1 ? (uint32_t)((my_len + my_n) >> 5) << 6 | (uint32_t)(WAVE - lane) : 0u;
+    const uint32_t cost = b0 < b1 ? (uint32_t)((my_len + my_n) >> 5) << 6 | (uint32_t)(WAVE - 1 - lane) : 0u;
     int rank = 0;
     for (int j = 0; j < c.batch; ++j) rank += (uint32_t)__builtin_amdgcn_readlane((int)cost, j) > cost;
     if (b0 >= b1) rank = lane;

@@ -13,6 +13,8 @@ static_assert(C2T_MAX_CACHE_BATCH == RESERVE_MAX_B && C2T_MAX_PATH == MAX_PATH_T
 
 constexpr int64_t MAX_STRIDE = (int64_t)1 << 40;             // elements: products of strides and indices then stay in 64 bits
 
+constexpr int64_t MAX_BLOCKS = (1 << 24) - 1;                // workgroups of 256 threads of a launch: fewer than 2^32 threads
+
 inline bool aligned16(const void* p) { return (uintptr_t)p % 16 == 0; }
 inline int hip_status() { return hipGetLastError() == hipSuccess ? C2T_OK : C2T_ERR_HIP; }
 
@@ -85,7 +87,7 @@ inline int attend_plan(const c2t_cache& c, const c2t_attention& a, AttendPlan* p
   p->shape.target_shift = !by_keys && p->units >= 1024 ? 9 : MAX_TARGET_SHIFT;
   p->shape.run = std::min(row_tiles(p->shape, a.tokens), MAX_RUN);
   p->items = workgroups_for(p->shape, p->units + (1 << p->shape.target_shift));
-  if (p->items > INT32_MAX / 2) return C2T_ERR_UNSUPPORTED;
+  if (p->items > MAX_BLOCKS) return C2T_ERR_UNSUPPORTED;
   // records of a unit: as many as its join reads in a few microseconds, by one workgroup where it has few rows, by one a record where it has more
   const int64_t record = std::min(rows, (int64_t)1 << p->shape.rows_shift) * c.head_dim * 4;
   p->shape.max_parts = by_keys ? (int)std::max<int64_t>(JOIN_BYTES / record, 2) : MAX_PARTS_ROWS;
@@ -178,7 +180,7 @@ int c2t_cache_write(const c2t_cache* c, int32_t layer, const void* k, const void
   if (!aligned16(k) || !aligned16(v) || batch_stride % 8 || token_stride % 8 || tokens > (1 << 24) || batch_stride > MAX_STRIDE || token_stride > MAX_STRIDE) return C2T_ERR_UNSUPPORTED;
   const NewTokens x{(const char*)k, (const char*)v, batch_stride * 2, token_stride * 2, n_new, tokens};
   const int64_t blocks = div_up64((int64_t)tokens * (row / 8), CACHE_NT);
-  if (blocks > INT32_MAX) return C2T_ERR_UNSUPPORTED;
+  if (blocks > MAX_BLOCKS) return C2T_ERR_UNSUPPORTED;
   hipLaunchKernelGGL(k_cache_write, dim3((unsigned)blocks, (unsigned)c->batch), dim3(CACHE_NT), 0, (hipStream_t)stream, view_of(*c), layer, x);
   return hip_status();
 }

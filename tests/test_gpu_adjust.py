@@ -128,6 +128,24 @@ def test_trees(B, N, width, V, few, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("B,N,width,V,few", [(3, 12, 4, 1000, 50), (2, 40, 10, 8193, 100), (1, 9, 3, 20011, 0)])
+def test_in_place_without_a_mask(B, N, width, V, few, dtype):
+    t = dict(make_terms(B, 1 + N, V, seed=V + 5, few=few), allowed=None)
+    check_tree(logits_of(B, 1 + N, V, dtype, 4, pad=1), tree_of(B, N, width, few or V, V + 1), t, V, "in place, no mask", in_place=True)
+
+
+@pytest.mark.parametrize("masked", [False, True])
+def test_the_largest_tree(masked):
+    """Deep paths whose tokens all lie in one stretch of the vocabulary."""
+    t = make_terms(1, 1025, 300, seed=8)
+    if not masked:
+        t["allowed"] = None
+    tree = tree_of(1, 1024, 8, 300, 3)
+    check_tree(logits_of(1, 1025, 300, F32, 4), tree, t, 300, "1024 nodes")
+    check_tree(logits_of(1, 1025, 300, BF, 4), tree, t, 300, "1024 nodes, in place", in_place=True)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("left_out", ["tokens", "n_prompt", "repetition", "frequency", "presence", "bias", "n_bias", "allowed", "all"])
 def test_terms_that_are_left_out(left_out, dtype):
     t = make_terms(3, 7, 3001, seed=11, allowed="sequence", few=60)

@@ -167,6 +167,32 @@ def test_long_sequences_are_split_and_joined(B, T, H, Hkv, D, lens):
     check(cache, 0, queries(B, T, H, D, BF, 3), [T - (b % 2) * (T > 1) for b in range(B)], tag="split")
 
 
+def test_the_largest_batch():
+    lens = [(b * 7919) % 70 for b in range(4096)]
+    cache = make_cache(lens, 1, 16, 1, 64, BF, seed=5)
+    n = [(b * 31) % 3 != 0 for b in range(4096)]
+    q = queries(4096, 1, 2, 64, BF, 1)
+    out = cache.attention(0, q, n_new=torch.tensor(n, dtype=torch.int32, device="cuda"), out=torch.full_like(q, 7.0))
+    few = list(range(0, 4096, 97))
+    for b in few:
+        want = attention_reference(_one(cache, b), 0, q[b:b + 1], [int(n[b])], None, 0.125, [lens[b]])
+        if n[b]:
+            assert bool(((out[b:b + 1].double() - want[0]).abs() <= want[2]).all()), b
+        else:
+            assert bool((out[b] == 7.0).all())
+
+
+def _one(cache, b):
+    from paper_2502_13652_amd import PagedCache
+    return PagedCache.of_tensors(cache.k, cache.v, cache.page_table[b:b + 1].contiguous(), cache.length[b:b + 1].contiguous(), cache.refcount)
+
+
+def test_the_largest_tree():
+    cache = make_cache([77], 1025, 32, 1, 64, BF, seed=9)
+    mask = random_tree(1024, 8, gen(3))[1][None].cuda()
+    check(cache, 0, queries(1, 1025, 2, 64, BF, 4), None, mask, tag="1024 nodes")
+
+
 def test_a_long_prompt_in_chunks():
     cache = make_cache([0, 700], 600, 64, 2, 64, HF, seed=4)
     check(cache, 0, queries(2, 600, 6, 64, HF, 3), [600, 333], tag="chunk")

@@ -83,8 +83,11 @@ def test_attention_is_refused(lib):
     assert lib.c2t_attention_workspace_bytes(c, None, ctypes.byref(need)) == -1 and lib.c2t_attention_workspace_bytes(c, ctypes.byref(attention()), None) == -1
     for bad in (dict(tokens=0), dict(q_heads=0), dict(q_heads=3), dict(nodes=-1), dict(nodes=5)):
         assert size(**bad) == -1, bad
-    for big in (dict(nodes=1025, tokens=2000), dict(tokens=1 << 29)):
+    for big in (dict(nodes=1025, tokens=2000), dict(tokens=1 << 29), dict(tokens=1 << 27, q_heads=8)):
         assert size(**big) == -2, big
+    many = cache(batch=4096, kv_heads=1024)                # more workgroups than a launch may have
+    assert lib.c2t_attention_workspace_bytes(ctypes.byref(many), ctypes.byref(attention(q_heads=1024, tokens=800)), ctypes.byref(need)) == -2
+    assert lib.c2t_cache_write(ctypes.byref(cache(kv_heads=1024)), 0, FAKE, FAKE, 0, 1 << 16, 1 << 22, None, None) == -2
     size()
     call = lambda ws=FAKE, n=None, **kw: lib.c2t_cache_attention(c, ctypes.byref(attention(**kw)), ws, need.value if n is None else n, None)
     for bad in (dict(q=None), dict(out=None), dict(layer=3), dict(layer=-1), dict(nodes=2), dict(mask=FAKE), dict(q_token_stride=248), dict(out_token_stride=0),
@@ -144,3 +147,17 @@ def test_work_lists_and_addresses_of_the_paged_cache_under_sanitizers():
         assert r.returncode == 0, r.stdout
         r = subprocess.run([exe], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, env=ENV)
         assert r.returncode == 0 and "paged driver ok" in r.stdout and "runtime error" not in r.stdout, r.stdout
+
+
+def test_serving_entry_points_under_sanitizers():
+    with tempfile.TemporaryDirectory() as d:
+        exe = os.path.join(d, "serving_driver")
+        r = subprocess.run(["hipcc", "-O1", "-g", "-std=c++17", "--offload-arch=gfx950",
+                            "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+                            "-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
+                            "-Xarch_host", "-fno-sanitize-recover=all", "-o", exe,
+                            os.path.join(SAN, "serving_driver.cpp"), os.path.join(ROOT, "paper_2502_13652_amd", "csrc", "c2t_lib.hip")],
+                           stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+        assert r.returncode == 0, r.stdout
+        r = subprocess.run([exe], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, env=ENV)
+        assert r.returncode == 0 and "serving driver ok" in r.stdout and "runtime error" not in r.stdout and "AddressSanitizer" not in r.stdout, r.stdout
