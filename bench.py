@@ -131,6 +131,49 @@ def time_full_layers(torch, np, C2TContext, cfg, cls, layers, dev, reps, a=None)
             "gbps": fb / us / 1e3, "frac": fb / us / 1e3 / HBM_PEAK_GBPS}
 
 
+def time_verification(torch, np, cfg, tree, dev, tokens, steps):
+    """What follows a draft phase, on its tree: the root's and the nodes' K and V into a paged cache that holds `tokens` tokens a
+    sequence, attention over it with the tree's mask, penalties on the target's logits, and the accepted path (here the root and,
+    where there is one, its first child) committed.  Synthetic K, V, queries and logits; microseconds a call, host included."""
+    from paper_2502_13652_amd import LogitAdjustments, PagedCache, adjust_tree_logits
+    B, V, N = cfg["B"], cfg["V"], tree["tokens"].shape[1]
+    layers, heads, kv_heads, width, page, T = 2, 32, 8, 128, 16, 1 + N
+    per = 16 // esz_of(cfg)
+    pages = -(-(tokens + T) // page)
+    cache = PagedCache(B, layers, B * pages, page, kv_heads, width, pages, device=dev)
+    g = torch.Generator(device=dev)
+    g.manual_seed(11)
+    cache.k.normal_(generator=g)
+    cache.v.normal_(generator=g)
+    i32 = dict(dtype=torch.int32, device=dev)
+    cache.reserve(torch.full((B,), tokens, **i32))
+    cache.length.fill_(tokens)
+    x = torch.randn((B, T, heads + 2 * kv_heads, width), generator=g, device=dev).to(torch.bfloat16)
+    q, k, v = x[:, :, :heads], x[:, :, heads:heads + kv_heads], x[:, :, heads + kv_heads:]
+    logits = torch.randn((B, T, -(-V // per) * per), generator=g, device=dev).to(torch.float32 if cfg["dtype"] == "f32" else torch.bfloat16)
+    ones = torch.ones(B, device=dev)
+    adj = LogitAdjustments(tokens=torch.randint(0, V, (B, tokens), generator=g, **i32), n_tokens=torch.full((B,), tokens, **i32),
+                           n_prompt=torch.full((B,), tokens // 2, **i32), repetition=1.1 * ones, frequency=0.1 * ones, presence=0.1 * ones)
+    start = torch.full((B,), tokens, **i32)
+    n_new, n_path = 1 + tree["n_nodes"], 1 + (tree["n_nodes"] > 0).to(torch.int32)
+    path, out, adjusted = torch.arange(2, **i32).repeat(B, 1), torch.empty((B, T, heads, width), dtype=torch.bfloat16, device=dev), torch.empty_like(logits)
+    calls = {"reserve": lambda: cache.reserve(n_new), "write": lambda: cache.write(0, k, v, n_new=n_new),
+             "attention": lambda: cache.attention(0, q, n_new=n_new, mask=tree["mask"], out=out),
+             "adjust": lambda: adjust_tree_logits(logits, tree, adj, vocab=V, out=adjusted),
+             "truncate_and_commit": lambda: (cache.truncate(start, keep=T), cache.commit(path, n_path))}
+    us = {}
+    for name, call in calls.items():
+        call()
+        torch.cuda.synchronize()
+        t0 = time.perf_counter()
+        for _ in range(steps):
+            call()
+        torch.cuda.synchronize()
+        us[name] = round((time.perf_counter() - t0) / steps * 1e6, 2)
+    assert int(cache.status.view(torch.int32).abs().sum()) == 0 and bool(torch.isfinite(out[0, 0]).all())
+    return {"us": us, "cached_tokens": tokens, "slots": T, "q_heads": heads, "kv_heads": kv_heads, "head_dim": width, "page_size": page, "calls": steps}
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--gpus", type=int, default=1)
@@ -148,6 +191,9 @@ def main():
     ap.add_argument("--graph", action="store_true",
                     help="capture one draft phase in a HIP graph and time K replays (the per-launch kernel times for "
                          "the roofline then come from further, un-captured phases after the timed region)")
+    ap.add_argument("--verify", type=int, default=0,
+                    help="n > 0: also time the verification of the tree (paged cache of n tokens a sequence, tree attention, adjusted logits, "
+                         "committed path), after the timed region; the figures are printed under `verification`")
     ap.add_argument("--no-cpu-baseline", action="store_true")
     ap.add_argument("--no-full-layer", action="store_true",
                     help="skip the extra full-layer launches (roofline.full_layer), so that a kernel trace of the run "
@@ -270,6 +316,8 @@ def main():
                      "full_layer": full_layer,
                      "stream_read_gbps": stream_gbps, "row_read_gbps": row_read_gbps, "per_layer": per_layer},
     }
+    if a.verify:
+        rec["verification"] = time_verification(torch, np, cfg, out, dev, a.verify, 20)
     del ctx, layers, out
     torch.cuda.empty_cache()
 

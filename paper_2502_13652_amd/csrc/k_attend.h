@@ -72,16 +72,20 @@ __device__ __forceinline__ bool find_item(const CacheView& c, const AttendArgs& 
     my_n = __builtin_amdgcn_ds_permute(rank * 4, my_n);
     my_len = __builtin_amdgcn_ds_permute(rank * 4, my_len);
   }
-  auto of = [&](int b, int* n) { if (b == b0) { *n = my_n; return my_len; } return load(b, n); };
-  double mine = 0.0;
-  for (int b = b0; b < b1; ++b) { int n; const int len = of(b, &n); mine += (double)sequence_tiles(c, a.shape, len, n); }
-  const int per = tiles_per_part(a.shape, (int64_t)wave_sum(mine));
-  int items = 0, slots = 0;
-  for (int b = b0; b < b1; ++b) {
-    int n; const int len = of(b, &n);
-    const int parts = sequence_parts(c, a.shape, per, len, n);
+  const int tiles = row_tiles(a.shape, my_n);
+  float mine = b0 < b1 ? sequence_tiles(c, a.shape, my_len, my_n) : 0.f;
+#pragma unroll 1
+  for (int b = b0 + 1; b < b1; ++b) { int n; const int len = load(b, &n); mine += sequence_tiles(c, a.shape, len, n); }
+  const int per = tiles_per_part(a.shape, (float)wave_sum((double)mine));
+  const float inv_per = __builtin_amdgcn_rcpf((float)per);
+  int my_parts = parts_of(a.shape, per, inv_per, my_len, my_n);
+  const int first_parts = b0 < b1 ? my_parts * tiles * c.kv_heads : 0;
+  int items = first_parts, slots = my_parts > 1 ? first_parts : 0;
+#pragma unroll 1
+  for (int b = b0 + 1; b < b1; ++b) {
+    int n; const int len = load(b, &n), p = parts_of(a.shape, per, inv_per, len, n), parts = p * row_tiles(a.shape, n) * c.kv_heads;
     items += parts;
-    if (parts_of(a.shape, per, len, n) > 1) slots += parts;
+    if (p > 1) slots += parts;
   }
   const int items_to = wave_scan_incl(items), slots_to = wave_scan_incl(slots);
   if (workgroup == 0 && threadIdx.x == WAVE - 1) *a.n_records = slots_to;
@@ -90,28 +94,32 @@ __device__ __forceinline__ bool find_item(const CacheView& c, const AttendArgs& 
   const bool here = w >= item0 && w < item0 + items;
   const uint64_t has = __ballot(here);
   if (has == 0ull) return false;
-  int rel = w - item0, at_slot = slot0;
-  if (here && each > 1) {
-    for (int b = b0; b < b1; ++b) {
-      int n; const int len = of(b, &n);
-      const int parts = sequence_parts(c, a.shape, per, len, n);
-      if (w < item0 + parts) { my_b = b; rel = w - item0; at_slot = slot0; my_len = len; my_n = n; break; }
+  if (each > 1 && here) {
+    int parts = first_parts;
+#pragma unroll 1
+    for (int b = b0; w >= item0 + parts; ) {                 // (it ends: the lane has the item)
       item0 += parts;
-      if (parts_of(a.shape, per, len, n) > 1) slot0 += parts;
+      if (my_parts > 1) slot0 += parts;
+      my_b = ++b;
+      my_len = load(b, &my_n);
+      my_parts = parts_of(a.shape, per, inv_per, my_len, my_n);
+      parts = my_parts * row_tiles(a.shape, my_n) * c.kv_heads;
     }
   }
   const int from = __builtin_ctzll(has);
   u->b = __builtin_amdgcn_readlane(my_b, from);
-  rel = __builtin_amdgcn_readlane(rel, from);
-  at_slot = __builtin_amdgcn_readlane(at_slot, from);
   u->len = __builtin_amdgcn_readlane(my_len, from);
   u->n_new = __builtin_amdgcn_readlane(my_n, from);
-  u->parts = parts_of(a.shape, per, u->len, u->n_new);
-  const int tiles = row_tiles(a.shape, u->n_new);
+  u->parts = __builtin_amdgcn_readlane(my_parts, from);
+  const int rel = __builtin_amdgcn_readlane(w - item0, from), first_slot = __builtin_amdgcn_readlane(slot0, from);
+  const int n_tiles = row_tiles(a.shape, u->n_new);
   // row tiles of the same keys next to each other: they run at the same time.  The last first: of a causal chunk they see the most keys
-  u->row_tile = tiles - 1 - rel % tiles; rel /= tiles;
-  u->part = rel % u->parts; u->head = rel / u->parts;
-  u->slot0 = at_slot + (u->head * tiles + u->row_tile) * u->parts;
+  int rest, tile, head, part;
+  split(rel, n_tiles, __builtin_amdgcn_rcpf((float)n_tiles), &rest, &tile);
+  split(rest, u->parts, __builtin_amdgcn_rcpf((float)u->parts), &head, &part);
+  u->row_tile = uniform(n_tiles - 1 - tile);
+  u->head = uniform(head); u->part = uniform(part);
+  u->slot0 = first_slot + (u->head * n_tiles + u->row_tile) * u->parts;
   return true;
 }
 
@@ -195,8 +203,9 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
   int tile, tile_end;
   part_range(key_tiles(a.shape, seen), u.parts, u.part, &tile, &tile_end);
   // keys below this are seen by every row of the wavefront
-  const int first_slot = wave_row0 < rows ? wave_row0 / G : 0;
-  const int all_see = u.len + min(first_slot + 1, a.chain);
+  int first_slot, first_g;
+  split(wave_row0 < rows ? wave_row0 : 0, G, a.shape.inv_group, &first_slot, &first_g);
+  const int all_see = uniform(u.len + min(first_slot + 1, a.chain));
   const bool idle = wave_row0 >= rows;                       // no row of the wavefront's: it only helps to load
   const int32_t* const table = c.table + (int64_t)u.b * c.max_pages;
   const uint8_t* const mask = a.mask ? a.mask + (int64_t)u.b * a.nodes * a.nodes : nullptr;
@@ -220,10 +229,12 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
     const int r = wave_row0 + m * 16 + col;
-    slot[m] = r < rows ? r / G : -1;
+    int g;
+    split(r, G, a.shape.inv_group, &slot[m], &g);
+    if (r >= rows) slot[m] = -1;
 #pragma unroll
     for (int kk = 0; kk < DK; ++kk) {
-      if (slot[m] >= 0) q[m][kk] = *(const T8*)(a.q + u.b * a.q_batch + slot[m] * a.q_token + (((int64_t)u.head * G + r % G) * D + kk * 32 + quad * 8) * 2);
+      if (slot[m] >= 0) q[m][kk] = *(const T8*)(a.q + u.b * a.q_batch + slot[m] * a.q_token + ((u.head * G + g) * D + kk * 32 + quad * 8) * 2);
       else q[m][kk] = T8{};
     }
   }
@@ -241,8 +252,9 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
   u32x4 kr[K_LDS ? LOADS : KB * DK];
   const int lt = RW > 1 ? tid : lane;                        // this thread among those that load the tile
   uint32_t there = 0u; bool full = false;                    // blocks of the requested tile that lie on a page; all do, and no key is past the last
-  // the pages of a tile's blocks, one a lane: asked for a tile ahead of the keys, which cannot be asked for without them
-  auto pages_of = [&](int t) { const int key = t * KT + (lane % KB) * 16; return key < seen ? table[key >> c.page_shift] : -1; };
+  // The pages of a tile's blocks, one a lane: asked for a tile ahead of the keys, which cannot be asked for without them.  Without a condition (blocks
+  // behind the last key take its page): with one, the register that some lanes leave alone is waited for, and every load before it.
+  auto pages_of = [&](int t) { return table[min(t * KT + (lane % KB) * 16, seen - 1) >> c.page_shift]; };
   // Every lane loads, without a condition that would make each load wait for itself: a block that is on no page comes from the pool's first page, and
   // rows behind the last key lie on its page; both are taken out before they are used.
   auto request = [&](int t, int pages) {
@@ -256,7 +268,7 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
       // scalar, and few: a quarter of what a tile's instructions were went into this
       const int key = key0 + kb * 16;
       const uint32_t page = (uint32_t)__builtin_amdgcn_readlane(pages, kb);
-      const bool ok = page < (uint32_t)c.pages;
+      const bool ok = page < (uint32_t)c.pages && key < seen;
       there |= ok ? 1u << kb : 0u;
       const uint64_t off = (uint64_t)(ok ? page : 0u) * page_bytes + (uint32_t)((key & in_page) * (D * 2));
       if (BLOCKS_A_LOAD == 1) {
@@ -321,6 +333,12 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
   bool all_there = false, odd = false;
   if (tile < tile_end) request(tile, pages);
   pages = pages_of(tile + step);
+  // The queries are here before the loop: loads that were still on their way when it starts would be waited for in each of its rounds, and the next
+  // tile's, which are younger, with them.
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int kk = 0; kk < DK; ++kk) { u32x4 x = __builtin_bit_cast(u32x4, q[m][kk]); settle(x); q[m][kk] = __builtin_bit_cast(T8, x); }
   if (RW > 1) {                                              // (the loop is the same for all wavefronts, which meet in it)
     if (tid == 0) odd_value = 0;
     __syncthreads();
@@ -524,8 +542,9 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
           l += f * jl[w * 16 + row];
           x += f * *(const f32x4*)(jo + (w * 16 + row) * D + dim);
         }
-        const int t = r / G;
-        put(m * 16 + row, t, r - t * G, dim, x, mm, l);
+        int t, g;
+        split(r, G, a.shape.inv_group, &t, &g);
+        put(m * 16 + row, t, g, dim, x, mm, l);
       }
     }
   }
@@ -558,8 +577,9 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
 #pragma unroll
       for (int p = 0; p < AT_ONCE; ++p) if (p0 + p < u.parts) x.add(ml[p], f32x4{lo[p].x, lo[p].y, hi[p].x, hi[p].y});
     }
-    const int at = row0 + row, t = at / G;
-    put_row<E, D>(c, a, u, t, at - t * G, dim, x.o, x.m, x.l);
+    int t, g;
+    split(row0 + row, G, a.shape.inv_group, &t, &g);
+    put_row<E, D>(c, a, u, t, g, dim, x.o, x.m, x.l);
   }
 }
 
@@ -580,8 +600,9 @@ __global__ __launch_bounds__(JOIN_NT) void k_attend_join(CacheView c, AttendArgs
       const int64_t rec = rec0 + ((int64_t)p << a.shape.rows_shift);
       x.add(a.part_ml[rec], *(const f32x4*)(a.part_o + rec * D + dim));
     }
-    const int at = row0 + row, t = at / G;
-    put_row<E, D>(c, a, u, t, at - t * G, dim, x.o, x.m, x.l);
+    int t, g;
+    split(row0 + row, G, a.shape.inv_group, &t, &g);
+    put_row<E, D>(c, a, u, t, g, dim, x.o, x.m, x.l);
   }
 }
 

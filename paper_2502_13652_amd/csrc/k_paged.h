@@ -9,8 +9,6 @@ namespace c2t {
 
 #define C2T_HD __host__ __device__ __forceinline__
 
-constexpr int KEY_BLOCK = 16;              // keys that lie in one page together: page sizes are multiples of it, pages start at multiples of it
-
 struct CacheView {
   char* k; char* v;                        // [layers][pages][kv_heads][page_size][head_dim], 2 bytes an element
   int32_t* table;                          // [batch][max_pages]
@@ -24,6 +22,18 @@ struct CacheView {
 C2T_HD int clamp_int(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
 C2T_HD int div_up(int a, int b) { return (a + b - 1) / b; }
 C2T_HD int64_t div_up64(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// n = q d + r, 0 <= r < d, for 0 <= n <= 2^30 + 2^20 and 1 <= d <= 2^30: from the reciprocal, of which `inverse` holds 22 bits or more.  The first quotient is off by at most 2^10 (and
+// 1), what is left over gives that within 1.  A fifth of an integer division's instructions, of which a workgroup's start had a dozen.
+C2T_HD void split(int n, int d, float inverse, int* q, int* r) {
+  int a = (int)((float)n * inverse);
+  int b = (int)((uint32_t)n - (uint32_t)a * (uint32_t)d);     // (a d may pass 31 bits where a is one too large)
+  const int more = (int)((float)b * inverse);
+  a += more; b -= more * d;
+  if (b < 0) { b += d; a -= 1; }
+  if (b >= d) { b -= d; a += 1; }
+  *q = a; *r = b;
+}
 
 // tokens that a sequence's row of the page table has room for (at most 2^30: checked by the host)
 C2T_HD int capacity_of(const CacheView& c) { return c.max_pages << c.page_shift; }
@@ -52,8 +62,9 @@ struct AttendShape {
   int32_t group;                           // query heads per cached head
   int32_t rows_shift, keys_shift;          // tiles of 1 << rows_shift query rows and 1 << keys_shift keys
   int32_t target_shift, min_per;           // about 1 << target_shift parts, of min_per key tiles or more
-  int32_t max_parts;                       // of a unit, 2 or more
+  int32_t max_parts;                       // of a unit, 2 to 1024
   int32_t run;                             // items in a row for one die
+  float inv_group;                         // 1 / group
 };
 // Workgroups go to the chip's eight dies in turn.  Neighbouring items, whose rows share keys, belong on one die and its L2; runs of
 // items are dealt to the dies in turn, since items come longest first.
@@ -63,36 +74,40 @@ C2T_HD int item_of_workgroup(const AttendShape& a, int workgroup) {
   return (i / a.run * DIES + workgroup % DIES) * a.run + i % a.run;
 }
 C2T_HD int64_t workgroups_for(const AttendShape& a, int64_t items) { return div_up64(items, DIES * a.run) * DIES * a.run; }
-C2T_HD int row_tiles(const AttendShape& a, int n_new) { return (int)(((int64_t)n_new * a.group + (1 << a.rows_shift) - 1) >> a.rows_shift); }
+// (rows: at most 2^30, checked by the host)
+C2T_HD int row_tiles(const AttendShape& a, int n_new) { return (n_new * a.group + (1 << a.rows_shift) - 1) >> a.rows_shift; }
 C2T_HD int key_tiles(const AttendShape& a, int keys) { return (keys + (1 << a.keys_shift) - 1) >> a.keys_shift; }
-C2T_HD int64_t sequence_tiles(const CacheView& c, const AttendShape& a, int len, int n_new) {
-  return (int64_t)row_tiles(a, n_new) * c.kv_heads * key_tiles(a, len + n_new);
+// key tiles of all units of a sequence; only their sum's size matters, in which 24 bits are plenty
+C2T_HD float sequence_tiles(const CacheView& c, const AttendShape& a, int len, int n_new) {
+  return (float)row_tiles(a, n_new) * (float)c.kv_heads * (float)key_tiles(a, len + n_new);
 }
-C2T_HD int tiles_per_part(const AttendShape& a, int64_t all_tiles) {
-  const int64_t per = (all_tiles + (1 << a.target_shift) - 1) >> a.target_shift;
-  return per < a.min_per ? a.min_per : per > (1 << 30) ? 1 << 30 : (int)per;
+// (a thousandth more than the share: the sum's roundings do not make it less)
+C2T_HD int tiles_per_part(const AttendShape& a, float all_tiles) {
+  const float per = all_tiles * (1.001f / (float)(1 << a.target_shift)) + 1.f;
+  return per < (float)a.min_per ? a.min_per : per > 1e9f ? 1000000000 : (int)per;
 }
-C2T_HD int parts_of(const AttendShape& a, int per, int len, int n_new) {
+C2T_HD int parts_of(const AttendShape& a, int per, float inv_per, int len, int n_new) {
   const int t = key_tiles(a, len + n_new);
-  const int parts = t <= per ? 1 : div_up(t, per);
-  return parts < a.max_parts ? parts : a.max_parts;
+  if (t <= per) return 1;
+  if ((int64_t)per * a.max_parts <= t) return a.max_parts;
+  int q, r;
+  split(t, per, inv_per, &q, &r);
+  return q + (r > 0);
 }
-// parts of all units of a sequence
-C2T_HD int sequence_parts(const CacheView& c, const AttendShape& a, int per, int len, int n_new) {
-  return n_new == 0 ? 0 : row_tiles(a, n_new) * c.kv_heads * parts_of(a, per, len, n_new);
-}
-// keys that some row of a tile of query rows sees, from the first: rows row0 .. of the sequence's n_new * group, `chain` causal slots ahead of the nodes
+// keys that some row of a tile of query rows sees, from the first: rows of the sequence's n_new * group, `chain` causal slots ahead of the nodes
 C2T_HD int keys_seen(const AttendShape& a, int len, int n_new, int chain, int row_tile) {
-  const int64_t last_row = ((int64_t)(row_tile + 1) << a.rows_shift) - 1, rows = (int64_t)n_new * a.group;
-  const int t = (int)((last_row < rows ? last_row : rows - 1) / a.group);
+  const int last_row = ((row_tile + 1) << a.rows_shift) - 1, rows = n_new * a.group;
+  int t, g;
+  split(last_row < rows ? last_row : rows - 1, a.group, a.inv_group, &t, &g);
   return t < chain ? len + t + 1 : len + n_new;
 }
 // key tiles first .. end-1 of part `part` of `parts`; empty for the last parts of a row tile that sees few keys
 C2T_HD void part_range(int tiles, int parts, int part, int* first, int* end) {
-  const int per = div_up(tiles, parts);
-  const int64_t f = (int64_t)per * part, e = f + per;
-  *first = f < tiles ? (int)f : tiles;
-  *end = e < tiles ? (int)e : tiles;
+  int q, r;
+  split(tiles, parts, 1.f / (float)parts, &q, &r);
+  const int per = q + (r > 0), f = per * part;
+  *first = f < tiles ? f : tiles;
+  *end = f + per < tiles ? f + per : tiles;
 }
 
 }  // namespace c2t

@@ -76,7 +76,7 @@ inline int attend_plan(const c2t_cache& c, const c2t_attention& a, AttendPlan* p
   const int group = a.q_heads / c.kv_heads;
   const int64_t rows = (int64_t)a.tokens * group;
   p->build = attend_build(rows, c.head_dim);
-  p->shape.slots = a.tokens; p->shape.group = group;
+  p->shape.slots = a.tokens; p->shape.group = group; p->shape.inv_group = 1.f / (float)group;
   const bool by_keys = p->build <= AB_ROWS_32;
   p->shape.rows_shift = 4 + p->build;
   p->shape.keys_shift = by_keys || c.head_dim > 128 ? 5 : 6;
@@ -90,7 +90,7 @@ inline int attend_plan(const c2t_cache& c, const c2t_attention& a, AttendPlan* p
   if (p->items > MAX_BLOCKS) return C2T_ERR_UNSUPPORTED;
   // records of a unit: as many as its join reads in a few microseconds, by one workgroup where it has few rows, by one a record where it has more
   const int64_t record = std::min(rows, (int64_t)1 << p->shape.rows_shift) * c.head_dim * 4;
-  p->shape.max_parts = by_keys ? (int)std::max<int64_t>(JOIN_BYTES / record, 2) : MAX_PARTS_ROWS;
+  p->shape.max_parts = by_keys ? (int)std::min<int64_t>(std::max<int64_t>(JOIN_BYTES / record, 2), 1024) : MAX_PARTS_ROWS;
   const size_t records = (size_t)2 << p->shape.target_shift, rows_of_them = records << p->shape.rows_shift;
   p->n_records = (size_t)(2 << MAX_TARGET_SHIFT) * 4;        // behind the counters, whose place is the same whatever the call's sizes
   p->units_at = p->n_records + 256;

@@ -21,7 +21,7 @@ static CacheView cache(int batch, int pages, int max_pages, int shift, int heads
 
 int main() {
   std::mt19937 rng(7);
-  auto pick = [&](int lo, int hi) { return (int)(lo + rng() % (uint32_t)(hi - lo + 1)); };
+  auto pick = [&](int lo, int hi) { return (int)(lo + rng() % ((uint32_t)hi - (uint32_t)lo + 1u)); };
   const int odd[] = {-2147483647 - 1, -1, 0, 1, 15, 16, 17, 1 << 20, 1 << 30, 2147483647};
   for (int shift = 4; shift <= 8; ++shift) {
     const CacheView c = cache(2, 1000, 64, shift, 8, 128);
@@ -37,6 +37,17 @@ int main() {
       EXPECT(p == -1 || (p >= 0 && p < c.pages && p == x));
     }
   }
+  // quotients from reciprocals, also ones as imprecise as the device's instruction gives them
+  for (int i = 0; i < 2000000; ++i) {
+    const int d = i < 1000 ? i + 1 : pick(1, 1 << pick(0, 30)), top = (1 << 30) + (1 << 20);
+    const int n = i % 7 == 0 ? (int)std::min<int64_t>((int64_t)d * pick(0, 1 << pick(0, 30)), top) - (i % 3 == 0) : pick(0, top);
+    if (n < 0) continue;
+    for (float off : {1.f, 1.f + 1.5e-7f, 1.f - 1.5e-7f}) {
+      int q, r;
+      split(n, d, off / (float)d, &q, &r);
+      EXPECT(q == n / d && r == n % d);
+    }
+  }
   {   // the largest pool there may be: offsets in 64 bits
     const CacheView c = cache(1, (1 << 27) - 1, 1 << 22, 4, 1024, 256);
     const int64_t last = row_offset(c, 2, c.pages - 1, c.kv_heads - 1, 15) + c.head_dim;
@@ -49,11 +60,11 @@ int main() {
     AttendShape a;
     a.slots = pick(1, 1 << pick(0, 9)); a.group = pick(1, 9);
     a.rows_shift = pick(4, 8); a.keys_shift = pick(5, 6);
-    a.target_shift = pick(0, 8); a.min_per = pick(1, 16); a.max_parts = round % 3 ? 1 << 30 : pick(2, 40);
+    a.target_shift = pick(0, 8); a.min_per = pick(1, 16); a.max_parts = round % 3 ? 1024 : pick(2, 40); a.inv_group = 1.f / (float)a.group;
     const int64_t target = (int64_t)1 << a.target_shift;
     const int chain = pick(0, a.slots);
     std::vector<int> len(batch), n(batch);
-    int64_t all = 0;
+    float all = 0.f;
     for (int b = 0; b < batch; ++b) {
       len[b] = tokens_in_cache(c, pick(-1, capacity_of(c) + 1));
       n[b] = new_tokens(c, len[b], pick(-1, a.slots + 1), a.slots);
@@ -61,11 +72,12 @@ int main() {
     }
     const int per = tiles_per_part(a, all);
     EXPECT(per >= a.min_per);
+    const float inv_per = 1.f / (float)per;
     const int64_t units_max = (int64_t)batch * heads * div_up64((int64_t)a.slots * a.group, 1 << a.rows_shift);
     int64_t items = 0, records = 0, units = 0;
     for (int b = 0; b < batch; ++b) {
-      const int parts = n[b] ? parts_of(a, per, len[b], n[b]) : 0, tiles = row_tiles(a, n[b]);
-      EXPECT(sequence_parts(c, a, per, len[b], n[b]) == parts * tiles * heads);
+      const int parts = n[b] ? parts_of(a, per, inv_per, len[b], n[b]) : 0, tiles = row_tiles(a, n[b]);
+      EXPECT(n[b] == 0 || parts == std::min(a.max_parts, std::max(1, div_up(key_tiles(a, len[b] + n[b]), per))));
       items += (int64_t)parts * tiles * heads;
       units += (int64_t)tiles * heads;
       if (parts > 1) records += (int64_t)parts * tiles * heads;
