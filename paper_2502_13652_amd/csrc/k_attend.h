@@ -171,8 +171,9 @@ __device__ __forceinline__ float2 ld_dev64(const uint64_t* p) {
 }
 
 // MT tiles of 16 rows a wavefront; RW wavefronts share the key tiles and have rows of their own, or (RW = 1) KW wavefronts have the same rows
-// and key tiles of their own, joined at the end.  KB blocks of 16 keys a tile.  OCC workgroups a CU.
-template <typename E, int D, int MT, int RW, int KW, int KB, int OCC>
+// and key tiles of their own, joined at the end.  KB blocks of 16 keys a tile.  OCC workgroups a CU.  NODES: some slots
+// are nodes with a mask; the code for it, where it is never used, costs a chunk of 2048 tokens 560 us for 505.
+template <typename E, int D, int MT, int RW, int KW, int KB, int OCC, bool NODES>
 __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, AttendArgs a) {
   static_assert(RW == 1 || KW == 1, "rows or keys");
   typedef typename E::T T; typedef typename E::T4 T4; typedef typename E::T8 T8;
@@ -212,7 +213,7 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
   auto sees = [&](int t, int key) {                          // slot t, key below `seen`
     const int s = key - u.len;
     bool yes = s < a.chain && (t >= a.chain || s <= t);
-    if (t >= a.chain && s >= a.chain) yes = mask[(t - a.chain) * a.nodes + (s - a.chain)] != 0;      // (nodes^2: at most 2^20)
+    if (NODES && t >= a.chain && s >= a.chain) yes = mask[(t - a.chain) * a.nodes + (s - a.chain)] != 0;      // (nodes^2: at most 2^20)
     return yes;
   };
   // the page that a block of 16 keys lies in, -1 behind the last key or if the table has none
@@ -387,16 +388,38 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) settle(s[m][kb]);
       if (!whole) {
+        // of nodes, mask bytes: a word of the lane's keys, asked for together and without a condition, from the nearest place that there is
+        uint32_t open[MT];
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
+        for (int m = 0; m < MT; ++m) open[m] = 0u;
+        if (NODES && key0 + KT > u.len + a.chain) {
+          const int s0 = key0 + quad * 4 - u.len - a.chain;    // node that the lane's first key is
+          uint8_t byte[MT][KB][4];
 #pragma unroll
           for (int m = 0; m < MT; ++m)
 #pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) byte[m][kb][r] = mask[max(slot[m] - a.chain, 0) * a.nodes + max(0, min(s0 + kb * 16 + r, a.nodes - 1))];
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) open[m] |= byte[m][kb][r] != 0 && slot[m] >= a.chain ? 1u << (kb * 4 + r) : 0u;
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          // keys that the row sees without a mask
+          const int below = min(seen, slot[m] < 0 ? 0 : u.len + min(slot[m] + 1, a.chain)), k = key0 + quad * 4;
+#pragma unroll
+          for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
             for (int r = 0; r < 4; ++r) {
-              const int key = key0 + kb * 16 + quad * 4 + r;
-              const bool yes = (blocks >> kb & 1u) && key < seen && slot[m] >= 0 && sees(slot[m], key);
+              const bool yes = (blocks >> kb & 1u) && (k + kb * 16 + r < below || (NODES && k + kb * 16 + r < seen && (open[m] >> (kb * 4 + r) & 1u)));
               s[m][kb][r] = yes ? s[m][kb][r] : -INFINITY;
             }
+        }
       }
 
       T8 p[MT][KB / 2];

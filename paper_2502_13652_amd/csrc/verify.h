@@ -48,17 +48,20 @@ inline int attend_build(int64_t rows, int head_dim) {
   return rows <= 16 ? AB_ROWS_16 : rows <= 32 && head_dim <= 128 ? AB_ROWS_32 : rows <= 64 ? AB_ROWS_64 : AB_ROWS_128;
 }
 typedef void (*AttendKernel)(CacheView, AttendArgs);
-template <typename E, int D> AttendKernel attend_kernel(int build) {
+template <typename E, int D, bool NODES> AttendKernel attend_kernel(int build) {
   constexpr int KB = D > 128 ? 2 : 4;
   switch (build) {
-    case AB_ROWS_16: return k_attend<E, D, 1, 1, 4, 2, (D > 128 ? 1 : 2)>;
-    case AB_ROWS_32: if constexpr (D <= 128) return k_attend<E, D, 2, 1, 4, 2, 2>; [[fallthrough]];      // (wider heads: not chosen)
-    case AB_ROWS_64: return k_attend<E, D, 1, 4, 1, KB, 2>;
-    default: return k_attend<E, D, 2, 4, 1, KB, (D > 128 ? 1 : 2)>;
+    case AB_ROWS_16: return k_attend<E, D, 1, 1, 4, 2, (D > 128 ? 1 : 2), NODES>;
+    case AB_ROWS_32: if constexpr (D <= 128) return k_attend<E, D, 2, 1, 4, 2, 2, NODES>; [[fallthrough]];      // (wider heads: not chosen)
+    case AB_ROWS_64: return k_attend<E, D, 1, 4, 1, KB, 2, NODES>;
+    default: return k_attend<E, D, 2, 4, 1, KB, (D > 128 ? 1 : 2), NODES>;
   }
 }
-template <typename E> AttendKernel attend_kernel(int build, int head_dim) {
-  return head_dim == 64 ? attend_kernel<E, 64>(build) : head_dim == 128 ? attend_kernel<E, 128>(build) : attend_kernel<E, 256>(build);
+template <typename E, bool NODES> AttendKernel attend_kernel(int build, int head_dim) {
+  return head_dim == 64 ? attend_kernel<E, 64, NODES>(build) : head_dim == 128 ? attend_kernel<E, 128, NODES>(build) : attend_kernel<E, 256, NODES>(build);
+}
+template <typename E> AttendKernel attend_kernel(int build, int head_dim, bool nodes) {
+  return nodes ? attend_kernel<E, true>(build, head_dim) : attend_kernel<E, false>(build, head_dim);
 }
 template <typename E> AttendKernel join_kernel(int head_dim) {
   return head_dim == 64 ? k_attend_join<E, 64> : head_dim == 128 ? k_attend_join<E, 128> : k_attend_join<E, 256>;
@@ -249,7 +252,7 @@ int c2t_cache_attention(const c2t_cache* c, const c2t_attention* a, void* ws, si
   g.shape = p.shape;
   const CacheView v = view_of(*c);
   const bool bf16 = c->dtype == C2T_BF16;
-  const AttendKernel fn = bf16 ? attend_kernel<Bf16>(p.build, c->head_dim) : attend_kernel<F16>(p.build, c->head_dim);
+  const AttendKernel fn = bf16 ? attend_kernel<Bf16>(p.build, c->head_dim, a->nodes > 0) : attend_kernel<F16>(p.build, c->head_dim, a->nodes > 0);
   hipLaunchKernelGGL(fn, dim3((unsigned)p.items), dim3(256), 0, (hipStream_t)stream, v, g);
   if (p.build >= AB_ROWS_64)
     hipLaunchKernelGGL(bf16 ? join_kernel<Bf16>(c->head_dim) : join_kernel<F16>(c->head_dim), dim3((unsigned)p.records), dim3(JOIN_NT), 0, (hipStream_t)stream, v, g);
