@@ -83,11 +83,14 @@ inline int attend_plan(const c2t_cache& c, const c2t_attention& a, AttendPlan* p
   const bool by_keys = p->build <= AB_ROWS_32;
   p->shape.rows_shift = 4 + p->build;
   p->shape.keys_shift = by_keys || c.head_dim > 128 ? 5 : 6;
-  p->shape.min_per = by_keys ? 8 : 4;
   p->units = (int64_t)c.batch * c.kv_heads * row_tiles(p->shape, a.tokens);
-  // Parts enough to fill two workgroups a CU twice; where there are units for that already, longest first, parts only of what is longer than its share:
-  // 1536 units of 64 sequences 243 us, with twice the parts 260, four times 347; 512 units of two prompts 604 and 571.
-  p->shape.target_shift = !by_keys && p->units >= 1024 ? 9 : MAX_TARGET_SHIFT;
+  // Parts: of few rows, enough to fill two workgroups a CU twice (64 single tokens of 300 to 8000 keys 202 us, with half of them 223).  Of many,
+  // enough to fill them once, since their records cost more than what an even end saves: a chunk of 2048 466 us, with twice the parts 514; 64 trees
+  // of 65 205 and 244; the other way only 4 chunks of 241 that are 256 wide, 369 and 363.
+  p->shape.target_shift = by_keys ? MAX_TARGET_SHIFT : MAX_TARGET_SHIFT - 1;
+  // The shortest part: of many rows the longer, the more units share the chip without parts, since a join is a launch and a trip of all rows
+  // through memory.  256 units of 5 tiles 24 us unsplit, 35 in parts of 4; 5 units of up to 59 tiles 19 us in parts of 4 and 37 in parts of 16.
+  p->shape.min_per = by_keys ? 8 : (int)std::min<int64_t>(std::max<int64_t>(p->units / 16, 4), 16);
   p->shape.run = std::min(row_tiles(p->shape, a.tokens), MAX_RUN);
   p->items = workgroups_for(p->shape, p->units + (1 << p->shape.target_shift));
   if (p->items > MAX_BLOCKS) return C2T_ERR_UNSUPPORTED;
