@@ -7,6 +7,9 @@
 // LDS once and lists the tokens that anything is done to: a few hundred of 4096 at most usually.  Rows then pass through LDS,
 // a few at a time: in as they are, the listed tokens changed in place (each by a thread of its own, so no lane waits for
 // another's), and out with the mask.  In place and without a mask only the listed tokens are read and written.
+//
+// Bound by the rows' bytes: 64 sequences, 65 rows of 128256 bf16 logits each, contexts of 4000 and a mask: 448 us, 4.9 TB/s read and written, what a large
+// copy gets (4.8); without a mask 430.  61 rows of 32000 fp32 logits of one sequence: 9.7 us, the launch and the lists.
 #pragma once
 #include "k_common.h"
 #include "k_paged.h"

@@ -10,6 +10,14 @@
 // fastest.  Products are taken transposed: S^T = K Q^T leaves in a lane one row (lane & 15) and 4 neighbouring keys of each
 // block of 16, which are just the operand that out^T = V^T P^T takes of two blocks: P never leaves its registers, and row
 // statistics are one number a lane, reduced over 4 lanes.
+//
+// Two layouts.  A tile of 16 rows (single tokens, small trees): the keys' bytes bound it, so each of a workgroup's four wavefronts goes over key tiles of
+// its own, K straight into the matrix operands, V through LDS for its transposition only.  64 single tokens of 300 to 8000 cached tokens, 32 heads
+// over 8: 201 us for 1.09 GB of K and V, 5.4 TB/s; a kernel that only reads rows gets 6.4.  More rows: the matrix products and the weights' exponentials
+// bound it, so the wavefronts share K and V tiles in LDS, two of them in turn, the next one's loads on their way while a tile is used.  Two
+// chunks of 2048 behind 9000 and 31000 tokens, 64 wide: 464 us for 353 GFLOP, 0.76 PFLOP/s; vector instructions are issued for 60 % of that time and the
+// matrix unit works for 35 %: the two hardly overlap.  64 trees of 65 behind 100 to 4000 tokens: 205 to 220 us for 116 GFLOP, 0.55 PFLOP/s; of 260 rows a head
+// the last four take a third pass.  One token behind 701: 9.7 us, of which 8 are the launch, the item's search and the join of its parts.
 #pragma once
 #include "k_common.h"
 #include "k_paged.h"
@@ -50,7 +58,8 @@ struct AttendArgs {
 struct Unit { int b, len, n_new, row_tile, head, part, parts, slot0; };   // slot0: record of the unit's first part
 
 // Deals a workgroup its item.  Every wavefront computes it for itself, each lane summing a stretch of sequences: no barrier.  Where
-// each lane has one sequence at most, the longest go first: workgroups start in about this order, and none that starts last is long.
+// each lane has one sequence at most, the longest go first: workgroups start in about this order, and none that starts last is long.  It costs
+// 8 to 12 us of a launch of 64 sequences; a launch of its own that left a list would cost a launch.
 // False: there is no item for it.
 __device__ __forceinline__ bool find_item(const CacheView& c, const AttendArgs& a, int workgroup, Unit* u) {
   const int lane = lane_id(), each = div_up(c.batch, WAVE), b0 = min(lane * each, c.batch), b1 = min(b0 + each, c.batch);
@@ -606,7 +615,8 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
   }
 }
 
-// The parts of units of many rows, joined: a workgroup a record, which takes its share of its unit's rows.
+// The parts of units of many rows, joined: a workgroup a record, which takes its share of its unit's rows.  Bound by the records' bytes, which are in the
+// L2 for the most part: 7 us after the two chunks of 2048 (8.7 MB from memory), 5 after the 64 trees.
 constexpr int JOIN_NT = 256;
 template <typename E, int D>
 __global__ __launch_bounds__(JOIN_NT) void k_attend_join(CacheView c, AttendArgs a) {

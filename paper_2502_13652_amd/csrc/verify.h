@@ -42,20 +42,21 @@ inline int reserve_cap(const c2t_cache& c) { return (int)std::min<int64_t>(c.pag
 inline size_t reserve_bytes(const c2t_cache& c) { return ((size_t)2 * reserve_cap(c) + c.batch) * 4; }
 
 // ---- attention ----
-// Which kernel a launch of that many rows a cached head takes.
-enum { AB_ROWS_16, AB_ROWS_32, AB_ROWS_64, AB_ROWS_128 };    // 16 << build rows a tile
-inline int attend_build(int64_t rows, int head_dim) {
-  return rows <= 16 ? AB_ROWS_16 : rows <= 32 && head_dim <= 128 ? AB_ROWS_32 : rows <= 64 ? AB_ROWS_64 : AB_ROWS_128;
+// Which kernel a launch of that many rows a cached head takes, 16 << build of them a tile: wavefronts that share rows and divide keys (16), or that divide rows.
+//   width 64 and 128, up to 16 rows: 16 (one token behind 700 tokens 10.0 us, with 64 12.4; 64 of 300 to 8000 200 and 211; it loses where lengths are alike and
+//   many: 64 trees of 4 behind 500 43 and 33).  Up to 32 rows, two tiles of 16 where there are few sequences (a tree of 8 behind 500 tokens 12.4 us, with 64 15.4),
+//   64 otherwise (64 such trees 43 and 35).  Width 256: never 16 (19 trees of 9 behind up to 3038 tokens 46 us, with 64 30; 5 tokens 14.7 and 14.1).
+//   Up to 64 rows: 64 (64 trees of 16 behind 2000 109 us, with 128 108; width 256, 4 of them behind 4000, 38 and 53); more: 128 (64 trees of 32 158 and 121).
+enum { AB_ROWS_16 = 0, AB_ROWS_64 = 2, AB_ROWS_128 = 3 };
+inline int attend_build(int64_t rows, int head_dim, int64_t heads) {       // heads: cached heads of all sequences
+  if (head_dim <= 128 && (rows <= 16 || (rows <= 32 && heads < 256))) return AB_ROWS_16;
+  return rows <= 64 ? AB_ROWS_64 : AB_ROWS_128;
 }
 typedef void (*AttendKernel)(CacheView, AttendArgs);
 template <typename E, int D, bool NODES> AttendKernel attend_kernel(int build) {
   constexpr int KB = D > 128 ? 2 : 4;
-  switch (build) {
-    case AB_ROWS_16: return k_attend<E, D, 1, 1, 4, 2, (D > 128 ? 1 : 2), NODES>;
-    case AB_ROWS_32: if constexpr (D <= 128) return k_attend<E, D, 2, 1, 4, 2, 2, NODES>; [[fallthrough]];      // (wider heads: not chosen)
-    case AB_ROWS_64: return k_attend<E, D, 1, 4, 1, KB, 2, NODES>;
-    default: return k_attend<E, D, 2, 4, 1, KB, (D > 128 ? 1 : 2), NODES>;
-  }
+  if constexpr (D <= 128) if (build == AB_ROWS_16) return k_attend<E, D, 1, 1, 4, 2, 2, NODES>;
+  return build == AB_ROWS_64 ? k_attend<E, D, 1, 4, 1, KB, 2, NODES> : k_attend<E, D, 2, 4, 1, KB, (D > 128 ? 1 : 2), NODES>;
 }
 template <typename E, bool NODES> AttendKernel attend_kernel(int build, int head_dim) {
   return head_dim == 64 ? attend_kernel<E, 64, NODES>(build) : head_dim == 128 ? attend_kernel<E, 128, NODES>(build) : attend_kernel<E, 256, NODES>(build);
@@ -66,9 +67,10 @@ template <typename E> AttendKernel attend_kernel(int build, int head_dim, bool n
 template <typename E> AttendKernel join_kernel(int head_dim) {
   return head_dim == 64 ? k_attend_join<E, 64> : head_dim == 128 ? k_attend_join<E, 128> : k_attend_join<E, 256>;
 }
-constexpr int MAX_RUN = 8;
+constexpr int MAX_RUN = 8;                                   // a chunk of 2048 463 us, in runs of one 472; 64 trees of 65 214 and 227
 constexpr int MAX_TARGET_SHIFT = 10, MAX_PARTS_ROWS = 64;
-constexpr int64_t JOIN_BYTES = 256 << 10;
+// 32 rows a cached head of one sequence behind 32000 tokens 31 us, with 256 KiB 39, with 64 45; of 16 rows 30, 33, 45; of 16 rows of a single cached head 28, 24, 41.
+constexpr int64_t JOIN_BYTES = 128 << 10;
 struct AttendPlan { AttendShape shape; int build, records; int64_t units, items; size_t n_records, units_at, part_o, part_ml, total; };
 
 // Sizes of a call alone: the workspace must not depend on what is on the device.
@@ -78,16 +80,16 @@ inline int attend_plan(const c2t_cache& c, const c2t_attention& a, AttendPlan* p
   if (a.nodes > C2T_MAX_BUDGET || (int64_t)a.tokens * a.q_heads > (1 << 30)) return C2T_ERR_UNSUPPORTED;
   const int group = a.q_heads / c.kv_heads;
   const int64_t rows = (int64_t)a.tokens * group;
-  p->build = attend_build(rows, c.head_dim);
+  p->build = attend_build(rows, c.head_dim, (int64_t)c.batch * c.kv_heads);
   p->shape.slots = a.tokens; p->shape.group = group; p->shape.inv_group = 1.f / (float)group;
-  const bool by_keys = p->build <= AB_ROWS_32;
+  const bool by_keys = p->build == AB_ROWS_16;
   p->shape.rows_shift = 4 + p->build;
   p->shape.keys_shift = by_keys || c.head_dim > 128 ? 5 : 6;
   p->units = (int64_t)c.batch * c.kv_heads * row_tiles(p->shape, a.tokens);
-  // Parts: of few rows, enough to fill two workgroups a CU twice (64 single tokens of 300 to 8000 keys 202 us, with half of them 223).  Of many,
-  // enough to fill them once, since their records cost more than what an even end saves: a chunk of 2048 466 us, with twice the parts 514; 64 trees
-  // of 65 205 and 244; the other way only 4 chunks of 241 that are 256 wide, 369 and 363.
-  p->shape.target_shift = by_keys ? MAX_TARGET_SHIFT : MAX_TARGET_SHIFT - 1;
+  // Parts: enough to fill the chip once, two workgroups a CU, since parts and their records cost more than what an even end saves: a chunk of 2048 466 us,
+  // with twice the parts 514; 64 trees of 65 205 and 244; one token behind 32000 32 and 43.  Many units of few rows go twice round: 64 tokens of 300
+  // to 8000 keys 202 us, with half of the parts 223; 32 tokens behind 4000 the other way, 105 and 100.
+  p->shape.target_shift = by_keys && p->units >= 512 ? MAX_TARGET_SHIFT : MAX_TARGET_SHIFT - 1;
   // The shortest part: of many rows the longer, the more units share the chip without parts, since a join is a launch and a trip of all rows
   // through memory.  256 units of 5 tiles 24 us unsplit, 35 in parts of 4; 5 units of up to 59 tiles 19 us in parts of 4 and 37 in parts of 16.
   p->shape.min_per = by_keys ? 8 : (int)std::min<int64_t>(std::max<int64_t>(p->units / 16, 4), 16);
@@ -122,7 +124,9 @@ inline int check_adjust(AdjustArgs& a, int dtype, int64_t in_stride, int64_t out
   return C2T_OK;
 }
 
-constexpr int ADJUST_WORKGROUPS = 1024;     // four rounds of two a CU
+// One round of two a CU: each workgroup makes its sequence's lists anew.  4 sequences of 65 rows of 128256: 25 us, with 1024 28, with 256 28, with 4096
+// 36; one sequence of 32000 15 whatever it is; 64 of 128253, more than either in any case, 372, in four times as many 364.
+constexpr int ADJUST_WORKGROUPS = 512;
 inline int fill_adjust(AdjustArgs& a, const c2t_adjustments* t) {
   if (!t) return C2T_ERR_INVALID_ARG;
   if (t->tokens && (!t->n_tokens || t->token_stride <= 0)) return C2T_ERR_INVALID_ARG;

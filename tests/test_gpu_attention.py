@@ -167,6 +167,16 @@ def test_long_sequences_are_split_and_joined(B, T, H, Hkv, D, lens):
     check(cache, 0, queries(B, T, H, D, BF, 3), [T - (b % 2) * (T > 1) for b in range(B)], tag="split")
 
 
+@pytest.mark.parametrize("D,dtype", [(64, HF), (128, BF), (256, BF)])
+@pytest.mark.parametrize("B,Hkv,T,H,nodes", [(31, 8, 5, 32, 4), (32, 8, 5, 32, 4), (255, 1, 17, 1, 0), (256, 1, 32, 1, 31), (64, 8, 3, 16, 2), (63, 8, 1, 8, 0)])
+def test_many_sequences_of_few_rows(B, Hkv, T, H, nodes, D, dtype):
+    """Numbers of sequences at which a call of few rows takes another kernel or other parts."""
+    lens = [(b * 37) % 150 + (900 if b == 7 else 0) for b in range(B)]
+    cache = make_cache(lens, T, 16, Hkv, D, dtype, seed=B + T)
+    mask = torch.stack([random_tree(nodes, 3, gen(b))[1] for b in range(B)]).cuda() if nodes else None
+    check(cache, 0, queries(B, T, H, D, dtype, 3), [T - (b % 3 == 1) * (T > 1) for b in range(B)], mask, tag="many")
+
+
 def test_the_largest_batch():
     lens = [(b * 7919) % 70 for b in range(4096)]
     cache = make_cache(lens, 1, 16, 1, 64, BF, seed=5)
