@@ -342,9 +342,10 @@ typedef struct {
 
 /* Every slot sees the length[b] tokens before; a chain slot the chain up to itself; node i the whole chain and the nodes j with mask[b][i][j] != 0
  * (j < n_new[b] - chain).  A key that a row does not see has no influence on it, whatever its bits.  A row that sees no key gets zeros.
- * Products in the cache's dtype, sums and the softmax in fp32.  The workspace ([device], 256-byte aligned, its size from the call's sizes
- * alone) is zero-filled by the caller before its first use (its counters are zero again after each call); calls that may run at the same time need
- * one each, others may share the largest. */
+ * Products in the cache's dtype, sums and the softmax in fp32.  The workspace is [device], 256-byte aligned, its size from the call's sizes
+ * alone.  Its first C2T_ATTENTION_COUNTERS bytes are zero-filled by the caller before its first use, on the stream that uses it or one that it waits
+ * for, and are zero again after each call.  Calls that may run at the same time need one each, others may share the largest. */
+#define C2T_ATTENTION_COUNTERS 8192
 int c2t_attention_workspace_bytes(const c2t_cache* cache, const c2t_attention* attention, size_t* out);
 int c2t_cache_attention(const c2t_cache* cache, const c2t_attention* attention, void* dev_workspace, size_t workspace_bytes, void* stream);
 

@@ -100,7 +100,8 @@ inline int attend_plan(const c2t_cache& c, const c2t_attention& a, AttendPlan* p
   const int64_t record = std::min(rows, (int64_t)1 << p->shape.rows_shift) * c.head_dim * 4;
   p->shape.max_parts = by_keys ? (int)std::min<int64_t>(std::max<int64_t>(JOIN_BYTES / record, 2), 1024) : MAX_PARTS_ROWS;
   const size_t records = (size_t)2 << p->shape.target_shift, rows_of_them = records << p->shape.rows_shift;
-  p->n_records = (size_t)(2 << MAX_TARGET_SHIFT) * 4;        // behind the counters, whose place is the same whatever the call's sizes
+  static_assert((2 << MAX_TARGET_SHIFT) * 4 == C2T_ATTENTION_COUNTERS, "one a record");
+  p->n_records = C2T_ATTENTION_COUNTERS;                     // behind the counters, whose place is the same whatever the call's sizes
   p->units_at = p->n_records + 256;
   p->part_o = p->units_at + (sizeof(Unit) << (MAX_TARGET_SHIFT + 1));
   p->records = (int)records;

@@ -11,6 +11,7 @@ from . import binding
 from .binding import BF16, F16, F32, _check, load_library
 
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+ATTENTION_COUNTERS = 8192                                   # C2T_ATTENTION_COUNTERS
 
 
 class _Adjustments(ctypes.Structure):
@@ -221,13 +222,11 @@ class PagedCache:
         need = ctypes.c_size_t()
         _check(self.L.c2t_cache_workspace_bytes(self._ref, ctypes.byref(need)), "c2t_cache_workspace_bytes")
         self._ws = self._workspace(need.value)
-        self._attention_ws = {}                            # (stream, capture, bytes) -> workspace; kept: a captured graph refers to it
-        self._capture = ctypes.c_uint64()
-        self._capture_ref = ctypes.byref(self._capture)
+        self._attention_ws = {}                            # (stream, in a capture) -> capture, {bytes: workspace}
         self._attention_bytes = {}
 
     def _workspace(self, nbytes):
-        w = torch.zeros(nbytes + 256, dtype=torch.uint8, device=self.device)
+        w = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
         pad = (-w.data_ptr()) % 256
         return w[pad:pad + nbytes]
 
@@ -281,7 +280,8 @@ class PagedCache:
         q [B][T][q_heads][head_dim]; mask uint8 [B][N][N] as finalize_tree writes it: the last N of the T slots are the tree's nodes, those
         before them (the root) a causal chain; no mask: all of them are.  scale: of the scores, default head_dim ** -0.5.  lse: float32
         [B][T][q_heads] for the log of the softmax's sums.  out: [B][T][q_heads][head_dim] (default: a new tensor), rows behind n_new left as
-        they are.  workspace: uint8, zeros, of attention_workspace_bytes and 256-byte aligned, for calls that run at once otherwise than by stream."""
+        they are.  workspace: uint8, zeros, of attention_workspace_bytes and 256-byte aligned, for calls that run at once otherwise than by stream.
+        Without one the cache keeps one a stream, and in a graph's capture one that is the graph's: from its pool, counters cleared at each replay."""
         _need(q.dim() == 4, "q: [B][T][q_heads][head_dim]")
         _, T, heads, _ = q.shape
         sq = self._tokens(q, heads, "q")
@@ -293,6 +293,8 @@ class PagedCache:
         if mask is not None:
             nodes = mask.shape[-1]
             p_mask = _whole(mask, self.device, torch.uint8, (self.batch, nodes, nodes), "mask") if nodes else 0
+        _need(workspace is None or (workspace.dtype is torch.uint8 and workspace.device == self.device and workspace.is_contiguous()),
+              "workspace: contiguous uint8 on %s" % self.device)
         if lse is not None:
             p_lse = _whole(lse, self.device, torch.float32, (self.batch, T, heads), "lse")
         a = _pack_attention(q.data_ptr(), sq[0], sq[1], out.data_ptr(), so[0], so[1], p_lse, 0 if n_new is None else self._per_sequence(n_new, "n_new"),
@@ -313,12 +315,18 @@ class PagedCache:
         """One a stream, and one a captured graph: graphs may be replayed at once, and an eager call beside them."""
         capture = 0
         if s:
-            _check(self.L.c2t_stream_capture_id(s, self._capture_ref), "c2t_stream_capture_id")
-            capture = self._capture.value
-        key = (s, capture, need)
-        w = self._attention_ws.get(key)
+            number = ctypes.c_uint64()
+            _check(self.L.c2t_stream_capture_id(s, ctypes.byref(number)), "c2t_stream_capture_id")
+            capture = number.value
+        entry = self._attention_ws.get((s, capture != 0))
+        if entry is None or entry[0] != capture:             # of a capture that has ended: its graph's pool holds the memory
+            entry = self._attention_ws[(s, capture != 0)] = (capture, {})
+        w = entry[1].get(need)
         if w is None:
-            w = self._attention_ws[key] = self._workspace(need)
+            here = torch.cuda.current_stream(self.device)
+            with torch.cuda.stream(here if here.cuda_stream == s else torch.cuda.ExternalStream(s, self.device)):
+                w = entry[1][need] = self._workspace(need)
+                w[:ATTENTION_COUNTERS].zero_()               # on the stream that is going to use them
         return w
 
     def attention_workspace_bytes(self, tokens, q_heads, nodes=0):

@@ -304,6 +304,56 @@ def test_graphs_replayed_at_once_have_workspaces_of_their_own():
             assert torch.equal(o, w)
 
 
+def test_a_stream_clears_the_counters_that_it_uses():
+    """The first call on a stream, where memory holds other values and the current stream is busy."""
+    cache = make_cache([20000], 1, 16, 1, 128, BF, seed=3)
+    q = queries(1, 1, 4, 128, BF, 4)
+    want = cache.attention(0, q)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    for stream in (torch.cuda.current_stream(), s):
+        with torch.cuda.stream(stream):
+            held = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in (1 << 21, 1 << 23, 1 << 24, 1 << 26)]
+            del held
+    torch.cuda.synchronize()
+    out = torch.zeros_like(q)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(20_000_000)
+    cache.attention(0, q, out=out, stream=s)
+    s.synchronize()
+    assert torch.equal(out, want)
+    torch.cuda.synchronize()
+    fresh = make_cache([20000], 1, 16, 1, 128, BF, seed=3)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        out = fresh.attention(0, q, stream=torch.cuda.default_stream())
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+
+
+def test_captures_leave_no_workspaces_behind():
+    cache = make_cache([3000, 7], 1, 16, 1, 64, BF, seed=3)
+    q = queries(2, 1, 4, 64, BF, 4)
+    want = cache.attention(0, q)
+    s = torch.cuda.Stream()
+    graphs = []
+    for _ in range(3):
+        g, out = torch.cuda.CUDAGraph(), torch.zeros_like(q)
+        with torch.cuda.graph(g, stream=s):
+            cache.attention(0, q, out=out)
+            cache.attention(0, q, out=out)
+        graphs.append((g, out))
+    assert sum(len(w) for _, w in cache._attention_ws.values()) == 2
+    for _ in range(3):
+        for g, out in graphs:
+            out.zero_()
+            g.replay()
+            other = torch.full((1 << 22,), 255, dtype=torch.uint8, device="cuda")
+            torch.cuda.synchronize()
+            assert torch.equal(out, want)
+            del other
+
+
 def test_refusals():
     from paper_2502_13652_amd import PagedCache
     from paper_2502_13652_amd.binding import C2TError
@@ -328,6 +378,10 @@ def test_refusals():
     with pytest.raises(C2TError) as e:
         cache.attention(0, q, workspace=torch.zeros(256, dtype=torch.uint8, device="cuda"))
     assert e.value.code == -3
+    need = cache.attention_workspace_bytes(4, 4)
+    for bad in (torch.zeros(need, dtype=torch.uint8), torch.zeros(need, dtype=torch.int32, device="cuda"), torch.zeros(2 * need, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(ValueError):
+            cache.attention(0, q, workspace=bad)
     for kw in (dict(page_size=24), dict(page_size=512), dict(head_dim=96), dict(batch=5000)):
         a = dict(batch=2, layers=1, pages=4, page_size=16, kv_heads=1, head_dim=64, max_pages=2)
         a.update(kw)

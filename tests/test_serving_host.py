@@ -161,3 +161,9 @@ def test_serving_entry_points_under_sanitizers():
         assert r.returncode == 0, r.stdout
         r = subprocess.run([exe], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, env=ENV)
         assert r.returncode == 0 and "serving driver ok" in r.stdout and "runtime error" not in r.stdout and "AddressSanitizer" not in r.stdout, r.stdout
+
+
+def test_the_header_and_the_binding_agree_on_the_counters():
+    from paper_2502_13652_amd.serving import ATTENTION_COUNTERS
+    with open(os.path.join(ROOT, "include", "c2t.h")) as f:
+        assert "#define C2T_ATTENTION_COUNTERS %d\n" % ATTENTION_COUNTERS in f.read()
