@@ -864,7 +864,8 @@ __device__ __forceinline__ void prune_sequence(int tid, const TreeState& s, cons
         }
         // rank = survivors with a greater key, and those with the same key (the same token under two parents, with
         // the same z: looked for only where a count shows them) and a lower candidate index; the survivor's T
-        // lanes take two keys a step each.  (Ties by one lane alone: 7.5 us for 100 survivors of equal z whose rows share tokens.)
+        // lanes take two keys a step each.  (Ties by one lane alone: 7.5 us for 100 survivors of equal z whose rows share tokens.  Indices asked for
+        // only where a key is equal, each wait by itself: a layer of them 13.3 us, without the condition 12.0.)
         int rank = 0;                                          // lower half: greater keys, upper half: equal ones (itself among them)
         if (mine) {
 #pragma unroll 2
@@ -881,8 +882,8 @@ __device__ __forceinline__ void prune_sequence(int tid, const TreeState& s, cons
         if (__builtin_amdgcn_ballot_w64(tied) != 0ull) {       // (uniform)
           int ahead = 0;
           if (tied) {
-#pragma unroll 4
-            for (int v = sub; v < ns; v += T) ahead += (int)(skey[v] == key && sidx[v] < i);
+#pragma unroll 8
+            for (int v = sub; v < ns; v += T) ahead += (int)((skey[v] == key) & (sidx[v] < i));
           }
           rank += sum_of_lanes(tshift, ahead);
         }
