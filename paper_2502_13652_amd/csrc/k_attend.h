@@ -16,7 +16,7 @@
 // over 8: 201 us for 1.09 GB of K and V, 5.4 TB/s; a kernel that only reads rows gets 6.4.  More rows: the matrix products and the weights' exponentials
 // bound it, so the wavefronts share K and V tiles in LDS, two of them in turn, the next one's loads on their way while a tile is used.  Two
 // chunks of 2048 behind 9000 and 31000 tokens, 64 wide: 464 us for 353 GFLOP, 0.76 PFLOP/s; vector instructions are issued for 60 % of that time and the
-// matrix unit works for 35 %: the two hardly overlap.  64 trees of 65 behind 100 to 4000 tokens: 205 to 220 us for 116 GFLOP, 0.55 PFLOP/s; of 260 rows a head
+// matrix unit works for 35 %: the two hardly overlap.  64 trees of 65 behind 100 to 4000 tokens: 204 to 238 us for 116 GFLOP, up to 0.57 PFLOP/s; of 260 rows a head
 // the last four take a third pass.  One token behind 701: 9.7 us, of which 8 are the launch, the item's search and the join of its parts.
 #pragma once
 #include "k_common.h"
@@ -271,6 +271,8 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
     const int key0 = t * KT;
     constexpr int BLOCKS_A_LOAD = ROWS_A_LOAD > 16 ? ROWS_A_LOAD / 16 : 1, LOADS_A_BLOCK = ROWS_A_LOAD > 16 ? 1 : 16 / ROWS_A_LOAD;
     const int in = lt / CH % 16 * (D * 2) + lt % CH * 16;
+    static_assert(64 / CH <= 16, "a wavefront's rows lie in one block");
+    const int block = uniform(lt / CH / 16);
     uint64_t mine = 0;
     there = 0u;
 #pragma unroll
@@ -289,7 +291,7 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
           if (K_LDS) kr[j] = *(const u32x4*)(k_head + off + in + x * ROWS_A_LOAD * (D * 2));
         }
       } else {
-        if (kb % BLOCKS_A_LOAD == 0 || lt / CH / 16 == kb % BLOCKS_A_LOAD) mine = off;
+        if (kb % BLOCKS_A_LOAD == 0 || block == kb % BLOCKS_A_LOAD) mine = off;
         if (kb % BLOCKS_A_LOAD == BLOCKS_A_LOAD - 1) {
           vr[kb / BLOCKS_A_LOAD] = *(const u32x4*)(v_head + mine + in);
           if (K_LDS) kr[kb / BLOCKS_A_LOAD] = *(const u32x4*)(k_head + mine + in);
