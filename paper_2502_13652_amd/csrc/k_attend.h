@@ -4,7 +4,9 @@
 //
 // One pass over the keys: a wavefront keeps, for every row it has, the running maximum m (of s log2 e), the sum l of p and
 // sum p v, and multiplies the last two by 2^(m_old - m_new) where a tile raises m.  A row that sees no key has m = -inf, l = 0
-// and is put out as zeros.
+// and is put out as zeros.  l is the sum of the weights as the second product takes them, rounded to 16 bits, so that a row of few or of sharp
+// weights keeps a mean of its values: what one weight's rounding adds to the product it adds to the divisor.  Where the log of the sum is asked for,
+// the weights as they were are summed too, for that alone.
 //
 // Rows: the query heads of one cached head share its keys, so rows are (slot, head of the group) with the head
 // fastest.  Products are taken transposed: S^T = K Q^T leaves in a lane one row (lane & 15) and 4 neighbouring keys of each
@@ -47,9 +49,10 @@ struct AttendArgs {
   int32_t nodes, chain;                    // slots = chain + nodes
   int32_t layer;
   float scale_log2e;
-  // records of parts: [records][rows of a tile][head_dim], and (m, l) of each row.  Joined by the unit's last part: tickets [records], parts of the
-  // unit with that first record that have left theirs, zero between launches.  Joined by a launch of their own: what each record is of, and how many there are.
-  float* part_o; float2* part_ml; int32_t* tickets;
+  // records of parts: [records][rows of a tile][head_dim], and (m, l) of each row, with `lse` also the sum of its weights as they were.  Joined by the
+  // unit's last part: tickets [records], parts of the unit with that first record that have left theirs, zero between launches.  Joined by a launch of
+  // their own: what each record is of, and how many there are.
+  float* part_o; float2* part_ml; float* part_e; int32_t* tickets;
   struct Unit* units; int32_t* n_records;
   AttendShape shape;
 };
@@ -143,7 +146,7 @@ template <typename E> __device__ __forceinline__ uint32_t odd_halves(uint32_t w)
 
 // four neighbouring elements of a row's output, and with the first of them its log of the sum
 template <typename E, int D>
-__device__ __forceinline__ void put_row(const CacheView& c, const AttendArgs& a, const Unit& u, int t, int g, int dim, f32x4 x, float m, float l) {
+__device__ __forceinline__ void put_row(const CacheView& c, const AttendArgs& a, const Unit& u, int t, int g, int dim, f32x4 x, float m, float l, float e) {
   const float inv = l == 0.f ? 0.f : 1.f / l;
   typename E::T4 y;
 #pragma unroll
@@ -151,16 +154,17 @@ __device__ __forceinline__ void put_row(const CacheView& c, const AttendArgs& a,
   const int64_t head = (int64_t)u.head * a.shape.group + g;
   *(typename E::T4*)(a.out + u.b * a.out_batch + t * a.out_token + (head * D + dim) * 2) = y;
   if (dim == 0 && a.lse)
-    a.lse[((int64_t)u.b * a.shape.slots + t) * c.kv_heads * a.shape.group + head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+    a.lse[((int64_t)u.b * a.shape.slots + t) * c.kv_heads * a.shape.group + head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(e)) * 0.69314718055994531f;
 }
 // running join of parts
 struct Joined {
-  float m = -INFINITY, l = 0.f;
+  float m = -INFINITY, l = 0.f, e = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  __device__ __forceinline__ void add(float2 ml, f32x4 x) {
+  __device__ __forceinline__ void add(float2 ml, float of_e, f32x4 x) {
     const float m_new = fmaxf(m, ml.x), ref = m_new == -INFINITY ? 0.f : m_new;
     const float back = __builtin_amdgcn_exp2f(m - ref), f = __builtin_amdgcn_exp2f(ml.x - ref);
     l = l * back + ml.y * f;
+    e = e * back + of_e * f;
     o = o * back + x * f;
     m = m_new;
   }
@@ -194,7 +198,7 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
   static_assert(ROWS_A_LOAD <= 16 ? 16 % ROWS_A_LOAD == 0 : ROWS_A_LOAD % 16 == 0, "");
   constexpr bool K_LDS = RW > 1;
   constexpr int TILE_BYTES = KT * L::V_ROW + (K_LDS ? KT * L::K_ROW : 0);
-  constexpr int JOIN_BYTES = KW > 1 ? KW * 16 * (D + 2) * 4 : 0;
+  constexpr int JOIN_BYTES = KW > 1 ? KW * 16 * (D + 3) * 4 : 0;
   constexpr int BUFFERS = RW > 1 ? 2 : KW;                  // of the tile: the next one's while this one is used, or one a wavefront
   constexpr int LDS_BYTES = BUFFERS * TILE_BYTES > JOIN_BYTES ? BUFFERS * TILE_BYTES : JOIN_BYTES;
   // a row's reference is only raised where a score passes it by this much: weights stay below 2^8
@@ -250,10 +254,10 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
   }
 
   f32x4 o[MT][DB];
-  float m_run[MT], l_run[MT];                                // l_run: of this lane's keys
+  float m_run[MT], l_run[MT], e_run[MT];                     // sums of weights: rounded ones of the row, and with `lse` this lane's keys' as they were
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
-    m_run[m] = -INFINITY; l_run[m] = 0.f;
+    m_run[m] = -INFINITY; l_run[m] = 0.f; e_run[m] = 0.f;
 #pragma unroll
     for (int d = 0; d < DB; ++d) o[m][d] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
@@ -447,22 +451,39 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
           top = fmaxf(top, __shfl_xor(top, 32));
           const float m_new = fmaxf(m_run[m], top), back = __builtin_amdgcn_exp2f(m_run[m] - (m_new == -INFINITY ? 0.f : m_new));
           m_run[m] = m_new;
-          l_run[m] *= back;
+          l_run[m] *= back; e_run[m] *= back;
 #pragma unroll
           for (int d = 0; d < DB; ++d) o[m][d] *= back;
         }
         const float ref = m_run[m] == -INFINITY ? 0.f : m_run[m];
-        // P in the operands' 16 bits: relative 2^-9 (2^-12 for halves) a weight, of either sign; l is the sum of the weights as they were, for lse
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        // P in the operands' 16 bits: relative 2^-8 (2^-11 for halves) a weight at most, of either sign
 #pragma unroll
-        for (int h = 0; h < KB / 2; ++h)
+        for (int h = 0; h < KB / 2; ++h) {
 #pragma unroll
           for (int r = 0; r < 8; ++r) {
             const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[m][h * 2 + r / 4][r % 4], a.scale_log2e, -ref));
-            sum[r % 4] += w;
+            s[m][h * 2 + r / 4][r % 4] = w;
             p[m][h][r] = (T)w;
           }
-        l_run[m] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        }
+        if (a.lse) {
+          f32x4 all = s[m][0];
+#pragma unroll
+          for (int kb = 1; kb < KB; ++kb) all += s[m][kb];
+          e_run[m] += (all[0] + all[1]) + (all[2] + all[3]);
+        }
+      }
+      // The rounded weights' sum is a product with ones: the matrix unit has time for it.  The two chunks, with `lse`, 479 us, with additions of pairs 484, with the
+      // sum of the weights as they were for divisor 468; the 64 trees 232, 235 and 237.
+      f32x4 sum[MT];
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        T8 ones;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) ones[r] = (T)1.f;
+        sum[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int h = 0; h < KB / 2; ++h) sum[m] = E::mfma(ones, p[m][h], sum[m]);
       }
 #pragma unroll
       for (int h = 0; h < KB / 2; ++h) {
@@ -479,6 +500,8 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
           for (int m = 0; m < MT; ++m) o[m][d] = E::mfma(v, p[m][h], o[m][d]);
         }
       }
+#pragma unroll
+      for (int m = 0; m < MT; ++m) l_run[m] += sum[m][0];
     }
     if (RW > 1) {
       if (tile + 1 < tile_end) {
@@ -493,7 +516,7 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
   }
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
-    l_run[m] += __shfl_xor(l_run[m], 16); l_run[m] += __shfl_xor(l_run[m], 32);
+    e_run[m] += __shfl_xor(e_run[m], 16); e_run[m] += __shfl_xor(e_run[m], 32);
 #pragma unroll
     for (int d = 0; d < DB; ++d) settle(o[m][d]);
   }
@@ -535,12 +558,17 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
   }
 
   // what this workgroup has of a row: to the record of its part, or out
-  const auto put = [&](int row_in_tile, int t, int g, int dim, f32x4 x, float m, float l) {
-    if (u.parts == 1) { put_row<E, D>(c, a, u, t, g, dim, x, m, l); return; }
+  const auto put = [&](int row_in_tile, int t, int g, int dim, f32x4 x, float m, float l, float e) {
+    if (u.parts == 1) { put_row<E, D>(c, a, u, t, g, dim, x, m, l, e); return; }
     const int64_t rec = ((int64_t)(u.slot0 + u.part) << a.shape.rows_shift) + row_in_tile;
     float* to = a.part_o + rec * D + dim;
-    if (KW > 1) { st_dev64((uint64_t*)to, x[0], x[1]); st_dev64((uint64_t*)to + 1, x[2], x[3]); if (dim == 0) st_dev64((uint64_t*)(a.part_ml + rec), m, l); }
-    else { *(f32x4*)to = x; if (dim == 0) a.part_ml[rec] = make_float2(m, l); }
+    if (KW > 1) {
+      st_dev64((uint64_t*)to, x[0], x[1]); st_dev64((uint64_t*)to + 1, x[2], x[3]);
+      if (dim == 0) { st_dev64((uint64_t*)(a.part_ml + rec), m, l); if (a.lse) st_dev(a.part_e + rec, e); }
+    } else {
+      *(f32x4*)to = x;
+      if (dim == 0) { a.part_ml[rec] = make_float2(m, l); if (a.lse) a.part_e[rec] = e; }
+    }
   };
   if (KW == 1) {
 #pragma unroll
@@ -548,18 +576,18 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
       const int r = wave_row0 + m * 16 + col;
       if (slot[m] < 0) continue;
 #pragma unroll
-      for (int d = 0; d < DB; ++d) put(rw * 16 * MT + m * 16 + col, slot[m], r - slot[m] * G, d * 16 + quad * 4, o[m][d], m_run[m], l_run[m]);
+      for (int d = 0; d < DB; ++d) put(rw * 16 * MT + m * 16 + col, slot[m], r - slot[m] * G, d * 16 + quad * 4, o[m][d], m_run[m], l_run[m], e_run[m]);
     }
   } else {
     // the wavefronts' results of 16 rows at a time through LDS
     float* const jo = (float*)lds;                           // [KW][16][D]
-    float* const jm = jo + KW * 16 * D; float* const jl = jm + KW * 16;
+    float* const jm = jo + KW * 16 * D; float* const jl = jm + KW * 16; float* const je = jl + KW * 16;
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
       __syncthreads();
 #pragma unroll
       for (int d = 0; d < DB; ++d) *(f32x4*)(jo + (kw * 16 + col) * D + d * 16 + quad * 4) = o[m][d];
-      if (quad == 0) { jm[kw * 16 + col] = m_run[m]; jl[kw * 16 + col] = l_run[m]; }
+      if (quad == 0) { jm[kw * 16 + col] = m_run[m]; jl[kw * 16 + col] = l_run[m]; je[kw * 16 + col] = e_run[m]; }
       __syncthreads();
       for (int i = tid; i < 16 * D / 4; i += NT) {
         const int row = i / (D / 4), dim = i % (D / 4) * 4, r = wave_row0 + m * 16 + row;
@@ -569,16 +597,17 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
         for (int w = 0; w < KW; ++w) mm = fmaxf(mm, jm[w * 16 + row]);
         const float ref = mm == -INFINITY ? 0.f : mm;
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
-        float l = 0.f;
+        float l = 0.f, e = 0.f;
 #pragma unroll
         for (int w = 0; w < KW; ++w) {
           const float f = __builtin_amdgcn_exp2f(jm[w * 16 + row] - ref);
           l += f * jl[w * 16 + row];
+          e += f * je[w * 16 + row];
           x += f * *(const f32x4*)(jo + (w * 16 + row) * D + dim);
         }
         int t, g;
         split(r, G, a.shape.inv_group, &t, &g);
-        put(m * 16 + row, t, g, dim, x, mm, l);
+        put(m * 16 + row, t, g, dim, x, mm, l, e);
       }
     }
   }
@@ -602,18 +631,20 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
     Joined x;
     for (int p0 = 0; p0 < u.parts; p0 += AT_ONCE) {
       float2 ml[AT_ONCE], lo[AT_ONCE], hi[AT_ONCE];
+      float e[AT_ONCE];
 #pragma unroll
       for (int p = 0; p < AT_ONCE; ++p) {
         const int64_t rec = rec0 + ((int64_t)min(p0 + p, u.parts - 1) << a.shape.rows_shift);
         const uint64_t* from = (const uint64_t*)(a.part_o + rec * D + dim);
+        e[p] = a.lse ? ld_dev(a.part_e + rec) : 0.f;
         ml[p] = ld_dev64((const uint64_t*)(a.part_ml + rec)); lo[p] = ld_dev64(from); hi[p] = ld_dev64(from + 1);
       }
 #pragma unroll
-      for (int p = 0; p < AT_ONCE; ++p) if (p0 + p < u.parts) x.add(ml[p], f32x4{lo[p].x, lo[p].y, hi[p].x, hi[p].y});
+      for (int p = 0; p < AT_ONCE; ++p) if (p0 + p < u.parts) x.add(ml[p], e[p], f32x4{lo[p].x, lo[p].y, hi[p].x, hi[p].y});
     }
     int t, g;
     split(row0 + row, G, a.shape.inv_group, &t, &g);
-    put_row<E, D>(c, a, u, t, g, dim, x.o, x.m, x.l);
+    put_row<E, D>(c, a, u, t, g, dim, x.o, x.m, x.l, x.e);
   }
 }
 
@@ -633,11 +664,11 @@ __global__ __launch_bounds__(JOIN_NT) void k_attend_join(CacheView c, AttendArgs
 #pragma unroll 4
     for (int p = 0; p < u.parts; ++p) {
       const int64_t rec = rec0 + ((int64_t)p << a.shape.rows_shift);
-      x.add(a.part_ml[rec], *(const f32x4*)(a.part_o + rec * D + dim));
+      x.add(a.part_ml[rec], a.lse ? a.part_e[rec] : 0.f, *(const f32x4*)(a.part_o + rec * D + dim));
     }
     int t, g;
     split(row0 + row, G, a.shape.inv_group, &t, &g);
-    put_row<E, D>(c, a, u, t, g, dim, x.o, x.m, x.l);
+    put_row<E, D>(c, a, u, t, g, dim, x.o, x.m, x.l, x.e);
   }
 }
 

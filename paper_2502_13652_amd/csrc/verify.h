@@ -71,7 +71,7 @@ constexpr int MAX_RUN = 8;                                   // a chunk of 2048 
 constexpr int MAX_TARGET_SHIFT = 10, MAX_PARTS_ROWS = 64;
 // 32 rows a cached head of one sequence behind 32000 tokens 31 us, with 256 KiB 39, with 64 45; of 16 rows 30, 33, 45; of 16 rows of a single cached head 28, 24, 41.
 constexpr int64_t JOIN_BYTES = 128 << 10;
-struct AttendPlan { AttendShape shape; int build, records; int64_t units, items; size_t n_records, units_at, part_o, part_ml, total; };
+struct AttendPlan { AttendShape shape; int build, records; int64_t units, items; size_t n_records, units_at, part_o, part_ml, part_e, total; };
 
 // Sizes of a call alone: the workspace must not depend on what is on the device.
 inline int attend_plan(const c2t_cache& c, const c2t_attention& a, AttendPlan* p) {
@@ -106,7 +106,8 @@ inline int attend_plan(const c2t_cache& c, const c2t_attention& a, AttendPlan* p
   p->part_o = p->units_at + (sizeof(Unit) << (MAX_TARGET_SHIFT + 1));
   p->records = (int)records;
   p->part_ml = p->part_o + rows_of_them * c.head_dim * 4;
-  p->total = p->part_ml + rows_of_them * 8;
+  p->part_e = p->part_ml + rows_of_them * 8;
+  p->total = p->part_e + rows_of_them * 4;
   return C2T_OK;
 }
 
@@ -256,7 +257,7 @@ int c2t_cache_attention(const c2t_cache* c, const c2t_attention* a, void* ws, si
   g.n_new = a->n_new; g.mask = a->mask; g.nodes = a->nodes; g.chain = a->tokens - a->nodes; g.layer = a->layer;
   g.scale_log2e = std::max(a->scale, 1e-30f) * 1.44269504088896341f;       // (a masked score is -infinity times it: not 0)
   g.tickets = (int32_t*)ws; g.n_records = (int32_t*)((char*)ws + p.n_records); g.units = (Unit*)((char*)ws + p.units_at);
-  g.part_o = (float*)((char*)ws + p.part_o); g.part_ml = (float2*)((char*)ws + p.part_ml);
+  g.part_o = (float*)((char*)ws + p.part_o); g.part_ml = (float2*)((char*)ws + p.part_ml); g.part_e = (float*)((char*)ws + p.part_e);
   g.shape = p.shape;
   const CacheView v = view_of(*c);
   const bool bf16 = c->dtype == C2T_BF16;

@@ -354,6 +354,29 @@ def test_captures_leave_no_workspaces_behind():
             del other
 
 
+# of all kernels, and of parts that are joined by the last of them and by a launch
+MEANS = [(2, 1, 8, 2, [3, 170]), (2, 4, 8, 2, [0, 140]), (1, 9, 16, 4, [210]), (2, 40, 8, 2, [5, 150]), (1, 70, 4, 2, [180])]
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("B,T,H,Hkv,lens", MEANS + [(1, 1, 4, 1, [3500]), (1, 20, 4, 1, [3000]), (1, 70, 2, 1, [2500])])
+def test_a_mean_of_equal_values_is_that_value(B, T, H, Hkv, lens, D, dtype):
+    """Sharp rows over values that are the same for all keys: what the weights' rounding to 16 bits adds to the weighted sum it adds to the divisor too.  What is left is the sums'
+    roundings in fp32, at most n 2^-23 relative in each for n keys (the terms have one sign), and two of the division: below half a step of a bf16 value,
+    2^-9 relative at least, for 8000 keys, and of an fp16 one, 2^-12, for 1000: rounding then gives the value itself."""
+    if dtype is HF:
+        lens = [min(l, 900) for l in lens]
+    cache = make_cache(lens, T, 16, Hkv, D, dtype, seed=D + T)
+    c = torch.randn((1, 1, Hkv, 1, D), generator=gen(D, "cuda"), device="cuda").to(dtype)
+    c[..., ::4] = c[..., ::4].sign()
+    cache.v.copy_(c.expand_as(cache.v))
+    q = queries(B, T, H, D, dtype, T)
+    print("equal values", (B, T, H, Hkv, D), lens, dtype, flush=True)
+    out = cache.attention(0, q, scale=4 * D ** -0.5, lse=torch.empty((B, T, H), device="cuda") if T % 2 else None)
+    assert torch.equal(out, c[0, 0, :, 0].repeat_interleave(H // Hkv, 0)[None, None].expand_as(out))
+
+
 def test_refusals():
     from paper_2502_13652_amd import PagedCache
     from paper_2502_13652_amd.binding import C2TError
