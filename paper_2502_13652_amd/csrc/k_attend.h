@@ -2,7 +2,7 @@
 //
 //   s_j = scale q.k_j over the keys j that the row sees,  p_j = e^(s_j - m),  m = max s,  out = sum p_j v_j / sum p_j
 //
-// One pass over the keys: a wavefront keeps, for every row it has, the running maximum m (of s log2 e), the sum l of p and
+// One pass over the keys: a wavefront keeps, for every row it has, a reference m that follows the running maximum (of s log2 e), the sum l of p and
 // sum p v, and multiplies the last two by 2^(m_old - m_new) where a tile raises m.  A row that sees no key has m = -inf, l = 0
 // and is put out as zeros.  l is the sum of the weights as the second product takes them, rounded to 16 bits, so that a row of few or of sharp
 // weights keeps a mean of its values: what one weight's rounding adds to the product it adds to the divisor.  Where the log of the sum is asked for,
@@ -34,11 +34,13 @@ struct Bf16 {
   typedef __bf16 T; typedef __bf16 T4 __attribute__((ext_vector_type(4))); typedef __bf16 T8 __attribute__((ext_vector_type(8)));
   static __device__ __forceinline__ f32x4 mfma(T8 a, T8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
   static constexpr uint32_t EXPONENT = 0x7f80u;
+  static constexpr float TOP = 8.f, SLACK = 8.f;
 };
 struct F16 {
   typedef _Float16 T; typedef _Float16 T4 __attribute__((ext_vector_type(4))); typedef _Float16 T8 __attribute__((ext_vector_type(8)));
   static __device__ __forceinline__ f32x4 mfma(T8 a, T8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
   static constexpr uint32_t EXPONENT = 0x7c00u;
+  static constexpr float TOP = 15.f, SLACK = 2.f;
 };
 
 struct AttendArgs {
@@ -201,8 +203,10 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
   constexpr int JOIN_BYTES = KW > 1 ? KW * 16 * (D + 3) * 4 : 0;
   constexpr int BUFFERS = RW > 1 ? 2 : KW;                  // of the tile: the next one's while this one is used, or one a wavefront
   constexpr int LDS_BYTES = BUFFERS * TILE_BYTES > JOIN_BYTES ? BUFFERS * TILE_BYTES : JOIN_BYTES;
-  // a row's reference is only raised where a score passes it by this much: weights stay below 2^8
-  constexpr float SLACK = 8.f;
+  // A row's reference is only raised where a weight would pass 2^TOP, and then to where the largest is 2^(TOP - SLACK).  Halves have 2^-14 for their least number of
+  // all bits and 2^-24 for their least: at the top of their range, weights of 2^-27 of a row's largest keep all bits, and what the others lose is 2^-38
+  // of the largest at most (keys of small weights are many, and all there is where a sharp key's value is 0).  A slack of 8 saves the two chunks 0.4 %.
+  constexpr float TOP = E::TOP, SLACK = E::SLACK;
   __shared__ __align__(16) char lds[LDS_BYTES];
   __shared__ int odd_value;                                  // a tile held a value that is not finite
 
@@ -446,17 +450,17 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
 #pragma unroll
           for (int r = 0; r < 4; ++r) top = fmaxf(top, s[m][kb][r]);
         top *= a.scale_log2e;
-        if (__any(top > m_run[m] + SLACK)) {                 // (uniform) of all four lanes of a row, then
+        if (__any(top > m_run[m] + TOP)) {                 // (uniform) of all four lanes of a row, then
           top = fmaxf(top, __shfl_xor(top, 16));
           top = fmaxf(top, __shfl_xor(top, 32));
-          const float m_new = fmaxf(m_run[m], top), back = __builtin_amdgcn_exp2f(m_run[m] - (m_new == -INFINITY ? 0.f : m_new));
+          const float m_new = fmaxf(m_run[m], top - (TOP - SLACK)), back = __builtin_amdgcn_exp2f(m_run[m] - (m_new == -INFINITY ? 0.f : m_new));
           m_run[m] = m_new;
           l_run[m] *= back; e_run[m] *= back;
 #pragma unroll
           for (int d = 0; d < DB; ++d) o[m][d] *= back;
         }
         const float ref = m_run[m] == -INFINITY ? 0.f : m_run[m];
-        // P in the operands' 16 bits: relative 2^-8 (2^-11 for halves) a weight at most, of either sign
+        // P in the operands' 16 bits: relative 2^-8 (2^-11 for halves that are not subnormal) a weight at most, of either sign
 #pragma unroll
         for (int h = 0; h < KB / 2; ++h) {
 #pragma unroll

@@ -377,6 +377,32 @@ def test_a_mean_of_equal_values_is_that_value(B, T, H, Hkv, lens, D, dtype):
     assert torch.equal(out, c[0, 0, :, 0].repeat_interleave(H // Hkv, 0)[None, None].expand_as(out))
 
 
+@pytest.mark.parametrize("bits", [24.9, 25.1, 28.0])
+@pytest.mark.parametrize("B,T,H,Hkv,D", [(1, 1, 4, 1, 64), (1, 20, 3, 1, 128), (1, 70, 2, 1, 64), (1, 5, 2, 1, 256), (1, 70, 2, 1, 256)])
+def test_half_precision_tails_behind_a_sharp_key(B, T, H, Hkv, D, bits):
+    """One key has next to all of a row's weight and a value of 0 in half of the dimensions: what comes out there is the sum of 30000 weights of about 2^-25 of its.
+    Halves below 2^-14 are multiples of 2^-24: with the row's largest weight at 2^13 or more a weight is off by 2^-38 of it at most, n of them by n 2^-38 (the values are 1), and the output,
+    itself such a half, by 2^-25."""
+    n = 30000
+    for at in (0, 17, n - 1):                                # where the sharp key lies
+        cache = make_cache([n], T, 64, Hkv, D, HF, seed=7)
+        cache.k.zero_()
+        cache.v.fill_(1.0)
+        page, row = int(cache.page_table[0, at // 64]), at % 64
+        cache.k[0, page, :, row, 0] = bits * 0.6931471805599453
+        cache.v[0, page, :, row, ::2] = 0.0
+        q = torch.zeros((B, T, H, D), dtype=HF, device="cuda")
+        q[..., 0] = 1.0
+        print("tail", (T, H, D), bits, at, flush=True)
+        lse = torch.zeros((B, T, H), device="cuda")
+        got = cache.attention(0, q, scale=1.0, lse=lse)
+        want, want_lse, tol, tol_lse = attention_reference(cache, 0, q, [T], None, 1.0)
+        assert 1e-6 * 2 ** (28 - bits) < float(want[0, 0, 0, 0]) < 1e-3
+        err = (got.double() - want).abs() - tol - n * 2.0 ** -38 - 2.0 ** -25
+        assert float(err.max()) <= 0, (float(got[0, 0, 0, 0]), float(want[0, 0, 0, 0]))
+        assert bool(((lse.double() - want_lse).abs() <= tol_lse).all())
+
+
 def test_refusals():
     from paper_2502_13652_amd import PagedCache
     from paper_2502_13652_amd.binding import C2TError
