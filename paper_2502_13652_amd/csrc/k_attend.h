@@ -34,7 +34,7 @@ struct Bf16 {
   typedef __bf16 T; typedef __bf16 T4 __attribute__((ext_vector_type(4))); typedef __bf16 T8 __attribute__((ext_vector_type(8)));
   static __device__ __forceinline__ f32x4 mfma(T8 a, T8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
   static constexpr uint32_t EXPONENT = 0x7f80u;
-  static constexpr float TOP = 8.f, SLACK = 8.f;
+  static constexpr float TOP = 0.f, SLACK = 8.f;
 };
 struct F16 {
   typedef _Float16 T; typedef _Float16 T4 __attribute__((ext_vector_type(4))); typedef _Float16 T8 __attribute__((ext_vector_type(8)));
@@ -203,7 +203,8 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
   constexpr int JOIN_BYTES = KW > 1 ? KW * 16 * (D + 3) * 4 : 0;
   constexpr int BUFFERS = RW > 1 ? 2 : KW;                  // of the tile: the next one's while this one is used, or one a wavefront
   constexpr int LDS_BYTES = BUFFERS * TILE_BYTES > JOIN_BYTES ? BUFFERS * TILE_BYTES : JOIN_BYTES;
-  // A row's reference is only raised where a weight would pass 2^TOP, and then to where the largest is 2^(TOP - SLACK).  Halves have 2^-14 for their least number of
+  // A row's reference is only raised where a weight would pass 2^TOP, and then to where the largest is 2^(TOP - SLACK).  Of bf16, whose values may be as large as an fp32
+  // number, no weight is above 1: the products then overflow only where their sum does.  Halves have 2^-14 for their least number of
   // all bits and 2^-24 for their least: at the top of their range, weights of 2^-27 of a row's largest keep all bits, and what the others lose is 2^-38
   // of the largest at most (keys of small weights are many, and all there is where a sharp key's value is 0).  A slack of 8 saves the two chunks 0.4 %.
   constexpr float TOP = E::TOP, SLACK = E::SLACK;

@@ -403,6 +403,21 @@ def test_half_precision_tails_behind_a_sharp_key(B, T, H, Hkv, D, bits):
         assert bool(((lse.double() - want_lse).abs() <= tol_lse).all())
 
 
+@pytest.mark.parametrize("T,H,Hkv,D", [(1, 4, 1, 128), (20, 3, 1, 64), (70, 2, 1, 128), (5, 2, 1, 256), (70, 2, 1, 256)])
+def test_values_near_the_largest_do_not_overflow(T, H, Hkv, D):
+    """Values of 2^125: two keys weigh something, the later one 2^6.9 times as much as the first, in another tile of the same wavefront's.  The sum
+    of their weights is below 2 where none is above 1, and the mean is 2^125."""
+    cache = make_cache([300], T, 16, Hkv, D, BF, seed=7)
+    cache.k.zero_()
+    cache.k[..., 0] = -80.0
+    for at, x in ((0, 0.0), (128, 4.8)):
+        cache.k[0, int(cache.page_table[0, at // 16]), :, at % 16, 0] = x
+    cache.v.fill_(2.0 ** 125)
+    q = torch.zeros((1, T, H, D), dtype=BF, device="cuda")
+    q[..., 0] = 1.0
+    assert bool((cache.attention(0, q, scale=1.0) == 2.0 ** 125).all())
+
+
 def test_refusals():
     from paper_2502_13652_amd import PagedCache
     from paper_2502_13652_amd.binding import C2TError
