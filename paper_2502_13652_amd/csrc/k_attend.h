@@ -153,10 +153,9 @@ __device__ __forceinline__ void put_row(const CacheView& c, const AttendArgs& a,
   typename E::T4 y;
 #pragma unroll
   for (int r = 0; r < 4; ++r) y[r] = (typename E::T)(x[r] * inv);
-  const int64_t head = (int64_t)u.head * a.shape.group + g;
-  *(typename E::T4*)(a.out + u.b * a.out_batch + t * a.out_token + (head * D + dim) * 2) = y;
+  *(typename E::T4*)(a.out + u.b * a.out_batch + t * a.out_token + (query_offset(u.head, a.shape.group, g, D) + dim) * 2) = y;
   if (dim == 0 && a.lse)
-    a.lse[((int64_t)u.b * a.shape.slots + t) * c.kv_heads * a.shape.group + head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(e)) * 0.69314718055994531f;
+    a.lse[((int64_t)u.b * a.shape.slots + t) * c.kv_heads * a.shape.group + query_offset(u.head, a.shape.group, g, 1)] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(e)) * 0.69314718055994531f;
 }
 // running join of parts
 struct Joined {
@@ -253,7 +252,7 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
     if (r >= rows) slot[m] = -1;
 #pragma unroll
     for (int kk = 0; kk < DK; ++kk) {
-      if (slot[m] >= 0) q[m][kk] = *(const T8*)(a.q + u.b * a.q_batch + slot[m] * a.q_token + ((u.head * G + g) * D + kk * 32 + quad * 8) * 2);
+      if (slot[m] >= 0) q[m][kk] = *(const T8*)(a.q + u.b * a.q_batch + slot[m] * a.q_token + (query_offset(u.head, G, g, D) + kk * 32 + quad * 8) * 2);
       else q[m][kk] = T8{};
     }
   }

@@ -51,6 +51,10 @@ C2T_HD int64_t row_offset(const CacheView& c, int layer, int page, int head, int
   return ((((int64_t)layer * c.pages + page) * c.kv_heads + head) << c.page_shift) * c.head_dim + (int64_t)row * c.head_dim;
 }
 
+// Offset, in elements, of a query head in its token's row (of queries, and of outputs): head `g` of the `group` that share cached head `head`.  Heads may be
+// as many as 2^30, so 31 bits do not hold it.
+C2T_HD int64_t query_offset(int head, int group, int g, int head_dim) { return ((int64_t)head * group + g) * head_dim; }
+
 // ---- Attention's work ----
 // A unit is a tile of query rows of one cached head of one sequence; it goes over the sequence's keys tile by tile.  Units
 // are split over their keys into parts so that the launch has about `target` parts of about the same length whatever

@@ -237,6 +237,22 @@ def test_offsets_past_32_bits():
     assert torch.equal(a, b)
 
 
+def test_heads_past_31_bits():
+    """So many query heads over one cached head that the last ones lie beyond 2^31 bytes of their token's row.  One key: each gets its value, whatever it asks."""
+    H, D = (1 << 22) + 200, 256
+    cache = make_cache([0], 1, 16, 1, D, BF, seed=3)
+    q = torch.zeros((1, 1, H, D), dtype=BF, device="cuda")
+    q[0, 0, -300:] = queries(1, 1, 300, D, BF, 5)[0, 0]
+    lse = torch.zeros((1, 1, H), device="cuda")
+    out = cache.attention(0, q, lse=lse)
+    page = int(cache.page_table[0, 0])
+    assert bool((out[0, 0] == cache.v[0, page, 0, 0]).all())
+    k, last = cache.k[0, page, 0, 0].double(), q[0, 0, -300:].double()
+    x, size = last @ k * D ** -0.5, last.abs() @ k.abs() * D ** -0.5
+    tol = (D + 4) * 2.0 ** -24 * size + 4 * 2.0 ** -23 * (1 + size) + 66 * 2.0 ** -23 + x.abs() * 2.0 ** -22       # as attention_reference counts them
+    assert bool((lse[0, 0, :-300].abs() <= 70 * 2.0 ** -23).all()) and bool(((lse[0, 0, -300:].double() - x).abs() <= tol).all())
+
+
 def test_strided_outputs_and_single_heads():
     cache = make_cache([33, 64], 5, 16, 1, 64, BF, seed=6)
     q = queries(2, 5, 3, 64, BF, 2, fused=2)

@@ -149,6 +149,17 @@ def test_work_lists_and_addresses_of_the_paged_cache_under_sanitizers():
         assert r.returncode == 0 and "paged driver ok" in r.stdout and "runtime error" not in r.stdout, r.stdout
 
 
+def test_places_of_as_many_heads_as_there_may_be_under_sanitizers():
+    with tempfile.TemporaryDirectory() as d:
+        exe = os.path.join(d, "heads_driver")
+        r = subprocess.run(["hipcc", "-O1", "-g", "-std=c++17", "--offload-arch=gfx950", "-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
+                            "-Xarch_host", "-fno-sanitize-recover=all", "-o", exe, os.path.join(SAN, "heads_driver.cpp")],
+                           stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+        assert r.returncode == 0, r.stdout
+        r = subprocess.run([exe], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, env=ENV)
+        assert r.returncode == 0 and "heads driver ok" in r.stdout and "runtime error" not in r.stdout, r.stdout
+
+
 def test_serving_entry_points_under_sanitizers():
     with tempfile.TemporaryDirectory() as d:
         exe = os.path.join(d, "serving_driver")
