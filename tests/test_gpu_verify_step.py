@@ -155,3 +155,36 @@ def test_forked_sequences_go_their_own_ways():
             at = torch.arange(37, device="cuda")
             k = c.k[layer, c.page_table[b].long()[at // ps], :, at % ps]
             assert torch.equal(k, x[0, :, :Hkv])
+
+
+def test_the_example_of_the_readme():
+    """The README's step, line for line, on the tree of a draft phase."""
+    from test_serving_host import readme_blocks
+    block = [b for b in readme_blocks() if "PagedCache" in b]
+    assert len(block) == 1
+    cfg = dict(idx=93, B=3, V=1009, dtype="bf16", D=3, F=6, K=4, h=6, beta=0.0, N=15, zipf_s=1.2, sigma=(0.5, 1.5), spike_frac=0.0, desc="the readme")
+    B, V, N, F, layers = cfg["B"], cfg["V"], cfg["N"], cfg["F"], 2
+    ctx = make_gpu(cfg, W.classifier(cfg, 2))
+    rows = lambda l: torch.nn.functional.pad(W.logits_layer(cfg, l, device="cuda"), (0, -V % 8))
+    ctx.reset()
+    for l in range(cfg["D"]):
+        ctx.expand_layer(rows(l))
+    out = ctx.finalize_tree()
+    ctx.reset()
+    x = torch.randn((B, 1 + N, 32 + 16, 128), generator=gen(1, "cuda"), device="cuda").to(torch.bfloat16)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    before = rows(0)
+    names = dict(B=B, layers=layers, pages=64, ctx=ctx, ctx_tokens=torch.randint(0, V, (B, 30), generator=gen(2, "cuda"), **i32), n=torch.full((B,), 30, **i32),
+                 r=torch.full((B,), 1.3, device="cuda"), grammar_words=torch.full((B, 1, (V + 31) // 32), -2, **i32), logits=before.clone(), out=out,
+                 q=x[:, :, :32], k=x[:, :, 32:40], v=x[:, :, 40:], target=torch.randn((B, 1 + N, 1016), generator=gen(3, "cuda"), device="cuda").to(torch.bfloat16)[:, :, :V],
+                 path=torch.zeros((B, 1), **i32), n_path=torch.ones(B, **i32))
+    exec(block[0], names)
+    cache, y, target = names["cache"], names["y"], names["target"]
+    assert names["logits"].data_ptr() != before.data_ptr() and bool((names["logits"][:, 0, 0:V:32] == float("-inf")).all()) and not torch.equal(names["logits"], before)
+    n_new = names["n_new"].tolist()
+    assert cache.length.tolist() == [1] * B and int(cache.status.view(torch.int32).abs().sum()) == 0 and int((cache.refcount > 0).sum()) == B
+    # the root's key is still there: its row sees itself alone
+    live = names["v"][:, 0].repeat_interleave(4, 1)
+    assert torch.equal(y[:, 0], live)
+    for b in range(B):
+        assert bool(torch.isfinite(y[b, :n_new[b]]).all()) and bool((target[b, :n_new[b], 0:V:32] == float("-inf")).all())

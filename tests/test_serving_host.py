@@ -178,3 +178,16 @@ def test_the_header_and_the_binding_agree_on_the_counters():
     from paper_2502_13652_amd.serving import ATTENTION_COUNTERS
     with open(os.path.join(ROOT, "include", "c2t.h")) as f:
         assert "#define C2T_ATTENTION_COUNTERS %d\n" % ATTENTION_COUNTERS in f.read()
+
+
+def readme_blocks():
+    """The README's python examples."""
+    with open(os.path.join(ROOT, "README.md")) as f:
+        return [part.split("```")[0] for part in f.read().split("```python\n")[1:]]
+
+
+def test_what_the_readme_imports_is_there():
+    lines = [line for block in readme_blocks() for line in block.split("\n") if line.startswith(("import ", "from "))]
+    assert len(lines) >= 2 and any("PagedCache" in line for line in lines)
+    for line in lines:
+        exec(line, {})
