@@ -290,8 +290,8 @@ typedef struct {
 
 enum {
   C2T_CACHE_POOL_EMPTY = 1, /* reserve: not enough free pages; this sequence got none                             */
-  C2T_CACHE_ROW_FULL = 2,   /* its row of page_table has no room for the tokens                                    */
-  C2T_CACHE_INVALID = 4,    /* a page number, path or pair of a fork that cannot be; what needed it was left out      */
+  C2T_CACHE_ROW_FULL = 2,   /* its row of page_table has no room for the tokens (write, attention: for the last of them) */
+  C2T_CACHE_INVALID = 4,    /* a page number, path or pair of a fork that cannot be; what needed it was left out (attention: the keys on the page) */
   C2T_CACHE_SHARED = 8      /* a page to be written is held by others too (nothing was reserved); not written      */
 };
 
@@ -342,6 +342,7 @@ typedef struct {
 
 /* Every slot sees the length[b] tokens before; a chain slot the chain up to itself; node i the whole chain and the nodes j with mask[b][i][j] != 0
  * (j < n_new[b] - chain).  A key that a row does not see has no influence on it, whatever its bits.  A row that sees no key gets zeros.
+ * Keys below length[b] + n_new[b] on no page of the pool are left out, and the sequence's status says so, as it does where n_new was cut for want of room.
  * Products in the cache's dtype, sums and the softmax in fp32.  The workspace is [device], 256-byte aligned, its size from the call's sizes
  * alone.  Its first C2T_ATTENTION_COUNTERS bytes are zero-filled by the caller before its first use, on the stream that uses it or one that it waits
  * for, and are zero again after each call.  Calls that may run at the same time need one each, others may share the largest. */

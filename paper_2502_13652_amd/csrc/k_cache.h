@@ -14,9 +14,6 @@ constexpr int RESERVE_MAX_B = 4096;        // sequences; their counts are kept i
 constexpr int RESERVE_LANES = 16;          // lanes that look at a sequence's pages together
 constexpr int MAX_PATH_TOKENS = 1025;             // tokens of an accepted path: the root and as many nodes as a tree may have
 
-enum : uint32_t { CACHE_POOL_EMPTY = 1u, CACHE_ROW_FULL = 2u, CACHE_INVALID = 4u, CACHE_SHARED = 8u };     // C2T_CACHE_* of the C ABI
-
-__device__ __forceinline__ void report(const CacheView& c, int b, uint32_t bit) { atomicOr(c.status + b, bit); }
 // one holder less; a count that is no one's is left alone
 __device__ __forceinline__ bool let_go(int32_t* refcount) {
   if (atomicSub(refcount, 1) > 0) return true;

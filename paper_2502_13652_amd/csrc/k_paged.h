@@ -19,6 +19,9 @@ struct CacheView {
   int32_t page_shift;                      // page_size = 1 << page_shift
 };
 
+enum : uint32_t { CACHE_POOL_EMPTY = 1u, CACHE_ROW_FULL = 2u, CACHE_INVALID = 4u, CACHE_SHARED = 8u };     // C2T_CACHE_* of the C ABI
+__device__ __forceinline__ void report(const CacheView& c, int b, uint32_t bit) { atomicOr(c.status + b, bit); }
+
 C2T_HD int clamp_int(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
 C2T_HD int div_up(int a, int b) { return (a + b - 1) / b; }
 C2T_HD int64_t div_up64(int64_t a, int64_t b) { return (a + b - 1) / b; }

@@ -278,7 +278,8 @@ class PagedCache:
         """Attention of the last n_new (int32 [B], default all) tokens, which have been written behind the length, over the cache.
 
         q [B][T][q_heads][head_dim]; mask uint8 [B][N][N] as finalize_tree writes it: the last N of the T slots are the tree's nodes, those
-        before them (the root) a causal chain; no mask: all of them are.  scale: of the scores, default head_dim ** -0.5.  lse: float32
+        before them (the root) a causal chain; no mask: all of them are.  Keys on no page are left out and set INVALID in the sequence's status, new
+        tokens that its row of page_table has no room for are left out and set ROW_FULL.  scale: of the scores, default head_dim ** -0.5.  lse: float32
         [B][T][q_heads] for the log of the softmax's sums.  out: [B][T][q_heads][head_dim] (default: a new tensor), rows behind n_new left as
         they are.  workspace: uint8, zeros, of attention_workspace_bytes and 256-byte aligned, for calls that run at once otherwise than by stream.
         Without one the cache keeps one a stream, and in a graph's capture one that is the graph's: from its pool, counters cleared at each replay."""

@@ -111,6 +111,37 @@ def test_pages_that_are_none_are_left_out(H, T):
     check(cache, 0, queries(3, T, H, 64, BF, 1), None, tag="bad pages")
 
 
+# of all kernels, of parts that are joined either way, and of more sequences than a wavefront has lanes
+@pytest.mark.parametrize("H,Hkv,T,D,B", [(2, 2, 1, 64, 3), (8, 2, 3, 128, 3), (8, 2, 8, 64, 3), (16, 2, 40, 128, 3), (4, 2, 70, 256, 3), (2, 1, 1, 64, 130)])
+def test_what_attention_leaves_out_shows_in_the_status(H, Hkv, T, D, B):
+    full, invalid = 2, 4
+    lens = ([100, 5000, 30] + [20] * B)[:B]
+    cache = make_cache(lens, T, 16, Hkv, D, BF, seed=9, max_pages=-(-(5000 + T) // 16))
+    q = queries(B, T, H, D, BF, 1)
+    status = lambda: cache.status.view(torch.int32).tolist()
+    n = [T] * B
+    cache.page_table[0, -(-(100 + T) // 16):] = -1           # none behind its keys: nothing is left out
+    check(cache, 0, q, None, tag="all there")
+    assert status() == [0] * B
+    n[2] = 0
+    cache.page_table[2] = -1                                 # nothing is asked of it
+    cache.page_table[1, 200] = -7
+    check(cache, 0, q, n, tag="a page is missing")
+    assert status() == [0, invalid] + [0] * (B - 2)
+    cache.status.view(torch.int32).zero_()
+    cache.length[B - 1] = cache.max_pages * 16 - T + 1       # room for all tokens but one
+    cache.page_table[B - 1, :] = 0
+    n[B - 1] = T
+    check(cache, 0, q, n, tag="no room")
+    want = [0, invalid] + [0] * (B - 2)
+    want[B - 1] |= full
+    assert status() == want
+    cache.length[B - 1] = 10 ** 9                            # and none at all, for more than there are slots
+    cache.status.view(torch.int32).zero_()
+    check(cache, 0, q, [0] * (B - 1) + [T + 5], tag="full")
+    assert status() == [0] * (B - 1) + [full]
+
+
 def test_lengths_and_counts_out_of_range():
     cache = make_cache([40, 40, 40, 40], 8, 16, 2, 64, BF, seed=1)
     cache.length.copy_(torch.tensor([-5, 10 ** 9, 44, 40], dtype=torch.int32))
