@@ -173,8 +173,9 @@ struct Joined {
   }
 };
 
-// A product's result, used in a later block than the product: the compiler has been seen to read it there before the matrix unit has
-// written it (it counts the wait from the wrong instruction), so it is moved to ordinary registers in the product's own block, where the wait is right.
+// A product's result may be read only some issue slots after the product, which the compiler counts.  An earlier form of the loop below, which read its scores in a later
+// block than the products', was compiled to read them too early, so scores are put into ordinary registers in the block that makes them.  Outputs are
+// read behind the next tile's products or after the loop, both far enough.  tests/test_matrix_waits.py looks at every path of the builds as compiled.
 template <typename X> __device__ __forceinline__ void settle(X& x) { asm volatile("" : "+v"(x)); }
 
 // pairs of numbers that one workgroup writes and another reads in the same launch
