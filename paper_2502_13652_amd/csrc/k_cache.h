@@ -195,6 +195,21 @@ __device__ __forceinline__ int block_scan(int v, int* of_waves, int* total) {
   return before + incl;
 }
 
+// The same of numbers of up to 2^26 each.  4096 rows of so many places pass 31 bits (a rank that wrapped would be looked up far outside the list of pages), so
+// the lanes' sums are made of halves of 16 bits and fewer.
+__device__ __forceinline__ int64_t block_scan64(int v, int64_t* of_waves, int64_t* total) {
+  const int64_t incl = ((int64_t)wave_scan_incl(v >> 16) << 16) + wave_scan_incl(v & 0xffff);
+  const int w = threadIdx.x >> 6;
+  if ((threadIdx.x & 63) == 63) of_waves[w] = incl;
+  __syncthreads();
+  int64_t before = 0, all = 0;
+#pragma unroll
+  for (int i = 0; i < RESERVE_NT / WAVE; ++i) { const int64_t x = of_waves[i]; before += i < w ? x : 0; all += x; }
+  __syncthreads();
+  *total = all;
+  return before + incl;
+}
+
 // One workgroup: decisions of all sequences are made on the counts as they are at the start (a page that two of them hold is replaced
 // for both), the lowest free pages go out in order of sequence and place.  Sequences are served in order until the pool runs out: one
 // whose places do not all get a page gets none.  Latency bounds it, three or four trips to memory that wait for each other: 6 us for 2 or 80 sequences.
@@ -202,6 +217,7 @@ __global__ __launch_bounds__(RESERVE_NT) void k_cache_reserve(CacheView c, const
   constexpr int GROUPS = RESERVE_NT / RESERVE_LANES;
   __shared__ int need[RESERVE_MAX_B];                        // places that need a page; then: those of the sequences before it
   __shared__ int of_waves[RESERVE_NT / WAVE];
+  __shared__ int64_t places_of_waves[RESERVE_NT / WAVE];
   const int tid = threadIdx.x, group = tid / RESERVE_LANES, lane = tid % RESERVE_LANES;
   const uint64_t group_lanes = (0xffffull) << ((tid & 63) / RESERVE_LANES * RESERVE_LANES);
   auto needs_page = [&](int page) { return page < 0 || c.refcount[page] > 1; };        // (of a valid page or -1)
@@ -227,16 +243,17 @@ __global__ __launch_bounds__(RESERVE_NT) void k_cache_reserve(CacheView c, const
   }
   __syncthreads();
 
-  int all = 0;                                               // of all sequences; need[b] becomes the count before b, sign: not served
+  constexpr int64_t TOO_MANY = 1 << 30;                      // more than there may be pages; with a row's places it still fits 31 bits
+  int64_t all = 0;                                           // of all sequences; need[b] becomes the count before b, sign: not served
   for (int b0 = 0; b0 < c.batch; b0 += RESERVE_NT) {
     const int b = b0 + tid, mine = b < c.batch ? need[b] : 0, v = max(mine, 0);
-    int total;
-    const int before = all + block_scan(v, of_waves, &total) - v;
-    if (b < c.batch) need[b] = mine < 0 ? -1 : before;
+    int64_t total;
+    const int64_t before = all + block_scan64(v, places_of_waves, &total) - v;
+    if (b < c.batch) need[b] = mine < 0 ? -1 : (int)min(before, TOO_MANY);
     all += total;
   }
   __syncthreads();
-  const int wanted = min(all, x.cap);
+  const int wanted = (int)min(all, (int64_t)x.cap);
 
   // the first `wanted` free pages, in order
   int found = 0;

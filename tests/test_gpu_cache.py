@@ -234,6 +234,27 @@ def test_the_largest_batch():
     assert bool((c.refcount == 0).all()) and bool((c.page_table == -1).all()) and bool((c.length == 0).all()) and int(c.status.view(torch.int32).abs().sum()) == 0
 
 
+def test_more_places_asked_for_than_31_bits_count():
+    """4096 sequences that ask for half a million pages each of a pool of 64 (a page table of 8.6 GB): nobody gets any, and all are told so, the last one too, which asks for one."""
+    from paper_2502_13652_amd import PagedCache
+    B, max_pages = 4096, (1 << 19) + 256
+    c = PagedCache(B, 1, 64, 16, 1, 64, max_pages, dtype=BF)
+    assert (B - 1) * max_pages > 1 << 31
+    n = torch.full((B,), max_pages * 16, dtype=torch.int32, device="cuda")
+    n[-1] = 1
+    print("reserve, %d places" % (B * max_pages), flush=True)
+    c.reserve(n)
+    torch.cuda.synchronize()
+    assert c.status.view(torch.int32).tolist() == [EMPTY] * B
+    assert bool((c.refcount == 0).all()) and int(c.page_table.max()) == -1 and int(c.page_table.min()) == -1
+    n[:64] = 16                                              # the first 64 get one each, the rest none
+    c.status.view(torch.int32).zero_()
+    c.reserve(n)
+    torch.cuda.synchronize()
+    assert c.status.view(torch.int32).tolist() == [0] * 64 + [EMPTY] * (B - 64)
+    assert c.page_table[:, 0].tolist() == list(range(64)) + [-1] * (B - 64) and bool((c.refcount == 1).all())
+
+
 def test_a_long_path_and_the_largest_tree():
     c = make_cache([5, 900], 1025, 64, 2, 64, BF, seed=4, layers=2)
     p = Plain(c)
