@@ -131,10 +131,23 @@ def time_full_layers(torch, np, C2TContext, cfg, cls, layers, dev, reps, a=None)
             "gbps": fb / us / 1e3, "frac": fb / us / 1e3 / HBM_PEAK_GBPS}
 
 
+def deepest_paths(parent, n_nodes):
+    """Per sequence the slots of the root and of the nodes down to the tree's last one (breadth first: one of the deepest); lists of a finalized tree's arrays."""
+    paths = []
+    for p, n in zip(parent, n_nodes):
+        path, node = [], n - 1
+        while node >= 0:
+            path.append(1 + node)
+            node = p[node]
+        paths.append([0] + path[::-1])
+    return paths
+
+
 def time_verification(torch, np, cfg, tree, dev, tokens, steps):
     """What follows a draft phase, on its tree: the root's and the nodes' K and V into a paged cache that holds `tokens` tokens a
-    sequence, attention over it with the tree's mask, penalties on the target's logits, and the accepted path (here the root and,
-    where there is one, its first child) committed.  Synthetic K, V, queries and logits; microseconds a call, host included."""
+    sequence, attention over it with the tree's mask, penalties on the target's logits, and the accepted path (here the one from the root
+    to the tree's last node) committed.  Reserve is timed with the truncate that lets the new pages go again, commit with the one that takes the
+    length back.  Synthetic K, V, queries and logits; microseconds a call, host included."""
     from paper_2502_13652_amd import LogitAdjustments, PagedCache, adjust_tree_logits
     B, V, N = cfg["B"], cfg["V"], tree["tokens"].shape[1]
     layers, heads, kv_heads, width, page, T = 2, 32, 8, 128, 16, 1 + N
@@ -155,9 +168,12 @@ def time_verification(torch, np, cfg, tree, dev, tokens, steps):
     adj = LogitAdjustments(tokens=torch.randint(0, V, (B, tokens), generator=g, **i32), n_tokens=torch.full((B,), tokens, **i32),
                            n_prompt=torch.full((B,), tokens // 2, **i32), repetition=1.1 * ones, frequency=0.1 * ones, presence=0.1 * ones)
     start = torch.full((B,), tokens, **i32)
-    n_new, n_path = 1 + tree["n_nodes"], 1 + (tree["n_nodes"] > 0).to(torch.int32)
-    path, out, adjusted = torch.arange(2, **i32).repeat(B, 1), torch.empty((B, T, heads, width), dtype=torch.bfloat16, device=dev), torch.empty_like(logits)
-    calls = {"reserve": lambda: cache.reserve(n_new), "write": lambda: cache.write(0, k, v, n_new=n_new),
+    n_new = 1 + tree["n_nodes"]
+    paths = deepest_paths(tree["parent"].tolist(), tree["n_nodes"].tolist())
+    n_path = torch.tensor([len(p) for p in paths], **i32)
+    path = torch.tensor([p + [0] * (T - len(p)) for p in paths], **i32)
+    out, adjusted = torch.empty((B, T, heads, width), dtype=torch.bfloat16, device=dev), torch.empty_like(logits)
+    calls = {"truncate_and_reserve": lambda: (cache.truncate(start), cache.reserve(n_new)), "write": lambda: cache.write(0, k, v, n_new=n_new),
              "attention": lambda: cache.attention(0, q, n_new=n_new, mask=tree["mask"], out=out),
              "adjust": lambda: adjust_tree_logits(logits, tree, adj, vocab=V, out=adjusted),
              "truncate_and_commit": lambda: (cache.truncate(start, keep=T), cache.commit(path, n_path))}
@@ -170,8 +186,8 @@ def time_verification(torch, np, cfg, tree, dev, tokens, steps):
             call()
         torch.cuda.synchronize()
         us[name] = round((time.perf_counter() - t0) / steps * 1e6, 2)
-    assert int(cache.status.view(torch.int32).abs().sum()) == 0 and bool(torch.isfinite(out[0, 0]).all())
-    return {"us": us, "cached_tokens": tokens, "slots": T, "q_heads": heads, "kv_heads": kv_heads, "head_dim": width, "page_size": page, "calls": steps}
+    assert int(cache.status.view(torch.int32).abs().sum()) == 0 and bool(torch.isfinite(out[0, 0]).all()) and torch.equal(cache.length, start + n_path)
+    return {"us": us, "moved_tokens": sum(slot != i for p in paths for i, slot in enumerate(p)), "new_pages": int(sum(-(-(tokens + n) // page) for n in n_new.tolist())) - B * -(-tokens // page), "cached_tokens": tokens, "slots": T, "q_heads": heads, "kv_heads": kv_heads, "head_dim": width, "page_size": page, "calls": steps}
 
 
 def main():
