@@ -178,6 +178,13 @@ struct Joined {
 // read behind the next tile's products or after the loop, both far enough.  tests/test_matrix_waits.py looks at every path of the builds as compiled.
 template <typename X> __device__ __forceinline__ void settle(X& x) { asm volatile("" : "+v"(x)); }
 
+// x scale - ref, the product rounded
+__device__ __forceinline__ float rounded_difference(float x, float scale, float ref) {
+#pragma clang fp contract(off)
+  const float y = x * scale;
+  return y - ref;
+}
+
 // pairs of numbers that one workgroup writes and another reads in the same launch
 __device__ __forceinline__ void st_dev64(uint64_t* p, float x, float y) {
   __hip_atomic_store(p, (uint64_t)__float_as_uint(y) << 32 | __float_as_uint(x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -210,6 +217,12 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
   // all bits and 2^-24 for their least: at the top of their range, weights of 2^-27 of a row's largest keep all bits, and what the others lose is 2^-38
   // of the largest at most (keys of small weights are many, and all there is where a sharp key's value is 0).  A slack of 8 saves the two chunks 0.4 %.
   constexpr float TOP = E::TOP, SLACK = E::SLACK;
+  // Weights are 2^(s log2 e - m), with one rounding, but m was rounded from such a product itself, and where it is this large the two are a fourth and more apart, in the end by
+  // more than exponents hold.  From there on the scores' products are rounded first, as the references' were (for all tiles so, one multiplication a weight more).  Rows of such scores are as
+  // sharp as rows get: it is for them to be the value of their largest score, and not zeros or NaN.
+  constexpr float BIG = 0x1p22f;
+  int big = 0;
+  float factor = a.scale_log2e;                              // of the scores, which from there on are multiplied already: 1
   __shared__ __align__(16) char lds[LDS_BYTES];
   __shared__ int odd_value;                                  // a tile held a value that is not finite
 
@@ -451,6 +464,13 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
         }
       }
 
+      if (big != 0) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int kb = 0; kb < KB; ++kb) s[m][kb] *= a.scale_log2e;
+      }
+
       T8 p[MT][KB / 2];
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
@@ -459,11 +479,20 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
           for (int r = 0; r < 4; ++r) top = fmaxf(top, s[m][kb][r]);
-        top *= a.scale_log2e;
-        if (__any(top > m_run[m] + TOP)) {                 // (uniform) of all four lanes of a row, then
+        top *= factor;
+        if (__any(top - m_run[m] > TOP)) {                 // (uniform) of all four lanes of a row, then
           top = fmaxf(top, __shfl_xor(top, 16));
           top = fmaxf(top, __shfl_xor(top, 32));
-          const float m_new = fmaxf(m_run[m], top - (TOP - SLACK)), back = __builtin_amdgcn_exp2f(m_run[m] - (m_new == -INFINITY ? 0.f : m_new));
+          float m_new = fmaxf(m_run[m], top - (TOP - SLACK));
+          if (top - m_new > TOP) m_new = top;                // (it was rounded further down)
+          if (big == 0 && __any(__builtin_fabsf(m_new) >= BIG && m_new != -INFINITY)) {
+            big = 1; factor = 1.f;
+#pragma unroll
+            for (int n = m; n < MT; ++n)
+#pragma unroll
+              for (int kb = 0; kb < KB; ++kb) s[n][kb] *= a.scale_log2e;
+          }
+          const float back = __builtin_amdgcn_exp2f(m_run[m] - (m_new == -INFINITY ? 0.f : m_new));
           m_run[m] = m_new;
           l_run[m] *= back; e_run[m] *= back;
 #pragma unroll
@@ -475,7 +504,7 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
         for (int h = 0; h < KB / 2; ++h) {
 #pragma unroll
           for (int r = 0; r < 8; ++r) {
-            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[m][h * 2 + r / 4][r % 4], a.scale_log2e, -ref));
+            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[m][h * 2 + r / 4][r % 4], factor, -ref));
             s[m][h * 2 + r / 4][r % 4] = w;
             p[m][h][r] = (T)w;
           }
@@ -561,7 +590,7 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
           for (int r = 0; r < 8; ++r) x = __builtin_fmaf((float)k[r], (float)q[m][kk][r], x);
         }
         x += __shfl_xor(x, 16); x += __shfl_xor(x, 32);
-        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x, a.scale_log2e, -(m_run[m] == -INFINITY ? 0.f : m_run[m])));
+        const float w = __builtin_amdgcn_exp2f(rounded_difference(x, a.scale_log2e, m_run[m] == -INFINITY ? 0.f : m_run[m]));
         if (slot[m] < 0 || !sees(slot[m], key)) continue;
 #pragma unroll
         for (int d = 0; d < DB; ++d)

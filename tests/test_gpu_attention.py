@@ -465,6 +465,39 @@ def test_values_near_the_largest_do_not_overflow(T, H, Hkv, D):
     assert bool((cache.attention(0, q, scale=1.0) == 2.0 ** 125).all())
 
 
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("T,H,Hkv,D,n", [(1, 4, 1, 128, 90), (1, 4, 1, 64, 5000), (20, 3, 1, 64, 300), (70, 2, 1, 128, 400), (5, 2, 1, 256, 90), (70, 2, 1, 256, 3000)])
+def test_scores_of_any_size(T, H, Hkv, D, n, sign, dtype):
+    """Scores of 2^19 to 2^35 (2^26 for halves), far apart or equal: a row is the value of its largest score's key, or the mean of two whose scores are the same.  The scores are
+    exact, two differ by 2^-7 of their size at least, so all other weights are 0."""
+    at = [n // 3, n - 2]
+    pick = torch.randint(0, 60, (n,), generator=gen(n))
+    for power in (10, 13) if dtype is HF else (10, 15, 17):
+        size = 2.0 ** power
+        for both in (False, True):
+            cache = make_cache([n], T, 16, Hkv, D, dtype, seed=7)
+            cache.k.zero_()
+            pos = torch.arange(n, device="cuda")
+            page, row = cache.page_table[0].long()[pos // 16], pos % 16
+            level = pick.clone()
+            level[at[0]], level[at[1]] = 64, 64 if both else 63       # 63 and fewer: at least a 128th less
+            cache.k[0, page, 0, row, 0] = (sign * size * (1 + sign * level.cuda() / 128)).to(dtype)
+            last = cache.page_table[0].long()[(n + torch.arange(T, device="cuda")) // 16]
+            cache.k[0, last, 0, (n + torch.arange(T, device="cuda")) % 16, 0] = float(sign * size)      # the new tokens: level 0
+            q = torch.zeros((1, T, H, D), dtype=dtype, device="cuda")
+            q[..., 0] = size
+            print("scores", (T, H, D, n), sign, dtype, power, both, flush=True)
+            lse = torch.zeros((1, T, H), device="cuda")
+            got = cache.attention(0, q, scale=1.0, lse=lse)
+            v = [cache.v[0, page[i], 0, row[i]].double() for i in at]
+            want = (v[0] + v[1]) / 2 if both else v[0]
+            u = torch.finfo(dtype).eps / 2
+            assert bool(((got.double() - want).abs() <= u * want.abs() + 2.0 ** -22 * (v[0].abs() + v[1].abs())).all())
+            top = float(cache.k[0, page[at[0]], 0, row[at[0]], 0]) * float(q[0, 0, 0, 0])
+            assert bool(((lse.double() - top).abs() <= 1 + 2.0 ** -22 * abs(top)).all())
+
+
 def test_refusals():
     from paper_2502_13652_amd import PagedCache
     from paper_2502_13652_amd.binding import C2TError
