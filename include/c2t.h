@@ -328,7 +328,7 @@ int c2t_cache_fork(const c2t_cache* cache, const int32_t* src, const int32_t* ds
 typedef struct {
   const void* q;               /* [device] [batch][tokens][q_heads][head_dim] of the cache's dtype, 16-byte aligned */
   int64_t q_batch_stride, q_token_stride;
-  void* out;                   /* [device] the same shape; rows t >= n_new[b] are left as they are; not q */
+  void* out;                   /* [device] the same shape, each row in a place of its own; rows t >= n_new[b] are left as they are; not q */
   int64_t out_batch_stride, out_token_stride;
   float* lse;                  /* [device] [batch][tokens][q_heads]: log of the sum of e^score, -inf for a row that sees nothing; or NULL */
   const int32_t* n_new;        /* [device] [batch], NULL: all `tokens`; cut to 0 .. tokens and to what page_table has room for */

@@ -250,6 +250,7 @@ int c2t_cache_attention(const c2t_cache* c, const c2t_attention* a, void* ws, si
   for (int64_t stride : {a->q_token_stride, a->q_batch_stride, a->out_token_stride, a->out_batch_stride}) if (stride > MAX_STRIDE) return C2T_ERR_UNSUPPORTED;
   if (!aligned16(a->q) || !aligned16(a->out) || a->q_batch_stride % 8 || a->q_token_stride % 8 || a->out_batch_stride % 8 || a->out_token_stride % 8)
     return C2T_ERR_UNSUPPORTED;
+  if (c->batch > 1 && a->out_batch_stride < row) return C2T_ERR_INVALID_ARG;       // one row in the place of several
   if (!ws || (uintptr_t)ws % 256 != 0 || bytes < p.total) return C2T_ERR_WORKSPACE;
   AttendArgs g;
   g.q = (const char*)a->q; g.out = (char*)a->out; g.lse = a->lse;

@@ -99,6 +99,19 @@ def test_attention_is_refused(lib):
     assert lib.c2t_cache_attention(None, ctypes.byref(attention()), FAKE, need.value, None) == -1 and lib.c2t_cache_attention(c, None, FAKE, need.value, None) == -1
 
 
+def test_outputs_in_one_place_are_refused(lib):
+    need = ctypes.c_size_t()
+    c, one = cache(), cache(batch=1)
+    assert lib.c2t_attention_workspace_bytes(ctypes.byref(c), ctypes.byref(attention()), ctypes.byref(need)) == 0
+    call = lambda c, **kw: lib.c2t_cache_attention(ctypes.byref(c), ctypes.byref(attention(**kw)), FAKE, need.value, None)
+    for stride in (0, 8, 248):                               # sequences' rows on top of each other
+        assert call(c, out_batch_stride=stride) == -1
+    launched = (0, -5)                                       # (without a GPU a launch fails)
+    import torch
+    if not torch.cuda.is_available():
+        assert call(one, out_batch_stride=0) in launched and call(c, out_batch_stride=256, out_token_stride=512) in launched and call(c, q_batch_stride=0) in launched
+
+
 def test_adjustments_are_refused(lib):
     def call(t=None, batch=2, vocab=1000, nodes=4, dtype=1, tokens=FAKE, parent=FAKE, n_nodes=FAKE, logits=FAKE, stride=1000, out=FAKE, out_stride=1000):
         return lib.c2t_adjust_tree_logits(ctypes.byref(adjustments(**(t or {}))), batch, vocab, nodes, dtype, tokens, parent, n_nodes, logits, stride, out, out_stride, None)
