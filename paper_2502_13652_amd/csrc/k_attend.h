@@ -156,8 +156,12 @@ __device__ __forceinline__ void put_row(const CacheView& c, const AttendArgs& a,
 #pragma unroll
   for (int r = 0; r < 4; ++r) y[r] = (typename E::T)(x[r] * inv);
   *(typename E::T4*)(a.out + u.b * a.out_batch + t * a.out_token + (query_offset(u.head, a.shape.group, g, D) + dim) * 2) = y;
-  if (dim == 0 && a.lse)
-    a.lse[((int64_t)u.b * a.shape.slots + t) * c.kv_heads * a.shape.group + query_offset(u.head, a.shape.group, g, 1)] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(e)) * 0.69314718055994531f;
+  if (dim == 0 && a.lse) {
+    // of a sum as if the reference were the largest score: the log's own rounding is then of its size, not of the distance between the two
+    constexpr float BELOW = E::TOP - E::SLACK;
+    constexpr float UNIT = BELOW < 0.f ? (float)(1 << (int)-BELOW) : 1.f / (float)(1 << (int)BELOW);     // 2^-BELOW
+        a.lse[((int64_t)u.b * a.shape.slots + t) * c.kv_heads * a.shape.group + query_offset(u.head, a.shape.group, g, 1)] = l == 0.f ? -INFINITY : ((m + BELOW) + __builtin_amdgcn_logf(e * UNIT)) * 0.69314718055994531f;
+  }
 }
 // running join of parts
 struct Joined {

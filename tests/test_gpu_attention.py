@@ -498,6 +498,18 @@ def test_scores_of_any_size(T, H, Hkv, D, n, sign, dtype):
             assert bool(((lse.double() - top).abs() <= 1 + 2.0 ** -22 * abs(top)).all())
 
 
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("H,T,D", [(4, 1, 128), (3, 20, 64), (2, 70, 128), (2, 5, 256)])
+def test_the_log_of_a_number_of_equal_weights(H, T, D, dtype):
+    """Scores of 0: the sum of n weights is exact, and what is left is the logarithm's step (2^-23 relative), its product's with log 2 and that constant's, 2^-24 each."""
+    lens = [0, 1, 2, 4, 6, 10, 30, 99, 700]
+    cache = make_cache(lens, T, 16, 1, D, dtype, seed=3)
+    lse = torch.zeros((len(lens), T, H), device="cuda")
+    cache.attention(0, torch.zeros((len(lens), T, H, D), dtype=dtype, device="cuda"), lse=lse)
+    want = torch.log(torch.tensor(lens, device="cuda").double()[:, None] + 1 + torch.arange(T, device="cuda"))[:, :, None]
+    assert bool(((lse.double() - want).abs() <= 2.0 ** -22 * want).all()), float(((lse.double() - want).abs() - 2.0 ** -22 * want).max())
+
+
 def test_refusals():
     from paper_2502_13652_amd import PagedCache
     from paper_2502_13652_amd.binding import C2TError
