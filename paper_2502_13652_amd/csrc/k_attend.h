@@ -4,9 +4,9 @@
 //
 // One pass over the keys: a wavefront keeps, for every row it has, a reference m that follows the running maximum (of s log2 e), the sum l of p and
 // sum p v, and multiplies the last two by 2^(m_old - m_new) where a tile raises m.  A row that sees no key has m = -inf, l = 0
-// and is put out as zeros.  l is the sum of the weights as the second product takes them, rounded to 16 bits, so that a row of few or of sharp
-// weights keeps a mean of its values: what one weight's rounding adds to the product it adds to the divisor.  Where the log of the sum is asked for,
-// the weights as they were are summed too, for that alone.
+// and is put out as zeros.  Where the second product takes weights rounded to 16 bits, l is their sum as rounded, so that a row of few or of sharp
+// weights keeps a mean of its values: what one weight's rounding adds to the product it adds to the divisor.  If the log of the sum is asked for,
+// the weights as they were are then summed too, for that alone.
 //
 // Rows: the query heads of one cached head share its keys, so rows are (slot, head of the group) with the head
 // fastest.  Products are taken transposed: S^T = K Q^T leaves in a lane one row (lane & 15) and 4 neighbouring keys of each
@@ -160,7 +160,7 @@ __device__ __forceinline__ void put_row(const CacheView& c, const AttendArgs& a,
     // of a sum as if the reference were the largest score: the log's own rounding is then of its size, not of the distance between the two
     constexpr float BELOW = E::TOP - E::SLACK;
     constexpr float UNIT = BELOW < 0.f ? (float)(1 << (int)-BELOW) : 1.f / (float)(1 << (int)BELOW);     // 2^-BELOW
-        a.lse[((int64_t)u.b * a.shape.slots + t) * c.kv_heads * a.shape.group + query_offset(u.head, a.shape.group, g, 1)] = l == 0.f ? -INFINITY : ((m + BELOW) + __builtin_amdgcn_logf(e * UNIT)) * 0.69314718055994531f;
+    a.lse[((int64_t)u.b * a.shape.slots + t) * c.kv_heads * a.shape.group + query_offset(u.head, a.shape.group, g, 1)] = l == 0.f ? -INFINITY : ((m + BELOW) + __builtin_amdgcn_logf(e * UNIT)) * 0.69314718055994531f;
   }
 }
 // running join of parts
@@ -212,6 +212,11 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
   constexpr int ROWS_A_LOAD = SHARERS / CH;
   static_assert(ROWS_A_LOAD <= 16 ? 16 % ROWS_A_LOAD == 0 : ROWS_A_LOAD % 16 == 0, "");
   constexpr bool K_LDS = RW > 1;
+  // A weight as the second product takes it: one number of 16 bits, off by 2^-8 of it at most (2^-11 for halves that are not subnormal), or a second one for what the first leaves,
+  // off by 2^-16 (2^-22).  Where the keys' bytes bound the kernel the second costs nothing (64 tokens 200 us with and without, one 9.6 and 9.8) and the output is as exact as its type; elsewhere it
+  // costs the 64 trees 261 us for 200, the two chunks 640 for 472 and tiles of 64 rows 1 to 12 %, and is left out: of Gaussian keys and values outputs are then off by 0.0022 of their size
+  // (rms, of bf16; 0.0017 of it are their own rounding, of halves 0.00027 and 0.00021).
+  constexpr bool PAIRS = KW > 1;
   constexpr int TILE_BYTES = KT * L::V_ROW + (K_LDS ? KT * L::K_ROW : 0);
   constexpr int JOIN_BYTES = KW > 1 ? KW * 16 * (D + 3) * 4 : 0;
   constexpr int BUFFERS = RW > 1 ? 2 : KW;                  // of the tile: the next one's while this one is used, or one a wavefront
@@ -475,7 +480,7 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
           for (int kb = 0; kb < KB; ++kb) s[m][kb] *= a.scale_log2e;
       }
 
-      T8 p[MT][KB / 2];
+      T8 p[MT][KB / 2], rest[PAIRS ? MT : 1][PAIRS ? KB / 2 : 1];
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
         float top = -INFINITY;
@@ -503,7 +508,6 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
           for (int d = 0; d < DB; ++d) o[m][d] *= back;
         }
         const float ref = m_run[m] == -INFINITY ? 0.f : m_run[m];
-        // P in the operands' 16 bits: relative 2^-8 (2^-11 for halves that are not subnormal) a weight at most, of either sign
 #pragma unroll
         for (int h = 0; h < KB / 2; ++h) {
 #pragma unroll
@@ -511,9 +515,10 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
             const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[m][h * 2 + r / 4][r % 4], factor, -ref));
             s[m][h * 2 + r / 4][r % 4] = w;
             p[m][h][r] = (T)w;
+            if (PAIRS) rest[PAIRS ? m : 0][PAIRS ? h : 0][r] = (T)(w - (float)p[m][h][r]);
           }
         }
-        if (a.lse) {
+        if (PAIRS || a.lse) {
           f32x4 all = s[m][0];
 #pragma unroll
           for (int kb = 1; kb < KB; ++kb) all += s[m][kb];
@@ -523,14 +528,16 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
       // The rounded weights' sum is a product with ones: the matrix unit has time for it.  The two chunks, with `lse`, 479 us, with additions of pairs 484, with the
       // sum of the weights as they were for divisor 468; the 64 trees 232, 235 and 237.
       f32x4 sum[MT];
+      if constexpr (!PAIRS) {
 #pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        T8 ones;
+        for (int m = 0; m < MT; ++m) {
+          T8 ones;
 #pragma unroll
-        for (int r = 0; r < 8; ++r) ones[r] = (T)1.f;
-        sum[m] = f32x4{0.f, 0.f, 0.f, 0.f};
+          for (int r = 0; r < 8; ++r) ones[r] = (T)1.f;
+          sum[m] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int h = 0; h < KB / 2; ++h) sum[m] = E::mfma(ones, p[m][h], sum[m]);
+          for (int h = 0; h < KB / 2; ++h) sum[m] = E::mfma(ones, p[m][h], sum[m]);
+        }
       }
 #pragma unroll
       for (int h = 0; h < KB / 2; ++h) {
@@ -544,11 +551,16 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
           struct { s16x4 a, b; } pair{lo, hi};
           const T8 v = __builtin_bit_cast(T8, pair);
 #pragma unroll
-          for (int m = 0; m < MT; ++m) o[m][d] = E::mfma(v, p[m][h], o[m][d]);
+          for (int m = 0; m < MT; ++m) {
+            o[m][d] = E::mfma(v, p[m][h], o[m][d]);
+            if (PAIRS) o[m][d] = E::mfma(v, rest[PAIRS ? m : 0][PAIRS ? h : 0], o[m][d]);
+          }
         }
       }
+      if constexpr (!PAIRS) {
 #pragma unroll
-      for (int m = 0; m < MT; ++m) l_run[m] += sum[m][0];
+        for (int m = 0; m < MT; ++m) l_run[m] += sum[m][0];
+      }
     }
     if (RW > 1) {
       if (tile + 1 < tile_end) {
@@ -564,6 +576,7 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
     e_run[m] += __shfl_xor(e_run[m], 16); e_run[m] += __shfl_xor(e_run[m], 32);
+    if (PAIRS) l_run[m] = e_run[m];
 #pragma unroll
     for (int d = 0; d < DB; ++d) settle(o[m][d]);
   }

@@ -510,6 +510,22 @@ def test_the_log_of_a_number_of_equal_weights(H, T, D, dtype):
     assert bool(((lse.double() - want).abs() <= 2.0 ** -22 * want).all()), float(((lse.double() - want).abs() - 2.0 ** -22 * want).max())
 
 
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("B,T,H,Hkv,D", [(7, 1, 8, 2, 128), (7, 1, 8, 8, 64), (7, 3, 16, 4, 128), (7, 5, 6, 2, 64)])
+def test_few_rows_are_as_exact_as_their_type(B, T, H, Hkv, D, dtype):
+    """Rows that share a tile of 16: their weights are taken as two numbers of 16 bits, which a weight differs from by 2^-16 of it at most (each leaves half a step, 2^-8 or less).  Values that are positive, so
+    that the sum of weighted sizes is the output itself; but for that difference the tolerance is attention_reference's without its term for weights of one such number."""
+    lens = [0, 1, 2, 5, 40, 300, 3000][:B]
+    cache = make_cache(lens, T, 16, Hkv, D, dtype, seed=D + T)
+    cache.v.copy_((cache.v.float().abs() * 3 + 0.01).to(dtype))
+    q = queries(B, T, H, D, dtype, T)
+    got = cache.attention(0, q)
+    want, _, tol, _ = attention_reference(cache, 0, q, [T] * B, None, D ** -0.5)
+    u = torch.finfo(dtype).eps / 2
+    tol = tol - want * u * (1 + u) + want * 2.0 ** -16
+    assert float(((got.double() - want).abs() - tol).max()) <= 0
+
+
 def test_refusals():
     from paper_2502_13652_amd import PagedCache
     from paper_2502_13652_amd.binding import C2TError
