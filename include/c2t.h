@@ -233,7 +233,8 @@ int c2t_stream_read_rows(const void* dev_ptr, int32_t rows, size_t row_bytes, si
  * c2t_cache_attention with the tree's mask), c2t_adjust_tree_logits on its logits, the caller's acceptance, and
  * c2t_cache_commit of the accepted path.  Lengths, tables and counts stay on the device, and the calls check them there:
  * whatever these arrays hold, no call reads or writes outside the buffers that it is given.  The calls
- * below keep nothing on the host, so they may be made from several threads; calls that change one cache belong on one stream. */
+ * below keep nothing on the host, so they may be made from several threads; calls that change one cache belong on one stream.  Some enqueue two kernels:
+ * two threads do not make calls of one workspace, or calls that change one cache, at the same time. */
 
 /* What is done to a token's logit x.  a: how often the token occurs in the sequence's context and on the path from the root to
  * the row's node, the node included; o: the same without the prompt.  In fp32, rounded once to the logits' type at the end:

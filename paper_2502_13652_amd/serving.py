@@ -3,6 +3,7 @@ include/c2t.h).  Argument marshalling and checks only; like the binding it needs
 import ctypes
 import dataclasses
 import struct
+import threading
 from typing import Optional
 
 import torch
@@ -184,7 +185,7 @@ class PagedCache:
     """A paged K/V cache (c2t_cache): tensors k, v [layers][pages][kv_heads][page_size][head_dim], page_table int32 [B][max_pages] (-1: no
     page), length int32 [B], refcount int32 [pages], status uint32 [B] (POOL_EMPTY, ROW_FULL, INVALID, SHARED; set by calls, cleared by the
     user).  All calls are enqueued on torch's current stream (or `stream`) and answer on the device alone.  Calls on one cache belong on one
-    stream; attention alone may run on several (each stream has a workspace of its own)."""
+    stream; attention alone may run on several (each stream has a workspace of its own).  Several threads may make them: each is enqueued whole."""
     POOL_EMPTY, ROW_FULL, INVALID, SHARED = 1, 2, 4, 8
 
     def __init__(self, batch, layers, pages, page_size, kv_heads, head_dim, max_pages, dtype=torch.bfloat16, device="cuda:0"):
@@ -219,6 +220,7 @@ class PagedCache:
                          self.status.data_ptr())
         self._ref = ctypes.byref(self._c)
         self._each, self._scale = (batch,), head_dim ** -0.5
+        self._launching = threading.Lock()                   # a call's launches share a workspace: no other call's come between them on the stream
         need = ctypes.c_size_t()
         _check(self.L.c2t_cache_workspace_bytes(self._ref, ctypes.byref(need)), "c2t_cache_workspace_bytes")
         self._ws = self._workspace(need.value)
@@ -231,7 +233,8 @@ class PagedCache:
         return w[pad:pad + nbytes]
 
     def _run(self, what, stream, *args):
-        rc = _launch(self.device, stream, getattr(self.L, what), self._ref, *args)
+        with self._launching:
+            rc = _launch(self.device, stream, getattr(self.L, what), self._ref, *args)
         if rc != 0:
             raise binding.C2TError(rc, what)
 
@@ -303,7 +306,8 @@ class PagedCache:
         need = self._attention_bytes.get((T, heads, nodes))
         if need is None:
             need = self._attention_bytes[(T, heads, nodes)] = self.attention_workspace_bytes(T, heads, nodes)
-        rc = _launch(self.device, stream, self._attend, a, workspace, need)
+        with self._launching:
+            rc = _launch(self.device, stream, self._attend, a, workspace, need)
         if rc != 0:
             raise binding.C2TError(rc, "c2t_cache_attention")
         return out

@@ -141,6 +141,45 @@ def test_adjustments_are_refused(lib):
     lib.c2t_destroy(ctx)
 
 
+def test_two_threads_do_not_enqueue_between_each_others_kernels(monkeypatch):
+    """A call of two kernels that share a workspace is enqueued whole, whichever thread makes it."""
+    import threading
+    import time
+    import types
+
+    import torch
+    from paper_2502_13652_amd import PagedCache, serving
+    inside, met = [], []
+
+    def enqueue(*args):                                      # as ctypes does, it lets other threads run
+        inside.append(args)
+        time.sleep(0.002)
+        met.append(len(inside))
+        inside.pop()
+        return 0
+    monkeypatch.setattr(serving, "_launch", lambda device, stream, fn, *args: fn(*args))
+    c = PagedCache.__new__(PagedCache)
+    monkeypatch.setattr(serving, "load_library", lambda: types.SimpleNamespace(
+        c2t_cache_workspace_bytes=lambda *a: 0, c2t_cache_truncate=enqueue, c2t_cache_attention=enqueue, c2t_attention_workspace_bytes=lambda *a: 0))
+    monkeypatch.setattr(serving, "_whole", lambda *a: FAKE)
+    monkeypatch.setattr(PagedCache, "_attention_workspace", lambda self, s, need: torch.zeros(1, dtype=torch.uint8))
+    on_gpu = types.SimpleNamespace(is_cuda=True, dim=lambda: 5, dtype=torch.bfloat16, device=torch.device("cpu"), shape=(1, 4, 1, 16, 64))
+    c._take(on_gpu, on_gpu, torch.zeros((2, 2), dtype=torch.int32), None, None)
+    q = torch.zeros((2, 1, 1, 64), dtype=torch.bfloat16)
+
+    def some(call):
+        for _ in range(10):
+            call()
+    attend = lambda: c.attention(0, q, out=q)
+    monkeypatch.setattr(PagedCache, "_attend", lambda self, a, workspace, need, *s: enqueue())
+    threads = [threading.Thread(target=some, args=(f,)) for f in (attend, attend, c.truncate, c.truncate)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert len(met) == 40 and set(met) == {1}
+
+
 def test_without_a_gpu_nothing_is_computed():
     import torch
     from paper_2502_13652_amd import PagedCache
