@@ -312,7 +312,7 @@ int c2t_cache_reserve(const c2t_cache* cache, const int32_t* n_new, void* dev_wo
 int c2t_cache_write(const c2t_cache* cache, int32_t layer, const void* k, const void* v, int64_t batch_stride, int64_t token_stride, int32_t tokens,
                     const int32_t* n_new, void* stream);
 
-/* The accepted path: path [device] [batch][path_stride], n_path [batch]: the tokens at length[b] + path[b][i] move to length[b] + i in all
+/* The accepted path: path [device] [batch][path_stride], n_path [batch] (cut to 0 .. path_stride): the tokens at length[b] + path[b][i] move to length[b] + i in all
  * layers, i < n_path[b], and length[b] grows by n_path[b].  A path rises strictly from 0 or more (slots of a root and its nodes in
  * breadth-first order do); of one that does not, or that leaves the reserved pages, nothing is moved. */
 int c2t_cache_commit(const c2t_cache* cache, const int32_t* path, int32_t path_stride, const int32_t* n_path, void* stream);
@@ -344,7 +344,8 @@ typedef struct {
 /* Every slot sees the length[b] tokens before; a chain slot the chain up to itself; node i the whole chain and the nodes j with mask[b][i][j] != 0
  * (j < n_new[b] - chain).  A key that a row does not see has no influence on it, whatever its bits.  A row that sees no key gets zeros.
  * Keys below length[b] + n_new[b] on no page of the pool are left out, and the sequence's status says so, as it does where n_new was cut for want of room.
- * Products in the cache's dtype, sums and the softmax in fp32.  The workspace is [device], 256-byte aligned, its size from the call's sizes
+ * Products in the cache's dtype, sums and the softmax in fp32.  Of the softmax the second product takes its weights rounded to that dtype, once, or, where a cached head has 16 rows or
+ * fewer (32 with few sequences; width 256 aside), with what the rounding left as a second number; lse is that of the weights as they were.  The workspace is [device], 256-byte aligned, its size from the call's sizes
  * alone.  Its first C2T_ATTENTION_COUNTERS bytes are zero-filled by the caller before its first use, on the stream that uses it or one that it waits
  * for, and are zero again after each call.  Calls that may run at the same time need one each, others may share the largest. */
 #define C2T_ATTENTION_COUNTERS 8192

@@ -17,9 +17,9 @@
 // its own, K straight into the matrix operands, V through LDS for its transposition only.  64 single tokens of 300 to 8000 cached tokens, 32 heads
 // over 8: 201 us for 1.09 GB of K and V, 5.4 TB/s; a kernel that only reads rows gets 6.4.  More rows: the matrix products and the weights' exponentials
 // bound it, so the wavefronts share K and V tiles in LDS, two of them in turn, the next one's loads on their way while a tile is used.  Two
-// chunks of 2048 behind 9000 and 31000 tokens, 64 wide: 464 us for 353 GFLOP, 0.76 PFLOP/s; vector instructions are issued for 60 % of that time and the
-// matrix unit works for 35 %: the two hardly overlap.  64 trees of 65 behind 100 to 4000 tokens: 204 to 238 us for 116 GFLOP, up to 0.57 PFLOP/s; of 260 rows a head
-// the last four take a third pass.  One token behind 701: 9.7 us, of which 8 are the launch, the item's search and the join of its parts.
+// chunks of 2048 behind 9000 and 31000 tokens, 64 wide, with the log of the sums: 470 to 488 us for 353 GFLOP, 0.75 PFLOP/s; vector instructions but the matrix unit's are issued for
+// 55 % of that time and the matrix unit works for 38 %: the two hardly overlap.  64 trees of 65 behind 100 to 4000 tokens: 200 to 232 us for 116 GFLOP, up to 0.58 PFLOP/s; of 260 rows a
+// head the last four take a third pass.  One token behind 701: 9.9 us, of which 8 are the launch, the item's search and the join of its parts.
 #pragma once
 #include "k_common.h"
 #include "k_paged.h"
@@ -64,7 +64,8 @@ struct Unit { int b, len, n_new, row_tile, head, part, parts, slot0; };   // slo
 
 // Deals a workgroup its item.  Every wavefront computes it for itself, each lane summing a stretch of sequences: no barrier.  Where
 // each lane has one sequence at most, the longest go first: workgroups start in about this order, and none that starts last is long.  It costs
-// 8 to 12 us of a launch of 64 sequences; a launch of its own that left a list would cost a launch.
+// 8 to 12 us of a launch of 64 sequences; a launch of its own that left a list would cost a launch.  Past 64 a lane reads its sequences one after the other, twice, and items come
+// in no order: 512 tokens behind 300 to 2000 take 438 us for bytes of 500, but 4096 behind 30 to 300 2.8 ms for 0.6, most of it the search (behind one token each 2.5 ms).
 // False: there is no item for it.
 __device__ __forceinline__ bool find_item(const CacheView& c, const AttendArgs& a, int workgroup, Unit* u) {
   const int lane = lane_id(), each = div_up(c.batch, WAVE), b0 = min(lane * each, c.batch), b1 = min(b0 + each, c.batch);

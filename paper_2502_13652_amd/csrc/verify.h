@@ -86,7 +86,8 @@ inline int attend_plan(const c2t_cache& c, const c2t_attention& a, AttendPlan* p
   p->shape.rows_shift = 4 + p->build;
   p->shape.keys_shift = by_keys || c.head_dim > 128 ? 5 : 6;
   p->units = (int64_t)c.batch * c.kv_heads * row_tiles(p->shape, a.tokens);
-  // Parts: enough to fill the chip once, two workgroups a CU, since parts and their records cost more than what an even end saves: a chunk of 2048 466 us,
+  // Parts: enough for two workgroups a CU (as many are resident of the builds of width 128; of width 64 two to four, of width 256 one or two: one number serves
+  // them all), since parts and their records cost more than what an even end saves: a chunk of 2048 466 us,
   // with twice the parts 514; 64 trees of 65 205 and 244; one token behind 32000 32 and 43.  Many units of few rows go twice round: 64 tokens of 300
   // to 8000 keys 202 us, with half of the parts 223; 32 tokens behind 4000 the other way, 105 and 100.
   p->shape.target_shift = by_keys && p->units >= 512 ? MAX_TARGET_SHIFT : MAX_TARGET_SHIFT - 1;

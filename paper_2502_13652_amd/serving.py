@@ -145,7 +145,7 @@ def _rows(x, B, rows, V, name):
 def adjust_tree_logits(logits, tree, adjustments, vocab=None, out=None, stream=None):
     """The target model's logits [B][1 + N][stride >= vocab] (float32 or bfloat16) of a tree's root and nodes with `adjustments` (a
     LogitAdjustments) made, into `out` (a new tensor; may be `logits`).  tree: a finalize_tree output (tokens, parent, n_nodes), or None for one
-    row a sequence.  Rows behind a sequence's nodes, and what is behind `vocab` (default: all), are left as they are."""
+    row a sequence.  Rows behind a sequence's nodes, and what is behind `vocab` (default: all), are left as they are; in a new tensor they are not filled in."""
     L = load_library()
     B, rows, width = logits.shape
     V = width if vocab is None else int(vocab)
@@ -283,8 +283,8 @@ class PagedCache:
         q [B][T][q_heads][head_dim]; mask uint8 [B][N][N] as finalize_tree writes it: the last N of the T slots are the tree's nodes, those
         before them (the root) a causal chain; no mask: all of them are.  Keys on no page are left out and set INVALID in the sequence's status, new
         tokens that its row of page_table has no room for are left out and set ROW_FULL.  scale: of the scores, default head_dim ** -0.5.  lse: float32
-        [B][T][q_heads] for the log of the softmax's sums.  out: [B][T][q_heads][head_dim] (default: a new tensor), rows behind n_new left as
-        they are.  workspace: uint8, zeros, of attention_workspace_bytes and 256-byte aligned, for calls that run at once otherwise than by stream.
+        [B][T][q_heads] for the log of the softmax's sums.  out: [B][T][q_heads][head_dim], rows behind n_new left as
+        they are (default: a new tensor, in which they are not filled in: they hold whatever the memory held).  workspace: uint8, zeros, of attention_workspace_bytes and 256-byte aligned, for calls that run at once otherwise than by stream.
         Without one the cache keeps one a stream, and in a graph's capture one that is the graph's: from its pool, counters cleared at each replay."""
         _need(q.dim() == 4, "q: [B][T][q_heads][head_dim]")
         _, T, heads, _ = q.shape
