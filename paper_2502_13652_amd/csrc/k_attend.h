@@ -214,7 +214,7 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
   static_assert(ROWS_A_LOAD <= 16 ? 16 % ROWS_A_LOAD == 0 : ROWS_A_LOAD % 16 == 0, "");
   constexpr bool K_LDS = RW > 1;
   // A weight as the second product takes it: one number of 16 bits, off by 2^-8 of it at most (2^-11 for halves that are not subnormal), or a second one for what the first leaves,
-  // off by 2^-16 (2^-22).  Where the keys' bytes bound the kernel the second costs nothing (64 tokens 200 us with and without, one 9.6 and 9.8) and the output is as exact as its type; elsewhere it
+  // off by 2^-16 (2^-22).  Where the keys' bytes bound the kernel the second costs next to nothing (64 tokens 200 us with and without, one 9.9 and 9.7) and the output is as exact as its type; elsewhere it
   // costs the 64 trees 261 us for 200, the two chunks 640 for 472 and tiles of 64 rows 1 to 12 %, and is left out: of Gaussian keys and values outputs are then off by 0.0022 of their size
   // (rms, of bf16; 0.0017 of it are their own rounding, of halves 0.00027 and 0.00021).
   constexpr bool PAIRS = KW > 1;
@@ -284,7 +284,7 @@ __global__ __launch_bounds__(64 * RW * KW, OCC) void k_attend(CacheView c, Atten
   }
 
   f32x4 o[MT][DB];
-  float m_run[MT], l_run[MT], e_run[MT];                     // sums of weights: rounded ones of the row, and with `lse` this lane's keys' as they were
+  float m_run[MT], l_run[MT], e_run[MT];                     // sums of weights: rounded ones of the row, and this lane's keys' as they were (with PAIRS or `lse`)
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
     m_run[m] = -INFINITY; l_run[m] = 0.f; e_run[m] = 0.f;
