@@ -17,7 +17,7 @@
 // its own, K straight into the matrix operands, V through LDS for its transposition only.  64 single tokens of 300 to 8000 cached tokens, 32 heads
 // over 8: 201 us for 1.09 GB of K and V, 5.4 TB/s; a kernel that only reads rows gets 6.4.  More rows: the matrix products and the weights' exponentials
 // bound it, so the wavefronts share K and V tiles in LDS, two of them in turn, the next one's loads on their way while a tile is used.  Two
-// chunks of 2048 behind 9000 and 31000 tokens, 64 wide, with the log of the sums: 470 to 488 us for 353 GFLOP, 0.75 PFLOP/s; vector instructions but the matrix unit's are issued for
+// chunks of 2048 behind 9000 and 31000 tokens, 64 wide, with the log of the sums: 465 to 488 us for 353 GFLOP, up to 0.76 PFLOP/s; vector instructions but the matrix unit's are issued for
 // 55 % of that time and the matrix unit works for 38 %: the two hardly overlap.  64 trees of 65 behind 100 to 4000 tokens: 200 to 232 us for 116 GFLOP, up to 0.58 PFLOP/s; of 260 rows a
 // head the last four take a third pass.  One token behind 701: 9.9 us, of which 8 are the launch, the item's search and the join of its parts.
 #pragma once
