@@ -46,7 +46,7 @@ extern "C" {
 
 typedef struct c2t_ctx c2t_ctx; /* opaque, host memory */
 
-enum { C2T_F32 = 0, C2T_BF16 = 1, C2T_F16 = 2 /* the paged cache and its attention only */ };
+enum { C2T_F32 = 0, C2T_BF16 = 1, C2T_F16 = 2 /* the paged cache and a layer's operators only */, C2T_E4M3 = 3 /* 8-bit outputs of c2t_rms_norm only */ };
 
 enum {
   C2T_OK = 0,
@@ -351,6 +351,79 @@ typedef struct {
 #define C2T_ATTENTION_COUNTERS 8192
 int c2t_attention_workspace_bytes(const c2t_cache* cache, const c2t_attention* attention, size_t* out);
 int c2t_cache_attention(const c2t_cache* cache, const c2t_attention* attention, void* dev_workspace, size_t workspace_bytes, void* stream);
+
+/* ---- A layer's other operators: norm, rotation on the way into the cache, attention over prompts ----------
+ *
+ * What a layer of the target model does on either side of c2t_cache_write and c2t_cache_attention.  All are enqueued on the stream, one kernel each, take no
+ * workspace and keep nothing. */
+
+/* Root-mean-square norm, with the residual's addition ahead of it: h = x + residual in fp32, residual_out = h rounded to its type,
+ * y = h / sqrt(mean(h^2) + eps) * weight of h as it was ahead of that rounding; out = y rounded to its type.  The mean is summed in 64 bits, so values
+ * of any size have their norm.  In C2T_E4M3, out = y / scale of the row's block of scale_block elements (the last one may be shorter),
+ * scale = max |y| of the block / 448, 1 where all are 0, and 2^-126 at least; a NaN stays one and counts for no maximum.
+ * Any width, strides and alignment of whole elements do; width and strides of multiples of 8 elements and 16-byte aligned arrays are faster. */
+typedef struct {
+  const void* x;               /* [device] [rows][width] of `dtype`; rows x_stride elements apart, as those of the others by theirs */
+  const void* weight;          /* [device] [width] of weight_dtype */
+  const void* residual;        /* [device] [rows][width] of residual_dtype, or NULL (then residual_out is NULL too) */
+  void* residual_out;          /* may be residual (same stride), or x (same stride and type) */
+  void* out;                   /* may be x (same stride and type); otherwise the arrays written do not overlap any other */
+  float* scales;               /* [device] [rows][ceil(width / scale_block)] with an out of C2T_E4M3, else NULL */
+  int64_t x_stride, residual_stride, residual_out_stride, out_stride, scales_stride;
+  int32_t rows, width;         /* width at most C2T_MAX_NORM_WIDTH */
+  int32_t dtype;               /* C2T_F32, C2T_BF16 or C2T_F16 */
+  int32_t weight_dtype, residual_dtype;        /* dtype or C2T_F32 */
+  int32_t out_dtype;           /* dtype or C2T_E4M3 */
+  int32_t scale_block;         /* 32, 64, 128 or width; 0 without scales */
+  float eps;                   /* above 0 */
+} c2t_norm;
+#define C2T_MAX_NORM_WIDTH 65536
+int c2t_rms_norm(const c2t_norm* norm, void* stream);
+
+/* Queries and keys of new tokens turned by their positions, keys and values into the pages of one layer (what c2t_cache_write does with keys that are turned already).
+ * Of each head's row the first 2 * pairs elements are turned: pair j is (a, b) -> magnitude (a cos - b sin, a sin + b cos), its angle position * turns[j] 2^-64
+ * of a full turn (whole numbers, so that a far position is as exact as a near one), rounded once.  Pair j is elements j and pairs + j, or 2j and 2j + 1.
+ *
+ * Tokens: slots t < n_new[b] of [batch][tokens], or, with `starts`, packed: [tokens] rows of which starts[b] .. starts[b + 1] - 1 are sequence b's, t from 0 on; rows
+ * in no sequence are left as they are.  Token t goes to place length[b] + t of the cache; the length stays.  Its position is that number, but
+ * for the last `nodes` slots of [batch][tokens], a tree's: node i is at length[b] + tokens - nodes - 1 + position[b][i] (as c2t_finalize_tree counts
+ * from the root, the slot ahead of the nodes).  What the cache has no room or page for is left out of it alone, and the status says so. */
+typedef struct {
+  const void* q;               /* [device] [batch][tokens][q_heads][head_dim] of the cache's dtype; strides in elements, multiples of 8, heads next to each other */
+  const void* k;               /* [device] [batch][tokens][kv_heads][head_dim], as v */
+  const void* v;
+  void* q_out;                 /* [device] as q, each row in a place of its own; may be q (same strides) */
+  void* k_out;                 /* [device] as k, may be k (same strides); or NULL */
+  int64_t q_batch_stride, q_token_stride, kv_batch_stride, kv_token_stride, q_out_batch_stride, q_out_token_stride, k_out_batch_stride, k_out_token_stride;
+  const int32_t* n_new;        /* [device] [batch], NULL: all `tokens`; cut to 0 .. tokens */
+  const int32_t* starts;       /* [device] [batch + 1], not falling; or NULL.  Sequences of which it does not make sense are left out */
+  const int32_t* position;     /* [device] [batch][nodes]; NULL with nodes = 0 */
+  const uint64_t* turns;       /* [device] [pairs] */
+  float magnitude;
+  int32_t tokens, q_heads, layer, nodes;       /* nodes: 0 with starts */
+  int32_t pairs;               /* a multiple of 8, at most head_dim / 2 */
+  int32_t neighbours;          /* 0: elements j and pairs + j; 1: 2j and 2j + 1 */
+} c2t_append;
+int c2t_cache_append(const c2t_cache* cache, const c2t_append* append, void* stream);
+
+/* Causal attention over whole prompts that are packed one behind the other: row i of sequence b sees its rows starts[b] .. i.  Rows in no
+ * sequence are left as they are, and nothing in them, or in rows that come later, has any influence.  Products in `dtype`, sums and the softmax in fp32,
+ * the weights rounded to `dtype` once for the second product; lse is that of the weights as they were. */
+typedef struct {
+  const void* q;               /* [device] [rows][q_heads][head_dim] of `dtype`, 16-byte aligned; strides in elements, multiples of 8, heads next to each other */
+  const void* k;               /* [device] [rows][kv_heads][head_dim] */
+  const void* v;
+  void* out;                   /* [device] as q, each row in a place of its own; not one of the others */
+  float* lse;                  /* [device] [rows][q_heads] log of the sum of e^score, or NULL */
+  int64_t q_stride, k_stride, v_stride, out_stride;    /* from row to row; at most 2^24 */
+  const int32_t* starts;       /* [device] [sequences + 1], not falling, 0 .. rows; sequences of which that is not so are left out */
+  int32_t rows, sequences;     /* sequences: at most C2T_MAX_CACHE_BATCH */
+  int32_t q_heads, kv_heads;   /* head i reads head i / (q_heads / kv_heads) */
+  int32_t head_dim;            /* 64, 128 or 256 */
+  int32_t dtype;               /* C2T_BF16 or C2T_F16 */
+  float scale;                 /* of the scores, usually head_dim^-0.5; 0 or more */
+} c2t_prompt;
+int c2t_prompt_attention(const c2t_prompt* prompt, void* stream);
 
 /* [host] out: a number that tells the captures of graphs apart, of the capture that `stream` is in; 0 outside of one.  For callers that keep a workspace a
  * stream: what a graph was captured with belongs to that graph. */

@@ -13,7 +13,7 @@ _LIB_DIR = os.path.join(_HERE, "lib")
 _LIB = os.path.join(_LIB_DIR, "libc2t_hip.so")
 _lib = None
 
-F32, BF16, F16 = 0, 1, 2
+F32, BF16, F16, E4M3 = 0, 1, 2, 3
 _ERR = {-1: "invalid argument", -2: "unsupported", -3: "workspace", -4: "state", -5: "hip", -6: "out of host memory"}
 
 _PRELOADED = 11                            # the layer kernels' first arguments, which arrive in registers (compared with their list in k_tree.h as it is compiled)
@@ -103,6 +103,9 @@ def load_library(path=None):
     L.c2t_cache_fork.argtypes = [vp, vp, vp, i32, vp]
     L.c2t_attention_workspace_bytes.argtypes = [vp, vp, P(sz)]
     L.c2t_cache_attention.argtypes = [vp, vp, vp, sz, vp]
+    L.c2t_rms_norm.argtypes = [vp, vp]
+    L.c2t_cache_append.argtypes = [vp, vp, vp]
+    L.c2t_prompt_attention.argtypes = [vp, vp]
     L.c2t_stream_capture_id.argtypes = [vp, P(ctypes.c_uint64)]
     L.c2t_strerror.argtypes = [ctypes.c_int]
     L.c2t_strerror.restype = ctypes.c_char_p

@@ -19,6 +19,7 @@
 #include "k_logits.h"
 #include "k_tree.h"
 #include "verify.h"
+#include "layer.h"
 
 using namespace c2t;
 

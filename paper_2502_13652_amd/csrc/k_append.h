@@ -1,0 +1,134 @@
+// Queries and keys turned by their tokens' positions, keys and values into the pages of the paged cache.
+//
+//   (a, b) -> m (a cos p - b sin p, a sin p + b cos p),   p = position * turns 2^-64 of a full turn
+//
+// Angles are whole numbers, 64-bit fractions of a turn, so that position * turns wraps as the angle does and a position of any size loses nothing; the leading 32 bits
+// of the product go into sine and cosine.
+#pragma once
+#include "k_cache.h"
+
+namespace c2t {
+
+struct AppendArgs {
+  const char* q; const char* k; const char* v; char* q_out; char* k_out;
+  int64_t q_batch, q_token, kv_batch, kv_token, q_out_batch, q_out_token, k_out_batch, k_out_token;    // bytes
+  const int32_t* n_new; const int32_t* starts; const int32_t* position;
+  const uint64_t* turns;
+  float magnitude;
+  int32_t slots, q_heads, layer, nodes, pairs, neighbours;
+  int32_t parts;                                             // wavefronts that share a token's heads
+};
+
+// Sine and cosine of an angle given as a 32-bit fraction of a turn.  The angle's distance from the nearest quarter turn, |x| <= pi / 4, goes into the Taylor series up to x^9 and
+// x^8: what they leave is at most x^11 / 11! = 1.8e-9 and x^10 / 10! = 2.5e-8, under half of an fp32 number's last place at 1.
+__device__ __forceinline__ void sine_cosine(uint32_t fraction, float* sine, float* cosine) {
+  const uint32_t quarter = (fraction + 0x20000000u) >> 30;
+  const float x = (float)(int32_t)(fraction - (quarter << 30)) * 1.4629180792671596e-9f;       // 2 pi / 2^32
+  const float z = x * x;
+  float s = 1.f / 362880.f, c = 1.f / 40320.f;
+  s = __builtin_fmaf(s, z, -1.f / 5040.f); s = __builtin_fmaf(s, z, 1.f / 120.f); s = __builtin_fmaf(s, z, -1.f / 6.f);
+  s = __builtin_fmaf(x * z, s, x);
+  c = __builtin_fmaf(c, z, -1.f / 720.f); c = __builtin_fmaf(c, z, 1.f / 24.f); c = __builtin_fmaf(c, z, -0.5f); c = __builtin_fmaf(c, z, 1.f);
+  const float a = quarter & 1u ? c : s, b = quarter & 1u ? s : c;
+  *sine = quarter & 2u ? -a : a;
+  *cosine = ((quarter + 1u) & 2u) ? -b : b;
+}
+
+// The sequence that packed row `row` is in, and which of its tokens it is; -1: none.  Two trips to memory: every 64th (or so) start, then the ones between.
+__device__ __forceinline__ int sequence_of_row(const int32_t* starts, int n, int row, int* t) {
+  const int lane = lane_id(), step = div_up(n, WAVE);
+  const auto below = [&](int i, int end) { return __popcll(__ballot(i < end && starts[min(i, n)] <= row)); };
+  const int first = (below(lane * step, n) - 1) * step;
+  if (first < 0) return -1;
+  const int b = first + below(first + lane, min(first + step, n)) - 1;
+  if (b < first) return -1;                                  // (starts that fall)
+  const int from = uniform(starts[b]), end = uniform(starts[b + 1]);
+  if (row < from || row >= end || from < 0) return -1;
+  *t = row - from;
+  return b;
+}
+
+// A wavefront has a token, or one of `parts` shares of its heads.  A lane has 16 elements of a head, 8 pairs of them or 16 that only move, and keeps its pairs' sines for
+// all heads that it comes to.
+template <typename T>
+__global__ __launch_bounds__(CACHE_NT) void k_cache_append(CacheView c, AppendArgs a) {
+  const int lane = lane_id(), wave = uniform((int)threadIdx.x >> 6);
+  const int64_t item = (int64_t)blockIdx.x * (CACHE_NT / WAVE) + wave;
+  const int row = (int)(item / a.parts), part = (int)(item % a.parts);
+  if (row >= a.slots) return;
+  int b = blockIdx.y, t = row;
+  int64_t batch = b;                                         // for the strides
+  if (a.starts) {
+    b = sequence_of_row(a.starts, c.batch, row, &t);
+    if (b < 0) return;
+    batch = 0;
+  } else {
+    if (a.n_new && t >= a.n_new[b]) return;
+  }
+  const int len = tokens_in_cache(c, c.length[b]);
+  const int64_t at = (int64_t)len + t;
+  // where it goes, and why not
+  int page = -1;
+  uint32_t why = 0u;
+  if (at >= capacity_of(c)) {
+    why = CACHE_ROW_FULL;
+  } else {
+    page = valid_page(c, c.table[(int64_t)b * c.max_pages + (at >> c.page_shift)]);
+    if (page < 0) why = CACHE_INVALID;
+    else if (c.refcount[page] > 1) { why = CACHE_SHARED; page = -1; }
+  }
+  if (why && lane == 0 && part == 0) report(c, b, why);
+  const int row_in = (int)(at & ((1 << c.page_shift) - 1));
+
+  const int chain = a.slots - a.nodes;
+  int64_t position = at;
+  if (a.nodes > 0 && t >= chain) position = (int64_t)len + chain - 1 + a.position[(int64_t)b * a.nodes + (t - chain)];
+
+  const int per_head = c.head_dim / 16, p = lane % per_head, heads_at_once = WAVE / per_head;
+  const bool turned = p * 8 < a.pairs;
+  const int first = (turned && !a.neighbours ? p * 8 : p * 16) * 2;                            // bytes of the lane's two pieces of 8 elements
+  const int second = turned && !a.neighbours ? first + a.pairs * 2 : first + 16;
+  float sine[8], cosine[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const uint64_t angle = turned ? (uint64_t)position * a.turns[p * 8 + j] : 0ull;
+    sine_cosine((uint32_t)((angle + 0x80000000ull) >> 32), &sine[j], &cosine[j]);
+    const float m = turned ? a.magnitude : 1.f;
+    sine[j] *= m; cosine[j] *= m;
+  }
+  const char* const q = a.q + batch * a.q_batch + row * a.q_token;
+  const char* const k = a.k + batch * a.kv_batch + row * a.kv_token;
+  const char* const v = a.v + batch * a.kv_batch + row * a.kv_token;
+  char* const q_out = a.q_out + batch * a.q_out_batch + row * a.q_out_token;
+  char* const k_out = a.k_out ? a.k_out + batch * a.k_out_batch + row * a.k_out_token : nullptr;
+  const int total = a.q_heads + 2 * c.kv_heads;              // queries, keys, values
+  for (int h = part * heads_at_once + lane / per_head; h < total; h += a.parts * heads_at_once) {
+    const bool is_q = h < a.q_heads, is_v = h >= a.q_heads + c.kv_heads;
+    const int head = is_q ? h : is_v ? h - a.q_heads - c.kv_heads : h - a.q_heads;
+    const char* from = (is_q ? q : is_v ? v : k) + (int64_t)head * c.head_dim * 2;
+    Eight<T> x = *(const Eight<T>*)(from + first), y = *(const Eight<T>*)(from + second);
+    if (turned && !is_v) {
+      if (a.neighbours) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          T& ra = j < 4 ? x.v[2 * j] : y.v[2 * j - 8];
+          T& rb = j < 4 ? x.v[2 * j + 1] : y.v[2 * j - 7];
+          const float f = (float)ra, g = (float)rb;
+          ra = (T)__builtin_fmaf(f, cosine[j], -(g * sine[j])); rb = (T)__builtin_fmaf(f, sine[j], g * cosine[j]);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float f = (float)x.v[j], g = (float)y.v[j];
+          x.v[j] = (T)__builtin_fmaf(f, cosine[j], -(g * sine[j])); y.v[j] = (T)__builtin_fmaf(f, sine[j], g * cosine[j]);
+        }
+      }
+    }
+    const auto put = [&](char* to) { *(Eight<T>*)(to + first) = x; *(Eight<T>*)(to + second) = y; };
+    if (is_q) { put(q_out + (int64_t)head * c.head_dim * 2); continue; }
+    if (!is_v && k_out) put(k_out + (int64_t)head * c.head_dim * 2);
+    if (page >= 0) put((is_v ? c.v : c.k) + row_offset(c, a.layer, page, head, row_in) * 2);
+  }
+}
+
+}  // namespace c2t

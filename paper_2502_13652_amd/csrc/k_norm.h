@@ -1,0 +1,170 @@
+// Root-mean-square norm with the residual's addition, outputs in the inputs' type or in 8 bits with scales.
+//
+//   h = x + residual,  y = h r w,  r = (mean h^2 + eps)^-1/2;   8 bits: out = y / s,  s = max |y| / 448 over a block of the row
+//
+// A row passes once: its threads keep h in registers between the sum and the output.  The sum of squares is held in 64 bits, in which the square of any
+// fp32 number fits, and r is used as a number in [1/2, 1) and a power of two, so rows of any size have their norm.
+#pragma once
+#include "k_common.h"
+
+namespace c2t {
+
+constexpr int NORM_NT = 256;
+constexpr float E4M3_MAX = 448.f;
+
+struct NormArgs {
+  const char* x; const char* weight; const char* residual; char* residual_out; char* out; float* scales;
+  int64_t x_row, residual_row, residual_out_row, out_row;    // bytes
+  int64_t scales_row;                                        // elements
+  int32_t rows, width;
+  int32_t block;                                             // elements a scale; 0: the row
+  bool weight_f32, residual_f32;
+  bool aligned;                                              // pieces of 8 elements of all arrays are 16-byte aligned (8 for 8 bits), the width a multiple
+  float eps;
+};
+
+// 8 elements of a row from `e` on; behind the row's end zeros
+template <typename T>
+__device__ __forceinline__ void load_eight(const char* row, int e, int width, bool aligned, float (&to)[8]) {
+  const T* p = (const T*)row + e;
+  if (aligned) {
+    const Eight<T> x = *(const Eight<T>*)p;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) to[j] = (float)x.v[j];
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) to[j] = e + j < width ? (float)p[j] : 0.f;
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store_eight(char* row, int e, int width, bool aligned, const float (&from)[8]) {
+  T* p = (T*)row + e;
+  if (aligned) {
+    Eight<T> x;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x.v[j] = (T)from[j];
+    *(Eight<T>*)p = x;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) if (e + j < width) p[j] = (T)from[j];
+  }
+}
+// four numbers as e4m3, to nearest even; a NaN stays one, and none is above 448 but by an fp32 rounding
+__device__ __forceinline__ uint32_t four_e4m3(float a, float b, float c, float d) {
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+
+// the largest of a group of 4, 8 or 16 lanes next to each other
+__device__ __forceinline__ float group_max(float v, int lanes) {
+  const auto with = [&](auto ctrl) { v = fmaxf(v, __uint_as_float(dpp_u32<decltype(ctrl)::value, 0xf>(0u, __float_as_uint(v)))); };
+  with(std::integral_constant<int, C2T_DPP_QUAD_XOR1>{});
+  with(std::integral_constant<int, C2T_DPP_QUAD_XOR2>{});
+  if (lanes > 4) with(std::integral_constant<int, C2T_DPP_ROW_HALF_MIRROR>{});
+  if (lanes > 8) with(std::integral_constant<int, C2T_DPP_ROW_MIRROR>{});
+  return v;
+}
+
+// NT threads a row, which has at most 8 CH of its elements each.
+template <typename T, bool E4, int NT, int CH>
+__global__ __launch_bounds__(NT < NORM_NT ? NORM_NT : NT) void k_rms_norm(NormArgs a) {
+  constexpr int ROWS = NT < NORM_NT ? NORM_NT / NT : 1, WAVES = NT / WAVE;
+  static_assert(NT == WAVE || ROWS == 1, "a wavefront a row, or the workgroup");
+  __shared__ double sums[WAVES];
+  __shared__ float tops[WAVES];
+  const int t = threadIdx.x % NT, wave = t / WAVE;
+  const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / NT;
+  if (row >= a.rows) return;                                 // (wavefronts of a workgroup that meet have the same row)
+  const char* x = a.x + row * a.x_row;
+  float h[CH][8];
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const int e = (c * NT + t) * 8;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) h[c][j] = 0.f;
+    if (e < a.width) load_eight<T>(x, e, a.width, a.aligned, h[c]);
+  }
+  if (a.residual) {
+    const char* res = a.residual + row * a.residual_row;
+    char* to = a.residual_out + row * a.residual_out_row;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int e = (c * NT + t) * 8;
+      if (e >= a.width) continue;
+      float r[8];
+      if (a.residual_f32) load_eight<float>(res, e, a.width, a.aligned, r); else load_eight<T>(res, e, a.width, a.aligned, r);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) h[c][j] += r[j];
+      if (a.residual_f32) store_eight<float>(to, e, a.width, a.aligned, h[c]); else store_eight<T>(to, e, a.width, a.aligned, h[c]);
+    }
+  }
+  double sum = 0.;
+#pragma unroll
+  for (int c = 0; c < CH; ++c)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum = __builtin_fma((double)h[c][j], (double)h[c][j], sum);
+  sum = wave_sum(sum);
+  if (NT > WAVE) {
+    if (t % WAVE == 0) sums[wave] = sum;
+    __syncthreads();
+    sum = 0.;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) sum += sums[w];
+  }
+  const double r = 1. / sqrt(sum / (double)a.width + (double)a.eps);
+  int power;
+  const float part = (float)frexp(r, &power);
+
+  float top = 0.f;
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const int e = (c * NT + t) * 8;
+    if (e >= a.width) continue;
+    float w[8];
+    if (a.weight_f32) load_eight<float>(a.weight, e, a.width, a.aligned, w); else load_eight<T>(a.weight, e, a.width, a.aligned, w);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      h[c][j] = ldexpf(h[c][j], power) * part * w[j];
+      if (E4) top = fmaxf(top, __builtin_fabsf(h[c][j]));
+    }
+    if (!E4) store_eight<T>(a.out + row * a.out_row, e, a.width, a.aligned, h[c]);
+  }
+  if constexpr (E4) {
+    if (a.block == 0) {
+      top = wave_max(top);
+      if (NT > WAVE) {
+        if (t % WAVE == 0) tops[wave] = top;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, tops[w]);
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int e = (c * NT + t) * 8;
+      float m = top;
+      if (a.block != 0) {
+        m = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m = fmaxf(m, __builtin_fabsf(h[c][j]));      // (zeros behind the row's end)
+        m = group_max(m, a.block / 8);
+      }
+      if (e >= a.width) continue;
+      const float scale = m == 0.f ? 1.f : fmaxf(m / E4M3_MAX, 0x1p-126f);
+      if (a.block == 0 ? c == 0 && t == 0 : e % a.block == 0) a.scales[row * a.scales_row + (a.block == 0 ? 0 : e / a.block)] = scale;
+      const float inv = 1.f / scale;
+      uint2 y;
+      y.x = four_e4m3(h[c][0] * inv, h[c][1] * inv, h[c][2] * inv, h[c][3] * inv);
+      y.y = four_e4m3(h[c][4] * inv, h[c][5] * inv, h[c][6] * inv, h[c][7] * inv);
+      char* to = a.out + row * a.out_row + e;
+      if (a.aligned) {
+        *(uint2*)to = y;
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) if (e + j < a.width) to[j] = (char)((j < 4 ? y.x : y.y) >> (j % 4 * 8));
+      }
+    }
+  }
+}
+
+}  // namespace c2t

@@ -1,7 +1,8 @@
-"""What goes around a draft phase: a paged K/V cache with its attention, and adjusted logits (the second part of
-include/c2t.h).  Argument marshalling and checks only; like the binding it needs a GPU and has no fallback."""
+"""What goes around a draft phase: a paged K/V cache with its attention, adjusted logits, and a layer's norm, rotation and attention over
+prompts (the second part of include/c2t.h).  Argument marshalling and checks only; like the binding it needs a GPU and has no fallback."""
 import ctypes
 import dataclasses
+import fractions
 import struct
 import threading
 from typing import Optional
@@ -9,7 +10,7 @@ from typing import Optional
 import torch
 
 from . import binding
-from .binding import BF16, F16, F32, _check, load_library
+from .binding import BF16, E4M3, F16, F32, _check, load_library
 
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 ATTENTION_COUNTERS = 8192                                   # C2T_ATTENTION_COUNTERS
@@ -34,6 +35,25 @@ class _Attention(ctypes.Structure):
                 ("layer", ctypes.c_int32), ("nodes", ctypes.c_int32), ("mask", ctypes.c_void_p), ("scale", ctypes.c_float)]
 
 
+class _Norm(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("x", "weight", "residual", "residual_out", "out", "scales")] + \
+               [(n, ctypes.c_int64) for n in ("x_stride", "residual_stride", "residual_out_stride", "out_stride", "scales_stride")] + \
+               [(n, ctypes.c_int32) for n in ("rows", "width", "dtype", "weight_dtype", "residual_dtype", "out_dtype", "scale_block")] + [("eps", ctypes.c_float)]
+
+
+class _Append(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q", "k", "v", "q_out", "k_out")] + \
+               [(n, ctypes.c_int64) for n in ("q_batch_stride", "q_token_stride", "kv_batch_stride", "kv_token_stride",
+                                              "q_out_batch_stride", "q_out_token_stride", "k_out_batch_stride", "k_out_token_stride")] + \
+               [(n, ctypes.c_void_p) for n in ("n_new", "starts", "position", "turns")] + [("magnitude", ctypes.c_float)] + \
+               [(n, ctypes.c_int32) for n in ("tokens", "q_heads", "layer", "nodes", "pairs", "neighbours")]
+
+
+class _Prompt(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q", "k", "v", "out", "lse")] + [(n, ctypes.c_int64) for n in ("q_stride", "k_stride", "v_stride", "out_stride")] + \
+               [("starts", ctypes.c_void_p)] + [(n, ctypes.c_int32) for n in ("rows", "sequences", "q_heads", "kv_heads", "head_dim", "dtype")] + [("scale", ctypes.c_float)]
+
+
 def _packer(fields):
     """A call's structure as bytes: a third of the time that ctypes takes to fill one.  The layout is the structure's."""
     code = {ctypes.c_void_p: "P", ctypes.c_int64: "q", ctypes.c_int32: "i", ctypes.c_float: "f"}
@@ -43,6 +63,7 @@ def _packer(fields):
 
 
 _pack_adjustments, _pack_attention = _packer(_Adjustments), _packer(_Attention)
+_pack_norm, _pack_append, _pack_prompt = _packer(_Norm), _packer(_Append), _packer(_Prompt)
 
 
 def _need(ok, what):
@@ -181,6 +202,125 @@ def adjust_frontier_logits(ctx, logits, adjustments, out=None, stream=None):
     return out
 
 
+def _even_rows(t, shape, device, name):
+    """The distance, in elements, of the rows of a tensor of that shape: its last dimension whole, the others as if they were one."""
+    have = t.shape
+    if have != shape or t.get_device() != device.index:
+        raise ValueError("%s: %s on %s" % (name, list(shape), device))
+    width = have[-1]
+    if t.is_contiguous():
+        return width
+    strides = t.stride()
+    at = [(n, s) for n, s in zip(have[:-1], strides[:-1]) if n > 1]        # (a stride over one element is of no use and may be any number)
+    _need((strides[-1] == 1 or width == 1) and all(a[1] == b[0] * b[1] for a, b in zip(at, at[1:])), "%s: rows evenly spaced, elements next to each other" % name)
+    return at[-1][1] if at else width
+
+
+def rms_norm(x, weight, eps=1e-5, residual=None, residual_out=None, out=None, scale_block=None, scales=None, stream=None):
+    """Root-mean-square norm of x + residual: h = x + residual, h / sqrt(mean(h^2) + eps) * weight over the last dimension, of h in fp32.
+
+    x [...][width] float32, bfloat16 or float16; weight [width] of that type or float32; residual, of x's shape, of that type or float32: h goes to
+    residual_out (default: residual itself), rounded to its type.  out: of x's shape and type (default: a new tensor; may be x).  With scale_block (32, 64, 128
+    or the width), out is float8_e4m3fn and stands for out * scale, with a scale for each scale_block elements of a row (the last may be fewer): scales float32
+    [...][ceil(width / scale_block)] (default: new), max |y| / 448 of the block; returns (out, scales), without it out."""
+    dtype, shape, dev = x.dtype, x.shape, x.device
+    _need(dtype in _DTYPES and x.is_cuda and len(shape) > 0 and shape[-1] > 0, "x: [...][width] of float32, bfloat16 or float16 on the GPU")
+    width = shape[-1]
+    rows = x.numel() // width
+    p_residual = p_residual_out = residual_stride = residual_out_stride = 0
+    code = residual_code = _DTYPES[dtype]
+    if residual is not None:
+        kind = residual.dtype
+        _need(kind is dtype or kind is torch.float32, "residual: of x's type or float32")
+        residual_code = _DTYPES[kind]
+        residual_stride = residual_out_stride = _even_rows(residual, shape, dev, "residual")
+        p_residual = p_residual_out = residual.data_ptr()
+        if residual_out is not None and residual_out is not residual:
+            _need(residual_out.dtype is kind, "residual_out: of the residual's type")
+            residual_out_stride = _even_rows(residual_out, shape, dev, "residual_out")
+            p_residual_out = residual_out.data_ptr()
+    else:
+        _need(residual_out is None, "residual_out: with a residual")
+    if weight.dtype is not dtype:
+        _whole(weight, dev, torch.float32, (width,), "weight")
+    p_weight = _whole(weight, dev, weight.dtype, (width,), "weight")
+    p_scales = scales_stride = 0
+    out_code, out_dtype = code, dtype
+    if scale_block is not None:
+        _need(scale_block == width or scale_block in (32, 64, 128), "scale_block: 32, 64, 128 or the width")
+        out_code, out_dtype = E4M3, torch.float8_e4m3fn
+        wanted = shape[:-1] + (-(-width // scale_block),)
+        if scales is None:
+            scales = _empty_like_on(stream, lambda: torch.empty(wanted, dtype=torch.float32, device=dev))
+        _need(scales.dtype is torch.float32, "scales: float32")
+        scales_stride, p_scales = _even_rows(scales, wanted, dev, "scales"), scales.data_ptr()
+    else:
+        _need(scales is None, "scales: with a scale_block")
+    if out is None:
+        out = _empty_like_on(stream, lambda: torch.empty(shape, dtype=out_dtype, device=dev))
+    _need(out.dtype is out_dtype, "out: %s" % out_dtype)
+    if rows > 0:
+        a = _pack_norm(x.data_ptr(), p_weight, p_residual, p_residual_out, out.data_ptr(), p_scales, _even_rows(x, shape, dev, "x"), residual_stride,
+                       residual_out_stride, _even_rows(out, shape, dev, "out"), scales_stride, rows, width, code, _DTYPES[weight.dtype], residual_code, out_code,
+                       scale_block or 0, eps)
+        _check(_launch(dev, stream, load_library().c2t_rms_norm, a), "c2t_rms_norm")
+    return out if scale_block is None else (out, scales)
+
+
+def _packed_rows(x, heads, head_dim, dtype, device, name):
+    """The distance, in elements, of the rows of [rows][heads][head_dim]."""
+    shape, strides = x.shape, x.stride()
+    if not (x.dtype is dtype and len(shape) == 3 and shape[1] == heads and shape[2] == head_dim and strides[2] == 1 and (heads == 1 or strides[1] == head_dim) and
+            x.device == device):
+        raise ValueError("%s: %s [rows][%d][%d] on %s, heads next to each other" % (name, dtype, heads, head_dim, device))
+    return strides[0] if shape[0] > 1 else heads * head_dim
+
+
+def prompt_attention(q, k, v, starts, scale=None, out=None, lse=None, stream=None):
+    """Causal attention over whole prompts packed one behind the other: rows starts[b] .. starts[b + 1] - 1 are sequence b's, and each sees those of its
+    sequence up to itself.
+
+    q [rows][q_heads][head_dim], k and v [rows][kv_heads][head_dim], bfloat16 or float16, e.g. slices of one projection's output; starts int32 [sequences + 1].
+    scale: of the scores, default head_dim ** -0.5.  out: as q (default: a new tensor), lse: float32 [rows][q_heads] for the log of the softmax's sums; rows in no
+    sequence are left as they are (in a new tensor they are not filled in)."""
+    _need(q.dim() == 3 and k.dim() == 3 and q.is_cuda and q.dtype in (torch.bfloat16, torch.float16), "q: [rows][q_heads][head_dim] of bfloat16 or float16 on the GPU")
+    dev, dtype = q.device, q.dtype
+    rows, heads, D = q.shape
+    kv_heads = k.shape[1]
+    sq, sk, sv = _packed_rows(q, heads, D, dtype, dev, "q"), _packed_rows(k, kv_heads, D, dtype, dev, "k"), _packed_rows(v, kv_heads, D, dtype, dev, "v")
+    _need(k.shape[0] == rows and v.shape[0] == rows, "k and v: as many rows as q")
+    if out is None:
+        out = _empty_like_on(stream, lambda: torch.empty((rows, heads, D), dtype=dtype, device=dev))
+    so = _packed_rows(out, heads, D, dtype, dev, "out")
+    _need(out.shape[0] == rows, "out: of q's shape")
+    p_lse = 0 if lse is None else _whole(lse, dev, torch.float32, (rows, heads), "lse")
+    p_starts = _whole(starts, dev, torch.int32, (-1,), "starts")
+    sequences = starts.shape[0] - 1
+    _need(sequences >= 0, "starts: int32 [sequences + 1]")
+    if rows > 0 and sequences > 0:
+        a = _pack_prompt(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), p_lse, sq, sk, sv, so, p_starts, rows, sequences, heads, kv_heads, D, _DTYPES[dtype],
+                         D ** -0.5 if scale is None else scale)
+        _check(_launch(dev, stream, load_library().c2t_prompt_attention, a), "c2t_prompt_attention")
+    return out
+
+
+_PI = fractions.Fraction("3.14159265358979323846264338327950288419716939937510582097")
+
+
+class Rotation:
+    """How queries and keys are turned by their positions (PagedCache.append): the first dim elements of each head's row in pairs, elements j and dim / 2 + j, or, with
+    `neighbours`, 2j and 2j + 1; pair j by position * base ** (-2j / dim), or by position * frequencies[j] (radians, dim / 2 of them), and times magnitude.
+    dim: a multiple of 16.  Held on the device as 64-bit fractions of a turn, so that far positions are as exact as near ones."""
+
+    def __init__(self, dim, base=10000.0, neighbours=False, frequencies=None, magnitude=1.0, device="cuda:0"):
+        _need(dim > 0 and dim % 16 == 0, "dim: a multiple of 16")
+        f = [float(base) ** (-2.0 * j / dim) for j in range(dim // 2)] if frequencies is None else [float(x) for x in frequencies]
+        _need(len(f) == dim // 2 and all(abs(x) < float("inf") for x in f), "frequencies: dim / 2 finite numbers")
+        turns = [round(fractions.Fraction(x) / (2 * _PI) * (1 << 64)) % (1 << 64) for x in f]
+        self.dim, self.neighbours, self.magnitude = dim, bool(neighbours), float(magnitude)
+        self.turns = torch.tensor([t - (1 << 64) if t >> 63 else t for t in turns], dtype=torch.int64, device=device)
+
+
 class PagedCache:
     """A paged K/V cache (c2t_cache): tensors k, v [layers][pages][kv_heads][page_size][head_dim], page_table int32 [B][max_pages] (-1: no
     page), length int32 [B], refcount int32 [pages], status uint32 [B] (POOL_EMPTY, ROW_FULL, INVALID, SHARED; set by calls, cleared by the
@@ -261,6 +401,44 @@ class PagedCache:
         _need(self._tokens(v, self.kv_heads, "v") == sk and k.shape == v.shape, "k and v: of one shape and strides")
         self._run("c2t_cache_write", stream, int(layer), k.data_ptr(), v.data_ptr(), sk[0], sk[1], k.shape[1],
                   None if n_new is None else self._per_sequence(n_new, "n_new"))
+
+    def append(self, layer, q, k, v, rotation, n_new=None, position=None, starts=None, q_out=None, k_out=None, stream=None):
+        """Queries and keys of new tokens turned by their positions (a Rotation), keys and values to places length + t of `layer`, as write does; returns q_out.
+
+        q [B][T][q_heads][head_dim], k and v [B][T][kv_heads][head_dim], n_new (int32 [B], default all) of them.  A token's position is its place, but for a
+        tree's nodes, the last N of the T slots: position int32 [B][N] as finalize_tree writes it, from the slot ahead of them (the root) on.
+        Or packed, with starts (int32 [B + 1]): [rows][heads][head_dim], rows starts[b] .. starts[b + 1] - 1 are sequence b's.
+        q_out: as q (default: a new tensor; may be q); k_out: as k, for the turned keys (may be k); rows of no token are left as they are.  What the cache has no room
+        or page for is left out of it alone, and its status says so."""
+        packed = starts is not None
+        _need(q.dim() == (3 if packed else 4), "q: [rows][q_heads][head_dim] with starts, [B][T][q_heads][head_dim] without")
+        T, heads, D, H = q.shape[-3], q.shape[-2], self.head_dim, self.kv_heads
+        if packed:
+            _need(n_new is None and position is None, "n_new and position: without starts")
+            rows = lambda x, n, name: (0, _packed_rows(x, n, D, self.dtype, self.device, name))
+        else:
+            rows = self._tokens
+        sq, sk = rows(q, heads, "q"), rows(k, H, "k")
+        _need(rows(v, H, "v") == sk and k.shape == v.shape and k.shape[:-2] == q.shape[:-2], "k and v: of one shape and strides, as many tokens as q")
+        if q_out is None:
+            q_out = _empty_like_on(stream, lambda: torch.empty(q.shape, dtype=self.dtype, device=self.device))
+        so = rows(q_out, heads, "q_out")
+        _need(q_out.shape == q.shape and (k_out is None or k_out.shape == k.shape), "q_out and k_out: of q's and k's shape")
+        ko = (0, 0) if k_out is None else rows(k_out, H, "k_out")
+        nodes = p_position = 0
+        if position is not None:
+            nodes = position.shape[-1]
+            p_position = _whole(position, self.device, torch.int32, (self.batch, nodes), "position") if nodes else 0
+        turns = rotation.turns
+        p_turns = _whole(turns, self.device, torch.int64, (rotation.dim // 2,), "rotation")
+        if T == 0:
+            return q_out
+        a = _pack_append(q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr(), 0 if k_out is None else k_out.data_ptr(), sq[0], sq[1], sk[0], sk[1],
+                         so[0], so[1], ko[0], ko[1], 0 if n_new is None else self._per_sequence(n_new, "n_new"),
+                         _whole(starts, self.device, torch.int32, (self.batch + 1,), "starts") if packed else 0, p_position, p_turns, rotation.magnitude,
+                         T, heads, layer, nodes, rotation.dim // 2, rotation.neighbours)
+        self._run("c2t_cache_append", stream, a)
+        return q_out
 
     def commit(self, path, n_path, stream=None):
         """The tokens in slots path[b][i] (int32 [B][P], rising) behind the length move to slots i < n_path[b]; the length grows by n_path."""
