@@ -18,6 +18,7 @@ struct PromptArgs {
   int64_t q_row, k_row, v_row, out_row;                      // bytes
   const int32_t* starts;
   int32_t rows, sequences, kv_heads, group;
+  float inv_group;                                           // 1 / group
   float scale_log2e;
 };
 
@@ -27,48 +28,90 @@ __device__ __forceinline__ f32x16 product32(F16::T8 a, F16::T8 b, f32x16 c) { re
 // A tile of rows of a sequence.
 struct PromptTile { int first, n, tile; };                   // the sequence's first row and length
 
-// The tile of rank `rank` of all sequences' tiles, those with the most keys first; equal ones in the sequences' order.  Every wavefront finds it for itself: a lane has every 64th
-// sequence, and the number of tiles from a level on is a sum over lanes, so that the rank's level is searched by halves.  False: there is no such tile.
+// The tile of rank `rank`.  Sequences of 2^c tiles and more come ahead of shorter ones; those of one c in their order, TOGETHER at a time, whose tiles go by the number of keys, most first.
+// So the longest start first, the tiles that run at one time share few sequences' keys in the dies' L2, and few sequences still end together: 64 prompts of up to 2000 tokens take
+// 940 us so, one sequence after the other 950, all sequences' tiles by their keys 1030; four of 1000 53, 57 and 53 (of the kernel as it was then).
+// Every wavefront finds it for itself: a lane has every 64th sequence, tiles of a class and above are a sum over lanes.  False: there is no such tile.
+constexpr int TOGETHER = 4;
 template <int ROWS>
 __device__ __forceinline__ bool find_tile(const PromptArgs& a, int rank, PromptTile* u) {
   const int lane = lane_id();
   const auto length = [&](int b, int* first) {
-    const int from = a.starts[min(b, a.sequences - 1)], end = a.starts[min(b, a.sequences - 1) + 1];
+    const int at = min(b, a.sequences - 1), from = a.starts[at], end = a.starts[at + 1];
     *first = from;
     return b < a.sequences && from >= 0 && end >= from && end <= a.rows ? end - from : 0;
   };
-  const auto tiles = [](int n) { return (int)(((int64_t)n + ROWS - 1) / ROWS); };
-  int my_first;
-  const int my_n = length(lane, &my_first), my_tiles = tiles(my_n);
-  const auto from_level = [&](int level) {
-    int mine = max(my_tiles - level, 0);
+  const auto tiles = [&](int n) { return (n * a.group + ROWS - 1) / ROWS; };  // (rows * group: at most 2^30, checked by the host)
+  int first[TOGETHER], n[TOGETHER], has[TOGETHER], left = rank;
+  if (a.sequences <= TOGETHER) {
+#pragma unroll
+    for (int i = 0; i < TOGETHER; ++i) { n[i] = length(i, &first[i]); has[i] = tiles(n[i]); }
+  } else {
+    int my_first;
+    const int my_n = length(lane, &my_first), my_tiles = tiles(my_n);
+    const auto from_class = [&](int c) {
+      int mine = my_tiles >> c != 0 ? my_tiles : 0;
 #pragma unroll 1
-    for (int b = lane + WAVE; b < a.sequences; b += WAVE) { int f; mine += max(tiles(length(b, &f)) - level, 0); }
-    return wave_sum_i(mine);
+      for (int b = lane + WAVE; b < a.sequences; b += WAVE) { int f; const int t = tiles(length(b, &f)); mine += t >> c != 0 ? t : 0; }
+      return wave_sum_i(mine);
+    };
+    if (from_class(0) <= rank) return false;
+    int c = 0, above = 32 - __builtin_clz(tiles(a.rows)), ahead = 0;           // tiles of class `above` and more: `ahead`, at most the rank
+    while (above - c > 1) {
+      const int mid = (c + above) / 2, count = from_class(mid);
+      if (count > rank) c = mid; else { above = mid; ahead = count; }
+    }
+    left -= ahead;                                           // which of the class's tiles
+    int f = my_first, m = my_n, mine, to, b0 = 0;
+    uint64_t past;
+    for (;;) {
+      const int t = tiles(m);
+      mine = t >> c == 1 ? t : 0; to = wave_scan_incl(mine);
+      past = __ballot(to > left);
+      if (past != 0ull) break;
+      b0 += WAVE;
+      if (b0 >= a.sequences) return false;                   // (starts that change while they are read)
+      left -= __builtin_amdgcn_readlane(to, WAVE - 1);
+      m = length(b0 + lane, &f);
+    }
+    // the TOGETHER sequences of the class that it is among
+    const int place = __popcll(__ballot(mine != 0) & ((1ull << lane) - 1ull)) / TOGETHER, at = __builtin_amdgcn_readlane(place, __builtin_ctzll(past));
+    uint64_t members = __ballot(mine != 0 && place == at);
+    left -= __builtin_amdgcn_readlane(to - mine, __builtin_ctzll(members));
+#pragma unroll
+    for (int i = 0; i < TOGETHER; ++i) {
+      const int from = members != 0ull ? __builtin_ctzll(members) : 0;
+      first[i] = __builtin_amdgcn_readlane(f, from);
+      n[i] = __builtin_amdgcn_readlane(m, from);
+      has[i] = members != 0ull ? __builtin_amdgcn_readlane(mine, from) : 0;
+      members &= members - 1ull;
+    }
+  }
+  const auto above_level = [&](int level) {
+    int sum = 0;
+#pragma unroll
+    for (int i = 0; i < TOGETHER; ++i) sum += max(has[i] - level, 0);
+    return sum;
   };
-  int level = 0, above = tiles(a.rows) + 1, ahead = 0;       // tiles of `above` and more: `ahead`, at most the rank
-  if (from_level(0) <= rank) return false;
-  while (above - level > 1) {
-    const int mid = level + (above - level) / 2, count = from_level(mid);
-    if (count > rank) level = mid; else { above = mid; ahead = count; }
+  if (above_level(0) <= left) return false;
+  int level = 0, most = 1;                                   // the highest with more than `left` tiles on it and above
+#pragma unroll
+  for (int i = 0; i < TOGETHER; ++i) most = max(most, has[i]);
+  for (int span = most; span > 1;) {
+    const int step = div_up(span, WAVE);
+    level += (__popcll(__ballot(lane * step < span && above_level(level + lane * step) > left)) - 1) * step;
+    span = step;
   }
-  int left = rank - ahead;                                   // which of the sequences that have that level
-  u->tile = level;
-#pragma unroll 1
-  for (int b0 = 0; b0 < a.sequences; b0 += WAVE) {
-    int f = my_first, n = my_n;
-    if (b0 > 0) n = length(b0 + lane, &f);
-    const bool has = tiles(n) > level;
-    const uint64_t those = __ballot(has);
-    const int count = __popcll(those);
-    if (left >= count) { left -= count; continue; }
-    const int before = __popcll(those & ((1ull << lane) - 1ull));
-    const int from = __builtin_ctzll(__ballot(has && before == left));
-    u->first = __builtin_amdgcn_readlane(f, from);
-    u->n = __builtin_amdgcn_readlane(n, from);
-    return true;
+  left -= above_level(level + 1);
+  bool found = false;
+#pragma unroll
+  for (int i = 0; i < TOGETHER; ++i) {
+    if (has[i] <= level) continue;
+    if (left-- != 0) continue;
+    u->first = first[i]; u->n = n[i]; u->tile = level;
+    found = true;
   }
-  return false;
+  return found;
 }
 
 // Where 16-byte piece `piece` of row `row` lies in a tile in LDS: pieces change places within a row so that 16 rows' same piece (a K operand), and 32 bytes each of 4
@@ -78,37 +121,124 @@ template <int D> __device__ __forceinline__ int piece_at(int row, int piece) {
   return row * (D * 2) + (piece ^ turn) * 16;
 }
 
+// 16 bytes a lane from memory into LDS, without a register on the way: lane i's to `to` + 16 i.  The compiler does not count it: whoever reads waits for it (wait_vector_memory, and a
+// barrier for what other wavefronts loaded), and no wavefront ends ahead of its own.
+__device__ __forceinline__ void load_to_lds(const char* base, uint32_t offset, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory", "m0");
+}
+__device__ __forceinline__ uint32_t lds_address(const char* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p; }
+
+// a + the sum of a pair's two numbers, in fp32
+__device__ __forceinline__ float add_pair(Bf16::T8 x, int pair, float a) {
+  typedef __bf16 T2 __attribute__((ext_vector_type(2)));
+  const T2 one = {(__bf16)1.f, (__bf16)1.f}, y = {x[pair * 2], x[pair * 2 + 1]};
+  return __builtin_amdgcn_fdot2_f32_bf16(y, one, a, false);
+}
+__device__ __forceinline__ float add_pair(F16::T8 x, int pair, float a) {
+  typedef _Float16 T2 __attribute__((ext_vector_type(2)));
+  const T2 one = {(_Float16)1.f, (_Float16)1.f}, y = {x[pair * 2], x[pair * 2 + 1]};
+  return __builtin_amdgcn_fdot2(y, one, a, false);
+}
+
 constexpr int PROMPT_WAVES = 4, PROMPT_ROWS = 32 * PROMPT_WAVES;
 
-// KB blocks of 32 keys a tile; OCC workgroups a CU.
-template <typename E, int D, int KB, int OCC, bool LSE>
+// How a block of PRODUCTS matrix instructions and READS reads of their operands is to be laid out: AHEAD reads, then EACH reads behind each product.
+template <int PRODUCTS, int READS, int AHEAD, int EACH> __device__ __forceinline__ void reads_ahead() {
+  __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+  for (int i = 0; i < PRODUCTS; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+    if (AHEAD + i * EACH < READS) __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
+  }
+}
+constexpr int K_AHEAD = 4;
+
+// DV of the D elements of an output row are one workgroup's (D, or the half where registers do not hold it all); KB blocks of 32 keys a tile; OCC workgroups a CU.
+template <typename E, int D, int DV, int KB, int OCC, bool LSE>
 __global__ __launch_bounds__(64 * PROMPT_WAVES, OCC) void k_prompt(PromptArgs a) {
   typedef typename E::T T; typedef typename E::T4 T4; typedef typename E::T8 T8;
-  constexpr int NT = 64 * PROMPT_WAVES, KT = 32 * KB, CH = D / 8, DB = D / 32, DK = D / 16, LOADS = KT * CH / NT, TILE = KT * D * 2;
+  constexpr int NT = 64 * PROMPT_WAVES, KT = 32 * KB, PARTS = D / DV, DB = DV / 32, DK = D / 16;
+  constexpr int K_LOADS = KT * D / 8 / NT, V_LOADS = KT * DV / 8 / NT, K_TILE = KT * D * 2, TILE = K_TILE + KT * DV * 2;
   constexpr float TOP = E::TOP, SLACK = E::SLACK, BIG = 0x1p22f;
-  __shared__ __align__(16) char lds[4 * TILE];               // K and V, two buffers
-  __shared__ int odd_value;
+  __shared__ __align__(16) char lds[2 * TILE];               // K and V, two buffers
+  __shared__ int odd_value;                                  // a tile held a value that is not finite
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, half = lane >> 5, G = a.group;
 
-  // work: units are tiles of one cached head; the heads of a group, which share its keys, follow each other on one die
-  const int in_die = blockIdx.x / DIES, unit = in_die / a.group * DIES + blockIdx.x % DIES, g = in_die % a.group;
-  const int head = unit % a.kv_heads;
+  // The query heads of one cached head share its keys: a tile's rows are (token, head of the group) with the head fastest, so that its wavefronts come to their last key together, however
+  // many heads there are, and short prompts fill tiles.
   PromptTile u;
+  const int unit = blockIdx.x / PARTS, part = blockIdx.x % PARTS, head = unit % a.kv_heads;
   if (!find_tile<PROMPT_ROWS>(a, unit / a.kv_heads, &u)) return;
-  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, half = lane >> 5;
-  const int row0 = u.tile * PROMPT_ROWS, wave_row0 = row0 + wave * 32, my_row = wave_row0 + col;
-  const int keys = min(u.n, row0 + PROMPT_ROWS), n_tiles = (keys + KT - 1) / KT;
-  const bool idle = wave_row0 >= u.n;
-  const int64_t first = u.first;
-  const char* const k_head = a.k + first * a.k_row + (int64_t)head * (D * 2);
-  const char* const v_head = a.v + first * a.v_row + (int64_t)head * (D * 2);
-  const int64_t q_head = query_offset(head, a.group, g, D) * 2;
+  const int row0 = u.tile * PROMPT_ROWS, wave_row0 = row0 + wave * 32, rows = u.n * G;
+  const auto token_of = [&](int row, int* g) { int t; split(min(row, rows - 1), G, a.inv_group, &t, g); return t; };      // (rows behind the last are not put out)
+  int my_g, no_g;
+  const int my_token = token_of(wave_row0 + col, &my_g);
+  const int first_token = uniform(token_of(row0, &no_g)), wave_first = uniform(token_of(wave_row0, &no_g)), wave_last = uniform(token_of(wave_row0 + 31, &no_g));
+  const int keys = uniform(token_of(row0 + PROMPT_ROWS - 1, &no_g)) + 1, n_tiles = div_up(keys, KT);
+  const bool idle = wave_row0 >= rows;
+  const char* const k_head = a.k + u.first * a.k_row + (int64_t)head * (D * 2);
+  const char* const v_head = a.v + u.first * a.v_row + (int64_t)head * (D * 2) + part * (DV * 2);
 
+  // A tile's pieces: this thread's j-th lies j NT + tid pieces into K's or V's tile in LDS, and is the piece of its row that piece_at puts there: the same one in every 16th row, so
+  // that one offset (two, of rows of 8 a load) does for all of a tile's.
+  constexpr int K_ROWS = NT / (D / 8), V_ROWS = NT / (DV / 8), K_KINDS = K_ROWS < 16 ? 16 / K_ROWS : 1, V_KINDS = V_ROWS < 16 ? 16 / V_ROWS : 1;      // rows a load, offsets
+  const auto k_piece = [&](int j) { const int row = j * K_ROWS + tid / (D / 8); return (uint32_t)(piece_at<D>(row, tid % (D / 8)) - row * (D * 2)); };
+  const auto v_piece = [&](int j) { const int row = j * V_ROWS + tid / (DV / 8); return (uint32_t)(piece_at<DV>(row, tid % (DV / 8)) - row * (DV * 2)); };
+  uint32_t k_off[K_KINDS], v_off[V_KINDS];
+#pragma unroll
+  for (int j = 0; j < K_KINDS; ++j) k_off[j] = tid / (D / 8) * (uint32_t)a.k_row + k_piece(j);
+#pragma unroll
+  for (int j = 0; j < V_KINDS; ++j) v_off[j] = tid / (DV / 8) * (uint32_t)a.v_row + v_piece(j);
+  const uint32_t lds_wave = lds_address(lds) + wave * 1024;
+  const char* k_at = k_head; const char* v_at = v_head;
+  int ahead = keys;                                          // keys from there on
+  const auto request = [&](int buffer) {
+    const uint32_t to = lds_wave + buffer * TILE;
+    if (ahead >= KT) {
+#pragma unroll
+      for (int j = 0; j < K_LOADS; ++j) load_to_lds(k_at + j * K_ROWS * a.k_row, k_off[j % K_KINDS], to + j * NT * 16);
+#pragma unroll
+      for (int j = 0; j < V_LOADS; ++j) load_to_lds(v_at + j * V_ROWS * a.v_row, v_off[j % V_KINDS], to + K_TILE + j * NT * 16);
+    } else {                                                 // rows behind the last key are taken from it (and masked)
+#pragma unroll
+      for (int j = 0; j < K_LOADS; ++j) load_to_lds(k_at, (uint32_t)min(j * K_ROWS + tid / (D / 8), ahead - 1) * (uint32_t)a.k_row + k_piece(j), to + j * NT * 16);
+#pragma unroll
+      for (int j = 0; j < V_LOADS; ++j) load_to_lds(v_at, (uint32_t)min(j * V_ROWS + tid / (DV / 8), ahead - 1) * (uint32_t)a.v_row + v_piece(j), to + K_TILE + j * NT * 16);
+    }
+    k_at += KT * a.k_row; v_at += KT * a.v_row; ahead -= KT;
+  };
+  // Waits for this wavefront's pieces.  Where some rows see a value that others do not, one that is not finite is left out of the product and added for the rows that see it.
+  const auto arrived = [&](int buffer, bool diagonal) {
+    wait_vector_memory();
+    if (!diagonal) return;
+    bool odd = false;
+#pragma unroll
+    for (int j = 0; j < V_LOADS; ++j) {
+      u32x4* const at = (u32x4*)(lds + buffer * TILE + K_TILE + (j * NT + tid) * 16);
+      const u32x4 x = *at;
+      const u32x4 bad = {odd_halves<E>(x.x), odd_halves<E>(x.y), odd_halves<E>(x.z), odd_halves<E>(x.w)};
+      if ((bad.x | bad.y | bad.z | bad.w) != 0u) { odd = true; *at = x & ~bad; }
+    }
+    if (odd) odd_value = 1;
+  };
+  // Where this lane's operands begin: of K row `col` and piece `half`, of V rows 4 half + (lane & 15) / 4 and the lane's 8 bytes of a block of 32 elements.  The others lie at these
+  // places but for whole rows and bits of the piece's number.
+  const int k_place = piece_at<D>(col, half);
+  const int v_place = K_TILE + piece_at<DV>(half * 4 + (lane & 15) / 4, (lane >> 4 & 1) * 2 + (lane & 3) / 2) + (lane & 1) * 8;
+  request(0);
   T8 q[DK];
   {
-    const char* const from = a.q + (first + min(my_row, u.n - 1)) * a.q_row + q_head + half * 16;
+    const char* const from = a.q + ((int64_t)u.first + my_token) * a.q_row + query_offset(head, G, my_g, D) * 2 + half * 16;
 #pragma unroll
     for (int kk = 0; kk < DK; ++kk) q[kk] = *(const T8*)(from + kk * 32);
   }
+  if (tid == 0) odd_value = 0;
+  __syncthreads();
+  arrived(0, KT > first_token);
+  // The queries are here before the loop, or each of its rounds would wait for them, and for the next tile's pieces, which are younger, with them.
+#pragma unroll
+  for (int kk = 0; kk < DK; ++kk) { u32x4 x = __builtin_bit_cast(u32x4, q[kk]); settle(x); q[kk] = __builtin_bit_cast(T8, x); }
+  __syncthreads();
   f32x16 o[DB];
 #pragma unroll
   for (int d = 0; d < DB; ++d)
@@ -117,65 +247,33 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, OCC) void k_prompt(PromptArgs a)
   float m_run = -INFINITY, e_run = 0.f, l_run = 0.f, factor = a.scale_log2e;
   int big = 0;
 
-  u32x4 kr[LOADS], vr[LOADS];
-  auto request = [&](int t) {
-#pragma unroll
-    for (int j = 0; j < LOADS; ++j) {
-      const int i = j * NT + tid, row = min(t * KT + i / CH, keys - 1);        // (rows behind the last key are masked)
-      kr[j] = *(const u32x4*)(k_head + row * a.k_row + i % CH * 16);
-      vr[j] = *(const u32x4*)(v_head + row * a.v_row + i % CH * 16);
-    }
-  };
-  auto stage = [&](int t, char* to) {
-    bool odd = false;
-    if (t * KT + KT > row0) {
-      // some rows see a value that others do not: one that is not finite is left out of the product and added for the rows that see it
-#pragma unroll
-      for (int j = 0; j < LOADS; ++j) {
-        const uint32_t x = odd_halves<E>(vr[j].x), y = odd_halves<E>(vr[j].y), z = odd_halves<E>(vr[j].z), w = odd_halves<E>(vr[j].w);
-        odd = odd || (x | y | z | w) != 0u;
-        vr[j].x &= ~x; vr[j].y &= ~y; vr[j].z &= ~z; vr[j].w &= ~w;
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < LOADS; ++j) {
-      const int i = j * NT + tid, at = piece_at<D>(i / CH, i % CH);
-      *(u32x4*)(to + at) = kr[j];
-      *(u32x4*)(to + TILE + at) = vr[j];
-    }
-    if (odd) odd_value = 1;
-  };
-  if (tid == 0) odd_value = 0;
-  request(0);
-  __syncthreads();
-  stage(0, lds);
-  if (n_tiles > 1) request(1);
-  __syncthreads();
-
   for (int t = 0; t < n_tiles; ++t) {
-    const int key0 = t * KT;
-    const char* const k_lds = lds + (t & 1) * 2 * TILE;
-    const char* const v_lds = k_lds + TILE;
-    if (!idle && key0 <= wave_row0 + 31) {
+    const int key0 = t * KT, buffer = t & 1;
+    if (t + 1 < n_tiles) request(buffer ^ 1);
+    if (!idle && key0 <= wave_last) {
+      int k_base = k_place + buffer * TILE, v_base = v_place + buffer * TILE;
+      settle(k_base); settle(v_base);                        // (what follows from them is made anew each time, and holds no registers)
       f32x16 s[KB];
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
+      for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
 #pragma unroll
-        for (int kk = 0; kk < DK; ++kk) s[kb] = product32(*(const T8*)(k_lds + piece_at<D>(kb * 32 + col, kk * 2 + half)), q[kk], s[kb]);
-      }
+      for (int kk = 0; kk < DK; ++kk)
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) s[kb] = product32(*(const T8*)(lds + (k_base ^ kk * 32) + kb * 32 * (D * 2)), q[kk], s[kb]);
+      reads_ahead<KB * DK, KB * DK, K_AHEAD, 1>();
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) settle(s[kb]);
-      if (key0 + KT - 1 > wave_row0) {
+      if (key0 + KB * 32 - 1 > wave_first) {
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) s[kb][i] = key0 + kb * 32 + i / 4 * 8 + half * 4 + i % 4 <= my_row ? s[kb][i] : -INFINITY;
+          for (int i = 0; i < 16; ++i) s[kb][i] = key0 + kb * 32 + i / 4 * 8 + half * 4 + i % 4 <= my_token ? s[kb][i] : -INFINITY;
       }
       if (big != 0) {
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) s[kb] *= a.scale_log2e;
+        for (int i = 0; i < KB * 16; ++i) s[i / 16][i % 16] *= a.scale_log2e;
       }
       float top = -INFINITY;
 #pragma unroll
@@ -190,58 +288,61 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, OCC) void k_prompt(PromptArgs a)
         if (big == 0 && __any(__builtin_fabsf(m_new) >= BIG && m_new != -INFINITY)) {
           big = 1; factor = 1.f;
 #pragma unroll
-          for (int kb = 0; kb < KB; ++kb) s[kb] *= a.scale_log2e;
+          for (int i = 0; i < KB * 16; ++i) s[i / 16][i % 16] *= a.scale_log2e;
         }
         const float back = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
         m_run = m_new;
         l_run *= back; e_run *= back;
 #pragma unroll
-        for (int d = 0; d < DB; ++d) o[d] *= back;
+        for (int i = 0; i < DB * 16; ++i) o[i / 16][i % 16] *= back;
       }
       const float ref = m_run == -INFINITY ? 0.f : m_run;
-      T8 p[KB * 2], ones;
+      // Weights are made, two at a time, and V's operands read one step of 16 keys ahead of the products that take them: between a step's products there are the next one's
+      // instructions.  The order is the one written here.
+      T8 p[2], v[2][DB];
+      const auto weights = [&](int h, int pair) {
 #pragma unroll
-      for (int r = 0; r < 8; ++r) ones[r] = (T)1.f;
-#pragma unroll
-      for (int h = 0; h < KB * 2; ++h)
-#pragma unroll
-        for (int r = 0; r < 8; ++r) {
+        for (int r = pair * 2; r < pair * 2 + 2; ++r) {
           const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h / 2][h % 2 * 8 + r], factor, -ref));
           if (LSE) e_run += w;
-          p[h][r] = (T)w;
+          p[h & 1][r] = (T)w;
         }
-      f32x16 sum;
+        l_run = add_pair(p[h & 1], pair, l_run);
+      };
+      const auto read_v = [&](int h, int d) {
+        typedef __attribute__((address_space(3))) s16x4* lds4;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(lds + (v_base ^ d * 64) + h * 16 * (DV * 2)));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(lds + (v_base ^ (d * 64 + 32)) + (h * 16 + 8) * (DV * 2)));
+        struct { s16x4 a, b; } both{lo, hi};
+        v[h & 1][d] = __builtin_bit_cast(T8, both);
+      };
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sum[i] = 0.f;
+      for (int d = 0; d < DB; ++d) read_v(0, d);
 #pragma unroll
-      for (int h = 0; h < KB * 2; ++h) sum = product32(ones, p[h], sum);
+      for (int pair = 0; pair < 4; ++pair) weights(0, pair);
 #pragma unroll
       for (int h = 0; h < KB * 2; ++h)
 #pragma unroll
         for (int d = 0; d < DB; ++d) {
-          const int row = h * 16 + half * 4 + (lane & 15) / 4, piece = d * 4 + (lane >> 4 & 1) * 2 + (lane & 3) / 2;
-          typedef __attribute__((address_space(3))) s16x4* lds4;
-          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(v_lds + piece_at<D>(row, piece) + (lane & 1) * 8));
-          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(v_lds + piece_at<D>(row + 8, piece) + (lane & 1) * 8));
-          struct { s16x4 a, b; } pair{lo, hi};
-          o[d] = product32(__builtin_bit_cast(T8, pair), p[h], o[d]);
+          __builtin_amdgcn_sched_barrier(0);
+          o[d] = product32(v[h & 1][d], p[h & 1], o[d]);
+          if (h + 1 < KB * 2) {
+            read_v(h + 1, d);
+#pragma unroll
+            for (int pair = d * 4 / DB; pair < (d + 1) * 4 / DB; ++pair) weights(h + 1, pair);
+          }
         }
-      settle(sum);
-      l_run += sum[0];
     }
-    if (t + 1 < n_tiles) {
-      stage(t + 1, lds + ((t + 1) & 1) * 2 * TILE);
-      if (t + 2 < n_tiles) request(t + 2);
-    }
+    if (t + 1 < n_tiles) arrived(buffer ^ 1, key0 + 2 * KT > first_token);
     __syncthreads();
   }
 #pragma unroll
   for (int d = 0; d < DB; ++d) settle(o[d]);
   if (idle) return;
-  e_run += __shfl_xor(e_run, 32);
+  l_run += __shfl_xor(l_run, 32); e_run += __shfl_xor(e_run, 32);
 
-  if (odd_value != 0) {                                      // values that are not finite: a weight is made again from its key
-    for (int key = row0 / KT * KT; key < min(keys, wave_row0 + 32); ++key) {
+  if (odd_value != 0) {                                    // values that are not finite: a weight is made again from its key
+    for (int key = first_token / KT * KT; key <= wave_last; ++key) {
       const char* const v = v_head + key * a.v_row;
       T4 x[DB * 4];
       bool any = false;
@@ -261,29 +362,29 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, OCC) void k_prompt(PromptArgs a)
       }
       dot += __shfl_xor(dot, 32);
       const float w = __builtin_amdgcn_exp2f(rounded_difference(dot, a.scale_log2e, m_run == -INFINITY ? 0.f : m_run));
-      if (key > my_row) continue;
+      if (key > my_token) continue;
 #pragma unroll
       for (int d = 0; d < DB * 4; ++d)
 #pragma unroll
         for (int r = 0; r < 4; ++r) { const float y = (float)x[d][r]; if (!(__builtin_fabsf(y) < INFINITY)) o[d / 4][d % 4 * 4 + r] += w * y; }
     }
   }
-  if (my_row >= u.n) return;
+  if (wave_row0 + col >= rows) return;
+  const int64_t row = (int64_t)u.first + my_token, query = query_offset(head, G, my_g, 1);
+  char* const out = a.out + row * a.out_row + query * (D * 2) + part * (DV * 2) + half * 8;
   const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
-  char* const out = a.out + (first + my_row) * a.out_row + q_head;
 #pragma unroll
   for (int d = 0; d < DB * 4; ++d) {
     T4 y;
 #pragma unroll
     for (int r = 0; r < 4; ++r) y[r] = (T)(o[d / 4][d % 4 * 4 + r] * inv);
-    *(T4*)(out + d * 16 + half * 8) = y;
+    *(T4*)(out + d * 16) = y;
   }
-  if (LSE && half == 0) {
+  if (LSE && half == 0 && part == 0) {
     // of a sum as if the reference were the largest score (k_attend.h)
     constexpr float BELOW = TOP - SLACK;
     const float UNIT = __builtin_ldexpf(1.f, -(int)BELOW);
-    a.lse[(first + my_row) * a.kv_heads * a.group + query_offset(head, a.group, g, 1)] =
-        l_run == 0.f ? -INFINITY : ((m_run + BELOW) + __builtin_amdgcn_logf(e_run * UNIT)) * 0.69314718055994531f;
+    a.lse[row * a.kv_heads * G + query] = l_run == 0.f ? -INFINITY : ((m_run + BELOW) + __builtin_amdgcn_logf(e_run * UNIT)) * 0.69314718055994531f;
   }
 }
 

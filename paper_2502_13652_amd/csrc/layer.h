@@ -30,9 +30,10 @@ inline bool pieces(int64_t stride) { return stride % 8 == 0; }
 // ---- prompt ----
 typedef void (*PromptKernel)(PromptArgs);
 template <typename E, bool LSE> PromptKernel prompt_kernel(int head_dim) {
-  return head_dim == 64 ? k_prompt<E, 64, 2, 2, LSE> : head_dim == 128 ? k_prompt<E, 128, 2, 2, LSE> : k_prompt<E, 256, 1, 1, LSE>;
+  return head_dim == 64 ? k_prompt<E, 64, 64, 2, 3, LSE> : head_dim == 128 ? k_prompt<E, 128, 128, 2, 2, LSE> : k_prompt<E, 256, 128, 1, 2, LSE>;
 }
 template <typename E> PromptKernel prompt_kernel(int head_dim, bool lse) { return lse ? prompt_kernel<E, true>(head_dim) : prompt_kernel<E, false>(head_dim); }
+inline int prompt_parts(int head_dim) { return head_dim > 128 ? 2 : 1; }    // of an output row
 constexpr int64_t MAX_PROMPT_STRIDE = 1 << 24;
 
 }  // namespace c2t
@@ -128,7 +129,7 @@ int c2t_prompt_attention(const c2t_prompt* p, void* stream) {
   if (p->dtype != C2T_BF16 && p->dtype != C2T_F16) return p->dtype == C2T_F32 ? C2T_ERR_UNSUPPORTED : C2T_ERR_INVALID_ARG;
   if (!p->q || !p->k || !p->v || !p->out || !p->starts || !(p->scale >= 0.f) || p->scale > 1e30f) return C2T_ERR_INVALID_ARG;
   if (p->head_dim != 64 && p->head_dim != 128 && p->head_dim != 256) return C2T_ERR_UNSUPPORTED;
-  if (p->sequences > C2T_MAX_CACHE_BATCH || p->rows > (1 << 24)) return C2T_ERR_UNSUPPORTED;
+  if (p->sequences > C2T_MAX_CACHE_BATCH || p->rows > (1 << 24) || (int64_t)p->rows * (p->q_heads / p->kv_heads) > (1 << 30)) return C2T_ERR_UNSUPPORTED;
   const int64_t q_row = (int64_t)p->q_heads * p->head_dim, k_row = (int64_t)p->kv_heads * p->head_dim;
   if (p->q_stride < q_row || p->out_stride < q_row || p->k_stride < k_row || p->v_stride < k_row) return C2T_ERR_INVALID_ARG;
   for (int64_t s : {p->q_stride, p->k_stride, p->v_stride, p->out_stride}) if (s > MAX_PROMPT_STRIDE || !pieces(s)) return C2T_ERR_UNSUPPORTED;
@@ -138,10 +139,10 @@ int c2t_prompt_attention(const c2t_prompt* p, void* stream) {
   PromptArgs a;
   a.q = (const char*)p->q; a.k = (const char*)p->k; a.v = (const char*)p->v; a.out = (char*)p->out; a.lse = p->lse;
   a.q_row = p->q_stride * 2; a.k_row = p->k_stride * 2; a.v_row = p->v_stride * 2; a.out_row = p->out_stride * 2;
-  a.starts = p->starts; a.rows = p->rows; a.sequences = p->sequences; a.kv_heads = p->kv_heads; a.group = p->q_heads / p->kv_heads;
+  a.starts = p->starts; a.rows = p->rows; a.sequences = p->sequences; a.kv_heads = p->kv_heads; a.group = p->q_heads / p->kv_heads; a.inv_group = 1.f / (float)a.group;
   a.scale_log2e = std::max(p->scale, 1e-30f) * 1.44269504088896341f;       // (a masked score is -infinity times it: not 0)
   // each sequence has one tile at most that it does not fill
-  const int64_t tiles = p->rows / PROMPT_ROWS + std::min(p->sequences, p->rows), units = div_up64(tiles * p->kv_heads, DIES) * DIES, blocks = units * a.group;
+  const int64_t tiles = (int64_t)p->rows * a.group / PROMPT_ROWS + std::min(p->sequences, p->rows), blocks = tiles * p->kv_heads * prompt_parts(p->head_dim);
   if (blocks > MAX_BLOCKS) return C2T_ERR_UNSUPPORTED;
   const PromptKernel fn = p->dtype == C2T_BF16 ? prompt_kernel<Bf16>(p->head_dim, p->lse != nullptr) : prompt_kernel<F16>(p->head_dim, p->lse != nullptr);
   hipLaunchKernelGGL(fn, dim3((unsigned)blocks), dim3(64 * PROMPT_WAVES), 0, (hipStream_t)stream, a);
