@@ -16,10 +16,13 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 struct PromptArgs {
   const char* q; const char* k; const char* v; char* out; float* lse;
   int64_t q_row, k_row, v_row, out_row;                      // bytes
+  float scale_log2e;
+};
+// What finding a tile takes: a kernel's first arguments, which are there when it starts.
+struct PromptShape {
   const int32_t* starts;
   int32_t rows, sequences, kv_heads, group;
-  float inv_group;                                           // 1 / group
-  float scale_log2e;
+  float inv_kv_heads, inv_group;                             // their reciprocals
 };
 
 __device__ __forceinline__ f32x16 product32(Bf16::T8 a, Bf16::T8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
@@ -34,7 +37,7 @@ struct PromptTile { int first, n, tile; };                   // the sequence's f
 // Every wavefront finds it for itself: a lane has every 64th sequence, tiles of a class and above are a sum over lanes.  False: there is no such tile.
 constexpr int TOGETHER = 4;
 template <int ROWS>
-__device__ __forceinline__ bool find_tile(const PromptArgs& a, int rank, PromptTile* u) {
+__device__ __forceinline__ bool find_tile(const PromptShape& a, int rank, PromptTile* u) {
   const int lane = lane_id();
   const auto length = [&](int b, int* first) {
     const int at = min(b, a.sequences - 1), from = a.starts[at], end = a.starts[at + 1];
@@ -45,7 +48,11 @@ __device__ __forceinline__ bool find_tile(const PromptArgs& a, int rank, PromptT
   int first[TOGETHER], n[TOGETHER], has[TOGETHER], left = rank;
   if (a.sequences <= TOGETHER) {
 #pragma unroll
-    for (int i = 0; i < TOGETHER; ++i) { n[i] = length(i, &first[i]); has[i] = tiles(n[i]); }
+    for (int i = 0; i < TOGETHER; ++i) {                     // (the same for all lanes)
+      n[i] = uniform(length(i, &first[i]));
+      first[i] = uniform(first[i]);
+      has[i] = tiles(n[i]);
+    }
   } else {
     int my_first;
     const int my_n = length(lane, &my_first), my_tiles = tiles(my_n);
@@ -151,26 +158,31 @@ template <int PRODUCTS, int READS, int AHEAD, int EACH> __device__ __forceinline
     if (AHEAD + i * EACH < READS) __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
   }
 }
-constexpr int K_AHEAD = 4;
+constexpr int K_AHEAD = 4, V_AHEAD = 2;                      // operands read ahead of their product
 
 // DV of the D elements of an output row are one workgroup's (D, or the half where registers do not hold it all); KB blocks of 32 keys a tile; OCC workgroups a CU.
 template <typename E, int D, int DV, int KB, int OCC, bool LSE>
-__global__ __launch_bounds__(64 * PROMPT_WAVES, OCC) void k_prompt(PromptArgs a) {
+__global__ __launch_bounds__(64 * PROMPT_WAVES, OCC) void k_prompt(const int32_t* starts, int32_t all_rows, int32_t sequences, int32_t kv_heads, int32_t G, float inv_kv_heads,
+                                                                      float inv_group, PromptArgs a) {
   typedef typename E::T T; typedef typename E::T4 T4; typedef typename E::T8 T8;
   constexpr int NT = 64 * PROMPT_WAVES, KT = 32 * KB, PARTS = D / DV, DB = DV / 32, DK = D / 16;
   constexpr int K_LOADS = KT * D / 8 / NT, V_LOADS = KT * DV / 8 / NT, K_TILE = KT * D * 2, TILE = K_TILE + KT * DV * 2;
   constexpr float TOP = E::TOP, SLACK = E::SLACK, BIG = 0x1p22f;
   __shared__ __align__(16) char lds[2 * TILE];               // K and V, two buffers
   __shared__ int odd_value;                                  // a tile held a value that is not finite
-  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, half = lane >> 5, G = a.group;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, half = lane >> 5;
 
   // The query heads of one cached head share its keys: a tile's rows are (token, head of the group) with the head fastest, so that its wavefronts come to their last key together, however
   // many heads there are, and short prompts fill tiles.
+  if (tid == 0) odd_value = 0;
   PromptTile u;
-  const int unit = blockIdx.x / PARTS, part = blockIdx.x % PARTS, head = unit % a.kv_heads;
-  if (!find_tile<PROMPT_ROWS>(a, unit / a.kv_heads, &u)) return;
+  const int part = blockIdx.x % PARTS;
+  int rank, head;
+  split(blockIdx.x / PARTS, kv_heads, inv_kv_heads, &rank, &head);
+  rank = uniform(rank); head = uniform(head);
+  if (!find_tile<PROMPT_ROWS>(PromptShape{starts, all_rows, sequences, kv_heads, G, inv_kv_heads, inv_group}, rank, &u)) return;
   const int row0 = u.tile * PROMPT_ROWS, wave_row0 = row0 + wave * 32, rows = u.n * G;
-  const auto token_of = [&](int row, int* g) { int t; split(min(row, rows - 1), G, a.inv_group, &t, g); return t; };      // (rows behind the last are not put out)
+  const auto token_of = [&](int row, int* g) { int t; split(min(row, rows - 1), G, inv_group, &t, g); return t; };      // (rows behind the last are not put out)
   int my_g, no_g;
   const int my_token = token_of(wave_row0 + col, &my_g);
   const int first_token = uniform(token_of(row0, &no_g)), wave_first = uniform(token_of(wave_row0, &no_g)), wave_last = uniform(token_of(wave_row0 + 31, &no_g));
@@ -232,8 +244,7 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, OCC) void k_prompt(PromptArgs a)
 #pragma unroll
     for (int kk = 0; kk < DK; ++kk) q[kk] = *(const T8*)(from + kk * 32);
   }
-  if (tid == 0) odd_value = 0;
-  __syncthreads();
+  if (KT > first_token) __syncthreads();                     // (odd_value)
   arrived(0, KT > first_token);
   // The queries are here before the loop, or each of its rounds would wait for them, and for the next tile's pieces, which are younger, with them.
 #pragma unroll
@@ -297,9 +308,10 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, OCC) void k_prompt(PromptArgs a)
         for (int i = 0; i < DB * 16; ++i) o[i / 16][i % 16] *= back;
       }
       const float ref = m_run == -INFINITY ? 0.f : m_run;
-      // Weights are made, two at a time, and V's operands read one step of 16 keys ahead of the products that take them: between a step's products there are the next one's
-      // instructions.  The order is the one written here.
-      T8 p[2], v[2][DB];
+      // Products by steps of 16 keys.  Weights are made, two at a time, a step ahead of the products that take them, V's operands read V_AHEAD products ahead: between a step's products
+      // are the next one's instructions, in the order that is written here.
+      constexpr int STEPS = KB * 2;
+      T8 p[2], v[STEPS * DB];
       const auto weights = [&](int h, int pair) {
 #pragma unroll
         for (int r = pair * 2; r < pair * 2 + 2; ++r) {
@@ -309,29 +321,28 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, OCC) void k_prompt(PromptArgs a)
         }
         l_run = add_pair(p[h & 1], pair, l_run);
       };
-      const auto read_v = [&](int h, int d) {
+      const auto read_v = [&](int i) {
+        const int h = i / DB, d = i % DB;
         typedef __attribute__((address_space(3))) s16x4* lds4;
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(lds + (v_base ^ d * 64) + h * 16 * (DV * 2)));
         const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(lds + (v_base ^ (d * 64 + 32)) + (h * 16 + 8) * (DV * 2)));
         struct { s16x4 a, b; } both{lo, hi};
-        v[h & 1][d] = __builtin_bit_cast(T8, both);
+        v[i] = __builtin_bit_cast(T8, both);
       };
 #pragma unroll
-      for (int d = 0; d < DB; ++d) read_v(0, d);
+      for (int i = 0; i < V_AHEAD; ++i) read_v(i);
 #pragma unroll
       for (int pair = 0; pair < 4; ++pair) weights(0, pair);
 #pragma unroll
-      for (int h = 0; h < KB * 2; ++h)
+      for (int i = 0; i < STEPS * DB; ++i) {
+        const int h = i / DB, d = i % DB;
+        __builtin_amdgcn_sched_barrier(0);
+        o[d] = product32(v[i], p[h & 1], o[d]);
+        if (i + V_AHEAD < STEPS * DB) read_v(i + V_AHEAD);
+        if (h + 1 < STEPS)
 #pragma unroll
-        for (int d = 0; d < DB; ++d) {
-          __builtin_amdgcn_sched_barrier(0);
-          o[d] = product32(v[h & 1][d], p[h & 1], o[d]);
-          if (h + 1 < KB * 2) {
-            read_v(h + 1, d);
-#pragma unroll
-            for (int pair = d * 4 / DB; pair < (d + 1) * 4 / DB; ++pair) weights(h + 1, pair);
-          }
-        }
+          for (int pair = d * 4 / DB; pair < (d + 1) * 4 / DB; ++pair) weights(h + 1, pair);
+      }
     }
     if (t + 1 < n_tiles) arrived(buffer ^ 1, key0 + 2 * KT > first_token);
     __syncthreads();
@@ -341,50 +352,75 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, OCC) void k_prompt(PromptArgs a)
   if (idle) return;
   l_run += __shfl_xor(l_run, 32); e_run += __shfl_xor(e_run, 32);
 
-  if (odd_value != 0) {                                    // values that are not finite: a weight is made again from its key
+  if (odd_value != 0) {                                      // values that are not finite: a weight is made again from its key
+    const char* const k_odd = k_head + half * 16;
+    const char* const v_odd = v_head + half * 8;
     for (int key = first_token / KT * KT; key <= wave_last; ++key) {
-      const char* const v = v_head + key * a.v_row;
-      T4 x[DB * 4];
+      const auto value = [&](int d) { return *(const T4*)(v_odd + key * a.v_row + d * 16); };
       bool any = false;
-#pragma unroll
       for (int d = 0; d < DB * 4; ++d) {
-        x[d] = *(const T4*)(v + d * 16 + half * 8);
+        const T4 x = value(d);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) any = any || !(__builtin_fabsf((float)x[d][r]) < INFINITY);
+        for (int r = 0; r < 4; ++r) any = any || !(__builtin_fabsf((float)x[r]) < INFINITY);
       }
       if (!__any(any)) continue;
       float dot = 0.f;
 #pragma unroll
       for (int kk = 0; kk < DK; ++kk) {
-        const T8 y = *(const T8*)(k_head + key * a.k_row + kk * 32 + half * 16);
+        __builtin_amdgcn_sched_barrier(0);                   // (one piece at a time, and none made ahead of the loop: this is rare, and the loop above has the registers)
+        u32x4 mine = __builtin_bit_cast(u32x4, q[kk]);
+        settle(mine);
+        const T8 x = __builtin_bit_cast(T8, mine);
+        const T8 y = *(const T8*)(k_odd + key * a.k_row + kk * 32);
 #pragma unroll
-        for (int r = 0; r < 8; ++r) dot = __builtin_fmaf((float)y[r], (float)q[kk][r], dot);
+        for (int r = 0; r < 8; ++r) dot = __builtin_fmaf((float)y[r], (float)x[r], dot);
       }
       dot += __shfl_xor(dot, 32);
       const float w = __builtin_amdgcn_exp2f(rounded_difference(dot, a.scale_log2e, m_run == -INFINITY ? 0.f : m_run));
       if (key > my_token) continue;
 #pragma unroll
-      for (int d = 0; d < DB * 4; ++d)
+      for (int d = 0; d < DB * 4; ++d) {
+        __builtin_amdgcn_sched_barrier(0);
+        const T4 x = value(d);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) { const float y = (float)x[d][r]; if (!(__builtin_fabsf(y) < INFINITY)) o[d / 4][d % 4 * 4 + r] += w * y; }
+        for (int r = 0; r < 4; ++r) { const float y = (float)x[r]; if (!(__builtin_fabsf(y) < INFINITY)) o[d / 4][d % 4 * 4 + r] += w * y; }
+      }
     }
   }
-  if (wave_row0 + col >= rows) return;
-  const int64_t row = (int64_t)u.first + my_token, query = query_offset(head, G, my_g, 1);
-  char* const out = a.out + row * a.out_row + query * (D * 2) + part * (DV * 2) + half * 8;
-  const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
-#pragma unroll
-  for (int d = 0; d < DB * 4; ++d) {
-    T4 y;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) y[r] = (T)(o[d / 4][d % 4 * 4 + r] * inv);
-    *(T4*)(out + d * 16) = y;
-  }
-  if (LSE && half == 0 && part == 0) {
+  if (LSE && half == 0 && part == 0 && wave_row0 + col < rows) {
     // of a sum as if the reference were the largest score (k_attend.h)
     constexpr float BELOW = TOP - SLACK;
     const float UNIT = __builtin_ldexpf(1.f, -(int)BELOW);
-    a.lse[row * a.kv_heads * G + query] = l_run == 0.f ? -INFINITY : ((m_run + BELOW) + __builtin_amdgcn_logf(e_run * UNIT)) * 0.69314718055994531f;
+    a.lse[((int64_t)u.first + my_token) * kv_heads * G + query_offset(head, G, my_g, 1)] =
+        l_run == 0.f ? -INFINITY : ((m_run + BELOW) + __builtin_amdgcn_logf(e_run * UNIT)) * 0.69314718055994531f;
+  }
+  // Out by whole lines: 64 elements of the wavefront's 32 rows at a time pass through LDS, in its own pieces of a tile (4 stretches of 1024 bytes).  A row's pieces of 16
+  // bytes change places so that 8 rows' fall on different banks.
+  const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
+  const auto place = [&](int row, int piece) { const int at = row * 128 + (piece ^ (row & 7)) * 16; return at / 1024 * (NT * 16) + wave * 1024 + at % 1024; };
+  char* to[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    int g;
+    const int t = token_of(wave_row0 + i * 8 + lane / 8, &g);
+    to[i] = a.out + ((int64_t)u.first + t) * a.out_row + query_offset(head, G, g, D) * 2 + part * (DV * 2) + lane % 8 * 16;
+  }
+#pragma unroll
+  for (int d0 = 0; d0 < DB; d0 += 2) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      T4 y;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) y[r] = (T)(o[d0 + i / 4][i % 4 * 4 + r] * inv);
+      *(T4*)(lds + place(col, i) + half * 8) = y;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront"); __builtin_amdgcn_wave_barrier(); __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    u32x4 x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = *(const u32x4*)(lds + place(i * 8 + lane / 8, lane % 8));
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront"); __builtin_amdgcn_wave_barrier(); __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+    for (int i = 0; i < 4; ++i) if (wave_row0 + i * 8 + lane / 8 < rows) *(u32x4*)(to[i] + d0 * 64) = x[i];
   }
 }
 

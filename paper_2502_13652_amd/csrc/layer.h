@@ -28,9 +28,9 @@ template <typename T, bool E4> NormShape norm_kernel(int width) {
 inline bool pieces(int64_t stride) { return stride % 8 == 0; }
 
 // ---- prompt ----
-typedef void (*PromptKernel)(PromptArgs);
+typedef void (*PromptKernel)(const int32_t*, int32_t, int32_t, int32_t, int32_t, float, float, PromptArgs);
 template <typename E, bool LSE> PromptKernel prompt_kernel(int head_dim) {
-  return head_dim == 64 ? k_prompt<E, 64, 64, 2, 3, LSE> : head_dim == 128 ? k_prompt<E, 128, 128, 2, 2, LSE> : k_prompt<E, 256, 128, 1, 2, LSE>;
+  return head_dim == 64 ? k_prompt<E, 64, 64, 2, 4, LSE> : head_dim == 128 ? k_prompt<E, 128, 128, 1, 3, LSE> : k_prompt<E, 256, 128, 1, 2, LSE>;
 }
 template <typename E> PromptKernel prompt_kernel(int head_dim, bool lse) { return lse ? prompt_kernel<E, true>(head_dim) : prompt_kernel<E, false>(head_dim); }
 inline int prompt_parts(int head_dim) { return head_dim > 128 ? 2 : 1; }    // of an output row
@@ -139,13 +139,14 @@ int c2t_prompt_attention(const c2t_prompt* p, void* stream) {
   PromptArgs a;
   a.q = (const char*)p->q; a.k = (const char*)p->k; a.v = (const char*)p->v; a.out = (char*)p->out; a.lse = p->lse;
   a.q_row = p->q_stride * 2; a.k_row = p->k_stride * 2; a.v_row = p->v_stride * 2; a.out_row = p->out_stride * 2;
-  a.starts = p->starts; a.rows = p->rows; a.sequences = p->sequences; a.kv_heads = p->kv_heads; a.group = p->q_heads / p->kv_heads; a.inv_group = 1.f / (float)a.group;
+  const int group = p->q_heads / p->kv_heads;
   a.scale_log2e = std::max(p->scale, 1e-30f) * 1.44269504088896341f;       // (a masked score is -infinity times it: not 0)
   // each sequence has one tile at most that it does not fill
-  const int64_t tiles = (int64_t)p->rows * a.group / PROMPT_ROWS + std::min(p->sequences, p->rows), blocks = tiles * p->kv_heads * prompt_parts(p->head_dim);
+  const int64_t tiles = (int64_t)p->rows * group / PROMPT_ROWS + std::min(p->sequences, p->rows), blocks = tiles * p->kv_heads * prompt_parts(p->head_dim);
   if (blocks > MAX_BLOCKS) return C2T_ERR_UNSUPPORTED;
   const PromptKernel fn = p->dtype == C2T_BF16 ? prompt_kernel<Bf16>(p->head_dim, p->lse != nullptr) : prompt_kernel<F16>(p->head_dim, p->lse != nullptr);
-  hipLaunchKernelGGL(fn, dim3((unsigned)blocks), dim3(64 * PROMPT_WAVES), 0, (hipStream_t)stream, a);
+  hipLaunchKernelGGL(fn, dim3((unsigned)blocks), dim3(64 * PROMPT_WAVES), 0, (hipStream_t)stream, p->starts, p->rows, p->sequences, p->kv_heads, group, 1.f / (float)p->kv_heads,
+                     1.f / (float)group, a);
   return hip_status();
 }
 
