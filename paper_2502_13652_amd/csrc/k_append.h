@@ -34,36 +34,64 @@ __device__ __forceinline__ void sine_cosine(uint32_t fraction, float* sine, floa
   *cosine = ((quarter + 1u) & 2u) ? -b : b;
 }
 
-// The sequence that packed row `row` is in, and which of its tokens it is; -1: none.  Two trips to memory: every 64th (or so) start, then the ones between.
+// The sequence that packed row `row` is in, and which of its tokens it is; -1: none.  A trip to memory, of more than 64 sequences two: every 64th (or so) start, then the ones between.
 __device__ __forceinline__ int sequence_of_row(const int32_t* starts, int n, int row, int* t) {
   const int lane = lane_id(), step = div_up(n, WAVE);
-  const auto below = [&](int i, int end) { return __popcll(__ballot(i < end && starts[min(i, n)] <= row)); };
-  const int first = (below(lane * step, n) - 1) * step;
-  if (first < 0) return -1;
-  const int b = first + below(first + lane, min(first + step, n)) - 1;
-  if (b < first) return -1;                                  // (starts that fall)
-  const int from = uniform(starts[b]), end = uniform(starts[b + 1]);
-  if (row < from || row >= end || from < 0) return -1;
-  *t = row - from;
-  return b;
+  int first = 0, end = n;
+  if (step > 1) {
+    first = (__popcll(__ballot(lane * step < n && starts[min(lane * step, n)] <= row)) - 1) * step;
+    if (first < 0) return -1;
+    end = min(first + step, n);
+  }
+  const int i = min(first + lane, n - 1), from = starts[i], to = starts[i + 1];
+  const int at = __popcll(__ballot(first + lane < end && from <= row)) - 1;
+  if (at < 0) return -1;                                     // (ahead of the first; or starts that fall)
+  const int my_from = __builtin_amdgcn_readlane(from, at), my_to = __builtin_amdgcn_readlane(to, at);
+  if (my_from < 0 || row < my_from || row >= my_to) return -1;
+  *t = row - my_from;
+  return first + at;
 }
 
 // A wavefront has a token, or one of `parts` shares of its heads.  A lane has 16 elements of a head, 8 pairs of them or 16 that only move, and keeps its pairs' sines for
-// all heads that it comes to.
+// all heads that it comes to.  Heads' elements are asked for PASSES passes at a time, the first ahead of where they go, which takes four trips to memory that wait for each other.
 template <typename T>
 __global__ __launch_bounds__(CACHE_NT) void k_cache_append(CacheView c, AppendArgs a) {
+  constexpr int PASSES = 3;
   const int lane = lane_id(), wave = uniform((int)threadIdx.x >> 6);
-  const int64_t item = (int64_t)blockIdx.x * (CACHE_NT / WAVE) + wave;
-  const int row = (int)(item / a.parts), part = (int)(item % a.parts);
+  const int item = blockIdx.x * (CACHE_NT / WAVE) + wave;    // (below 2^31: the host has seen to it)
+  const int row = item / a.parts, part = item % a.parts;
   if (row >= a.slots) return;
   int b = blockIdx.y, t = row;
-  int64_t batch = b;                                         // for the strides
+  if (a.n_new && t >= a.n_new[b]) return;
+  const int64_t batch = a.starts ? 0 : b;                    // for the strides
+  const char* const q = a.q + batch * a.q_batch + row * a.q_token;
+  const char* const k = a.k + batch * a.kv_batch + row * a.kv_token;
+  const char* const v = a.v + batch * a.kv_batch + row * a.kv_token;
+
+  const int per_head = c.head_dim / 16, p = lane % per_head, at_once = WAVE / per_head;
+  const bool turned = p * 8 < a.pairs;
+  const int first = (turned && !a.neighbours ? p * 8 : p * 16) * 2;                            // bytes of the lane's two pieces of 8 elements
+  const int second = turned && !a.neighbours ? first + a.pairs * 2 : first + 16;
+  const int total = a.q_heads + 2 * c.kv_heads, each = a.parts * at_once;                      // queries, keys, values
+  int h0 = part * at_once + lane / per_head;
+  Eight<T> x[PASSES], y[PASSES];
+  const auto load = [&]() {
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+      const int h = h0 + i * each;
+      if (h >= total) continue;
+      const char* const from = h < a.q_heads ? q + h * (c.head_dim * 2) : h < a.q_heads + c.kv_heads ? k + (h - a.q_heads) * (c.head_dim * 2) : v + (h - a.q_heads - c.kv_heads) * (c.head_dim * 2);
+      x[i] = *(const Eight<T>*)(from + first); y[i] = *(const Eight<T>*)(from + second);
+    }
+  };
+  load();
+  uint64_t turns[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) turns[j] = turned ? a.turns[p * 8 + j] : 0ull;
+
   if (a.starts) {
     b = sequence_of_row(a.starts, c.batch, row, &t);
     if (b < 0) return;
-    batch = 0;
-  } else {
-    if (a.n_new && t >= a.n_new[b]) return;
   }
   const int len = tokens_in_cache(c, c.length[b]);
   const int64_t at = (int64_t)len + t;
@@ -78,56 +106,50 @@ __global__ __launch_bounds__(CACHE_NT) void k_cache_append(CacheView c, AppendAr
     else if (c.refcount[page] > 1) { why = CACHE_SHARED; page = -1; }
   }
   if (why && lane == 0 && part == 0) report(c, b, why);
-  const int row_in = (int)(at & ((1 << c.page_shift) - 1));
-
-  const int chain = a.slots - a.nodes;
+  const int row_in = (int)(at & ((1 << c.page_shift) - 1)), chain = a.slots - a.nodes;
   int64_t position = at;
   if (a.nodes > 0 && t >= chain) position = (int64_t)len + chain - 1 + a.position[(int64_t)b * a.nodes + (t - chain)];
-
-  const int per_head = c.head_dim / 16, p = lane % per_head, heads_at_once = WAVE / per_head;
-  const bool turned = p * 8 < a.pairs;
-  const int first = (turned && !a.neighbours ? p * 8 : p * 16) * 2;                            // bytes of the lane's two pieces of 8 elements
-  const int second = turned && !a.neighbours ? first + a.pairs * 2 : first + 16;
   float sine[8], cosine[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const uint64_t angle = turned ? (uint64_t)position * a.turns[p * 8 + j] : 0ull;
-    sine_cosine((uint32_t)((angle + 0x80000000ull) >> 32), &sine[j], &cosine[j]);
+    sine_cosine((uint32_t)(((uint64_t)position * turns[j] + 0x80000000ull) >> 32), &sine[j], &cosine[j]);
     const float m = turned ? a.magnitude : 1.f;
     sine[j] *= m; cosine[j] *= m;
   }
-  const char* const q = a.q + batch * a.q_batch + row * a.q_token;
-  const char* const k = a.k + batch * a.kv_batch + row * a.kv_token;
-  const char* const v = a.v + batch * a.kv_batch + row * a.kv_token;
   char* const q_out = a.q_out + batch * a.q_out_batch + row * a.q_out_token;
   char* const k_out = a.k_out ? a.k_out + batch * a.k_out_batch + row * a.k_out_token : nullptr;
-  const int total = a.q_heads + 2 * c.kv_heads;              // queries, keys, values
-  for (int h = part * heads_at_once + lane / per_head; h < total; h += a.parts * heads_at_once) {
-    const bool is_q = h < a.q_heads, is_v = h >= a.q_heads + c.kv_heads;
-    const int head = is_q ? h : is_v ? h - a.q_heads - c.kv_heads : h - a.q_heads;
-    const char* from = (is_q ? q : is_v ? v : k) + (int64_t)head * c.head_dim * 2;
-    Eight<T> x = *(const Eight<T>*)(from + first), y = *(const Eight<T>*)(from + second);
-    if (turned && !is_v) {
-      if (a.neighbours) {
+  for (; h0 - lane / per_head < total; h0 += PASSES * each) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          T& ra = j < 4 ? x.v[2 * j] : y.v[2 * j - 8];
-          T& rb = j < 4 ? x.v[2 * j + 1] : y.v[2 * j - 7];
-          const float f = (float)ra, g = (float)rb;
-          ra = (T)__builtin_fmaf(f, cosine[j], -(g * sine[j])); rb = (T)__builtin_fmaf(f, sine[j], g * cosine[j]);
-        }
-      } else {
+    for (int i = 0; i < PASSES; ++i) {
+      const int h = h0 + i * each;
+      if (h >= total) continue;
+      const bool is_q = h < a.q_heads, is_v = h >= a.q_heads + c.kv_heads;
+      const int head = is_q ? h : is_v ? h - a.q_heads - c.kv_heads : h - a.q_heads;
+      if (turned && !is_v) {
+        if (a.neighbours) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float f = (float)x.v[j], g = (float)y.v[j];
-          x.v[j] = (T)__builtin_fmaf(f, cosine[j], -(g * sine[j])); y.v[j] = (T)__builtin_fmaf(f, sine[j], g * cosine[j]);
+          for (int j = 0; j < 8; ++j) {
+            T& ra = j < 4 ? x[i].v[2 * j] : y[i].v[2 * j - 8];
+            T& rb = j < 4 ? x[i].v[2 * j + 1] : y[i].v[2 * j - 7];
+            const float f = (float)ra, g = (float)rb;
+            ra = (T)__builtin_fmaf(f, cosine[j], -(g * sine[j])); rb = (T)__builtin_fmaf(f, sine[j], g * cosine[j]);
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float f = (float)x[i].v[j], g = (float)y[i].v[j];
+            x[i].v[j] = (T)__builtin_fmaf(f, cosine[j], -(g * sine[j])); y[i].v[j] = (T)__builtin_fmaf(f, sine[j], g * cosine[j]);
+          }
         }
       }
+      const auto put = [&](char* to) { *(Eight<T>*)(to + first) = x[i]; *(Eight<T>*)(to + second) = y[i]; };
+      if (is_q) { put(q_out + head * (c.head_dim * 2)); continue; }
+      if (!is_v && k_out) put(k_out + head * (c.head_dim * 2));
+      if (page >= 0) put((is_v ? c.v : c.k) + row_offset(c, a.layer, page, head, row_in) * 2);
     }
-    const auto put = [&](char* to) { *(Eight<T>*)(to + first) = x; *(Eight<T>*)(to + second) = y; };
-    if (is_q) { put(q_out + (int64_t)head * c.head_dim * 2); continue; }
-    if (!is_v && k_out) put(k_out + (int64_t)head * c.head_dim * 2);
-    if (page >= 0) put((is_v ? c.v : c.k) + row_offset(c, a.layer, page, head, row_in) * 2);
+    if (h0 + PASSES * each - lane / per_head < total) {
+      h0 += PASSES * each; load(); h0 -= PASSES * each;
+    }
   }
 }
 

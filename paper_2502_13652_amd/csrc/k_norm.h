@@ -19,34 +19,35 @@ struct NormArgs {
   int32_t rows, width;
   int32_t block;                                             // elements a scale; 0: the row
   bool weight_f32, residual_f32;
-  bool aligned;                                              // pieces of 8 elements of all arrays are 16-byte aligned (8 for 8 bits), the width a multiple
   float eps;
 };
 
-// 8 elements of a row from `e` on; behind the row's end zeros
-template <typename T>
-__device__ __forceinline__ void load_eight(const char* row, int e, int width, bool aligned, float (&to)[8]) {
-  const T* p = (const T*)row + e;
-  if (aligned) {
+// Which elements of a row the eight of a thread's piece are: next to each other from `first` on, or `step` apart, so that a wavefront's lanes have neighbours: what rows that are not
+// made of aligned pieces are loaded and stored by.
+template <bool WHOLE> struct Piece { int first, step; };
+template <typename T, bool WHOLE>
+__device__ __forceinline__ void load_eight(const char* row, const Piece<WHOLE>& e, int width, float (&to)[8]) {
+  const T* p = (const T*)row + e.first;
+  if (WHOLE) {
     const Eight<T> x = *(const Eight<T>*)p;
 #pragma unroll
     for (int j = 0; j < 8; ++j) to[j] = (float)x.v[j];
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) to[j] = e + j < width ? (float)p[j] : 0.f;
+    for (int j = 0; j < 8; ++j) to[j] = e.first + j * e.step < width ? (float)p[j * e.step] : 0.f;      // (zeros behind the row's end)
   }
 }
-template <typename T>
-__device__ __forceinline__ void store_eight(char* row, int e, int width, bool aligned, const float (&from)[8]) {
-  T* p = (T*)row + e;
-  if (aligned) {
+template <typename T, bool WHOLE>
+__device__ __forceinline__ void store_eight(char* row, const Piece<WHOLE>& e, int width, const float (&from)[8]) {
+  T* p = (T*)row + e.first;
+  if (WHOLE) {
     Eight<T> x;
 #pragma unroll
     for (int j = 0; j < 8; ++j) x.v[j] = (T)from[j];
     *(Eight<T>*)p = x;
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) if (e + j < width) p[j] = (T)from[j];
+    for (int j = 0; j < 8; ++j) if (e.first + j * e.step < width) p[j * e.step] = (T)from[j];
   }
 }
 // four numbers as e4m3, to nearest even; a NaN stays one, and none is above 448 but by an fp32 rounding
@@ -65,8 +66,8 @@ __device__ __forceinline__ float group_max(float v, int lanes) {
   return v;
 }
 
-// NT threads a row, which has at most 8 CH of its elements each.
-template <typename T, bool E4, int NT, int CH>
+// NT threads a row, which has at most 8 CH of its elements each.  WHOLE: rows are made of pieces that are aligned.
+template <typename T, bool E4, int NT, int CH, bool WHOLE>
 __global__ __launch_bounds__(NT < NORM_NT ? NORM_NT : NT) void k_rms_norm(NormArgs a) {
   constexpr int ROWS = NT < NORM_NT ? NORM_NT / NT : 1, WAVES = NT / WAVE;
   static_assert(NT == WAVE || ROWS == 1, "a wavefront a row, or the workgroup");
@@ -75,27 +76,26 @@ __global__ __launch_bounds__(NT < NORM_NT ? NORM_NT : NT) void k_rms_norm(NormAr
   const int t = threadIdx.x % NT, wave = t / WAVE;
   const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / NT;
   if (row >= a.rows) return;                                 // (wavefronts of a workgroup that meet have the same row)
-  const char* x = a.x + row * a.x_row;
+  const bool apart = !WHOLE && !(E4 && a.block != 0);        // (a block's largest is looked for among neighbouring pieces)
+  const auto piece = [&](int c) { return apart ? Piece<WHOLE>{c * 8 * NT + t, NT} : Piece<WHOLE>{(c * NT + t) * 8, 1}; };
   float h[CH][8];
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
-    const int e = (c * NT + t) * 8;
 #pragma unroll
     for (int j = 0; j < 8; ++j) h[c][j] = 0.f;
-    if (e < a.width) load_eight<T>(x, e, a.width, a.aligned, h[c]);
+    if (piece(c).first < a.width) load_eight<T>(a.x + row * a.x_row, piece(c), a.width, h[c]);
   }
   if (a.residual) {
-    const char* res = a.residual + row * a.residual_row;
-    char* to = a.residual_out + row * a.residual_out_row;
+    const char* const from = a.residual + row * a.residual_row;
+    char* const to = a.residual_out + row * a.residual_out_row;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      const int e = (c * NT + t) * 8;
-      if (e >= a.width) continue;
+      if (piece(c).first >= a.width) continue;
       float r[8];
-      if (a.residual_f32) load_eight<float>(res, e, a.width, a.aligned, r); else load_eight<T>(res, e, a.width, a.aligned, r);
+      if (a.residual_f32) load_eight<float>(from, piece(c), a.width, r); else load_eight<T>(from, piece(c), a.width, r);
 #pragma unroll
       for (int j = 0; j < 8; ++j) h[c][j] += r[j];
-      if (a.residual_f32) store_eight<float>(to, e, a.width, a.aligned, h[c]); else store_eight<T>(to, e, a.width, a.aligned, h[c]);
+      if (a.residual_f32) store_eight<float>(to, piece(c), a.width, h[c]); else store_eight<T>(to, piece(c), a.width, h[c]);
     }
   }
   double sum = 0.;
@@ -109,7 +109,7 @@ __global__ __launch_bounds__(NT < NORM_NT ? NORM_NT : NT) void k_rms_norm(NormAr
     __syncthreads();
     sum = 0.;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) sum += sums[w];
+    for (int i = 0; i < WAVES; ++i) sum += sums[i];
   }
   const double r = 1. / sqrt(sum / (double)a.width + (double)a.eps);
   int power;
@@ -118,16 +118,15 @@ __global__ __launch_bounds__(NT < NORM_NT ? NORM_NT : NT) void k_rms_norm(NormAr
   float top = 0.f;
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
-    const int e = (c * NT + t) * 8;
-    if (e >= a.width) continue;
+    if (piece(c).first >= a.width) continue;
     float w[8];
-    if (a.weight_f32) load_eight<float>(a.weight, e, a.width, a.aligned, w); else load_eight<T>(a.weight, e, a.width, a.aligned, w);
+    if (a.weight_f32) load_eight<float>(a.weight, piece(c), a.width, w); else load_eight<T>(a.weight, piece(c), a.width, w);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       h[c][j] = ldexpf(h[c][j], power) * part * w[j];
       if (E4) top = fmaxf(top, __builtin_fabsf(h[c][j]));
     }
-    if (!E4) store_eight<T>(a.out + row * a.out_row, e, a.width, a.aligned, h[c]);
+    if (!E4) store_eight<T>(a.out + row * a.out_row, piece(c), a.width, h[c]);
   }
   if constexpr (E4) {
     if (a.block == 0) {
@@ -136,12 +135,12 @@ __global__ __launch_bounds__(NT < NORM_NT ? NORM_NT : NT) void k_rms_norm(NormAr
         if (t % WAVE == 0) tops[wave] = top;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, tops[w]);
+        for (int i = 0; i < WAVES; ++i) top = fmaxf(top, tops[i]);
       }
     }
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      const int e = (c * NT + t) * 8;
+      const Piece<WHOLE> e = piece(c);
       float m = top;
       if (a.block != 0) {
         m = 0.f;
@@ -149,19 +148,19 @@ __global__ __launch_bounds__(NT < NORM_NT ? NORM_NT : NT) void k_rms_norm(NormAr
         for (int j = 0; j < 8; ++j) m = fmaxf(m, __builtin_fabsf(h[c][j]));      // (zeros behind the row's end)
         m = group_max(m, a.block / 8);
       }
-      if (e >= a.width) continue;
+      if (e.first >= a.width) continue;
       const float scale = m == 0.f ? 1.f : fmaxf(m / E4M3_MAX, 0x1p-126f);
-      if (a.block == 0 ? c == 0 && t == 0 : e % a.block == 0) a.scales[row * a.scales_row + (a.block == 0 ? 0 : e / a.block)] = scale;
+      if (a.block == 0 ? c == 0 && t == 0 : e.first % a.block == 0) a.scales[row * a.scales_row + (a.block == 0 ? 0 : e.first / a.block)] = scale;
       const float inv = 1.f / scale;
       uint2 y;
       y.x = four_e4m3(h[c][0] * inv, h[c][1] * inv, h[c][2] * inv, h[c][3] * inv);
       y.y = four_e4m3(h[c][4] * inv, h[c][5] * inv, h[c][6] * inv, h[c][7] * inv);
-      char* to = a.out + row * a.out_row + e;
-      if (a.aligned) {
+      char* const to = a.out + row * a.out_row + e.first;
+      if (WHOLE) {
         *(uint2*)to = y;
       } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) if (e + j < a.width) to[j] = (char)((j < 4 ? y.x : y.y) >> (j % 4 * 8));
+        for (int j = 0; j < 8; ++j) if (e.first + j * e.step < a.width) to[j * e.step] = (char)((j < 4 ? y.x : y.y) >> (j % 4 * 8));
       }
     }
   }
