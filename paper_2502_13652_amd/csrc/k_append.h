@@ -53,10 +53,10 @@ __device__ __forceinline__ int sequence_of_row(const int32_t* starts, int n, int
 }
 
 // A wavefront has a token, or one of `parts` shares of its heads.  A lane has 16 elements of a head, 8 pairs of them or 16 that only move, and keeps its pairs' sines for
-// all heads that it comes to.  Heads' elements are asked for PASSES passes at a time, the first ahead of where they go, which takes four trips to memory that wait for each other.
+// all heads that it comes to.  A pass's elements are asked for a pass ahead, the first ones ahead of where they go, which takes four trips to memory that wait for each
+// other; without a condition (lanes behind the last head take its), or what some lanes leave alone would be waited for at once.
 template <typename T>
 __global__ __launch_bounds__(CACHE_NT) void k_cache_append(CacheView c, AppendArgs a) {
-  constexpr int PASSES = 3;
   const int lane = lane_id(), wave = uniform((int)threadIdx.x >> 6);
   const int item = blockIdx.x * (CACHE_NT / WAVE) + wave;    // (below 2^31: the host has seen to it)
   const int row = item / a.parts, part = item % a.parts;
@@ -68,26 +68,22 @@ __global__ __launch_bounds__(CACHE_NT) void k_cache_append(CacheView c, AppendAr
   const char* const k = a.k + batch * a.kv_batch + row * a.kv_token;
   const char* const v = a.v + batch * a.kv_batch + row * a.kv_token;
 
-  const int per_head = c.head_dim / 16, p = lane % per_head, at_once = WAVE / per_head;
+  const int per_head = c.head_dim / 16, p = lane % per_head, at_once = WAVE / per_head, head_bytes = c.head_dim * 2;
   const bool turned = p * 8 < a.pairs;
   const int first = (turned && !a.neighbours ? p * 8 : p * 16) * 2;                            // bytes of the lane's two pieces of 8 elements
   const int second = turned && !a.neighbours ? first + a.pairs * 2 : first + 16;
-  const int total = a.q_heads + 2 * c.kv_heads, each = a.parts * at_once;                      // queries, keys, values
-  int h0 = part * at_once + lane / per_head;
-  Eight<T> x[PASSES], y[PASSES];
-  const auto load = [&]() {
-#pragma unroll
-    for (int i = 0; i < PASSES; ++i) {
-      const int h = h0 + i * each;
-      if (h >= total) continue;
-      const char* const from = h < a.q_heads ? q + h * (c.head_dim * 2) : h < a.q_heads + c.kv_heads ? k + (h - a.q_heads) * (c.head_dim * 2) : v + (h - a.q_heads - c.kv_heads) * (c.head_dim * 2);
-      x[i] = *(const Eight<T>*)(from + first); y[i] = *(const Eight<T>*)(from + second);
-    }
+  const int total = a.q_heads + 2 * c.kv_heads, each = a.parts * at_once, h0 = part * at_once;  // queries, keys, values
+  typedef Eight<T> Piece;
+  const auto load = [&](int h, Piece* x, Piece* y) {
+    h = min(h + lane / per_head, total - 1);
+    const char* const from = h < a.q_heads ? q + h * head_bytes : h < a.q_heads + c.kv_heads ? k + (h - a.q_heads) * head_bytes : v + (h - a.q_heads - c.kv_heads) * head_bytes;
+    *x = *(const Piece*)(from + first); *y = *(const Piece*)(from + second);
   };
-  load();
+  Piece x, y, x_next, y_next;
+  load(h0, &x, &y);
   uint64_t turns[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) turns[j] = turned ? a.turns[p * 8 + j] : 0ull;
+  for (int j = 0; j < 8; ++j) turns[j] = a.turns[min(p * 8, a.pairs - 8) + j];
 
   if (a.starts) {
     b = sequence_of_row(a.starts, c.batch, row, &t);
@@ -113,43 +109,45 @@ __global__ __launch_bounds__(CACHE_NT) void k_cache_append(CacheView c, AppendAr
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     sine_cosine((uint32_t)(((uint64_t)position * turns[j] + 0x80000000ull) >> 32), &sine[j], &cosine[j]);
-    const float m = turned ? a.magnitude : 1.f;
-    sine[j] *= m; cosine[j] *= m;
+    sine[j] *= a.magnitude; cosine[j] *= a.magnitude;
   }
   char* const q_out = a.q_out + batch * a.q_out_batch + row * a.q_out_token;
   char* const k_out = a.k_out ? a.k_out + batch * a.k_out_batch + row * a.k_out_token : nullptr;
-  for (; h0 - lane / per_head < total; h0 += PASSES * each) {
-#pragma unroll
-    for (int i = 0; i < PASSES; ++i) {
-      const int h = h0 + i * each;
-      if (h >= total) continue;
+  char* const k_page = c.k + row_offset(c, a.layer, max(page, 0), 0, row_in) * 2;
+  char* const v_page = c.v + row_offset(c, a.layer, max(page, 0), 0, row_in) * 2;
+  const int page_head = head_bytes << c.page_shift;
+  for (int h1 = h0; h1 < total; h1 += each) {
+    load(h1 + each, &x_next, &y_next);
+    const int h = h1 + lane / per_head;
+    if (h < total) {
       const bool is_q = h < a.q_heads, is_v = h >= a.q_heads + c.kv_heads;
       const int head = is_q ? h : is_v ? h - a.q_heads - c.kv_heads : h - a.q_heads;
       if (turned && !is_v) {
         if (a.neighbours) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            T& ra = j < 4 ? x[i].v[2 * j] : y[i].v[2 * j - 8];
-            T& rb = j < 4 ? x[i].v[2 * j + 1] : y[i].v[2 * j - 7];
+            T& ra = j < 4 ? x.v[2 * j] : y.v[2 * j - 8];
+            T& rb = j < 4 ? x.v[2 * j + 1] : y.v[2 * j - 7];
             const float f = (float)ra, g = (float)rb;
             ra = (T)__builtin_fmaf(f, cosine[j], -(g * sine[j])); rb = (T)__builtin_fmaf(f, sine[j], g * cosine[j]);
           }
         } else {
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            const float f = (float)x[i].v[j], g = (float)y[i].v[j];
-            x[i].v[j] = (T)__builtin_fmaf(f, cosine[j], -(g * sine[j])); y[i].v[j] = (T)__builtin_fmaf(f, sine[j], g * cosine[j]);
+            const float f = (float)x.v[j], g = (float)y.v[j];
+            x.v[j] = (T)__builtin_fmaf(f, cosine[j], -(g * sine[j])); y.v[j] = (T)__builtin_fmaf(f, sine[j], g * cosine[j]);
           }
         }
       }
-      const auto put = [&](char* to) { *(Eight<T>*)(to + first) = x[i]; *(Eight<T>*)(to + second) = y[i]; };
-      if (is_q) { put(q_out + head * (c.head_dim * 2)); continue; }
-      if (!is_v && k_out) put(k_out + head * (c.head_dim * 2));
-      if (page >= 0) put((is_v ? c.v : c.k) + row_offset(c, a.layer, page, head, row_in) * 2);
+      const auto put = [&](char* to) { *(Piece*)(to + first) = x; *(Piece*)(to + second) = y; };
+      if (is_q) {
+        put(q_out + head * head_bytes);
+      } else {
+        if (!is_v && k_out) put(k_out + head * head_bytes);
+        if (page >= 0) put((is_v ? v_page : k_page) + (int64_t)head * page_head);
+      }
     }
-    if (h0 + PASSES * each - lane / per_head < total) {
-      h0 += PASSES * each; load(); h0 -= PASSES * each;
-    }
+    x = x_next; y = y_next;
   }
 }
 

@@ -31,7 +31,10 @@ template <typename T> NormShape norm_kernel(int width, bool e4, bool whole) {
 
 // ---- append ----
 inline bool pieces(int64_t stride) { return stride % 8 == 0; }
-constexpr int APPEND_WAVEFRONTS = 2048;                      // eight a CU, where there are as many shares of tokens
+// Wavefronts that share a token: of calls of few tokens one for each pass over its heads, of others one for two passes, so that a pass's elements are on their way while another's
+// are turned (8 prompts of 1000 to 2011, 48 heads of 128: 62 us, with one a token 66, with one a pass 79; 64 trees of 65 19, 23 and 25).
+constexpr int APPEND_FEW_TOKENS = 256;
+inline int append_parts(int64_t tokens, int passes) { return tokens < APPEND_FEW_TOKENS ? passes : std::max(passes / 2, 1); }
 
 // ---- prompt ----
 typedef void (*PromptKernel)(const int32_t*, int32_t, int32_t, int32_t, int32_t, float, float, PromptArgs);
@@ -121,7 +124,8 @@ int c2t_cache_append(const c2t_cache* c, const c2t_append* x, void* stream) {
   a.slots = x->tokens; a.q_heads = x->q_heads; a.layer = x->layer; a.nodes = x->nodes; a.pairs = x->pairs; a.neighbours = x->neighbours;
   const int passes = div_up((x->q_heads + 2 * c->kv_heads) * (c->head_dim / 16), WAVE);       // of a wavefront over a token
   const int64_t rows = (int64_t)x->tokens * (batches ? c->batch : 1);
-  a.parts = (int)std::min<int64_t>(std::max<int64_t>(APPEND_WAVEFRONTS / rows, 1), passes);
+  a.parts = append_parts(rows, passes);
+  if ((int64_t)x->tokens * a.parts > INT32_MAX) return C2T_ERR_UNSUPPORTED;
   const int64_t blocks = div_up64((int64_t)x->tokens * a.parts, CACHE_NT / WAVE);
   const unsigned batch = batches ? (unsigned)c->batch : 1u;
   if (blocks * batch > MAX_BLOCKS) return C2T_ERR_UNSUPPORTED;
