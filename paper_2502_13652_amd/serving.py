@@ -202,17 +202,17 @@ def adjust_frontier_logits(ctx, logits, adjustments, out=None, stream=None):
     return out
 
 
-def _even_rows(t, shape, device, name):
-    """The distance, in elements, of the rows of a tensor of that shape: its last dimension whole, the others as if they were one."""
-    have = t.shape
-    if have != shape or t.get_device() != device.index:
-        raise ValueError("%s: %s on %s" % (name, list(shape), device))
-    width = have[-1]
+def _even_rows(t, shape, index, name):
+    """The distance, in elements, of the rows of a tensor of that shape on that device: its last dimension whole, the others as if they were one."""
+    if t.shape != shape or t.get_device() != index:
+        raise ValueError("%s: %s on the same device" % (name, list(shape)))
+    width = shape[-1]
     if t.is_contiguous():
         return width
     strides = t.stride()
-    at = [(n, s) for n, s in zip(have[:-1], strides[:-1]) if n > 1]        # (a stride over one element is of no use and may be any number)
-    _need((strides[-1] == 1 or width == 1) and all(a[1] == b[0] * b[1] for a, b in zip(at, at[1:])), "%s: rows evenly spaced, elements next to each other" % name)
+    at = [(n, s) for n, s in zip(shape[:-1], strides[:-1]) if n > 1]       # (a stride over one element is of no use and may be any number)
+    if (strides[-1] != 1 and width != 1) or any(a[1] != b[0] * b[1] for a, b in zip(at, at[1:])):
+        raise ValueError("%s: rows evenly spaced, elements next to each other" % name)
     return at[-1][1] if at else width
 
 
@@ -223,29 +223,28 @@ def rms_norm(x, weight, eps=1e-5, residual=None, residual_out=None, out=None, sc
     residual_out (default: residual itself), rounded to its type.  out: of x's shape and type (default: a new tensor; may be x).  With scale_block (32, 64, 128
     or the width), out is float8_e4m3fn and stands for out * scale, with a scale for each scale_block elements of a row (the last may be fewer): scales float32
     [...][ceil(width / scale_block)] (default: new), max |y| / 448 of the block; returns (out, scales), without it out."""
-    dtype, shape, dev = x.dtype, x.shape, x.device
-    _need(dtype in _DTYPES and x.is_cuda and len(shape) > 0 and shape[-1] > 0, "x: [...][width] of float32, bfloat16 or float16 on the GPU")
-    width = shape[-1]
-    rows = x.numel() // width
-    p_residual = p_residual_out = residual_stride = residual_out_stride = 0
-    code = residual_code = _DTYPES[dtype]
+    dtype, shape, index = x.dtype, x.shape, x.get_device()
+    code = out_code = residual_code = _DTYPES.get(dtype)
+    if code is None or index < 0 or not shape or shape[-1] < 1:
+        raise ValueError("x: [...][width] of float32, bfloat16 or float16 on the GPU")
+    dev, width, out_dtype = x.device, shape[-1], dtype
+    x_stride = _even_rows(x, shape, index, "x")
+    p_residual = p_residual_out = residual_stride = residual_out_stride = p_scales = scales_stride = 0
     if residual is not None:
         kind = residual.dtype
-        _need(kind is dtype or kind is torch.float32, "residual: of x's type or float32")
-        residual_code = _DTYPES[kind]
-        residual_stride = residual_out_stride = _even_rows(residual, shape, dev, "residual")
+        if kind is not dtype:
+            _need(kind is torch.float32, "residual: of x's type or float32")
+            residual_code = F32
+        residual_stride = residual_out_stride = _even_rows(residual, shape, index, "residual")
         p_residual = p_residual_out = residual.data_ptr()
         if residual_out is not None and residual_out is not residual:
             _need(residual_out.dtype is kind, "residual_out: of the residual's type")
-            residual_out_stride = _even_rows(residual_out, shape, dev, "residual_out")
+            residual_out_stride = _even_rows(residual_out, shape, index, "residual_out")
             p_residual_out = residual_out.data_ptr()
     else:
         _need(residual_out is None, "residual_out: with a residual")
-    if weight.dtype is not dtype:
-        _whole(weight, dev, torch.float32, (width,), "weight")
-    p_weight = _whole(weight, dev, weight.dtype, (width,), "weight")
-    p_scales = scales_stride = 0
-    out_code, out_dtype = code, dtype
+    weight_code = code if weight.dtype is dtype else F32
+    p_weight = _whole(weight, dev, dtype if weight_code == code else torch.float32, (width,), "weight")
     if scale_block is not None:
         _need(scale_block == width or scale_block in (32, 64, 128), "scale_block: 32, 64, 128 or the width")
         out_code, out_dtype = E4M3, torch.float8_e4m3fn
@@ -253,27 +252,27 @@ def rms_norm(x, weight, eps=1e-5, residual=None, residual_out=None, out=None, sc
         if scales is None:
             scales = _empty_like_on(stream, lambda: torch.empty(wanted, dtype=torch.float32, device=dev))
         _need(scales.dtype is torch.float32, "scales: float32")
-        scales_stride, p_scales = _even_rows(scales, wanted, dev, "scales"), scales.data_ptr()
+        scales_stride, p_scales = _even_rows(scales, wanted, index, "scales"), scales.data_ptr()
     else:
         _need(scales is None, "scales: with a scale_block")
     if out is None:
         out = _empty_like_on(stream, lambda: torch.empty(shape, dtype=out_dtype, device=dev))
-    _need(out.dtype is out_dtype, "out: %s" % out_dtype)
+    elif out.dtype is not out_dtype:
+        raise ValueError("out: %s" % out_dtype)
+    rows = x.numel() // width
     if rows > 0:
-        a = _pack_norm(x.data_ptr(), p_weight, p_residual, p_residual_out, out.data_ptr(), p_scales, _even_rows(x, shape, dev, "x"), residual_stride,
-                       residual_out_stride, _even_rows(out, shape, dev, "out"), scales_stride, rows, width, code, _DTYPES[weight.dtype], residual_code, out_code,
-                       scale_block or 0, eps)
+        a = _pack_norm(x.data_ptr(), p_weight, p_residual, p_residual_out, out.data_ptr(), p_scales, x_stride, residual_stride, residual_out_stride,
+                       _even_rows(out, shape, index, "out"), scales_stride, rows, width, code, weight_code, residual_code, out_code, scale_block or 0, eps)
         _check(_launch(dev, stream, load_library().c2t_rms_norm, a), "c2t_rms_norm")
     return out if scale_block is None else (out, scales)
 
 
-def _packed_rows(x, heads, head_dim, dtype, device, name):
+def _packed_rows(x, rows, heads, head_dim, dtype, index, name):
     """The distance, in elements, of the rows of [rows][heads][head_dim]."""
-    shape, strides = x.shape, x.stride()
-    if not (x.dtype is dtype and len(shape) == 3 and shape[1] == heads and shape[2] == head_dim and strides[2] == 1 and (heads == 1 or strides[1] == head_dim) and
-            x.device == device):
-        raise ValueError("%s: %s [rows][%d][%d] on %s, heads next to each other" % (name, dtype, heads, head_dim, device))
-    return strides[0] if shape[0] > 1 else heads * head_dim
+    strides = x.stride()
+    if not (x.shape == (rows, heads, head_dim) and x.dtype is dtype and strides[2] == 1 and (heads == 1 or strides[1] == head_dim) and x.get_device() == index):
+        raise ValueError("%s: %s [%d][%d][%d] on the same device, heads next to each other" % (name, dtype, rows, heads, head_dim))
+    return strides[0] if rows > 1 else heads * head_dim
 
 
 def prompt_attention(q, k, v, starts, scale=None, out=None, lse=None, stream=None):
@@ -283,16 +282,17 @@ def prompt_attention(q, k, v, starts, scale=None, out=None, lse=None, stream=Non
     q [rows][q_heads][head_dim], k and v [rows][kv_heads][head_dim], bfloat16 or float16, e.g. slices of one projection's output; starts int32 [sequences + 1].
     scale: of the scores, default head_dim ** -0.5.  out: as q (default: a new tensor), lse: float32 [rows][q_heads] for the log of the softmax's sums; rows in no
     sequence are left as they are (in a new tensor they are not filled in)."""
-    _need(q.dim() == 3 and k.dim() == 3 and q.is_cuda and q.dtype in (torch.bfloat16, torch.float16), "q: [rows][q_heads][head_dim] of bfloat16 or float16 on the GPU")
-    dev, dtype = q.device, q.dtype
-    rows, heads, D = q.shape
+    shape, dtype, index = q.shape, q.dtype, q.get_device()
+    if len(shape) != 3 or k.dim() != 3 or index < 0 or not (dtype is torch.bfloat16 or dtype is torch.float16):
+        raise ValueError("q: [rows][q_heads][head_dim] of bfloat16 or float16 on the GPU")
+    dev = q.device
+    rows, heads, D = shape
     kv_heads = k.shape[1]
-    sq, sk, sv = _packed_rows(q, heads, D, dtype, dev, "q"), _packed_rows(k, kv_heads, D, dtype, dev, "k"), _packed_rows(v, kv_heads, D, dtype, dev, "v")
-    _need(k.shape[0] == rows and v.shape[0] == rows, "k and v: as many rows as q")
+    sq, sk = _packed_rows(q, rows, heads, D, dtype, index, "q"), _packed_rows(k, rows, kv_heads, D, dtype, index, "k")
+    sv = _packed_rows(v, rows, kv_heads, D, dtype, index, "v")
     if out is None:
         out = _empty_like_on(stream, lambda: torch.empty((rows, heads, D), dtype=dtype, device=dev))
-    so = _packed_rows(out, heads, D, dtype, dev, "out")
-    _need(out.shape[0] == rows, "out: of q's shape")
+    so = _packed_rows(out, rows, heads, D, dtype, index, "out")
     p_lse = 0 if lse is None else _whole(lse, dev, torch.float32, (rows, heads), "lse")
     p_starts = _whole(starts, dev, torch.int32, (-1,), "starts")
     sequences = starts.shape[0] - 1
@@ -411,19 +411,22 @@ class PagedCache:
         q_out: as q (default: a new tensor; may be q); k_out: as k, for the turned keys (may be k); rows of no token are left as they are.  What the cache has no room
         or page for is left out of it alone, and its status says so."""
         packed = starts is not None
-        _need(q.dim() == (3 if packed else 4), "q: [rows][q_heads][head_dim] with starts, [B][T][q_heads][head_dim] without")
-        T, heads, D, H = q.shape[-3], q.shape[-2], self.head_dim, self.kv_heads
+        shape, D, H, index = q.shape, self.head_dim, self.kv_heads, self.device.index
+        if len(shape) != (3 if packed else 4):
+            raise ValueError("q: [rows][q_heads][head_dim] with starts, [B][T][q_heads][head_dim] without")
+        T, heads = shape[-3], shape[-2]
         if packed:
             _need(n_new is None and position is None, "n_new and position: without starts")
-            rows = lambda x, n, name: (0, _packed_rows(x, n, D, self.dtype, self.device, name))
+            rows = lambda x, n, name: (0, _packed_rows(x, T, n, D, self.dtype, index, name))
         else:
             rows = self._tokens
         sq, sk = rows(q, heads, "q"), rows(k, H, "k")
-        _need(rows(v, H, "v") == sk and k.shape == v.shape and k.shape[:-2] == q.shape[:-2], "k and v: of one shape and strides, as many tokens as q")
+        if not (v.shape == k.shape and (v.stride() == k.stride() or rows(v, H, "v") == sk) and v.dtype is k.dtype and v.get_device() == index and k.shape[-3] == T):
+            raise ValueError("k and v: of one shape, type and strides, as many tokens as q")
         if q_out is None:
             q_out = _empty_like_on(stream, lambda: torch.empty(q.shape, dtype=self.dtype, device=self.device))
-        so = rows(q_out, heads, "q_out")
-        _need(q_out.shape == q.shape and (k_out is None or k_out.shape == k.shape), "q_out and k_out: of q's and k's shape")
+        so = sq if q_out is q else rows(q_out, heads, "q_out")
+        _need(q_out.shape == shape and (k_out is None or k_out.shape == k.shape), "q_out and k_out: of q's and k's shape")
         ko = (0, 0) if k_out is None else rows(k_out, H, "k_out")
         nodes = p_position = 0
         if position is not None:
