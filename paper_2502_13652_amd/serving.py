@@ -260,6 +260,7 @@ def rms_norm(x, weight, eps=1e-5, residual=None, residual_out=None, out=None, sc
     elif out.dtype is not out_dtype:
         raise ValueError("out: %s" % out_dtype)
     rows = x.numel() // width
+    _need(rows < 1 << 31, "x: fewer than 2^31 rows")
     if rows > 0:
         a = _pack_norm(x.data_ptr(), p_weight, p_residual, p_residual_out, out.data_ptr(), p_scales, x_stride, residual_stride, residual_out_stride,
                        _even_rows(out, shape, index, "out"), scales_stride, rows, width, code, weight_code, residual_code, out_code, scale_block or 0, eps)

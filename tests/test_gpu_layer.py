@@ -1,0 +1,204 @@
+"""Layers of a target model taken through packed prompts, draft trees and single tokens with rms_norm, append, prompt_attention and the paged cache's attention: each step against
+its 64-bit form on what the step before it made, and the cache against one that had the accepted tokens appended one by one."""
+import pytest
+import torch
+
+import workloads as W
+from _harness import make_gpu
+from _layer import norm_reference, norm_tolerance, prompt_reference, turned_reference
+from _serving import attention_reference, gen, gathered
+from test_gpu_append import frequencies, ints, near
+
+pytestmark = pytest.mark.gpu
+BF = torch.bfloat16
+
+
+class Layers:
+    """Weights of a few layers; what is between the operators is torch's."""
+
+    def __init__(self, layers, H, Hq, Hkv, D, vocab):
+        g = gen(5, "cuda")
+        rand = lambda *shape: torch.randn(shape, generator=g, device="cuda")
+        self.layers, self.H, self.Hq, self.Hkv, self.D = layers, H, Hq, Hkv, D
+        self.emb = rand(vocab, H).to(BF)
+        self.norm = (1 + 0.2 * rand(layers, H)).to(BF)
+        self.qkv = (rand(layers, H, (Hq + 2 * Hkv) * D) * H ** -0.5).to(BF)
+        self.o = (rand(layers, Hq * D, H) * (Hq * D) ** -0.5).to(BF)
+
+    def start(self, x, layer, residual):
+        """Norm and projection; residual fp32, in place."""
+        from paper_2502_13652_amd import rms_norm
+        before = residual.clone()
+        y = rms_norm(x, self.norm[layer], 1e-5, residual=residual)
+        h, want = norm_reference(x, self.norm[layer], 1e-5, before)
+        assert bool(((y.double() - want).abs() <= norm_tolerance(want, BF)).all()) and bool(((residual.double() - h).abs() <= h.abs() * 2.0 ** -23).all())
+        z = torch.matmul(y.reshape(-1, self.H), self.qkv[layer]).view(y.shape[:-1] + (self.Hq + 2 * self.Hkv, self.D))
+        return z[..., :self.Hq, :], z[..., self.Hq:self.Hq + self.Hkv, :], z[..., self.Hq + self.Hkv:, :]
+
+    def end(self, y, layer):
+        return torch.matmul(y.reshape(-1, self.Hq * self.D), self.o[layer]).view(y.shape[:-2] + (self.H,))
+
+
+@pytest.mark.parametrize("page_size,neighbours,dim", [(16, False, 64), (64, True, 32)])
+def test_prompts_trees_and_tokens(page_size, neighbours, dim):
+    from paper_2502_13652_amd import PagedCache, Rotation, prompt_attention
+    cfg = dict(idx=93, B=3, V=1009, dtype="bf16", D=3, F=6, K=4, h=6, beta=0.0, N=15, zipf_s=1.2, sigma=(0.5, 1.5), spike_frac=0.0, desc="layers")
+    B, V, N = cfg["B"], cfg["V"], cfg["N"]
+    layers, H, Hq, Hkv, D, T = 2, 512, 6, 2, 64, 1 + cfg["N"]
+    net, rotation, f = Layers(layers, H, Hq, Hkv, D, V), Rotation(dim, neighbours=neighbours), frequencies(dim)
+    cache = PagedCache(B, layers, 80, page_size, Hkv, D, 16)
+    # prompts, packed
+    lens = [70, 1, 133]
+    at = [0, 70, 71, 204]
+    starts = ints(at)
+    tokens = torch.randint(0, V, (at[-1],), generator=gen(6), dtype=torch.int64).cuda()
+    cache.reserve(ints(lens))
+    x, residual = net.emb[tokens], torch.zeros((at[-1], H), device="cuda")
+    where = [t for n in lens for t in range(n)]
+    for layer in range(layers):
+        q, k, v = net.start(x, layer, residual)
+        q0, k0 = q.clone(), k.clone()
+        cache.append(layer, q, k, v, rotation, starts=starts, q_out=q, k_out=k)               # in place: slices of the projection's output
+        for now, was in ((q, q0), (k, k0)):
+            near(now, *turned_reference(was, where, dim, f, neighbours, 1.0))
+        y = prompt_attention(q, k, v, starts)
+        want, _, tol, _ = prompt_reference(q, k, v, at, D ** -0.5)
+        near(y, want, tol)
+        for b, n in enumerate(lens):
+            kc, vc, ok = gathered(cache, b, layer, n)
+            assert bool(ok.all()) and torch.equal(kc.transpose(0, 1), k[at[b]:at[b + 1]].double()) and torch.equal(vc.transpose(0, 1), v[at[b]:at[b + 1]].double())
+        x = net.end(y, layer)
+    cache.length += ints(lens)
+    assert int(cache.status.view(torch.int32).abs().sum()) == 0
+
+    ctx = make_gpu(cfg, W.classifier(cfg, 2))
+    plain = PagedCache(B, 1, 80, page_size, Hkv, D, 16)     # the first layer's keys and values, token by token
+    plain.reserve(ints(lens))
+    first = lambda ids: net.start(net.emb[ids], 0, torch.zeros(ids.shape + (H,), device="cuda"))
+    q, k, v = first(tokens)
+    plain.append(0, q, k, v, rotation, starts=starts)
+    plain.length += ints(lens)
+    root = torch.randint(0, V, (B,), generator=gen(7), dtype=torch.int32).cuda()
+    for step in range(3):
+        ctx.reset()
+        for l in range(cfg["D"]):
+            logits = torch.zeros((B, cfg["F"], 1016), dtype=BF, device="cuda")
+            logits[:, :, :V] = W.logits_layer(cfg, l, device="cuda", instance=step)
+            ctx.expand_layer(logits)
+        out = ctx.finalize_tree()
+        n_new = 1 + out["n_nodes"]
+        news, before = n_new.tolist(), cache.length.tolist()
+        cache.reserve(n_new)
+        ids = torch.cat([root[:, None], out["tokens"].clamp(min=0)], 1).long()
+        x, residual = net.emb[ids], torch.zeros((B, T, H), device="cuda")
+        for layer in range(layers):
+            q, k, v = net.start(x, layer, residual)
+            turned = cache.append(layer, q, k, v, rotation, n_new=n_new, position=out["position"])
+            for b, n in enumerate(news):
+                places = [before[b]] + [before[b] + int(out["position"][b, i]) for i in range(n - 1)]
+                near(turned[b, :n], *turned_reference(q[b, :n], places, dim, f, neighbours, 1.0))
+                kc, vc, _ = gathered(cache, b, layer, before[b] + n)
+                near(kc[:, before[b]:].transpose(0, 1), *turned_reference(k[b, :n], places, dim, f, neighbours, 1.0))
+                assert torch.equal(vc[:, before[b]:].transpose(0, 1), v[b, :n].double())
+            y = cache.attention(layer, turned, n_new=n_new, mask=out["mask"], out=torch.zeros_like(turned))
+            want, _, tol, _ = attention_reference(cache, layer, turned, news, out["mask"], D ** -0.5)
+            live = torch.isfinite(want)
+            assert bool(((y.double() - want).abs() <= tol)[live].all()), (step, layer)
+            x = net.end(y, layer)
+        # a path to the last node: its slots, from the root on
+        paths = []
+        for b, n in enumerate(news):
+            p, node = [], n - 2
+            while node >= 0:
+                p.append(node + 1)
+                node = int(out["parent"][b, node])
+            paths.append([0] + p[::-1])
+        n_path = ints([len(p) for p in paths])
+        path = ints([p + [0] * (T - len(p)) for p in paths])
+        cache.commit(path, n_path)
+        cache.truncate()
+        taken = torch.gather(ids, 1, path.long())
+        for t in range(int(n_path.max())):                   # single tokens, at the positions that their depths were
+            now = (t < n_path).to(torch.int32)
+            plain.reserve(now)
+            # of the tree's own rows: torch's products of one row are not those of many, bit for bit
+            q, k, v = (torch.gather(z, 1, path[:, t:t + 1, None, None].long().expand(-1, -1, z.shape[2], D)) for z in first(ids))
+            plain.append(0, q.contiguous(), k.contiguous(), v.contiguous(), rotation, n_new=now)
+            plain.commit(torch.zeros((B, 1), dtype=torch.int32, device="cuda"), now)
+        root = taken.gather(1, (n_path - 1)[:, None].long())[:, 0].to(torch.int32)
+        assert torch.equal(cache.length, plain.length)
+        for b in range(B):
+            places = torch.arange(int(plain.length[b]), device="cuda")
+            for name in ("k", "v"):
+                rows = [getattr(c, name)[0, c.page_table[b].long()[places // page_size], :, places % page_size] for c in (cache, plain)]
+                assert torch.equal(*rows), (step, b, name)
+        assert int(sum(c.status.view(torch.int32).abs().sum() for c in (cache, plain))) == 0
+
+
+def test_a_prompt_and_the_cache_agree():
+    """The last chunk of a prompt by prompt_attention and by the cache's attention over the same keys."""
+    from paper_2502_13652_amd import PagedCache, Rotation, prompt_attention
+    lens, Hq, Hkv, D = [150, 64, 33], 8, 2, 128
+    at = [0, 150, 214, 247]
+    z = torch.randn((at[-1], Hq + 2 * Hkv, D), generator=gen(8, "cuda"), device="cuda").to(BF)
+    q, k, v = z[:, :Hq], z[:, Hq:Hq + Hkv], z[:, Hq + Hkv:]
+    cache = PagedCache(3, 1, 40, 16, Hkv, D, 16)
+    cache.reserve(ints(lens))
+    cache.append(0, q, k, v, Rotation(D), starts=ints(at), q_out=q, k_out=k)
+    lse = torch.zeros((at[-1], Hq), device="cuda")
+    y = prompt_attention(q, k, v, ints(at), lse=lse)
+    cache.length += ints([n - 33 for n in lens])
+    last = torch.stack([q[z - 33:z] for z in at[1:]])
+    lse2 = torch.zeros((3, 33, Hq), device="cuda")
+    other = cache.attention(0, last, lse=lse2)
+    want, want_lse, tol, tol_lse = prompt_reference(q, k, v, at, D ** -0.5)
+    for b, end in enumerate(at[1:]):
+        rows = slice(end - 33, end)
+        near(y[rows], want[rows], tol[rows])
+        near(other[b], want[rows], tol[rows])
+        near(lse[rows], want_lse[rows], tol_lse[rows])
+        near(lse2[b], want_lse[rows], tol_lse[rows])
+
+
+def test_a_graph_of_a_prompts_layer_between_eager_calls():
+    """Norm, append and attention captured together, replayed with other lengths and tokens while the same operators run beside it on another stream."""
+    from paper_2502_13652_amd import PagedCache, Rotation, prompt_attention, rms_norm
+    Hq, Hkv, D, H, rows = 4, 2, 64, 256, 96
+    net, rotation = Layers(1, H, Hq, Hkv, D, 50), Rotation(D)
+    cache, other = (PagedCache(2, 1, 20, 16, Hkv, D, 8) for _ in range(2))
+    for c in (cache, other):
+        c.reserve(ints([96, 96]))
+    x, starts = torch.zeros((rows, H), dtype=BF, device="cuda"), ints([0, 40, 96])
+    y, z = torch.zeros_like(x), torch.zeros((rows, Hq + 2 * Hkv, D), dtype=BF, device="cuda")
+    out = torch.zeros((rows, Hq, D), dtype=BF, device="cuda")
+    q, k, v = z[:, :Hq], z[:, Hq:Hq + Hkv], z[:, Hq + Hkv:]
+
+    def layer(c, x, y, z, starts, out):
+        q, k, v = z[:, :Hq], z[:, Hq:Hq + Hkv], z[:, Hq + Hkv:]
+        rms_norm(x, net.norm[0], out=y)
+        torch.matmul(y, net.qkv[0], out=z.view(rows, -1))
+        c.append(0, q, k, v, rotation, starts=starts, q_out=q, k_out=k)
+        prompt_attention(q, k, v, starts, out=out)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):                            # (torch's product picks its way before the capture)
+        layer(cache, x, y, z, starts, out)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        layer(cache, x, y, z, starts, out)
+    mine = [torch.zeros_like(t) for t in (x, y, z, starts, out)]
+    for seed, at in enumerate(([0, 40, 96], [0, 0, 95], [3, 90, 90])):
+        x.copy_(torch.randn((rows, H), generator=gen(seed, "cuda"), device="cuda"))
+        starts.copy_(torch.tensor(at, dtype=torch.int32))
+        out.fill_(2.0), mine[4].fill_(2.0)
+        mine[0].copy_(x), mine[3].copy_(starts)
+        torch.cuda.synchronize()
+        graph.replay()
+        with torch.cuda.stream(side):
+            layer(other, *mine)
+        torch.cuda.synchronize()
+        assert torch.equal(out, mine[4]) and torch.equal(z, mine[2])
+        live = slice(at[0], at[2])
+        want, _, tol, _ = prompt_reference(q, k, v, at, D ** -0.5)
+        near(out[live], want[live], tol[live])
+        assert bool((out[:at[0]] == 2.0).all()) and bool((out[at[2]:] == 2.0).all())

@@ -59,6 +59,16 @@ def test_prompts(D, Hq, Hkv, dtype, lens):
     assert bool((lse[:at[0]] == 7.0).all()) and bool((lse[at[-1]:] == 7.0).all())
 
 
+@pytest.mark.parametrize("Hq,Hkv,D", [(40, 1, 64), (129, 1, 64), (33, 11, 128), (200, 1, 128), (7, 7, 256)])
+def test_groups_that_do_not_fill_a_tile_evenly(Hq, Hkv, D):
+    from paper_2502_13652_amd import prompt_attention
+    at = starts_of([1, 70, 5, 33])
+    q, k, v = inputs(at[-1], Hq, Hkv, D, BF, Hq)
+    lse = torch.zeros((at[-1], Hq), device="cuda")
+    out = prompt_attention(q, k, v, torch.tensor(at, dtype=torch.int32, device="cuda"), lse=lse)
+    compare(q, k, v, at, out, lse)
+
+
 @pytest.mark.parametrize("n,longest", [(65, 40), (130, 300), (700, 9), (4096, 3)])
 def test_many_sequences(n, longest):
     from paper_2502_13652_amd import prompt_attention
