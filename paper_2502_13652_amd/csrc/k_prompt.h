@@ -147,7 +147,8 @@ __device__ __forceinline__ float add_pair(F16::T8 x, int pair, float a) {
   return __builtin_amdgcn_fdot2(y, one, a, false);
 }
 
-constexpr int PROMPT_WAVES = 4, PROMPT_ROWS = 32 * PROMPT_WAVES;
+constexpr int prompt_waves(int kw) { return kw > 1 ? kw : 4; }                   // of a workgroup, and its rows
+constexpr int prompt_rows(int kw) { return kw > 1 ? 32 : 32 * prompt_waves(kw); }
 
 // How a block of PRODUCTS matrix instructions and READS reads of their operands is to be laid out: AHEAD reads, then EACH reads behind each product.
 template <int PRODUCTS, int READS, int AHEAD, int EACH> __device__ __forceinline__ void reads_ahead() {
@@ -160,64 +161,69 @@ template <int PRODUCTS, int READS, int AHEAD, int EACH> __device__ __forceinline
 }
 constexpr int K_AHEAD = 4, V_AHEAD = 2;                      // operands read ahead of their product
 
-// DV of the D elements of an output row are one workgroup's (D, or the half where registers do not hold it all); KB blocks of 32 keys a tile; OCC workgroups a CU.
-template <typename E, int D, int DV, int KB, int OCC, bool LSE>
-__global__ __launch_bounds__(64 * PROMPT_WAVES, OCC) void k_prompt(const int32_t* starts, int32_t all_rows, int32_t sequences, int32_t kv_heads, int32_t G, float inv_kv_heads,
-                                                                      float inv_group, PromptArgs a) {
+// DV of the D elements of an output row are one workgroup's (D, or a part of them); KB blocks of 32 keys a tile; OCC workgroups a CU.  The wavefronts have 32 rows each and share the
+// tiles (KW = 1), or the same 32 rows and KW wavefronts every KW-th tile each, joined at the end: a quarter of the way along the keys where there are few rows.
+template <typename E, int D, int DV, int KB, int KW, int OCC, bool LSE>
+__global__ __launch_bounds__(64 * prompt_waves(KW), OCC) void k_prompt(const int32_t* starts, int32_t all_rows, int32_t sequences, int32_t kv_heads, int32_t G, float inv_kv_heads,
+                                                                       float inv_group, PromptArgs a) {
   typedef typename E::T T; typedef typename E::T4 T4; typedef typename E::T8 T8;
-  constexpr int NT = 64 * PROMPT_WAVES, KT = 32 * KB, PARTS = D / DV, DB = DV / 32, DK = D / 16;
-  constexpr int K_LOADS = KT * D / 8 / NT, V_LOADS = KT * DV / 8 / NT, K_TILE = KT * D * 2, TILE = K_TILE + KT * DV * 2;
+  constexpr int WAVES = prompt_waves(KW), NT = 64 * WAVES, ROWS = prompt_rows(KW), KT = 32 * KB, PARTS = D / DV, DB = DV / 32, DK = D / 16;
+  constexpr int SHARERS = KW > 1 ? 64 : NT;                  // threads that load a tile together
+  constexpr int K_LOADS = KT * D / 8 / SHARERS, V_LOADS = KT * DV / 8 / SHARERS, K_TILE = KT * D * 2, TILE = K_TILE + KT * DV * 2;
   constexpr float TOP = E::TOP, SLACK = E::SLACK, BIG = 0x1p22f;
-  __shared__ __align__(16) char lds[2 * TILE];               // K and V, two buffers
-  __shared__ int odd_value;                                  // a tile held a value that is not finite
+  __shared__ __align__(16) char lds[2 * TILE * KW];          // K and V, two buffers, of each wavefront that has tiles of its own
+  __shared__ int odd_value;                                  // a tile held a value that is not finite (KW = 1)
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, half = lane >> 5;
+  const int kw = KW > 1 ? wave : 0, lt = KW > 1 ? lane : tid;        // this thread among those that load a tile
+  char* const tiles = lds + kw * 2 * TILE;
+  bool my_odd = false;
 
   // The query heads of one cached head share its keys: a tile's rows are (token, head of the group) with the head fastest, so that its wavefronts come to their last key together, however
   // many heads there are, and short prompts fill tiles.
-  if (tid == 0) odd_value = 0;
+  if (KW == 1 && tid == 0) odd_value = 0;
   PromptTile u;
   const int part = blockIdx.x % PARTS;
   int rank, head;
   split(blockIdx.x / PARTS, kv_heads, inv_kv_heads, &rank, &head);
   rank = uniform(rank); head = uniform(head);
-  if (!find_tile<PROMPT_ROWS>(PromptShape{starts, all_rows, sequences, kv_heads, G, inv_kv_heads, inv_group}, rank, &u)) return;
-  const int row0 = u.tile * PROMPT_ROWS, wave_row0 = row0 + wave * 32, rows = u.n * G;
+  if (!find_tile<ROWS>(PromptShape{starts, all_rows, sequences, kv_heads, G, inv_kv_heads, inv_group}, rank, &u)) return;
+  const int row0 = u.tile * ROWS, wave_row0 = row0 + (KW > 1 ? 0 : wave * 32), rows = u.n * G;
   const auto token_of = [&](int row, int* g) { int t; split(min(row, rows - 1), G, inv_group, &t, g); return t; };      // (rows behind the last are not put out)
   int my_g, no_g;
   const int my_token = token_of(wave_row0 + col, &my_g);
   const int first_token = uniform(token_of(row0, &no_g)), wave_first = uniform(token_of(wave_row0, &no_g)), wave_last = uniform(token_of(wave_row0 + 31, &no_g));
-  const int keys = uniform(token_of(row0 + PROMPT_ROWS - 1, &no_g)) + 1, n_tiles = div_up(keys, KT);
+  const int keys = uniform(token_of(row0 + ROWS - 1, &no_g)) + 1, n_tiles = div_up(keys, KT);
   const bool idle = wave_row0 >= rows;
   const char* const k_head = a.k + u.first * a.k_row + (int64_t)head * (D * 2);
   const char* const v_head = a.v + u.first * a.v_row + (int64_t)head * (D * 2) + part * (DV * 2);
 
-  // A tile's pieces: this thread's j-th lies j NT + tid pieces into K's or V's tile in LDS, and is the piece of its row that piece_at puts there: the same one in every 16th row, so
+  // A tile's pieces: this thread's j-th lies j SHARERS + lt pieces into K's or V's tile in LDS, and is the piece of its row that piece_at puts there: the same one in every 16th row, so
   // that one offset (two, of rows of 8 a load) does for all of a tile's.
-  constexpr int K_ROWS = NT / (D / 8), V_ROWS = NT / (DV / 8), K_KINDS = K_ROWS < 16 ? 16 / K_ROWS : 1, V_KINDS = V_ROWS < 16 ? 16 / V_ROWS : 1;      // rows a load, offsets
-  const auto k_piece = [&](int j) { const int row = j * K_ROWS + tid / (D / 8); return (uint32_t)(piece_at<D>(row, tid % (D / 8)) - row * (D * 2)); };
-  const auto v_piece = [&](int j) { const int row = j * V_ROWS + tid / (DV / 8); return (uint32_t)(piece_at<DV>(row, tid % (DV / 8)) - row * (DV * 2)); };
+  constexpr int K_ROWS = SHARERS / (D / 8), V_ROWS = SHARERS / (DV / 8), K_KINDS = K_ROWS < 16 ? 16 / K_ROWS : 1, V_KINDS = V_ROWS < 16 ? 16 / V_ROWS : 1;      // rows a load, offsets
+  const auto k_piece = [&](int j) { const int row = j * K_ROWS + lt / (D / 8); return (uint32_t)(piece_at<D>(row, lt % (D / 8)) - row * (D * 2)); };
+  const auto v_piece = [&](int j) { const int row = j * V_ROWS + lt / (DV / 8); return (uint32_t)(piece_at<DV>(row, lt % (DV / 8)) - row * (DV * 2)); };
   uint32_t k_off[K_KINDS], v_off[V_KINDS];
 #pragma unroll
-  for (int j = 0; j < K_KINDS; ++j) k_off[j] = tid / (D / 8) * (uint32_t)a.k_row + k_piece(j);
+  for (int j = 0; j < K_KINDS; ++j) k_off[j] = lt / (D / 8) * (uint32_t)a.k_row + k_piece(j);
 #pragma unroll
-  for (int j = 0; j < V_KINDS; ++j) v_off[j] = tid / (DV / 8) * (uint32_t)a.v_row + v_piece(j);
-  const uint32_t lds_wave = lds_address(lds) + wave * 1024;
-  const char* k_at = k_head; const char* v_at = v_head;
-  int ahead = keys;                                          // keys from there on
+  for (int j = 0; j < V_KINDS; ++j) v_off[j] = lt / (DV / 8) * (uint32_t)a.v_row + v_piece(j);
+  const uint32_t lds_wave = lds_address(tiles) + (KW > 1 ? 0 : wave * 1024);
+  const char* k_at = k_head + kw * KT * a.k_row; const char* v_at = v_head + kw * KT * a.v_row;
+  int ahead = keys - kw * KT;                                          // keys from there on
   const auto request = [&](int buffer) {
     const uint32_t to = lds_wave + buffer * TILE;
     if (ahead >= KT) {
 #pragma unroll
-      for (int j = 0; j < K_LOADS; ++j) load_to_lds(k_at + j * K_ROWS * a.k_row, k_off[j % K_KINDS], to + j * NT * 16);
+      for (int j = 0; j < K_LOADS; ++j) load_to_lds(k_at + j * K_ROWS * a.k_row, k_off[j % K_KINDS], to + j * SHARERS * 16);
 #pragma unroll
-      for (int j = 0; j < V_LOADS; ++j) load_to_lds(v_at + j * V_ROWS * a.v_row, v_off[j % V_KINDS], to + K_TILE + j * NT * 16);
+      for (int j = 0; j < V_LOADS; ++j) load_to_lds(v_at + j * V_ROWS * a.v_row, v_off[j % V_KINDS], to + K_TILE + j * SHARERS * 16);
     } else {                                                 // rows behind the last key are taken from it (and masked)
 #pragma unroll
-      for (int j = 0; j < K_LOADS; ++j) load_to_lds(k_at, (uint32_t)min(j * K_ROWS + tid / (D / 8), ahead - 1) * (uint32_t)a.k_row + k_piece(j), to + j * NT * 16);
+      for (int j = 0; j < K_LOADS; ++j) load_to_lds(k_at, (uint32_t)min(j * K_ROWS + lt / (D / 8), ahead - 1) * (uint32_t)a.k_row + k_piece(j), to + j * SHARERS * 16);
 #pragma unroll
-      for (int j = 0; j < V_LOADS; ++j) load_to_lds(v_at, (uint32_t)min(j * V_ROWS + tid / (DV / 8), ahead - 1) * (uint32_t)a.v_row + v_piece(j), to + K_TILE + j * NT * 16);
+      for (int j = 0; j < V_LOADS; ++j) load_to_lds(v_at, (uint32_t)min(j * V_ROWS + lt / (DV / 8), ahead - 1) * (uint32_t)a.v_row + v_piece(j), to + K_TILE + j * SHARERS * 16);
     }
-    k_at += KT * a.k_row; v_at += KT * a.v_row; ahead -= KT;
+    k_at += KW * KT * a.k_row; v_at += KW * KT * a.v_row; ahead -= KW * KT;
   };
   // Waits for this wavefront's pieces.  Where some rows see a value that others do not, one that is not finite is left out of the product and added for the rows that see it.
   const auto arrived = [&](int buffer, bool diagonal) {
@@ -226,30 +232,31 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, OCC) void k_prompt(const int32_t
     bool odd = false;
 #pragma unroll
     for (int j = 0; j < V_LOADS; ++j) {
-      u32x4* const at = (u32x4*)(lds + buffer * TILE + K_TILE + (j * NT + tid) * 16);
+      u32x4* const at = (u32x4*)(tiles + buffer * TILE + K_TILE + (j * SHARERS + lt) * 16);
       const u32x4 x = *at;
       const u32x4 bad = {odd_halves<E>(x.x), odd_halves<E>(x.y), odd_halves<E>(x.z), odd_halves<E>(x.w)};
       if ((bad.x | bad.y | bad.z | bad.w) != 0u) { odd = true; *at = x & ~bad; }
     }
-    if (odd) odd_value = 1;
+    if (KW > 1) my_odd = my_odd || __any(odd);
+    else if (odd) odd_value = 1;
   };
   // Where this lane's operands begin: of K row `col` and piece `half`, of V rows 4 half + (lane & 15) / 4 and the lane's 8 bytes of a block of 32 elements.  The others lie at these
   // places but for whole rows and bits of the piece's number.
   const int k_place = piece_at<D>(col, half);
   const int v_place = K_TILE + piece_at<DV>(half * 4 + (lane & 15) / 4, (lane >> 4 & 1) * 2 + (lane & 3) / 2) + (lane & 1) * 8;
-  request(0);
+  if (kw < n_tiles) request(0);
   T8 q[DK];
   {
     const char* const from = a.q + ((int64_t)u.first + my_token) * a.q_row + query_offset(head, G, my_g, D) * 2 + half * 16;
 #pragma unroll
     for (int kk = 0; kk < DK; ++kk) q[kk] = *(const T8*)(from + kk * 32);
   }
-  if (KT > first_token) __syncthreads();                     // (odd_value)
-  arrived(0, KT > first_token);
+  if (KW == 1 && KT > first_token) __syncthreads();          // (odd_value)
+  if (kw < n_tiles) arrived(0, kw * KT + KT > first_token);
   // The queries are here before the loop, or each of its rounds would wait for them, and for the next tile's pieces, which are younger, with them.
 #pragma unroll
   for (int kk = 0; kk < DK; ++kk) { u32x4 x = __builtin_bit_cast(u32x4, q[kk]); settle(x); q[kk] = __builtin_bit_cast(T8, x); }
-  __syncthreads();
+  if (KW == 1) __syncthreads();
   f32x16 o[DB];
 #pragma unroll
   for (int d = 0; d < DB; ++d)
@@ -258,9 +265,9 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, OCC) void k_prompt(const int32_t
   float m_run = -INFINITY, e_run = 0.f, l_run = 0.f, factor = a.scale_log2e;
   int big = 0;
 
-  for (int t = 0; t < n_tiles; ++t) {
-    const int key0 = t * KT, buffer = t & 1;
-    if (t + 1 < n_tiles) request(buffer ^ 1);
+  for (int t = kw; t < n_tiles; t += KW) {
+    const int key0 = t * KT, buffer = t / KW & 1;
+    if (t + KW < n_tiles) request(buffer ^ 1);
     if (!idle && key0 <= wave_last) {
       int k_base = k_place + buffer * TILE, v_base = v_place + buffer * TILE;
       settle(k_base); settle(v_base);                        // (what follows from them is made anew each time, and holds no registers)
@@ -272,7 +279,7 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, OCC) void k_prompt(const int32_t
 #pragma unroll
       for (int kk = 0; kk < DK; ++kk)
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) s[kb] = product32(*(const T8*)(lds + (k_base ^ kk * 32) + kb * 32 * (D * 2)), q[kk], s[kb]);
+        for (int kb = 0; kb < KB; ++kb) s[kb] = product32(*(const T8*)(tiles + (k_base ^ kk * 32) + kb * 32 * (D * 2)), q[kk], s[kb]);
       reads_ahead<KB * DK, KB * DK, K_AHEAD, 1>();
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) settle(s[kb]);
@@ -324,8 +331,8 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, OCC) void k_prompt(const int32_t
       const auto read_v = [&](int i) {
         const int h = i / DB, d = i % DB;
         typedef __attribute__((address_space(3))) s16x4* lds4;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(lds + (v_base ^ d * 64) + h * 16 * (DV * 2)));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(lds + (v_base ^ (d * 64 + 32)) + (h * 16 + 8) * (DV * 2)));
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(tiles + (v_base ^ d * 64) + h * 16 * (DV * 2)));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(tiles + (v_base ^ (d * 64 + 32)) + (h * 16 + 8) * (DV * 2)));
         struct { s16x4 a, b; } both{lo, hi};
         v[i] = __builtin_bit_cast(T8, both);
       };
@@ -344,18 +351,19 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, OCC) void k_prompt(const int32_t
           for (int pair = d * 4 / DB; pair < (d + 1) * 4 / DB; ++pair) weights(h + 1, pair);
       }
     }
-    if (t + 1 < n_tiles) arrived(buffer ^ 1, key0 + 2 * KT > first_token);
-    __syncthreads();
+    if (t + KW < n_tiles) arrived(buffer ^ 1, key0 + (KW + 1) * KT > first_token);
+    if (KW == 1) __syncthreads();
   }
 #pragma unroll
   for (int d = 0; d < DB; ++d) settle(o[d]);
   if (idle) return;
   l_run += __shfl_xor(l_run, 32); e_run += __shfl_xor(e_run, 32);
 
-  if (odd_value != 0) {                                      // values that are not finite: a weight is made again from its key
+  if (KW > 1 ? my_odd : odd_value != 0) {                    // values that are not finite: a weight is made again from its key
     const char* const k_odd = k_head + half * 16;
     const char* const v_odd = v_head + half * 8;
     for (int key = first_token / KT * KT; key <= wave_last; ++key) {
+      if (KW > 1 && key / KT % KW != kw) continue;
       const auto value = [&](int d) { return *(const T4*)(v_odd + key * a.v_row + d * 16); };
       bool any = false;
       for (int d = 0; d < DB * 4; ++d) {
@@ -387,13 +395,55 @@ __global__ __launch_bounds__(64 * PROMPT_WAVES, OCC) void k_prompt(const int32_t
       }
     }
   }
-  if (LSE && half == 0 && part == 0 && wave_row0 + col < rows) {
-    // of a sum as if the reference were the largest score (k_attend.h)
+  // of a sum as if the reference were the largest score (k_attend.h)
+  const auto log_of = [&](float m, float e) {
     constexpr float BELOW = TOP - SLACK;
-    const float UNIT = __builtin_ldexpf(1.f, -(int)BELOW);
-    a.lse[((int64_t)u.first + my_token) * kv_heads * G + query_offset(head, G, my_g, 1)] =
-        l_run == 0.f ? -INFINITY : ((m_run + BELOW) + __builtin_amdgcn_logf(e_run * UNIT)) * 0.69314718055994531f;
+    return ((m + BELOW) + __builtin_amdgcn_logf(e * __builtin_ldexpf(1.f, -(int)BELOW))) * 0.69314718055994531f;
+  };
+  if constexpr (KW > 1) {
+    // The wavefronts' shares of the rows, joined through LDS: sums of products with their pieces of 16 bytes at other places from row to row, references and sums of weights behind them.
+    constexpr int SUMS = 32 * DV * 4;
+    static_assert(SUMS + 3 * 32 * 4 <= 2 * TILE, "");
+    const auto place = [&](int row, int piece) { return (row * (DV / 4) + (piece ^ (row & (DV / 4 - 1)))) * 16; };
+    float* const stats = (float*)(tiles + SUMS);
+#pragma unroll
+    for (int d = 0; d < DB * 4; ++d) {
+      f32x4 x;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) x[r] = o[d / 4][d % 4 * 4 + r];
+      *(f32x4*)(tiles + place(col, d * 2 + half)) = x;
+    }
+    if (half == 0) { stats[col] = m_run; stats[32 + col] = l_run; stats[64 + col] = e_run; }
+    __syncthreads();
+    for (int i = tid; i < 32 * (DV / 8); i += NT) {
+      const int row = i / (DV / 8), piece = i % (DV / 8);
+      if (wave_row0 + row >= rows) continue;
+      const auto of = [&](int w) { return (const float*)(lds + w * 2 * TILE + SUMS) + row; };
+      float m = -INFINITY, l = 0.f, e = 0.f;
+#pragma unroll
+      for (int w = 0; w < KW; ++w) m = fmaxf(m, of(w)[0]);
+      const float ref = m == -INFINITY ? 0.f : m;
+      f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
+#pragma unroll
+      for (int w = 0; w < KW; ++w) {
+        const float f = __builtin_amdgcn_exp2f(of(w)[0] - ref);
+        l += f * of(w)[32]; e += f * of(w)[64];
+        x += f * *(const f32x4*)(lds + w * 2 * TILE + place(row, piece * 2));
+        y += f * *(const f32x4*)(lds + w * 2 * TILE + place(row, piece * 2 + 1));
+      }
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      T8 z;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) { z[r] = (T)(x[r] * inv); z[4 + r] = (T)(y[r] * inv); }
+      int g;
+      const int64_t t = u.first + token_of(wave_row0 + row, &g);
+      *(T8*)(a.out + t * a.out_row + query_offset(head, G, g, D) * 2 + part * (DV * 2) + piece * 16) = z;
+      if (LSE && piece == 0 && part == 0) a.lse[t * kv_heads * G + query_offset(head, G, g, 1)] = l == 0.f ? -INFINITY : log_of(m, e);
+    }
+    return;
   }
+  if (LSE && half == 0 && part == 0 && wave_row0 + col < rows)
+    a.lse[((int64_t)u.first + my_token) * kv_heads * G + query_offset(head, G, my_g, 1)] = l_run == 0.f ? -INFINITY : log_of(m_run, e_run);
   // Out by whole lines: 64 elements of the wavefront's 32 rows at a time pass through LDS, in its own pieces of a tile (4 stretches of 1024 bytes).  A row's pieces of 16
   // bytes change places so that 8 rows' fall on different banks.
   const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
