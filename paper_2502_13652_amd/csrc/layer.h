@@ -42,16 +42,21 @@ inline int append_parts(int64_t tokens, int passes) { return tokens < APPEND_FEW
 // 4 heads over one of 128: 44 us so, and 22 divided; of 8192, one head, 170 and 68; 4 of 500, 8 over one, 15.9 and 17.8; one of 350, 32 over 8, 12.3 and 14.9.  Width 64, of which two such
 // workgroups fit a CU: 27 and 13, 97 and 39, 10.5 and 7.7, 8.9 and 6.9.  Of width 256, whose tiles hardly fit in LDS four times, the keys are never divided.
 typedef void (*PromptKernel)(const int32_t*, int32_t, int32_t, int32_t, int32_t, float, float, PromptArgs);
-constexpr int PROMPT_DIVIDED = 4;
-inline bool prompt_divided(int64_t tiles, int64_t rows, int64_t sequences, int head_dim) {     // tiles: of 128 rows, of all heads
+enum { PROMPT_MANY, PROMPT_SOME, PROMPT_DIVIDED };
+constexpr int PROMPT_KEYS = 4;                               // wavefronts that divide the keys
+inline int prompt_build(int64_t tiles, int64_t rows, int64_t sequences, int head_dim) {        // tiles: of 128 rows, of all heads
   const int64_t length = rows / sequences;
-  return head_dim == 64 ? tiles <= 4096 && tiles * tiles <= 64 * length : head_dim == 128 && tiles <= 4096 && tiles * tiles <= 20 * length;
+  if (head_dim <= 128 && tiles <= 4096 && tiles * tiles <= (head_dim == 64 ? 64 : 20) * length) return PROMPT_DIVIDED;
+  // Width 128, up to as many tiles as workgroups fit the card by three: two a CU with tiles of 64 keys (one prompt of 3000 tokens, 32 heads over 8, 79 us, by three with tiles of 32 88; of
+  // 1000 23.5 and 26.3); with more tiles three hide each other's start and end (64 prompts of up to 2000 850 and 780).
+  return head_dim == 128 && tiles <= 3 * 256 ? PROMPT_SOME : PROMPT_MANY;
 }
-template <typename E, bool LSE> PromptKernel prompt_kernel(int head_dim, bool divided) {
-  if (divided) return head_dim == 64 ? k_prompt<E, 64, 64, 1, PROMPT_DIVIDED, 2, LSE> : k_prompt<E, 128, 128, 1, PROMPT_DIVIDED, 1, LSE>;
+template <typename E, bool LSE> PromptKernel prompt_kernel(int head_dim, int build) {
+  if (build == PROMPT_DIVIDED) return head_dim == 64 ? k_prompt<E, 64, 64, 1, PROMPT_KEYS, 2, LSE> : k_prompt<E, 128, 128, 1, PROMPT_KEYS, 1, LSE>;
+  if (build == PROMPT_SOME) return k_prompt<E, 128, 128, 2, 1, 2, LSE>;
   return head_dim == 64 ? k_prompt<E, 64, 64, 2, 1, 4, LSE> : head_dim == 128 ? k_prompt<E, 128, 128, 1, 1, 3, LSE> : k_prompt<E, 256, 128, 1, 1, 2, LSE>;
 }
-template <typename E> PromptKernel prompt_kernel(int head_dim, bool divided, bool lse) { return lse ? prompt_kernel<E, true>(head_dim, divided) : prompt_kernel<E, false>(head_dim, divided); }
+template <typename E> PromptKernel prompt_kernel(int head_dim, int build, bool lse) { return lse ? prompt_kernel<E, true>(head_dim, build) : prompt_kernel<E, false>(head_dim, build); }
 inline int prompt_parts(int head_dim) { return head_dim > 128 ? 2 : 1; }    // of an output row
 constexpr int64_t MAX_PROMPT_STRIDE = 1 << 24;
 
@@ -163,11 +168,10 @@ int c2t_prompt_attention(const c2t_prompt* p, void* stream) {
   a.scale_log2e = std::max(p->scale, 1e-30f) * 1.44269504088896341f;       // (a masked score is -infinity times it: not 0)
   // each sequence has one tile at most that it does not fill
   const auto tiles = [&](int of) { return ((int64_t)p->rows * group / of + std::min(p->sequences, p->rows)) * p->kv_heads; };
-  const bool divided = prompt_divided(tiles(prompt_rows(1)), p->rows, p->sequences, p->head_dim);
-  const int kw = divided ? PROMPT_DIVIDED : 1;
+  const int build = prompt_build(tiles(prompt_rows(1)), p->rows, p->sequences, p->head_dim), kw = build == PROMPT_DIVIDED ? PROMPT_KEYS : 1;
   const int64_t blocks = tiles(prompt_rows(kw)) * prompt_parts(p->head_dim);
   if (blocks > MAX_BLOCKS) return C2T_ERR_UNSUPPORTED;
-  const PromptKernel fn = p->dtype == C2T_BF16 ? prompt_kernel<Bf16>(p->head_dim, divided, p->lse != nullptr) : prompt_kernel<F16>(p->head_dim, divided, p->lse != nullptr);
+  const PromptKernel fn = p->dtype == C2T_BF16 ? prompt_kernel<Bf16>(p->head_dim, build, p->lse != nullptr) : prompt_kernel<F16>(p->head_dim, build, p->lse != nullptr);
   hipLaunchKernelGGL(fn, dim3((unsigned)blocks), dim3((unsigned)(64 * prompt_waves(kw))), 0, (hipStream_t)stream, p->starts, p->rows, p->sequences, p->kv_heads, group,
                      1.f / (float)p->kv_heads, 1.f / (float)group, a);
   return hip_status();

@@ -39,8 +39,8 @@ def compare(q, k, v, at, out, lse=None, scale=None, before=None):
         assert torch.equal(out[~live].view(torch.int16), before[~live].view(torch.int16))
 
 
-# few heads: workgroups whose wavefronts divide the keys (widths 64 and 128); many: such as share them
-@pytest.mark.parametrize("D,Hq,Hkv,dtype", [(64, 4, 2, BF), (64, 5, 1, HF), (128, 2, 2, BF), (128, 8, 2, HF), (256, 3, 1, BF), (256, 4, 4, HF), (64, 80, 40, BF), (128, 48, 24, HF), (128, 27, 27, BF)])
+# few heads: workgroups whose wavefronts divide the keys (widths 64 and 128); more: such as share them, of width 128 by two and, of most, by three a CU
+@pytest.mark.parametrize("D,Hq,Hkv,dtype", [(64, 4, 2, BF), (64, 5, 1, HF), (128, 2, 2, BF), (128, 8, 2, HF), (256, 3, 1, BF), (256, 4, 4, HF), (64, 80, 40, BF), (128, 48, 24, HF), (128, 27, 27, BF), (128, 270, 90, BF)])
 @pytest.mark.parametrize("lens", [[1], [2], [31], [33], [64], [127], [128], [129], [257], [300], [1000], [1, 2, 3], [0, 5, 0, 0, 64, 1, 33, 0], [200, 17, 129, 1, 512], [5] * 30])
 def test_prompts(D, Hq, Hkv, dtype, lens):
     from paper_2502_13652_amd import prompt_attention
@@ -81,7 +81,7 @@ def test_many_sequences(n, longest):
     compare(q, k, v, at, out, before=torch.zeros_like(out))
 
 
-@pytest.mark.parametrize("dtype,D,Hq,Hkv", [(BF, 128, 2, 1), (HF, 64, 2, 1), (BF, 256, 2, 1), (BF, 128, 26, 26), (HF, 64, 45, 45)])
+@pytest.mark.parametrize("dtype,D,Hq,Hkv", [(BF, 128, 2, 1), (HF, 64, 2, 1), (BF, 256, 2, 1), (BF, 128, 26, 26), (HF, 64, 45, 45), (HF, 128, 260, 260)])
 @pytest.mark.parametrize("size,scale", [(30.0, None), (300.0, None), (1.0, 0.0), (1.0, 3.0), (2000.0, 1.0)])
 def test_sharp_and_flat_rows(dtype, D, Hq, Hkv, size, scale):
     """Scores of some thousands and more: a row is then the value of its largest score."""
@@ -110,7 +110,7 @@ def test_scores_past_what_exponents_hold(H):
     assert torch.equal(out.transpose(0, 1)[clear], want[clear])
 
 
-@pytest.mark.parametrize("D,dtype,Hq,Hkv", [(64, BF, 2, 1), (128, HF, 2, 1), (256, BF, 2, 1), (64, BF, 50, 50), (128, HF, 30, 30)])
+@pytest.mark.parametrize("D,dtype,Hq,Hkv", [(64, BF, 2, 1), (128, HF, 2, 1), (256, BF, 2, 1), (64, BF, 50, 50), (128, HF, 30, 30), (128, BF, 200, 200)])
 @pytest.mark.parametrize("value", [float("inf"), float("nan")])
 def test_values_that_are_not_finite_count_for_the_rows_that_see_them(D, dtype, Hq, Hkv, value):
     from paper_2502_13652_amd import prompt_attention
@@ -186,7 +186,7 @@ def test_empty_refused_streams_and_graphs():
         compare(q, k, v, at, out, lse, before=torch.full_like(out, 2.0))
 
 
-@pytest.mark.parametrize("Hq,Hkv", [(4, 1), (16, 8)])
+@pytest.mark.parametrize("Hq,Hkv", [(4, 1), (16, 8), (48, 24)])
 def test_the_bits_are_the_same_each_time(Hq, Hkv):
     from paper_2502_13652_amd import prompt_attention
     q, k, v = inputs(3000, Hq, Hkv, 128, BF, 16)
