@@ -161,7 +161,7 @@ def test_starts_that_make_no_sense():
     cache = make_cache([0, 0, 0, 0], 40, 16, 1, 64, BF, 9)
     k0 = cache.k.clone()
     q, k, v = projected((40,), 2, 1, 64, BF, 10)
-    for at in ([-5, -1, -1, -1, -1], [100, 200, 300, 400, 500], [2 ** 31 - 1, -2 ** 31, 0, 0, 0], [-3, 50, 50, 50, 50]):
+    for at in ([-5, -1, -1, -1, -1], [100, 200, 300, 400, 500], [2 ** 31 - 1, -2 ** 31, 0, 0, 0], [-3, 50, 50, 50, 50], [0, 0, 41, 41, 41], [0, 2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1]):
         out = cache.append(0, q, k, v, Rotation(64), starts=ints(at), q_out=torch.full((40, 2, 64), 3.0, dtype=BF, device="cuda"))
         assert bool((out == 3.0).all()) and torch.equal(cache.k, k0)
 
