@@ -202,3 +202,34 @@ def test_a_graph_of_a_prompts_layer_between_eager_calls():
         want, _, tol, _ = prompt_reference(q, k, v, at, D ** -0.5)
         near(out[live], want[live], tol[live])
         assert bool((out[:at[0]] == 2.0).all()) and bool((out[at[2]:] == 2.0).all())
+
+
+def test_the_example_of_the_readme():
+    """The README's prompts, line for line, through two layers."""
+    from paper_2502_13652_amd import PagedCache
+    from test_serving_host import readme_blocks
+    block = [b for b in readme_blocks() if "prompt_attention" in b]
+    assert len(block) == 1
+    layers, lens, at = 2, [37, 1, 300], [0, 37, 38, 338]
+    net = Layers(layers, 512, 16, 4, 128, 50)
+    cache = PagedCache(3, layers, 64, 16, 4, 128, 24)
+    made = []
+
+    def project(layer, y):
+        z = torch.matmul(y, net.qkv[layer]).view(-1, 24, 128)
+        made.append(z.clone())
+        return z[:, :16], z[:, 16:20], z[:, 20:]
+
+    names = dict(cache=cache, starts=ints(at), layers=layers, w_norm=net.norm, x=net.emb[torch.arange(338, device="cuda") % 50], h=torch.zeros((338, 512), device="cuda"),
+                 project=project, finish=lambda layer, y: net.end(y, layer))
+    exec(block[0], names)
+    assert cache.length.tolist() == lens and int(cache.status.view(torch.int32).abs().sum()) == 0
+    q, k, v = names["q"], names["k"], names["v"]
+    where = [p for n in lens for p in range(n)]
+    near(q, *turned_reference(made[1][:, :16], where, 128, frequencies(128), False, 1.0))
+    near(k, *turned_reference(made[1][:, 16:20], where, 128, frequencies(128), False, 1.0))
+    want, _, tol, _ = prompt_reference(q, k, v, at, 128 ** -0.5)
+    near(names["y"], want, tol)
+    for b, n in enumerate(lens):
+        kc, vc, ok = gathered(cache, b, 1, n)
+        assert bool(ok.all()) and torch.equal(kc.transpose(0, 1), k[at[b]:at[b + 1]].double()) and torch.equal(vc.transpose(0, 1), made[1][at[b]:at[b + 1], 20:].double())
