@@ -6,6 +6,15 @@
 // sum of the weights as the second product takes them, rounded to 16 bits, and the log of the sum is that of the weights as they were.  Products are taken transposed,
 // S^T = K Q^T in blocks of 32 keys and 32 rows: a lane then has one row (lane & 31) and, of each block, the keys 8 i + 4 (lane / 32) + 0..3, which are two operands of
 // out^T = V^T P^T, so weights never leave their registers.
+//
+// Keys and values go from memory into LDS without passing registers, a tile ahead.  A wavefront has 32 rows: of 64 it would read LDS half as often, but the sums of two would not fit its registers with
+// three wavefronts a SIMD, which is what hides a workgroup's start (finding its tile 3000 to 5000 cycles under load, its first keys 4000) and end (3000) behind others' products: 64 prompts of
+// up to 2000 tokens take 780 us, with two 850; workgroups that stay and take tile after tile, the next one's keys on their way, took 900 for 845 (tiles dealt ahead of time do not stay together in the L2).
+//
+// Measured, 32 heads over 8 of 128: one prompt of 8192 tokens 505 us for 550 GFLOP, 1.09 PFLOP/s, where an 8192-cubed matrix product gets 1.20: the matrix unit is busy for 64 % of the cycles, whose rate the
+// card's power then holds at 1.6 to 1.7 GHz; the 64 prompts 780 to 810 us, 0.87 to 0.90, busy for 50 %; one prompt of 200 8.6 us.  Width 64 (3 prompts of 2100 to 5001, halves, with the log of the sums) 118 us,
+// 0.73: vector instructions, five a score, take longer than its products.  Width 256 (6 prompts of 77 to 2500, 8 heads over one) 97 us, 0.6: half of a row's output is a workgroup's, and the scores are made
+// twice; all of it leaves one wavefront a SIMD, which took 170 us for one of 4096 tokens where this takes 128.
 #pragma once
 #include "k_attend.h"
 
