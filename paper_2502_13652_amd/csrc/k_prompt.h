@@ -13,8 +13,9 @@
 //
 // Measured, 32 heads over 8 of 128: one prompt of 8192 tokens 505 us for 550 GFLOP, 1.09 PFLOP/s, where an 8192-cubed matrix product gets 1.20: the matrix unit is busy for 64 % of the cycles, whose rate the
 // card's power then holds at 1.6 to 1.7 GHz; the 64 prompts 780 to 810 us, 0.87 to 0.90, busy for 50 %; one prompt of 200 8.6 us.  Width 64 (3 prompts of 2100 to 5001, halves, with the log of the sums) 118 us,
-// 0.73: vector instructions, five a score, take longer than its products.  Width 256 (6 prompts of 77 to 2500, 8 heads over one) 97 us, 0.6: half of a row's output is a workgroup's, and the scores are made
-// twice; all of it leaves one wavefront a SIMD, which took 170 us for one of 4096 tokens where this takes 128.
+// 0.73: vector instructions, five a score, take longer than its products.  Width 256 (6 prompts of 77 to 2500, 8 heads over one) 87 us, 0.66, of 8192 tokens 292, 0.94: pairs of
+// wavefronts wait for keys, weights and values in turn, 3600 cycles a tile of 64 keys of which the products take 1024, beside one other workgroup. Halves of the output by workgroups, with the scores
+// made twice, 97 and 348; a row's whole output in one wavefront, of which then one fits a SIMD, 170 for 4096 tokens where pairs take 114.
 #pragma once
 #include "k_attend.h"
 
@@ -157,7 +158,7 @@ __device__ __forceinline__ float add_pair(F16::T8 x, int pair, float a) {
 }
 
 constexpr int prompt_waves(int kw) { return kw > 1 ? kw : 4; }                   // of a workgroup, and its rows
-constexpr int prompt_rows(int kw) { return kw > 1 ? 32 : 32 * prompt_waves(kw); }
+constexpr int prompt_rows(int kw, bool pairs) { return kw > 1 ? 32 : 32 * prompt_waves(kw) / (pairs ? 2 : 1); }
 
 // How a block of PRODUCTS matrix instructions and READS reads of their operands is to be laid out: AHEAD reads, then EACH reads behind each product.
 template <int PRODUCTS, int READS, int AHEAD, int EACH> __device__ __forceinline__ void reads_ahead() {
@@ -170,17 +171,25 @@ template <int PRODUCTS, int READS, int AHEAD, int EACH> __device__ __forceinline
 }
 constexpr int K_AHEAD = 4, V_AHEAD = 2;                      // operands read ahead of their product
 
-// DV of the D elements of an output row are one workgroup's (D, or a part of them); KB blocks of 32 keys a tile; OCC workgroups a CU.  The wavefronts have 32 rows each and share the
-// tiles (KW = 1), or the same 32 rows and KW wavefronts every KW-th tile each, joined at the end: a quarter of the way along the keys where there are few rows.
+// KB blocks of 32 keys a tile; OCC workgroups a CU.  The wavefronts have 32 rows each and share the tiles (KW = 1), or the same 32 rows and KW wavefronts every KW-th tile each, joined at
+// the end: a quarter of the way along the keys where there are few rows.  DV of the D elements of an output row are one wavefront's: D; or half, as more sums do not fit its registers.  The
+// other half is then another workgroup's, which makes the scores once more (KB = 1), or PAIRS (KB = 2): two wavefronts have the same 32 rows, each makes the weights of one of a
+// tile's two blocks, which both take from LDS, and half of the output.
 template <typename E, int D, int DV, int KB, int KW, int OCC, bool LSE>
 __global__ __launch_bounds__(64 * prompt_waves(KW), OCC) void k_prompt(const int32_t* starts, int32_t all_rows, int32_t sequences, int32_t kv_heads, int32_t G, float inv_kv_heads,
                                                                        float inv_group, PromptArgs a) {
   typedef typename E::T T; typedef typename E::T4 T4; typedef typename E::T8 T8;
-  constexpr int WAVES = prompt_waves(KW), NT = 64 * WAVES, ROWS = prompt_rows(KW), KT = 32 * KB, PARTS = D / DV, DB = DV / 32, DK = D / 16;
+  constexpr bool PAIRS = DV < D && KB == 2;
+  static_assert(!PAIRS || (KW == 1 && D == 2 * DV), "");
+  constexpr int WAVES = prompt_waves(KW), NT = 64 * WAVES, ROWS = prompt_rows(KW, PAIRS), KT = 32 * KB, PARTS = PAIRS ? 1 : D / DV, DB = DV / 32, DK = D / 16;
+  constexpr int VW = PAIRS ? D : DV;                         // elements of a V row in LDS
   constexpr int SHARERS = KW > 1 ? 64 : NT;                  // threads that load a tile together
-  constexpr int K_LOADS = KT * D / 8 / SHARERS, V_LOADS = KT * DV / 8 / SHARERS, K_TILE = KT * D * 2, TILE = K_TILE + KT * DV * 2;
+  constexpr int K_LOADS = KT * D / 8 / SHARERS, V_LOADS = KT * VW / 8 / SHARERS, K_TILE = KT * D * 2, TILE = K_TILE + KT * VW * 2;
   constexpr float TOP = E::TOP, SLACK = E::SLACK, BIG = 0x1p22f;
-  __shared__ __align__(16) char lds[2 * TILE * KW];          // K and V, two buffers, of each wavefront that has tiles of its own
+  constexpr int WEIGHTS = 2 * 64 * 16;                       // PAIRS: a wavefront's of a tile, two operands a lane
+  __shared__ __align__(16) char lds[PAIRS ? TILE + WAVES * WEIGHTS : 2 * TILE * KW];  // K and V, two buffers, of each wavefront that has tiles of its own; PAIRS: one, and weights
+  __shared__ __align__(16) int moves_of[4];                  // PAIRS: whether a wavefront's scores ask for another reference,
+  __shared__ float tops[PAIRS ? WAVES * 32 : 1];             // and its rows' largest then
   __shared__ int odd_value;                                  // a tile held a value that is not finite (KW = 1)
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), col = lane & 31, half = lane >> 5;
   const int kw = KW > 1 ? wave : 0, lt = KW > 1 ? lane : tid;        // this thread among those that load a tile
@@ -191,12 +200,12 @@ __global__ __launch_bounds__(64 * prompt_waves(KW), OCC) void k_prompt(const int
   // many heads there are, and short prompts fill tiles.
   if (KW == 1 && tid == 0) odd_value = 0;
   PromptTile u;
-  const int part = blockIdx.x % PARTS;
+  const int part = PAIRS ? wave & 1 : blockIdx.x % PARTS;
   int rank, head;
   split(blockIdx.x / PARTS, kv_heads, inv_kv_heads, &rank, &head);
   rank = uniform(rank); head = uniform(head);
   if (!find_tile<ROWS>(PromptShape{starts, all_rows, sequences, kv_heads, G, inv_kv_heads, inv_group}, rank, &u)) return;
-  const int row0 = u.tile * ROWS, wave_row0 = row0 + (KW > 1 ? 0 : wave * 32), rows = u.n * G;
+  const int row0 = u.tile * ROWS, wave_row0 = row0 + (KW > 1 ? 0 : PAIRS ? wave / 2 * 32 : wave * 32), rows = u.n * G;
   const auto token_of = [&](int row, int* g) { int t; split(min(row, rows - 1), G, inv_group, &t, g); return t; };      // (rows behind the last are not put out)
   int my_g, no_g;
   const int my_token = token_of(wave_row0 + col, &my_g);
@@ -204,18 +213,18 @@ __global__ __launch_bounds__(64 * prompt_waves(KW), OCC) void k_prompt(const int
   const int keys = uniform(token_of(row0 + ROWS - 1, &no_g)) + 1, n_tiles = div_up(keys, KT);
   const bool idle = wave_row0 >= rows;
   const char* const k_head = a.k + u.first * a.k_row + (int64_t)head * (D * 2);
-  const char* const v_head = a.v + u.first * a.v_row + (int64_t)head * (D * 2) + part * (DV * 2);
+  const char* const v_head = a.v + u.first * a.v_row + (int64_t)head * (D * 2) + (PAIRS ? 0 : part * (DV * 2));
 
   // A tile's pieces: this thread's j-th lies j SHARERS + lt pieces into K's or V's tile in LDS, and is the piece of its row that piece_at puts there: the same one in every 16th row, so
   // that one offset (two, of rows of 8 a load) does for all of a tile's.
-  constexpr int K_ROWS = SHARERS / (D / 8), V_ROWS = SHARERS / (DV / 8), K_KINDS = K_ROWS < 16 ? 16 / K_ROWS : 1, V_KINDS = V_ROWS < 16 ? 16 / V_ROWS : 1;      // rows a load, offsets
+  constexpr int K_ROWS = SHARERS / (D / 8), V_ROWS = SHARERS / (VW / 8), K_KINDS = K_ROWS < 16 ? 16 / K_ROWS : 1, V_KINDS = V_ROWS < 16 ? 16 / V_ROWS : 1;      // rows a load, offsets
   const auto k_piece = [&](int j) { const int row = j * K_ROWS + lt / (D / 8); return (uint32_t)(piece_at<D>(row, lt % (D / 8)) - row * (D * 2)); };
-  const auto v_piece = [&](int j) { const int row = j * V_ROWS + lt / (DV / 8); return (uint32_t)(piece_at<DV>(row, lt % (DV / 8)) - row * (DV * 2)); };
+  const auto v_piece = [&](int j) { const int row = j * V_ROWS + lt / (VW / 8); return (uint32_t)(piece_at<VW>(row, lt % (VW / 8)) - row * (VW * 2)); };
   uint32_t k_off[K_KINDS], v_off[V_KINDS];
 #pragma unroll
   for (int j = 0; j < K_KINDS; ++j) k_off[j] = lt / (D / 8) * (uint32_t)a.k_row + k_piece(j);
 #pragma unroll
-  for (int j = 0; j < V_KINDS; ++j) v_off[j] = lt / (DV / 8) * (uint32_t)a.v_row + v_piece(j);
+  for (int j = 0; j < V_KINDS; ++j) v_off[j] = lt / (VW / 8) * (uint32_t)a.v_row + v_piece(j);
   const uint32_t lds_wave = lds_address(tiles) + (KW > 1 ? 0 : wave * 1024);
   const char* k_at = k_head + kw * KT * a.k_row; const char* v_at = v_head + kw * KT * a.v_row;
   int ahead = keys - kw * KT;                                          // keys from there on
@@ -230,9 +239,31 @@ __global__ __launch_bounds__(64 * prompt_waves(KW), OCC) void k_prompt(const int
 #pragma unroll
       for (int j = 0; j < K_LOADS; ++j) load_to_lds(k_at, (uint32_t)min(j * K_ROWS + lt / (D / 8), ahead - 1) * (uint32_t)a.k_row + k_piece(j), to + j * SHARERS * 16);
 #pragma unroll
-      for (int j = 0; j < V_LOADS; ++j) load_to_lds(v_at, (uint32_t)min(j * V_ROWS + lt / (DV / 8), ahead - 1) * (uint32_t)a.v_row + v_piece(j), to + K_TILE + j * SHARERS * 16);
+      for (int j = 0; j < V_LOADS; ++j) load_to_lds(v_at, (uint32_t)min(j * V_ROWS + lt / (VW / 8), ahead - 1) * (uint32_t)a.v_row + v_piece(j), to + K_TILE + j * SHARERS * 16);
     }
     k_at += KW * KT * a.k_row; v_at += KW * KT * a.v_row; ahead -= KW * KT;
+  };
+  // PAIRS: K or V alone (whose tiles are alike), a load at a time between the products: asked for at once, a tile's loads wait 700 cycles for each other.  Loads behind the one with the last of `left`
+  // keys ask for that one's rows, rows behind the last key for the last key's.
+  struct Ask { const char* at; int last; uint32_t off[K_KINDS], end[K_KINDS]; };
+  const auto ask = [&](const char* at, const uint32_t* off, int64_t row, int left) {
+    Ask x;
+    x.at = at; x.last = min((left - 1) / K_ROWS, K_LOADS - 1);
+#pragma unroll
+    for (int j = 0; j < K_KINDS; ++j) x.off[j] = x.end[j] = off[j];
+    if (left < KT) {
+      int t = lt;
+      settle(t);                                             // (rare: nothing of it is kept in registers)
+#pragma unroll
+      for (int j = 0; j < K_KINDS; ++j) {
+        const int r = j * K_ROWS + t / (D / 8);
+        x.end[j] = (uint32_t)min(t / (D / 8), left - 1 - x.last * K_ROWS) * (uint32_t)row + (uint32_t)(piece_at<D>(r, t % (D / 8)) - r * (D * 2));
+      }
+    }
+    return x;
+  };
+  const auto ask_piece = [&](const Ask& x, int64_t row, uint32_t to, int j) {
+    load_to_lds(x.at + (uint32_t)min(j, x.last) * (uint32_t)(K_ROWS * row), j < x.last ? x.off[j % K_KINDS] : x.end[j % K_KINDS], to + j * SHARERS * 16);
   };
   // Waits for this wavefront's pieces.  Where some rows see a value that others do not, one that is not finite is left out of the product and added for the rows that see it.
   const auto arrived = [&](int buffer, bool diagonal) {
@@ -241,6 +272,7 @@ __global__ __launch_bounds__(64 * prompt_waves(KW), OCC) void k_prompt(const int
     bool odd = false;
 #pragma unroll
     for (int j = 0; j < V_LOADS; ++j) {
+      if (PAIRS) __builtin_amdgcn_sched_barrier(0);          // (one at a time: scores are in registers here)
       u32x4* const at = (u32x4*)(tiles + buffer * TILE + K_TILE + (j * SHARERS + lt) * 16);
       const u32x4 x = *at;
       const u32x4 bad = {odd_halves<E>(x.x), odd_halves<E>(x.y), odd_halves<E>(x.z), odd_halves<E>(x.w)};
@@ -252,8 +284,15 @@ __global__ __launch_bounds__(64 * prompt_waves(KW), OCC) void k_prompt(const int
   // Where this lane's operands begin: of K row `col` and piece `half`, of V rows 4 half + (lane & 15) / 4 and the lane's 8 bytes of a block of 32 elements.  The others lie at these
   // places but for whole rows and bits of the piece's number.
   const int k_place = piece_at<D>(col, half);
-  const int v_place = K_TILE + piece_at<DV>(half * 4 + (lane & 15) / 4, (lane >> 4 & 1) * 2 + (lane & 3) / 2) + (lane & 1) * 8;
-  if (kw < n_tiles) request(0);
+  const int v_place = K_TILE + piece_at<VW>(half * 4 + (lane & 15) / 4, (lane >> 4 & 1) * 2 + (lane & 3) / 2) + (lane & 1) * 8 + (PAIRS ? part * (DV * 2) : 0);
+  if constexpr (PAIRS) {
+    const Ask x = ask(k_at, k_off, a.k_row, keys);
+#pragma unroll
+    for (int j = 0; j < K_LOADS; ++j) ask_piece(x, a.k_row, lds_wave, j);
+    k_at += KT * a.k_row;
+  } else {
+    if (kw < n_tiles) request(0);
+  }
   T8 q[DK];
   {
     const char* const from = a.q + ((int64_t)u.first + my_token) * a.q_row + query_offset(head, G, my_g, D) * 2 + half * 16;
@@ -261,7 +300,8 @@ __global__ __launch_bounds__(64 * prompt_waves(KW), OCC) void k_prompt(const int
     for (int kk = 0; kk < DK; ++kk) q[kk] = *(const T8*)(from + kk * 32);
   }
   if (KW == 1 && KT > first_token) __syncthreads();          // (odd_value)
-  if (kw < n_tiles) arrived(0, kw * KT + KT > first_token);
+  if constexpr (PAIRS) wait_vector_memory();
+  else if (kw < n_tiles) arrived(0, kw * KT + KT > first_token);
   // The queries are here before the loop, or each of its rounds would wait for them, and for the next tile's pieces, which are younger, with them.
 #pragma unroll
   for (int kk = 0; kk < DK; ++kk) { u32x4 x = __builtin_bit_cast(u32x4, q[kk]); settle(x); q[kk] = __builtin_bit_cast(T8, x); }
@@ -274,7 +314,141 @@ __global__ __launch_bounds__(64 * prompt_waves(KW), OCC) void k_prompt(const int
   float m_run = -INFINITY, e_run = 0.f, l_run = 0.f, factor = a.scale_log2e;
   int big = 0;
 
-  for (int t = kw; t < n_tiles; t += KW) {
+  if constexpr (PAIRS) {
+    // One buffer each: V of this tile comes while its scores are made, K of the next one during the second product.  Weights are made with the reference as it is; where a row's scores ask for another,
+    // all wavefronts know it behind the barrier, and they are made once more.
+    const int my_keys = part * 32;
+    char* const pair_weights = lds + TILE + (wave & ~1) * WEIGHTS + lane * 16; char* const my_weights = pair_weights + part * WEIGHTS;
+    for (int t = 0; t < n_tiles; ++t) {
+      const int key0 = t * KT;
+      const bool sees = !idle && key0 + my_keys <= wave_last;
+      const Ask ask_v = ask(v_at, v_off, a.v_row, keys - key0);
+      v_at += KT * a.v_row;
+      f32x16 s;
+      float top = -INFINITY, l_add = 0.f, e_add = 0.f;
+      T8 p[4];
+      const auto weights = [&](float ref) {
+        l_add = e_add = 0.f;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int pair = 0; pair < 4; ++pair) {
+#pragma unroll
+            for (int r = pair * 2; r < pair * 2 + 2; ++r) {
+              const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h * 8 + r], factor, -ref));
+              if (LSE) e_add += w;
+              p[h][r] = (T)w;
+            }
+            l_add = add_pair(p[h], pair, l_add);
+          }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) *(T8*)(my_weights + h * 1024) = p[h];
+      };
+      bool moves = false;
+      if (sees) {
+        int k_base = k_place + part * 32 * (D * 2);
+        settle(k_base);
+        T8 k[DK];
+        const auto read_k = [&](int i) { k[i] = *(const T8*)(tiles + (k_base ^ i * 32)); };
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+        for (int i = 0; i < K_AHEAD; ++i) read_k(i);
+#pragma unroll
+        for (int kk = 0; kk < DK; ++kk) {
+          __builtin_amdgcn_sched_barrier(0);
+          s = product32(k[kk], q[kk], s);
+          if (kk + K_AHEAD < DK) read_k(kk + K_AHEAD);
+          if (kk % 2 == 1) ask_piece(ask_v, a.v_row, lds_wave + K_TILE, kk / 2);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        settle(s);
+        if (key0 + my_keys + 31 > wave_first) {
+          const int last_seen = my_token - key0 - my_keys - half * 4;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[i] = i / 4 * 8 + i % 4 <= last_seen ? s[i] : -INFINITY;
+        }
+        if (big != 0) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[i] *= a.scale_log2e;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[i]);
+        top *= factor;
+        moves = __any(top - m_run > TOP);
+        if (!moves) {
+          weights(m_run == -INFINITY ? 0.f : m_run);
+        } else {
+          top = fmaxf(top, __shfl_xor(top, 32));
+          if (half == 0) tops[wave * 32 + col] = top;
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < V_LOADS; ++j) ask_piece(ask_v, a.v_row, lds_wave + K_TILE, j);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) *(u32x4*)(my_weights + h * 1024) = u32x4{0u, 0u, 0u, 0u};
+      }
+      if (lane == 0) moves_of[wave] = moves;
+      arrived(0, key0 + KT > first_token);
+      __syncthreads();
+      typedef int i32x4 __attribute__((ext_vector_type(4)));
+      const i32x4 moving = *(const i32x4*)moves_of;
+      const int other_moves = moves_of[wave ^ 1];
+      const auto read_p = [&]() {
+#pragma unroll
+        for (int h = 0; h < 4; ++h) p[h] = *(const T8*)(pair_weights + h * 1024);
+      };
+      read_p();
+      if (uniform(moving.x | moving.y | moving.z | moving.w) != 0) {       // of all wavefronts together
+        if (!moves) top = -INFINITY;
+        if (uniform(other_moves) != 0) top = fmaxf(top, tops[(wave ^ 1) * 32 + col]);
+        float m_new = fmaxf(m_run, top - (TOP - SLACK));
+        if (top - m_new > TOP) m_new = top;
+        if (big == 0 && __any(__builtin_fabsf(m_new) >= BIG && m_new != -INFINITY)) {
+          big = 1; factor = 1.f;
+          if (sees)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] *= a.scale_log2e;
+        }
+        const float back = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
+        m_run = m_new;
+        l_run *= back; e_run *= back;
+#pragma unroll
+        for (int i = 0; i < DB * 16; ++i) o[i / 16][i % 16] *= back;
+        if (sees) weights(m_run == -INFINITY ? 0.f : m_run);
+        __syncthreads();
+        read_p();
+      }
+      const bool more = t + 1 < n_tiles;                     // (behind the last tile: the first key's row, which nothing reads)
+      const Ask ask_k = ask(more ? k_at : k_head, k_off, a.k_row, more ? keys - key0 - KT : 1);
+      k_at += KT * a.k_row;
+      l_run += l_add; e_run += e_add;
+      // (Wavefronts whose rows see none of the tile take part with weights of zero; from such a tile, values that are not finite have been taken out.)
+      int v_base = v_place;
+      settle(v_base);
+      T8 v[4 * DB];
+      const auto read_v = [&](int i) {
+        const int h = i / DB, d = i % DB;
+        typedef __attribute__((address_space(3))) s16x4* lds4;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(tiles + (v_base ^ d * 64) + h * 16 * (VW * 2)));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(tiles + (v_base ^ (d * 64 + 32)) + (h * 16 + 8) * (VW * 2)));
+        struct { s16x4 a, b; } both{lo, hi};
+        v[i] = __builtin_bit_cast(T8, both);
+      };
+#pragma unroll
+      for (int i = 0; i < V_AHEAD; ++i) read_v(i);
+#pragma unroll
+      for (int i = 0; i < 4 * DB; ++i) {
+        __builtin_amdgcn_sched_barrier(0);
+        o[i % DB] = product32(v[i], p[i / DB], o[i % DB]);
+        if (i + V_AHEAD < 4 * DB) read_v(i + V_AHEAD);
+        if (i % 2 == 1) ask_piece(ask_k, a.k_row, lds_wave, i / 2);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      wait_vector_memory();
+      __syncthreads();
+    }
+  } else for (int t = kw; t < n_tiles; t += KW) {
     const int key0 = t * KT, buffer = t / KW & 1;
     if (t + KW < n_tiles) request(buffer ^ 1);
     if (!idle && key0 <= wave_last) {
@@ -340,8 +514,8 @@ __global__ __launch_bounds__(64 * prompt_waves(KW), OCC) void k_prompt(const int
       const auto read_v = [&](int i) {
         const int h = i / DB, d = i % DB;
         typedef __attribute__((address_space(3))) s16x4* lds4;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(tiles + (v_base ^ d * 64) + h * 16 * (DV * 2)));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(tiles + (v_base ^ (d * 64 + 32)) + (h * 16 + 8) * (DV * 2)));
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(tiles + (v_base ^ d * 64) + h * 16 * (VW * 2)));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(tiles + (v_base ^ (d * 64 + 32)) + (h * 16 + 8) * (VW * 2)));
         struct { s16x4 a, b; } both{lo, hi};
         v[i] = __builtin_bit_cast(T8, both);
       };
@@ -365,12 +539,19 @@ __global__ __launch_bounds__(64 * prompt_waves(KW), OCC) void k_prompt(const int
   }
 #pragma unroll
   for (int d = 0; d < DB; ++d) settle(o[d]);
-  if (idle) return;
+  if (!PAIRS && idle) return;
   l_run += __shfl_xor(l_run, 32); e_run += __shfl_xor(e_run, 32);
+  if constexpr (PAIRS) {                                     // (each has those of its keys, by one reference)
+    float* const sums = (float*)(lds + TILE);
+    if (half == 0) { sums[wave * 64 + col] = l_run; sums[wave * 64 + 32 + col] = e_run; }
+    __syncthreads();
+    l_run += sums[(wave ^ 1) * 64 + col]; e_run += sums[(wave ^ 1) * 64 + 32 + col];
+    if (idle) return;
+  }
 
   if (KW > 1 ? my_odd : odd_value != 0) {                    // values that are not finite: a weight is made again from its key
     const char* const k_odd = k_head + half * 16;
-    const char* const v_odd = v_head + half * 8;
+    const char* const v_odd = v_head + (PAIRS ? part * (DV * 2) : 0) + half * 8;
     for (int key = first_token / KT * KT; key <= wave_last; ++key) {
       if (KW > 1 && key / KT % KW != kw) continue;
       const auto value = [&](int d) { return *(const T4*)(v_odd + key * a.v_row + d * 16); };

@@ -60,6 +60,36 @@ def test_prompts(D, Hq, Hkv, dtype, lens):
     assert bool((lse[:at[0]] == 7.0).all()) and bool((lse[at[-1]:] == 7.0).all())
 
 
+# width 256 with rows enough for each sequence: pairs of wavefronts that share a tile's weights
+@pytest.mark.parametrize("Hq,Hkv,dtype", [(8, 1, BF), (3, 1, HF), (4, 4, BF), (64, 2, HF), (65, 1, BF)])
+@pytest.mark.parametrize("lens", [[1], [31, 32, 33], [63, 64, 65], [15, 16, 17, 128, 129], [1000], [257, 0, 1, 700, 0], [450, 400, 1, 2, 3, 900]])
+def test_pairs(Hq, Hkv, dtype, lens):
+    from paper_2502_13652_amd import prompt_attention
+    at = starts_of(lens, first=len(lens) % 2)
+    rows = max(at[-1] + 2, 400 * len(lens))
+    q, k, v = inputs(rows, Hq, Hkv, 256, dtype, sum(lens) + Hq)
+    out, lse = torch.full((rows, Hq, 256), 7.0, dtype=dtype, device="cuda"), torch.full((rows, Hq), 7.0, device="cuda")
+    before = out.clone()
+    starts = torch.tensor(at, dtype=torch.int32, device="cuda")
+    prompt_attention(q, k, v, starts, out=out, lse=lse)
+    compare(q, k, v, at, out, lse, before=before)
+    assert bool((lse[:at[0]] == 7.0).all()) and bool((lse[at[-1]:] == 7.0).all())
+    again = prompt_attention(q.contiguous(), k.contiguous(), v.contiguous(), starts, out=before)
+    assert again is before and torch.equal(before, out)
+
+
+def test_pairs_where_the_largest_scores_come_late():
+    """References move in each tile, of some rows and for one of a pair's wavefronts at a time; rows of the last tile, of which the array ends within."""
+    from paper_2502_13652_amd import prompt_attention
+    q, k, v = (x.clone() for x in inputs(777, 4, 1, 256, BF, 17))
+    step = torch.arange(777, device="cuda")
+    k *= (1 + step // 32 * 2.0).to(BF)[:, None, None]
+    k[step % 96 == 5] *= 3
+    lse = torch.zeros((777, 4), device="cuda")
+    out = prompt_attention(q, k, v, torch.tensor([0, 777], dtype=torch.int32, device="cuda"), lse=lse)
+    compare(q, k, v, [0, 777], out, lse)
+
+
 @pytest.mark.parametrize("Hq,Hkv,D", [(40, 1, 64), (129, 1, 64), (33, 11, 128), (200, 1, 128), (7, 7, 256)])
 def test_groups_that_do_not_fill_a_tile_evenly(Hq, Hkv, D):
     from paper_2502_13652_amd import prompt_attention
@@ -81,14 +111,15 @@ def test_many_sequences(n, longest):
     compare(q, k, v, at, out, before=torch.zeros_like(out))
 
 
-@pytest.mark.parametrize("dtype,D,Hq,Hkv", [(BF, 128, 2, 1), (HF, 64, 2, 1), (BF, 256, 2, 1), (BF, 128, 26, 26), (HF, 64, 45, 45), (HF, 128, 260, 260)])
+@pytest.mark.parametrize("dtype,D,Hq,Hkv", [(BF, 128, 2, 1), (HF, 64, 2, 1), (BF, 256, 2, 1), (BF, 128, 26, 26), (HF, 64, 45, 45), (HF, 128, 260, 260), (BF, 256, 8, 2), (HF, 256, 8, 2)])
 @pytest.mark.parametrize("size,scale", [(30.0, None), (300.0, None), (1.0, 0.0), (1.0, 3.0), (2000.0, 1.0)])
 def test_sharp_and_flat_rows(dtype, D, Hq, Hkv, size, scale):
     """Scores of some thousands and more: a row is then the value of its largest score."""
     from paper_2502_13652_amd import prompt_attention
     at = starts_of([150, 40])
-    q, k, v = inputs(190, Hq, Hkv, D, dtype, 11, size)
-    lse = torch.zeros((190, Hq), device="cuda")
+    rows = 900 if (Hq, D) == (8, 256) else 190               # (pairs)
+    q, k, v = inputs(rows, Hq, Hkv, D, dtype, 11, size)
+    lse = torch.zeros((rows, Hq), device="cuda")
     out = prompt_attention(q, k, v, torch.tensor(at, dtype=torch.int32, device="cuda"), scale=scale, lse=lse)
     compare(q, k, v, at, out, lse, scale=scale)
 
@@ -110,13 +141,13 @@ def test_scores_past_what_exponents_hold(H):
     assert torch.equal(out.transpose(0, 1)[clear], want[clear])
 
 
-@pytest.mark.parametrize("D,dtype,Hq,Hkv", [(64, BF, 2, 1), (128, HF, 2, 1), (256, BF, 2, 1), (64, BF, 50, 50), (128, HF, 30, 30), (128, BF, 200, 200)])
+@pytest.mark.parametrize("D,dtype,Hq,Hkv", [(64, BF, 2, 1), (128, HF, 2, 1), (256, BF, 2, 1), (64, BF, 50, 50), (128, HF, 30, 30), (128, BF, 200, 200), (256, BF, 8, 2), (256, HF, 8, 2)])
 @pytest.mark.parametrize("value", [float("inf"), float("nan")])
 def test_values_that_are_not_finite_count_for_the_rows_that_see_them(D, dtype, Hq, Hkv, value):
     from paper_2502_13652_amd import prompt_attention
     lens = [140, 200]
     at = starts_of(lens, 2)
-    rows = at[-1] + 4
+    rows = 900 if (Hq, D) == (8, 256) else at[-1] + 4        # (pairs)
     q, k, v = (x.clone() for x in inputs(rows, Hq, Hkv, D, dtype, 13))
     starts = torch.tensor(at, dtype=torch.int32, device="cuda")
     clean = prompt_attention(q, k, v, starts)
@@ -186,10 +217,10 @@ def test_empty_refused_streams_and_graphs():
         compare(q, k, v, at, out, lse, before=torch.full_like(out, 2.0))
 
 
-@pytest.mark.parametrize("Hq,Hkv", [(4, 1), (16, 8), (48, 24)])
-def test_the_bits_are_the_same_each_time(Hq, Hkv):
+@pytest.mark.parametrize("Hq,Hkv,D", [(4, 1, 128), (16, 8, 128), (48, 24, 128), (8, 2, 256)])
+def test_the_bits_are_the_same_each_time(Hq, Hkv, D):
     from paper_2502_13652_amd import prompt_attention
-    q, k, v = inputs(3000, Hq, Hkv, 128, BF, 16)
+    q, k, v = inputs(3000, Hq, Hkv, D, BF, 16)
     starts = torch.tensor([0, 1700, 1701, 3000], dtype=torch.int32, device="cuda")
     first = prompt_attention(q, k, v, starts)
     for _ in range(5):
