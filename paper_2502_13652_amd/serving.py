@@ -84,12 +84,14 @@ def _whole(t, device, dtype, shape, name):
 
 
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_current_stream = binding._current_raw_stream or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 def _launch(device, stream, fn, *args):
     """fn(*args, stream handle) with the tensors' device current."""
-    if stream is None and _current_device() == device.index:
-        return fn(*args, binding._stream_ptr(None))
+    index = device.index
+    if stream is None and _current_device() == index:
+        return fn(*args, _current_stream(index))
     _need(stream is None or stream.device == device, "stream: of another device than the tensors")
     with torch.cuda.device(device):
         return fn(*args, binding._stream_ptr(stream))
