@@ -208,3 +208,26 @@ def test_empty_refused_streams_and_graphs():
             if n:
                 near(out[b, :n], *turned_reference(q[b, :n], [lens[b] + t for t in range(n)], 64, frequencies(64), False, 1.0))
             assert bool((out[b, n:] == 2.0).all())
+
+
+def test_rows_and_pages_whose_offsets_pass_32_bits():
+    from paper_2502_13652_amd import PagedCache, Rotation
+    pages = 140000                                           # of 32 KiB each: 4.6 GB of keys
+    cache = PagedCache(3, 1, pages, 16, 8, 128, 4)
+    taken = [7, pages - 1, pages - 2, 131072, 3, 100000]
+    cache.page_table.copy_(torch.tensor([taken[0:2] + [-1, -1], taken[2:4] + [-1, -1], taken[4:6] + [-1, -1]], dtype=torch.int32))
+    cache.refcount[taken] = 1
+    cache.length.copy_(torch.tensor([3, 14, 0], dtype=torch.int32))
+    q, k, v = (x.contiguous() for x in projected((3, 17), 8, 8, 128, BF, 23))
+    apart = torch.empty(2 * 2 ** 30 + 40 * 17 * 1024, dtype=BF, device="cuda")
+    far = [apart.as_strided((3, 17, 8, 128), (2 ** 30, 1024, 128, 1), 17 * 1024 * i) for i in range(5)]
+    for to, x in zip(far, (q, k, v)):
+        to.copy_(x)
+    cache.append(0, *far[:3], Rotation(128), q_out=far[3], k_out=far[4])
+    assert int(cache.status.view(torch.int32).abs().sum()) == 0
+    for b, n in enumerate((3, 14, 0)):
+        where = list(range(n, n + 17))
+        for got, x in ((far[3], q), (far[4], k)):
+            near(got[b], *turned_reference(x[b], where, 128, frequencies(128), False, 1.0))
+        kc, vc, ok = gathered(cache, b, 0, n + 17)
+        assert bool(ok.all()) and torch.equal(kc[:, n:].transpose(0, 1), far[4][b].double()) and torch.equal(vc[:, n:].transpose(0, 1), v[b].double())

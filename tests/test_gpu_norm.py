@@ -163,3 +163,16 @@ def test_empty_refused_streams_and_graphs():
         graph.replay()
         torch.cuda.synchronize()
         check(x, w, r, out8, sc, to, 128)
+
+
+@pytest.mark.parametrize("width,shift", [(512, 0), (501, 3)])
+def test_rows_whose_offsets_pass_32_bits(width, shift):
+    from paper_2502_13652_amd import rms_norm
+    x, w, r = inputs(4, width, BF, BF, BF, 21)
+    apart = torch.empty(3 * 2 ** 30 + 4096, dtype=BF, device="cuda")
+    far = [apart.as_strided((4, width), (2 ** 30, 1), 1024 * i + shift) for i in range(3)]
+    far[0].copy_(x)
+    far[1].copy_(r)
+    rms_norm(far[0], w, EPS, residual=far[1], out=far[2])
+    want = rms_norm(x, w, EPS, residual=r)
+    assert torch.equal(far[2], want) and torch.equal(far[1], r) and torch.equal(far[0], x)

@@ -225,3 +225,21 @@ def test_the_bits_are_the_same_each_time(Hq, Hkv, D):
     first = prompt_attention(q, k, v, starts)
     for _ in range(5):
         assert torch.equal(prompt_attention(q, k, v, starts), first)
+
+
+@pytest.mark.parametrize("D,Hq,Hkv,rows", [(64, 2, 1, 150), (128, 2, 2, 150), (128, 300, 75, 130), (256, 2, 1, 150), (256, 2, 1, 420)])
+def test_rows_whose_offsets_pass_32_bits(D, Hq, Hkv, rows):
+    from paper_2502_13652_amd import prompt_attention
+    q, k, v = inputs(rows, Hq, Hkv, D, BF, 18)
+    starts = torch.tensor([0, rows - 30, rows], dtype=torch.int32, device="cuda") if rows < 400 else torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+    step = 1 << 24
+    apart = torch.empty((rows - 1) * step + 3 * Hq * D + Hkv * D, dtype=BF, device="cuda")
+    places, far = 0, []
+    for x in (q, k, v, q):
+        heads = x.shape[1]
+        far.append(apart.as_strided((rows, heads, D), (step, D, 1), places))
+        places += heads * D
+    for to, x in zip(far, (q, k, v)):
+        to.copy_(x)
+    prompt_attention(far[0], far[1], far[2], starts, out=far[3])
+    assert torch.equal(far[3], prompt_attention(q, k, v, starts))
