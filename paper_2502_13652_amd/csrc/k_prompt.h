@@ -12,16 +12,17 @@
 // up to 2000 tokens take 780 us, with two 850; workgroups that stay and take tile after tile, the next one's keys on their way, took 900 for 845 (tiles dealt ahead of time do not stay together in the L2).
 //
 // Measured, 32 heads over 8 of 128: one prompt of 8192 tokens 505 us for 550 GFLOP, 1.09 PFLOP/s, where an 8192-cubed matrix product gets 1.20: the matrix unit is busy for 64 % of the cycles, whose rate the
-// card's power then holds at 1.6 to 1.7 GHz; the 64 prompts 780 to 810 us, 0.87 to 0.90, busy for 50 %; one prompt of 200 8.6 us.  Width 64 (3 prompts of 2100 to 5001, halves, with the log of the sums) 118 us,
-// 0.73: vector instructions, five a score, take longer than its products.  Width 256 (6 prompts of 77 to 2500, 8 heads over one) 87 us, 0.66, of 8192 tokens 292, 0.94: pairs of
-// wavefronts wait for keys, weights and values in turn, 3600 cycles a tile of 64 keys of which the products take 1024, beside one other workgroup. Halves of the output by workgroups, with the scores
-// made twice, 97 and 348; a row's whole output in one wavefront, of which then one fits a SIMD, 170 for 4096 tokens where pairs take 114.
+// card's power then holds at 1.6 to 1.7 GHz; the 64 prompts 780 to 810 us, 0.87 to 0.90, busy for 50 %; one prompt of 200 7.8 us: the tile found after 1.4, its first keys there after 2.7, two tiles 2.5.
+// Width 64 (3 prompts of 2100 to 5001, halves, with the log of the sums) 118 us, 0.73: vector instructions, five a score, take longer than its products.  Width 256 (6 prompts of 77 to 2500, 8 heads
+// over one) 85 us, 0.68, of 8192 tokens 292, 0.94: pairs of wavefronts wait for keys, weights and values in turn, 3600 cycles a tile of 64 keys of which the products take 1024, beside one other
+// workgroup.  Halves of the output by workgroups, with the scores made twice, took 97 and 348; a row's whole output in one wavefront, of which then one fits a SIMD, 170 for 4096 tokens where pairs take 114.
 #pragma once
 #include "k_attend.h"
 
 namespace c2t {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
 struct PromptArgs {
   const char* q; const char* k; const char* v; char* out; float* lse;
@@ -172,19 +173,17 @@ template <int PRODUCTS, int READS, int AHEAD, int EACH> __device__ __forceinline
 constexpr int K_AHEAD = 4, V_AHEAD = 2;                      // operands read ahead of their product
 
 // KB blocks of 32 keys a tile; OCC workgroups a CU.  The wavefronts have 32 rows each and share the tiles (KW = 1), or the same 32 rows and KW wavefronts every KW-th tile each, joined at
-// the end: a quarter of the way along the keys where there are few rows.  DV of the D elements of an output row are one wavefront's: D; or half, as more sums do not fit its registers.  The
-// other half is then another workgroup's, which makes the scores once more (KB = 1), or PAIRS (KB = 2): two wavefronts have the same 32 rows, each makes the weights of one of a
-// tile's two blocks, which both take from LDS, and half of the output.
+// the end: a quarter of the way along the keys where there are few rows.  DV of the D elements of an output row are one wavefront's: D; or half, as more sums do not fit its registers.
+// Then two wavefronts have the same 32 rows (PAIRS): each makes the weights of one of a tile's two blocks, which both take from LDS, and half of the output.
 template <typename E, int D, int DV, int KB, int KW, int OCC, bool LSE>
 __global__ __launch_bounds__(64 * prompt_waves(KW), OCC) void k_prompt(const int32_t* starts, int32_t all_rows, int32_t sequences, int32_t kv_heads, int32_t G, float inv_kv_heads,
                                                                        float inv_group, PromptArgs a) {
   typedef typename E::T T; typedef typename E::T4 T4; typedef typename E::T8 T8;
-  constexpr bool PAIRS = DV < D && KB == 2;
-  static_assert(!PAIRS || (KW == 1 && D == 2 * DV), "");
-  constexpr int WAVES = prompt_waves(KW), NT = 64 * WAVES, ROWS = prompt_rows(KW, PAIRS), KT = 32 * KB, PARTS = PAIRS ? 1 : D / DV, DB = DV / 32, DK = D / 16;
-  constexpr int VW = PAIRS ? D : DV;                         // elements of a V row in LDS
+  constexpr bool PAIRS = DV < D;
+  static_assert(!PAIRS || (KB == 2 && KW == 1 && D == 2 * DV), "");
+  constexpr int WAVES = prompt_waves(KW), NT = 64 * WAVES, ROWS = prompt_rows(KW, PAIRS), KT = 32 * KB, DB = DV / 32, DK = D / 16;
   constexpr int SHARERS = KW > 1 ? 64 : NT;                  // threads that load a tile together
-  constexpr int K_LOADS = KT * D / 8 / SHARERS, V_LOADS = KT * VW / 8 / SHARERS, K_TILE = KT * D * 2, TILE = K_TILE + KT * VW * 2;
+  constexpr int K_LOADS = KT * D / 8 / SHARERS, V_LOADS = KT * D / 8 / SHARERS, K_TILE = KT * D * 2, TILE = K_TILE + KT * D * 2;
   constexpr float TOP = E::TOP, SLACK = E::SLACK, BIG = 0x1p22f;
   constexpr int WEIGHTS = 2 * 64 * 16;                       // PAIRS: a wavefront's of a tile, two operands a lane
   __shared__ __align__(16) char lds[PAIRS ? TILE + WAVES * WEIGHTS : 2 * TILE * KW];  // K and V, two buffers, of each wavefront that has tiles of its own; PAIRS: one, and weights
@@ -200,9 +199,9 @@ __global__ __launch_bounds__(64 * prompt_waves(KW), OCC) void k_prompt(const int
   // many heads there are, and short prompts fill tiles.
   if (KW == 1 && tid == 0) odd_value = 0;
   PromptTile u;
-  const int part = PAIRS ? wave & 1 : blockIdx.x % PARTS;
+  const int part = PAIRS ? wave & 1 : 0;                     // of an output row
   int rank, head;
-  split(blockIdx.x / PARTS, kv_heads, inv_kv_heads, &rank, &head);
+  split(blockIdx.x, kv_heads, inv_kv_heads, &rank, &head);
   rank = uniform(rank); head = uniform(head);
   if (!find_tile<ROWS>(PromptShape{starts, all_rows, sequences, kv_heads, G, inv_kv_heads, inv_group}, rank, &u)) return;
   const int row0 = u.tile * ROWS, wave_row0 = row0 + (KW > 1 ? 0 : PAIRS ? wave / 2 * 32 : wave * 32), rows = u.n * G;
@@ -213,18 +212,18 @@ __global__ __launch_bounds__(64 * prompt_waves(KW), OCC) void k_prompt(const int
   const int keys = uniform(token_of(row0 + ROWS - 1, &no_g)) + 1, n_tiles = div_up(keys, KT);
   const bool idle = wave_row0 >= rows;
   const char* const k_head = a.k + u.first * a.k_row + (int64_t)head * (D * 2);
-  const char* const v_head = a.v + u.first * a.v_row + (int64_t)head * (D * 2) + (PAIRS ? 0 : part * (DV * 2));
+  const char* const v_head = a.v + u.first * a.v_row + (int64_t)head * (D * 2);
 
   // A tile's pieces: this thread's j-th lies j SHARERS + lt pieces into K's or V's tile in LDS, and is the piece of its row that piece_at puts there: the same one in every 16th row, so
   // that one offset (two, of rows of 8 a load) does for all of a tile's.
-  constexpr int K_ROWS = SHARERS / (D / 8), V_ROWS = SHARERS / (VW / 8), K_KINDS = K_ROWS < 16 ? 16 / K_ROWS : 1, V_KINDS = V_ROWS < 16 ? 16 / V_ROWS : 1;      // rows a load, offsets
+  constexpr int K_ROWS = SHARERS / (D / 8), V_ROWS = SHARERS / (D / 8), K_KINDS = K_ROWS < 16 ? 16 / K_ROWS : 1, V_KINDS = V_ROWS < 16 ? 16 / V_ROWS : 1;      // rows a load, offsets
   const auto k_piece = [&](int j) { const int row = j * K_ROWS + lt / (D / 8); return (uint32_t)(piece_at<D>(row, lt % (D / 8)) - row * (D * 2)); };
-  const auto v_piece = [&](int j) { const int row = j * V_ROWS + lt / (VW / 8); return (uint32_t)(piece_at<VW>(row, lt % (VW / 8)) - row * (VW * 2)); };
+  const auto v_piece = [&](int j) { const int row = j * V_ROWS + lt / (D / 8); return (uint32_t)(piece_at<D>(row, lt % (D / 8)) - row * (D * 2)); };
   uint32_t k_off[K_KINDS], v_off[V_KINDS];
 #pragma unroll
   for (int j = 0; j < K_KINDS; ++j) k_off[j] = lt / (D / 8) * (uint32_t)a.k_row + k_piece(j);
 #pragma unroll
-  for (int j = 0; j < V_KINDS; ++j) v_off[j] = lt / (VW / 8) * (uint32_t)a.v_row + v_piece(j);
+  for (int j = 0; j < V_KINDS; ++j) v_off[j] = lt / (D / 8) * (uint32_t)a.v_row + v_piece(j);
   const uint32_t lds_wave = lds_address(tiles) + (KW > 1 ? 0 : wave * 1024);
   const char* k_at = k_head + kw * KT * a.k_row; const char* v_at = v_head + kw * KT * a.v_row;
   int ahead = keys - kw * KT;                                          // keys from there on
@@ -239,7 +238,7 @@ __global__ __launch_bounds__(64 * prompt_waves(KW), OCC) void k_prompt(const int
 #pragma unroll
       for (int j = 0; j < K_LOADS; ++j) load_to_lds(k_at, (uint32_t)min(j * K_ROWS + lt / (D / 8), ahead - 1) * (uint32_t)a.k_row + k_piece(j), to + j * SHARERS * 16);
 #pragma unroll
-      for (int j = 0; j < V_LOADS; ++j) load_to_lds(v_at, (uint32_t)min(j * V_ROWS + lt / (VW / 8), ahead - 1) * (uint32_t)a.v_row + v_piece(j), to + K_TILE + j * SHARERS * 16);
+      for (int j = 0; j < V_LOADS; ++j) load_to_lds(v_at, (uint32_t)min(j * V_ROWS + lt / (D / 8), ahead - 1) * (uint32_t)a.v_row + v_piece(j), to + K_TILE + j * SHARERS * 16);
     }
     k_at += KW * KT * a.k_row; v_at += KW * KT * a.v_row; ahead -= KW * KT;
   };
@@ -269,14 +268,31 @@ __global__ __launch_bounds__(64 * prompt_waves(KW), OCC) void k_prompt(const int
   const auto arrived = [&](int buffer, bool diagonal) {
     wait_vector_memory();
     if (!diagonal) return;
-    bool odd = false;
-#pragma unroll
-    for (int j = 0; j < V_LOADS; ++j) {
-      if (PAIRS) __builtin_amdgcn_sched_barrier(0);          // (one at a time: scores are in registers here)
-      u32x4* const at = (u32x4*)(tiles + buffer * TILE + K_TILE + (j * SHARERS + lt) * 16);
-      const u32x4 x = *at;
+    u32x4* const mine = (u32x4*)(tiles + buffer * TILE + K_TILE + lt * 16);
+    const auto clean = [&](int j) {
+      const u32x4 x = mine[j * SHARERS];
       const u32x4 bad = {odd_halves<E>(x.x), odd_halves<E>(x.y), odd_halves<E>(x.z), odd_halves<E>(x.w)};
-      if ((bad.x | bad.y | bad.z | bad.w) != 0u) { odd = true; *at = x & ~bad; }
+      const bool any = (bad.x | bad.y | bad.z | bad.w) != 0u;
+      if (any) mine[j * SHARERS] = x & ~bad;
+      return any;
+    };
+    bool odd = false;
+    if constexpr (V_LOADS > 2) {
+      // of all together whether there is one: one piece after the other takes 2500 cycles of 8 (one prompt of 200 tokens 8.7 us, so 7.8)
+      u16x2 most = {0, 0};                                   // of the halves without their signs
+#pragma unroll
+      for (int j = 0; j < V_LOADS; ++j) {
+        if (PAIRS && j % 2 == 0) __builtin_amdgcn_sched_barrier(0);      // (two at a time: scores are in registers here)
+        const u32x4 x = mine[j * SHARERS] & 0x7fff7fffu;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { const uint32_t two = x[i]; most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, two)); }
+      }
+      if (!__any(odd_halves<E>(__builtin_bit_cast(uint32_t, most)) != 0u)) return;
+#pragma unroll 1
+      for (int j = 0; j < V_LOADS; ++j) odd = clean(j) || odd;
+    } else {                                                 // (of 2 pieces that costs registers, which a loop of width 128 has not: 64 prompts 1081 us for 809)
+#pragma unroll
+      for (int j = 0; j < V_LOADS; ++j) odd = clean(j) || odd;
     }
     if (KW > 1) my_odd = my_odd || __any(odd);
     else if (odd) odd_value = 1;
@@ -284,7 +300,7 @@ __global__ __launch_bounds__(64 * prompt_waves(KW), OCC) void k_prompt(const int
   // Where this lane's operands begin: of K row `col` and piece `half`, of V rows 4 half + (lane & 15) / 4 and the lane's 8 bytes of a block of 32 elements.  The others lie at these
   // places but for whole rows and bits of the piece's number.
   const int k_place = piece_at<D>(col, half);
-  const int v_place = K_TILE + piece_at<VW>(half * 4 + (lane & 15) / 4, (lane >> 4 & 1) * 2 + (lane & 3) / 2) + (lane & 1) * 8 + (PAIRS ? part * (DV * 2) : 0);
+  const int v_place = K_TILE + piece_at<D>(half * 4 + (lane & 15) / 4, (lane >> 4 & 1) * 2 + (lane & 3) / 2) + (lane & 1) * 8 + part * (DV * 2);
   if constexpr (PAIRS) {
     const Ask x = ask(k_at, k_off, a.k_row, keys);
 #pragma unroll
@@ -430,8 +446,8 @@ __global__ __launch_bounds__(64 * prompt_waves(KW), OCC) void k_prompt(const int
       const auto read_v = [&](int i) {
         const int h = i / DB, d = i % DB;
         typedef __attribute__((address_space(3))) s16x4* lds4;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(tiles + (v_base ^ d * 64) + h * 16 * (VW * 2)));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(tiles + (v_base ^ (d * 64 + 32)) + (h * 16 + 8) * (VW * 2)));
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(tiles + (v_base ^ d * 64) + h * 16 * (D * 2)));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(tiles + (v_base ^ (d * 64 + 32)) + (h * 16 + 8) * (D * 2)));
         struct { s16x4 a, b; } both{lo, hi};
         v[i] = __builtin_bit_cast(T8, both);
       };
@@ -514,8 +530,8 @@ __global__ __launch_bounds__(64 * prompt_waves(KW), OCC) void k_prompt(const int
       const auto read_v = [&](int i) {
         const int h = i / DB, d = i % DB;
         typedef __attribute__((address_space(3))) s16x4* lds4;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(tiles + (v_base ^ d * 64) + h * 16 * (VW * 2)));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(tiles + (v_base ^ (d * 64 + 32)) + (h * 16 + 8) * (VW * 2)));
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(tiles + (v_base ^ d * 64) + h * 16 * (D * 2)));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(tiles + (v_base ^ (d * 64 + 32)) + (h * 16 + 8) * (D * 2)));
         struct { s16x4 a, b; } both{lo, hi};
         v[i] = __builtin_bit_cast(T8, both);
       };
@@ -551,7 +567,7 @@ __global__ __launch_bounds__(64 * prompt_waves(KW), OCC) void k_prompt(const int
 
   if (KW > 1 ? my_odd : odd_value != 0) {                    // values that are not finite: a weight is made again from its key
     const char* const k_odd = k_head + half * 16;
-    const char* const v_odd = v_head + (PAIRS ? part * (DV * 2) : 0) + half * 8;
+    const char* const v_odd = v_head + part * (DV * 2) + half * 8;
     for (int key = first_token / KT * KT; key <= wave_last; ++key) {
       if (KW > 1 && key / KT % KW != kw) continue;
       const auto value = [&](int d) { return *(const T4*)(v_odd + key * a.v_row + d * 16); };
@@ -605,8 +621,9 @@ __global__ __launch_bounds__(64 * prompt_waves(KW), OCC) void k_prompt(const int
     }
     if (half == 0) { stats[col] = m_run; stats[32 + col] = l_run; stats[64 + col] = e_run; }
     __syncthreads();
-    for (int i = tid; i < 32 * (DV / 8); i += NT) {
-      const int row = i / (DV / 8), piece = i % (DV / 8);
+#pragma unroll
+    for (int i0 = 0; i0 < 32 * (DV / 8); i0 += NT) {
+      const int i = i0 + tid, row = i / (DV / 8), piece = i % (DV / 8);
       if (wave_row0 + row >= rows) continue;
       const auto of = [&](int w) { return (const float*)(lds + w * 2 * TILE + SUMS) + row; };
       float m = -INFINITY, l = 0.f, e = 0.f;

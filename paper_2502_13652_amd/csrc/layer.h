@@ -38,31 +38,26 @@ inline int append_parts(int64_t tokens, int passes) { return tokens < APPEND_FEW
 
 // ---- prompt ----
 // Which kernel a call takes.  Tiles of 128 rows of a workgroup, whose wavefronts share the keys; or, where there are few of those and the prompts are long, tiles of 32 rows whose four
-// wavefronts divide the keys: four times the workgroups, each a quarter of the way.  Both are known but for the lengths, of which the mean stands for all.  One prompt of 2000 tokens,
-// 4 heads over one of 128: 44 us so, and 22 divided; of 8192, one head, 170 and 68; 4 of 500, 8 over one, 15.9 and 17.8; one of 350, 32 over 8, 12.3 and 14.9.  Width 64, of which two such
-// workgroups fit a CU: 27 and 13, 97 and 39, 10.5 and 7.7, 8.9 and 6.9.  Of width 256, whose tiles hardly fit in LDS four times, the keys are never divided.
+// wavefronts divide the keys: four times the workgroups, each a quarter of the way.  Both are known but for the lengths, of which the mean stands for all.  Width 128, shared and divided: one prompt of
+// 2000 tokens, 4 heads over one, 37.6 and 21.6 us; of 8192, one head, 135 and 67, 4 over one 137 and 142; 4 of 500, 8 over one, 13.6 and 16.3; one of 200, 32 over 8, 8.5 and 7.9, of 350 11.5 and 13.2.
+// Width 64, of which two workgroups that divide fit a CU: 32 and 14; 116 and 42, 119 and 72; 11.9 and 7.6; 7.5 and 5.7, 10.0 and 6.9, of 1000 19.7 and 17.2, of 1500 27.1 and 26.8, of 2000 35 and 41.
+// Of width 256, whose tiles hardly fit in LDS four times, the keys are never divided.
 typedef void (*PromptKernel)(const int32_t*, int32_t, int32_t, int32_t, int32_t, float, float, PromptArgs);
-enum { PROMPT_MANY, PROMPT_SOME, PROMPT_DIVIDED, PROMPT_PAIRS };
+enum { PROMPT_MANY, PROMPT_SOME, PROMPT_DIVIDED };
 constexpr int PROMPT_KEYS = 4;                               // wavefronts that divide the keys
-constexpr int PROMPT_PAIRS_LENGTH = 400;
 inline int prompt_build(int64_t tiles, int64_t rows, int64_t sequences, int head_dim) {        // tiles: of 128 rows, of all heads
   const int64_t length = rows / sequences;
-  if (head_dim <= 128 && tiles <= 4096 && tiles * tiles <= (head_dim == 64 ? 64 : 20) * length) return PROMPT_DIVIDED;
-  // Width 256: the output halved over workgroups, or, of longer prompts, over pairs of wavefronts, which make the scores once but wait for each other (200 tokens, 16 heads over 4, 10.5 us by
-  // workgroups and 11.9 by pairs; 64 of 50 to 302 76 and 82; four of 300 16.2 and 16.9, of 500 24.0 and 22.9; one of 4096, 8 heads over one, 126 and 114, of 8192 348 and 293).
-  if (head_dim > 128) return length >= PROMPT_PAIRS_LENGTH ? PROMPT_PAIRS : PROMPT_MANY;
-  // Width 128, up to as many tiles as workgroups fit the card by three: two a CU with tiles of 64 keys (one prompt of 3000 tokens, 32 heads over 8, 79 us, by three with tiles of 32 88; of
-  // 1000 23.5 and 26.3); with more tiles three hide each other's start and end (64 prompts of up to 2000 850 and 780).
+  if (head_dim <= 128 && tiles <= 4096 && tiles * tiles <= (head_dim == 64 ? 72 : 20) * length) return PROMPT_DIVIDED;
+  // Width 128, up to as many tiles as workgroups fit the card by three: two a CU with tiles of 64 keys (one prompt of 3000 tokens, 32 heads over 8, 78 us, by three with tiles of 32 88; of
+  // 1000 22.8 and 26.4); with more tiles three hide each other's start and end (64 prompts of up to 2000 856 and 806).
   return head_dim == 128 && tiles <= 3 * 256 ? PROMPT_SOME : PROMPT_MANY;
 }
 template <typename E, bool LSE> PromptKernel prompt_kernel(int head_dim, int build) {
   if (build == PROMPT_DIVIDED) return head_dim == 64 ? k_prompt<E, 64, 64, 1, PROMPT_KEYS, 2, LSE> : k_prompt<E, 128, 128, 1, PROMPT_KEYS, 1, LSE>;
   if (build == PROMPT_SOME) return k_prompt<E, 128, 128, 2, 1, 2, LSE>;
-  if (build == PROMPT_PAIRS) return k_prompt<E, 256, 128, 2, 1, 2, LSE>;
-  return head_dim == 64 ? k_prompt<E, 64, 64, 2, 1, 4, LSE> : head_dim == 128 ? k_prompt<E, 128, 128, 1, 1, 3, LSE> : k_prompt<E, 256, 128, 1, 1, 2, LSE>;
+  return head_dim == 64 ? k_prompt<E, 64, 64, 2, 1, 4, LSE> : head_dim == 128 ? k_prompt<E, 128, 128, 1, 1, 3, LSE> : k_prompt<E, 256, 128, 2, 1, 2, LSE>;
 }
 template <typename E> PromptKernel prompt_kernel(int head_dim, int build, bool lse) { return lse ? prompt_kernel<E, true>(head_dim, build) : prompt_kernel<E, false>(head_dim, build); }
-inline int prompt_parts(int head_dim, int build) { return head_dim > 128 && build != PROMPT_PAIRS ? 2 : 1; }    // of an output row, workgroups
 constexpr int64_t MAX_PROMPT_STRIDE = 1 << 24;
 
 }  // namespace c2t
@@ -174,7 +169,7 @@ int c2t_prompt_attention(const c2t_prompt* p, void* stream) {
   // each sequence has one tile at most that it does not fill
   const auto tiles = [&](int of) { return ((int64_t)p->rows * group / of + std::min(p->sequences, p->rows)) * p->kv_heads; };
   const int build = prompt_build(tiles(prompt_rows(1, false)), p->rows, p->sequences, p->head_dim), kw = build == PROMPT_DIVIDED ? PROMPT_KEYS : 1;
-  const int64_t blocks = tiles(prompt_rows(kw, build == PROMPT_PAIRS)) * prompt_parts(p->head_dim, build);
+  const int64_t blocks = tiles(prompt_rows(kw, p->head_dim > 128));
   if (blocks > MAX_BLOCKS) return C2T_ERR_UNSUPPORTED;
   const PromptKernel fn = p->dtype == C2T_BF16 ? prompt_kernel<Bf16>(p->head_dim, build, p->lse != nullptr) : prompt_kernel<F16>(p->head_dim, build, p->lse != nullptr);
   hipLaunchKernelGGL(fn, dim3((unsigned)blocks), dim3((unsigned)(64 * prompt_waves(kw))), 0, (hipStream_t)stream, p->starts, p->rows, p->sequences, p->kv_heads, group,
