@@ -269,30 +269,23 @@ __global__ __launch_bounds__(64 * prompt_waves(KW), OCC) void k_prompt(const int
     wait_vector_memory();
     if (!diagonal) return;
     u32x4* const mine = (u32x4*)(tiles + buffer * TILE + K_TILE + lt * 16);
-    const auto clean = [&](int j) {
+    // Of all together whether there is one: one piece after the other takes 2500 cycles of 8 (one prompt of 200 tokens 8.7 us, so 7.8).
+    u16x2 most = {0, 0};                                     // of the halves without their signs
+#pragma unroll
+    for (int j = 0; j < V_LOADS; ++j) {
+      if (PAIRS && j % 2 == 0) __builtin_amdgcn_sched_barrier(0);        // (two at a time: scores are in registers here)
+      const u32x4 x = mine[j * SHARERS] & 0x7fff7fffu;
+#pragma unroll                                               // (by way of `two`: a bit cast of x[i] itself takes the vector's first element)
+      for (int i = 0; i < 4; ++i) { const uint32_t two = x[i]; most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, two)); }
+    }
+    if (!__any(odd_halves<E>(__builtin_bit_cast(uint32_t, most)) != 0u)) return;
+    bool odd = false;
+#pragma unroll
+    for (int j = 0; j < V_LOADS; ++j) {                      // (rare; as a loop it costs registers that the scores' loop has not)
+      __builtin_amdgcn_sched_barrier(0);
       const u32x4 x = mine[j * SHARERS];
       const u32x4 bad = {odd_halves<E>(x.x), odd_halves<E>(x.y), odd_halves<E>(x.z), odd_halves<E>(x.w)};
-      const bool any = (bad.x | bad.y | bad.z | bad.w) != 0u;
-      if (any) mine[j * SHARERS] = x & ~bad;
-      return any;
-    };
-    bool odd = false;
-    if constexpr (V_LOADS > 2) {
-      // of all together whether there is one: one piece after the other takes 2500 cycles of 8 (one prompt of 200 tokens 8.7 us, so 7.8)
-      u16x2 most = {0, 0};                                   // of the halves without their signs
-#pragma unroll
-      for (int j = 0; j < V_LOADS; ++j) {
-        if (PAIRS && j % 2 == 0) __builtin_amdgcn_sched_barrier(0);      // (two at a time: scores are in registers here)
-        const u32x4 x = mine[j * SHARERS] & 0x7fff7fffu;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { const uint32_t two = x[i]; most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, two)); }
-      }
-      if (!__any(odd_halves<E>(__builtin_bit_cast(uint32_t, most)) != 0u)) return;
-#pragma unroll 1
-      for (int j = 0; j < V_LOADS; ++j) odd = clean(j) || odd;
-    } else {                                                 // (of 2 pieces that costs registers, which a loop of width 128 has not: 64 prompts 1081 us for 809)
-#pragma unroll
-      for (int j = 0; j < V_LOADS; ++j) odd = clean(j) || odd;
+      if ((bad.x | bad.y | bad.z | bad.w) != 0u) { odd = true; mine[j * SHARERS] = x & ~bad; }
     }
     if (KW > 1) my_odd = my_odd || __any(odd);
     else if (odd) odd_value = 1;
