@@ -396,7 +396,7 @@ typedef struct {
   void* k_out;                 /* [device] as k, may be k (same strides); or NULL */
   int64_t q_batch_stride, q_token_stride, kv_batch_stride, kv_token_stride, q_out_batch_stride, q_out_token_stride, k_out_batch_stride, k_out_token_stride;
   const int32_t* n_new;        /* [device] [batch], NULL: all `tokens`; cut to 0 .. tokens */
-  const int32_t* starts;       /* [device] [batch + 1], not falling, 0 .. tokens; or NULL.  Sequences of which that is not so are left out */
+  const int32_t* starts;       /* [device] [batch + 1], not falling, 0 .. tokens; or NULL.  Sequences of which that is not so are left out whole (a row that others then share goes to one of them) */
   const int32_t* position;     /* [device] [batch][nodes]; NULL with nodes = 0 */
   const uint64_t* turns;       /* [device] [pairs] */
   float magnitude;
@@ -416,7 +416,7 @@ typedef struct {
   void* out;                   /* [device] as q, each row in a place of its own; not one of the others */
   float* lse;                  /* [device] [rows][q_heads] log of the sum of e^score, or NULL */
   int64_t q_stride, k_stride, v_stride, out_stride;    /* from row to row; at most 2^24 */
-  const int32_t* starts;       /* [device] [sequences + 1], not falling, 0 .. rows; sequences of which that is not so are left out */
+  const int32_t* starts;       /* [device] [sequences + 1], not falling, 0 .. rows; sequences of which that is not so are left out whole (where others then share rows, out is undefined) */
   int32_t rows, sequences;     /* sequences: at most C2T_MAX_CACHE_BATCH */
   int32_t q_heads, kv_heads;   /* head i reads head i / (q_heads / kv_heads) */
   int32_t head_dim;            /* 64, 128 or 256 */

@@ -37,22 +37,25 @@ __device__ __forceinline__ void sine_cosine(uint32_t fraction, float* sine, floa
   *cosine = ((quarter + 1u) & 2u) ? -b : b;
 }
 
-// The sequence that packed row `row` of `rows` is in, and which of its tokens it is; -1: none, or one that does not end by the last row.  A trip to memory, of more than 64 sequences two: every 64th (or so) start, then the ones between.
+// The sequence that holds packed row `row` of `rows`, and which of its tokens that is; -1: none, or one that does not begin and end among the rows.  A trip to memory, of more than 64 sequences two:
+// every 64th (or so) start, then the ones from the last that is not behind the row.  That is the place where starts rise; a row that is not found there may be of a sequence between starts that fall, so
+// then all are gone through.
 __device__ __forceinline__ int sequence_of_row(const int32_t* starts, int n, int row, int rows, int* t) {
-  const int lane = lane_id(), step = div_up(n, WAVE);
-  int first = 0, end = n;
-  if (step > 1) {
-    first = (__popcll(__ballot(lane * step < n && starts[min(lane * step, n)] <= row)) - 1) * step;
-    if (first < 0) return -1;
-    end = min(first + step, n);
-  }
-  const int i = min(first + lane, n - 1), from = starts[i], to = starts[i + 1];
-  const int at = __popcll(__ballot(first + lane < end && from <= row)) - 1;
-  if (at < 0) return -1;                                     // (ahead of the first; or starts that fall)
-  const int my_from = __builtin_amdgcn_readlane(from, at), my_to = __builtin_amdgcn_readlane(to, at);
-  if (my_from < 0 || row < my_from || row >= my_to || my_to > rows) return -1;
-  *t = row - my_from;
-  return first + at;
+  const int lane = lane_id();
+  const auto among = [&](int first) {                        // 64 sequences from `first` on
+    const int i = min(first + lane, n - 1), from = starts[i], to = starts[i + 1];
+    const uint64_t holds = __ballot((first + lane < n) & (from >= 0) & (from <= row) & (row < to) & (to <= rows));      // (&: both numbers in one trip)
+    if (holds == 0ull) return -1;
+    const int at = __builtin_ctzll(holds);
+    *t = row - __builtin_amdgcn_readlane(from, at);
+    return first + at;
+  };
+  if (n <= WAVE) return among(0);
+  const int step = div_up(n, WAVE);
+  const int up_to = (int)__popcll(__ballot(lane * step < n && starts[min(lane * step, n)] <= row));       // (0: a row ahead of all)
+  int b = among(up_to > 0 ? (up_to - 1) * step : 0);
+  for (int first = 0; b < 0 && first < n; first += WAVE) b = among(first);
+  return b;
 }
 
 // A wavefront has a token, or one of `parts` shares of its heads.  A lane has 16 elements of a head, 8 pairs of them or 16 that only move, and keeps its pairs' sines for

@@ -166,6 +166,36 @@ def test_starts_that_make_no_sense():
         assert bool((out == 3.0).all()) and torch.equal(cache.k, k0)
 
 
+@pytest.mark.parametrize("n,at", [(3, [50, 20, 90, 10]), (4, [50, 20, 90, 10, 10]), (5, [90, 95, 0, 30, 200, 0]), (2, [10, 0, 100]),
+                                  (200, [0, 10] + [200] * 70 + [40, 60] + [30] * 3 + [200] * 122 + [90, 100]), (130, [100] * 65 + [3, 40] + [2 ** 31 - 1, -1] * 32)])
+def test_sequences_between_starts_that_fall(n, at):
+    """A sequence whose own start and end make sense is taken whole, others are left out whole."""
+    from paper_2502_13652_amd import Rotation
+    assert len(at) == n + 1
+    lens = [b % 20 for b in range(n)]
+    cache = make_cache(lens, 100, 16, 1, 64, BF, n)
+    k0, v0 = cache.k.clone(), cache.v.clone()
+    q, k, v = projected((100,), 2, 1, 64, BF, 10 + n)
+    out, k_out = (torch.full((100, h, 64), 3.0, dtype=BF, device="cuda") for h in (2, 1))
+    cache.append(0, q, k, v, Rotation(64), starts=ints(at), q_out=out, k_out=k_out)
+    held = torch.zeros(100, dtype=torch.bool)
+    for b in range(n):
+        a, z = at[b], at[b + 1]
+        if not 0 <= a < z <= 100:
+            continue
+        assert not bool(held[a:z].any())                     # (the lists are made so that no two share a row)
+        held[a:z] = True
+        where = [lens[b] + t for t in range(z - a)]
+        near(out[a:z], *turned_reference(q[a:z], where, 64, frequencies(64), False, 1.0))
+        near(k_out[a:z], *turned_reference(k[a:z], where, 64, frequencies(64), False, 1.0))
+        for t in range(z - a):
+            page = int(cache.page_table[b, where[t] // 16])
+            k0[0, page, :, where[t] % 16], v0[0, page, :, where[t] % 16] = k_out[a + t], v[a + t]
+    assert bool(held.any()) and bool((out[~held] == 3.0).all()) and bool((k_out[~held] == 3.0).all())
+    same_pool(cache, k0, v0)
+    assert int(cache.status.view(torch.int32).abs().sum()) == 0
+
+
 def test_empty_refused_streams_and_graphs():
     from paper_2502_13652_amd import Rotation
     cache = make_cache([5, 6], 12, 16, 2, 64, BF, 11)
