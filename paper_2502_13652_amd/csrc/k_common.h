@@ -93,8 +93,8 @@ __device__ __forceinline__ void touch_kernel_arguments() {
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
-// eight numbers that are loaded and stored together
-template <typename T> struct alignas(8 * sizeof(T)) Eight { T v[8]; };
+// eight numbers that are loaded and stored together, in pieces of 16 bytes: no more than that is asked of their place
+template <typename T> struct alignas(8 * sizeof(T) < 16 ? 8 * sizeof(T) : 16) Eight { T v[8]; };
 
 // a value that is the same in every lane, as the compiler cannot know of one that comes from LDS: what is decided by it is then branched on, not masked
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }

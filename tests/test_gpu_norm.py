@@ -93,6 +93,30 @@ def test_strides_and_what_lies_between():
     assert torch.equal(rms_norm(off, w, EPS), rms_norm(x, w, EPS))
 
 
+@pytest.mark.parametrize("dtype,residual,weight", [(F32, F32, F32), (BF, F32, F32), (HF, F32, HF), (F32, None, F32)])
+@pytest.mark.parametrize("width,stride,shift", [(8, 12, 0), (16, 20, 4), (1024, 1028, 12), (2048, 2052, 4), (8200, 8204, 20)])
+def test_32_bit_rows_aligned_to_16_bytes_and_no_more(dtype, residual, weight, width, stride, shift):
+    """Such rows are taken by whole pieces; 16-bit ones beside them keep to multiples of 8 elements."""
+    from paper_2502_13652_amd import rms_norm
+
+    def place(kind):
+        at, step = (shift, stride) if kind is F32 else (shift // 4 * 8, (stride + 7) // 8 * 8)
+        return torch.full((at + 5 * step,), 9.0, dtype=kind, device="cuda").as_strided((5, width), (step, 1), at)
+
+    x, w, r = inputs(5, width, dtype, residual, weight, width + shift)
+    xs, outs, ws = place(dtype), place(dtype), torch.zeros(width + 4, dtype=weight, device="cuda")[4 if weight is F32 else 0:][:width]
+    xs.copy_(x), ws.copy_(w)
+    rs, to = (None, None) if r is None else (place(residual), place(residual))
+    if r is not None:
+        rs.copy_(r)
+    assert xs.data_ptr() % 16 == 0 and xs.stride(0) * xs.element_size() % 16 == 0 and (r is None or rs.data_ptr() % 16 == 0 and rs.stride(0) * 4 % 16 == 0)
+    rms_norm(xs, ws, EPS, residual=rs, residual_out=to, out=outs)
+    check(x, w, r, outs, None, to)
+    eight, scales = rms_norm(xs, ws, EPS, residual=rs, residual_out=to, scale_block=32)
+    check(x, w, r, eight, scales, to, 32)
+    assert torch.equal(xs, x) and (r is None or torch.equal(rs, r))
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_rows_of_any_size(dtype):
     """Squares of such numbers pass fp32; the mean does not."""

@@ -52,6 +52,16 @@ def test_norm_is_refused(lib):
             assert call(**fine) in LAUNCHED, fine
 
 
+@pytest.mark.parametrize("kind,bytes_", [("float", 16), ("__bf16", 16), ("_Float16", 16), ("uint8_t", 8)])
+def test_pieces_promise_no_more_than_is_asked_for(kind, bytes_, tmp_path):
+    """Arrays whose rows begin at multiples of 16 bytes (of 8, of 8 bits) are taken as made of aligned pieces: the pieces' type may not promise the compiler more."""
+    source = tmp_path / "piece.hip"
+    source.write_text('#include "k_norm.h"\nstatic_assert(alignof(c2t::Eight<%s>) <= %d && sizeof(c2t::Eight<%s>) == 8 * sizeof(%s), "");\n' % (kind, bytes_, kind, kind))
+    r = subprocess.run(["hipcc", "-std=c++17", "--offload-arch=gfx950", "-fsyntax-only", "-I", os.path.join(ROOT, "include"), "-I", os.path.join(ROOT, "paper_2502_13652_amd", "csrc"), str(source)],
+                       stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    assert r.returncode == 0, r.stdout
+
+
 def test_append_is_refused(lib):
     from paper_2502_13652_amd.serving import _Append
 
