@@ -142,7 +142,7 @@ template <int D> __device__ __forceinline__ int piece_at(int row, int piece) {
 // 16 bytes a lane from memory into LDS, without a register on the way: lane i's to `to` + 16 i.  The compiler does not count it: whoever reads waits for it (wait_vector_memory, and a
 // barrier for what other wavefronts loaded), and no wavefront ends ahead of its own.
 __device__ __forceinline__ void load_to_lds(const char* base, uint32_t offset, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(offset), "s"(base) : "memory", "m0");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"{m0}"(to), "v"(offset), "s"(base) : "memory");
 }
 __device__ __forceinline__ uint32_t lds_address(const char* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p; }
 

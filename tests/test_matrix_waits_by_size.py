@@ -40,13 +40,35 @@ _Zk:
         assert not found or min(s for _, _, s in found) == nop + 2
 
 
-def test_no_matrix_result_is_read_early(tmp_path, monkeypatch):
-    out = str(tmp_path / "device.s")
+@pytest.fixture(scope="module")
+def compiled(tmp_path_factory):
+    """The library's device code as assembly, and what the compiler printed."""
+    out = str(tmp_path_factory.mktemp("waits") / "device.s")
     flags = [f for f in binding.HIPCC_FLAGS if f not in ("-shared", "-fPIC")]
     package = os.path.dirname(binding.__file__)
     r = subprocess.run(["hipcc"] + flags + ["-S", "--offload-device-only", "-I", os.path.join(os.path.dirname(package), "include"), os.path.join(package, "csrc", "c2t_lib.hip"), "-o", out],
                        stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     assert r.returncode == 0, r.stdout
     with open(out) as f:
-        total, found = early_reads(f.read(), monkeypatch)
+        return f.read(), r.stdout
+
+
+def test_no_matrix_result_is_read_early(compiled, monkeypatch):
+    total, found = early_reads(compiled[0], monkeypatch)
     assert total > 500 and not found, found[:8]
+
+
+def test_loads_into_lds_find_their_place_in_m0(compiled):
+    """Each load into LDS has its address set for it in its own block, by the compiler, which knows of it: no warning of a register that is not the code's to change."""
+    assert "inline-asm" not in compiled[1], compiled[1][:1000]
+    loads = 0
+    for block in re.split(r"\n\.L\w+:", compiled[0]):
+        code = [line.strip() for line in block.split("\n")]
+        m0 = False
+        for line in code:
+            m0 = m0 or re.match(r"s_\w+ m0,", line) is not None
+            if line.startswith("global_load_lds"):
+                loads += 1
+                assert m0, line
+                m0 = False
+    assert loads > 100
