@@ -157,9 +157,13 @@ __global__ __launch_bounds__(NT < NORM_NT ? NORM_NT : NT) void k_rms_norm(NormAr
       const float scale = m == 0.f ? 1.f : fmaxf(m / E4M3_MAX, 0x1p-126f);
       if (a.block == 0 ? c == 0 && t == 0 : e.first % a.block == 0) a.scales[row * a.scales_row + (a.block == 0 ? 0 : e.first / a.block)] = scale;
       const float inv = 1.f / scale;
+      // x / scale as one rounding makes it (Markstein: a product with the rounded reciprocal, corrected by what it leaves of x), or a number between two of 8 bits goes to the wrong one: the product alone
+      // takes 4160 rows of 4096 1 % less, a division by the instruction set's steps 11 % more.
+      const float back = inv == 0.f ? 0.f : scale;           // (of an infinite scale: what is finite is 0)
+      const auto divided = [&](float x) { const float q = x * inv; return __builtin_fmaf(__builtin_fmaf(-q, back, x), inv, q); };
       uint2 y;
-      y.x = four_e4m3(h[c][0] * inv, h[c][1] * inv, h[c][2] * inv, h[c][3] * inv);
-      y.y = four_e4m3(h[c][4] * inv, h[c][5] * inv, h[c][6] * inv, h[c][7] * inv);
+      y.x = four_e4m3(divided(h[c][0]), divided(h[c][1]), divided(h[c][2]), divided(h[c][3]));
+      y.y = four_e4m3(divided(h[c][4]), divided(h[c][5]), divided(h[c][6]), divided(h[c][7]));
       char* const to = a.out + row * a.out_row + e.first;
       if (WHOLE) {
         *(uint2*)to = y;

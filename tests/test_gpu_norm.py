@@ -67,6 +67,31 @@ def test_eight_bits(dtype, residual, rows, width, block):
     check(x, w, r, out, scales, to, block)
 
 
+@pytest.mark.parametrize("width,block", [(1024, 1024), (1024, 32), (4096, 128), (333, 333), (1000, 64)])
+def test_eight_bits_between_two_numbers(width, block):
+    """Quotients that lie exactly between two numbers of 8 bits go to the even one.  x is 1 and -1 and eps too small to count, so y is the weight with x's sign and nothing is rounded ahead of the
+    division; a block's weights are its scale times 448 and times numbers of 5 bits, 24 bits in all."""
+    from paper_2502_13652_amd import rms_norm
+    g = gen(width + block)
+    blocks = -(-width // block)
+    scale = torch.randint(2 ** 17 + 1, 2 ** 18, (blocks,), generator=g).double() * 2.0 ** -20               # 18 bits, the last one set
+    scale = scale + (scale * 2 ** 20 % 2 == 0) * 2.0 ** -20
+    each = scale.repeat_interleave(block)[:width]
+    between = (torch.randint(8, 16, (width,), generator=g).double() + 0.5) * 2.0 ** torch.randint(-6, 5, (width,), generator=g).double()       # e4m3 has 8 .. 15 times powers of two
+    first = torch.arange(0, width, block)
+    between[first] = 448.0
+    weight = between * each
+    assert torch.equal(weight.float().double(), weight)
+    x = torch.where(torch.rand((3, width), generator=g) < 0.5, -1.0, 1.0)
+    out, scales = rms_norm(x.cuda(), weight.float().cuda(), 1e-30, scale_block=block)
+    assert torch.equal(scales.cpu().double(), scale.expand(3, blocks))
+    t = between.clone()
+    t[first] = 0.0
+    step = 2.0 ** torch.floor(torch.log2(torch.where(t > 0, t, 1.0))) / 8
+    want = torch.where(t > 0, torch.round(t / step) * step, 448.0)                               # (torch.round: to even)
+    assert torch.equal(out.float().cpu().double(), want * x.double())
+
+
 def test_strides_and_what_lies_between():
     from paper_2502_13652_amd import rms_norm
     for pad, width in ((8, 256), (5, 256), (16, 250), (1, 1)):
