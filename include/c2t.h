@@ -396,7 +396,7 @@ typedef struct {
   void* k_out;                 /* [device] as k, may be k (same strides); or NULL */
   int64_t q_batch_stride, q_token_stride, kv_batch_stride, kv_token_stride, q_out_batch_stride, q_out_token_stride, k_out_batch_stride, k_out_token_stride;
   const int32_t* n_new;        /* [device] [batch], NULL: all `tokens`; cut to 0 .. tokens */
-  const int32_t* starts;       /* [device] [batch + 1], not falling, 0 .. tokens; or NULL.  Sequences of which that is not so are left out whole (a row that others then share goes to one of them) */
+  const int32_t* starts;       /* [device] [batch + 1], not falling, 0 .. tokens; or NULL.  Sequences of which that is not so are left out whole (and of others that then share rows, any) */
   const int32_t* position;     /* [device] [batch][nodes]; NULL with nodes = 0 */
   const uint64_t* turns;       /* [device] [pairs] */
   float magnitude;

@@ -167,7 +167,8 @@ def test_starts_that_make_no_sense():
 
 
 @pytest.mark.parametrize("n,at", [(3, [50, 20, 90, 10]), (4, [50, 20, 90, 10, 10]), (5, [90, 95, 0, 30, 200, 0]), (2, [10, 0, 100]),
-                                  (200, [0, 10] + [200] * 70 + [40, 60] + [30] * 3 + [200] * 122 + [90, 100]), (130, [100] * 65 + [3, 40] + [2 ** 31 - 1, -1] * 32)])
+                                  (200, [0, 10] + [200] * 70 + [40, 60] + [30] * 3 + [200] * 122 + [90, 100]), (130, [100] * 65 + [3, 40] + [2 ** 31 - 1, -1] * 32),
+                                  (70, [0, 300, 10, 40, 40, -5] + [40] * 60 + [70, 200, 70, 95, 100])])
 def test_sequences_between_starts_that_fall(n, at):
     """A sequence whose own start and end make sense is taken whole, others are left out whole."""
     from paper_2502_13652_amd import Rotation
