@@ -6,7 +6,7 @@
 // of the product go into sine and cosine.  No table of angles is read: they are made anew for each token, once for all heads that a wavefront turns.
 //
 // Bound by the bytes, which move in rows of a head: 12000 packed tokens, 32 query heads over 8 of 128, 62 us, 5.2 TB/s as a large copy; 64 trees of up to 65 slots 17.4 us, 4.4; 24 prompts of 3 to
-// 2011 tokens, 16 heads over 4 of 64, turned keys put out too, 38 us, 4.2; one token 3.6 us, of which the host's call takes 9.
+// 2011 tokens, 16 heads over 4 of 64, turned keys put out too, 37 us, 4.4; one token: the kernel 3.6 us, the whole call from the host 8.3.
 #pragma once
 #include "k_cache.h"
 

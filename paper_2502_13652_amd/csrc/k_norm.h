@@ -6,9 +6,10 @@
 // fp32 number fits, and r is used as a number in [1/2, 1) and a power of two, so rows of any size have their norm; a sum in 32 bits takes as long (4160 rows of 4096 27.4 us
 // either way, 16384 of 8192 259, 20000 of 2048 58.4).
 //
-// Bound by the bytes: 16384 rows of 8192 bf16 with an fp32 residual, 8 bits with a scale for each 128, 259 us for 1.48 GB, 5.7 TB/s (a large copy gets 5.2); 20000 of 2048 bf16 58 us,
-// 5.6; 4160 of 4096, 8 bits with a scale a row, 26.5 us, 4.5, of which some 4 us are the launch's start and end; one row 2.5 us, of which the host's call takes 7.  Rows that are not made of aligned pieces
-// of 8 elements are loaded and stored by single elements, a wavefront's lanes next to each other: 3001 of 1111 fp32 9.4 us, with a thread's elements next to each other 21.5.
+// Bound by the bytes: 16384 rows of 8192 bf16 with an fp32 residual, 8 bits with a scale for each 128, 260 us for 1.48 GB, 5.7 TB/s (a large copy gets 5.2); 20000 of 2048 bf16 58 us,
+// 5.6; 4160 of 4096, 8 bits with a scale a row, 26.7 us, 4.4, of which some 4 us are the launch's start and end; one row: the kernel 2.4 us, the whole call from the host 7.  Rows that are not made of
+// aligned pieces of 8 elements are loaded and stored by single elements, a wavefront's lanes next to each other: 3001 of 1111 fp32 8.3 to 9 us from memory, with a thread's elements next to each other 21.5.
+// (Of 8 bits with a scale a block they are next to each other all the same, as its largest is looked for among neighbouring pieces.)
 #pragma once
 #include "k_common.h"
 

@@ -3,7 +3,10 @@
 //   s_j = scale q_i.k_j,  j <= i of the same sequence,  p_j = e^(s_j - m),  out_i = sum p_j v_j / sum p_j
 //
 // One pass over the keys with a running reference m and sum, as in k_attend.h and by its rules: m moves only where a tile passes it, the divisor is the
-// sum of the weights as the second product takes them, rounded to 16 bits, and the log of the sum is that of the weights as they were.  Products are taken transposed,
+// sum of the weights as the second product takes them, rounded to 16 bits, and the log of the sum is that of the weights as they were.  That one rounding leaves outputs of Gaussian values off by 0.0018 to
+// 0.0020 of their size (rms, of bf16, of which 0.0016 are their own rounding; of halves 0.00022 to 0.00025 and 0.0002).  A second number of 16 bits for what the first leaves of a weight, as k_attend.h has it for few rows, makes
+// outputs as exact as their type, for half again of the matrix unit's time: one prompt of 200 tokens 8.6 us for 8.25, of 8192 738 for 522, the 64 prompts 1111 for 795, divided keys 15 % more.  Nowhere is that for nothing,
+// and it is left out of all forms.  Products are taken transposed,
 // S^T = K Q^T in blocks of 32 keys and 32 rows: a lane then has one row (lane & 31) and, of each block, the keys 8 i + 4 (lane / 32) + 0..3, which are two operands of
 // out^T = V^T P^T, so weights never leave their registers.
 //
@@ -11,10 +14,10 @@
 // three wavefronts a SIMD, which is what hides a workgroup's start (finding its tile 3000 to 5000 cycles under load, its first keys 4000) and end (3000) behind others' products: 64 prompts of
 // up to 2000 tokens take 780 us, with two 850; workgroups that stay and take tile after tile, the next one's keys on their way, took 900 for 845 (tiles dealt ahead of time do not stay together in the L2).
 //
-// Measured, 32 heads over 8 of 128: one prompt of 8192 tokens 505 us for 550 GFLOP, 1.09 PFLOP/s, where an 8192-cubed matrix product gets 1.20: the matrix unit is busy for 64 % of the cycles, whose rate the
-// card's power then holds at 1.6 to 1.7 GHz; the 64 prompts 780 to 810 us, 0.87 to 0.90, busy for 50 %; one prompt of 200 7.8 us: the tile found after 1.4, its first keys there after 2.7, two tiles 2.5.
-// Width 64 (3 prompts of 2100 to 5001, halves, with the log of the sums) 118 us, 0.73: vector instructions, five a score, take longer than its products.  Width 256 (6 prompts of 77 to 2500, 8 heads
-// over one) 85 us, 0.68, of 8192 tokens 292, 0.94: pairs of wavefronts wait for keys, weights and values in turn, 3600 cycles a tile of 64 keys of which the products take 1024, beside one other
+// Measured, 32 heads over 8 of 128, from card to card: one prompt of 8192 tokens 490 to 530 us for 550 GFLOP, 1.04 to 1.12 PFLOP/s, where an 8192-cubed matrix product gets 1.20: the matrix unit is busy for
+// 64 % of the cycles, whose rate the card's power then holds at 1.6 to 1.7 GHz; the 64 prompts 770 to 830 us, 0.85 to 0.91, busy for 50 %; one prompt of 200 7.8 us: the tile found after 1.4, its first keys there after 2.7, two tiles 2.5.
+// Width 64 (3 prompts of 2100 to 5001, halves, with the log of the sums) 116 to 124 us, 0.69 to 0.74: vector instructions, five a score, take longer than its products.  Width 256 (6 prompts of 77 to 2500, 8 heads
+// over one) 84 to 87 us, 0.66 to 0.69, of 8192 tokens 292 to 309, 0.89 to 0.94: pairs of wavefronts wait for keys, weights and values in turn, 3600 cycles a tile of 64 keys of which the products take 1024, beside one other
 // workgroup.  Halves of the output by workgroups, with the scores made twice, took 97 and 348; a row's whole output in one wavefront, of which then one fits a SIMD, 170 for 4096 tokens where pairs take 114.
 #pragma once
 #include "k_attend.h"
@@ -172,7 +175,7 @@ template <int PRODUCTS, int READS, int AHEAD, int EACH> __device__ __forceinline
 }
 constexpr int K_AHEAD = 4, V_AHEAD = 2;                      // operands read ahead of their product
 
-// Ends a block of products whose results another block reads: a result is there 12 issue slots behind its product, and the compiler, which has been seen to count too few of them from block to
+// Stands between products and a block behind theirs that reads their results: a result is there 12 issue slots behind its product, and the compiler, which has been seen to count too few of them from block to
 // block (9 from the last product of the form whose wavefronts divide the keys to the sums' first reader behind the loop), is left none to count.
 __device__ __forceinline__ void products_done() {
   __builtin_amdgcn_sched_barrier(0);

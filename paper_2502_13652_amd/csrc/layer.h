@@ -39,7 +39,7 @@ inline int append_parts(int64_t tokens, int passes) { return tokens < APPEND_FEW
 // ---- prompt ----
 // Which kernel a call takes.  Tiles of 128 rows of a workgroup, whose wavefronts share the keys; or, where there are few of those and the prompts are long, tiles of 32 rows whose four
 // wavefronts divide the keys: four times the workgroups, each a quarter of the way.  Both are known but for the lengths, of which the mean stands for all.  Width 128, shared and divided: one prompt of
-// 2000 tokens, 4 heads over one, 37.6 and 21.6 us; of 8192, one head, 135 and 67, 4 over one 137 and 142; 4 of 500, 8 over one, 13.6 and 16.3; one of 200, 32 over 8, 8.5 and 7.9, of 350 11.5 and 13.2.
+// 2000 tokens, 4 heads over one, 37.6 and 21.2 us; of 8192, one head, 135 and 65, 4 over one 137 and 143; 4 of 500, 8 over one, 13.6 and 16.3; one of 200, 32 over 8, 8.5 and 7.9, of 350 11.5 and 13.2.
 // Width 64, of which two workgroups that divide fit a CU: 32 and 14; 116 and 42, 119 and 72; 11.9 and 7.6; 7.5 and 5.7, 10.0 and 6.9, of 1000 19.7 and 17.2, of 1500 27.1 and 26.8, of 2000 35 and 41.
 // Of width 256, whose tiles hardly fit in LDS four times, the keys are never divided.
 typedef void (*PromptKernel)(const int32_t*, int32_t, int32_t, int32_t, int32_t, float, float, PromptArgs);

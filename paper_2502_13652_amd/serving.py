@@ -221,7 +221,8 @@ def _even_rows(t, shape, index, name):
 def rms_norm(x, weight, eps=1e-5, residual=None, residual_out=None, out=None, scale_block=None, scales=None, stream=None):
     """Root-mean-square norm of x + residual: h = x + residual, h / sqrt(mean(h^2) + eps) * weight over the last dimension, of h in fp32.
 
-    x [...][width] float32, bfloat16 or float16; weight [width] of that type or float32; residual, of x's shape, of that type or float32: h goes to
+    x [...][width] float32, bfloat16 or float16, its rows evenly spaced, as those of the other arrays (some heads of a fused projection, [:, :heads], are not, and are refused);
+    weight [width] of that type or float32; residual, of x's shape, of that type or float32: h goes to
     residual_out (default: residual itself), rounded to its type.  out: of x's shape and type (default: a new tensor; may be x).  With scale_block (32, 64, 128
     or the width), out is float8_e4m3fn and stands for out * scale, with a scale for each scale_block elements of a row (the last may be fewer): scales float32
     [...][ceil(width / scale_block)] (default: new), max |y| / 448 of the block; returns (out, scales), without it out."""
